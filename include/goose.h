@@ -277,6 +277,102 @@ typedef struct {
 int goose_verify_step_batched(goose_ctx* ctx, const goose_model_ptrs* model, const goose_request* reqs, int n_req,
                               int32_t* d_argmax_all, void* stream);
 
+/* ---- 6c. a paged cache: requests that share a prompt (16-bit models only) ---------------------------------
+ * Instead of `cap` slots per request, K and V live in one pool of pages of GOOSE_PAGE slots, and a table names the pages of
+ * every sequence: slot s of sequence q lies in page d_table[q * table_ld + s / 64], at s % 64.  A page may stand in the tables
+ * of several sequences (a shared prompt); d_refs counts those entries.  All arrays are DEVICE memory of the caller; the
+ * descriptor itself is read during the call.
+ *   d_kpool, d_vpool  T [n_layers][n_pages][n_kv_heads][64 * head_dim], a head's part of a page in the operand order given
+ *                     above (g = s % 64: two blocks of 32 slots), 16-byte aligned
+ *   d_table           int32 [n_seqs][table_ld], -1 where there is no page
+ *   d_len             int32 [n_seqs], committed slots of every sequence (what *d_P is elsewhere)
+ *   d_refs            int32 [n_pages], 0 = the page is free
+ * The calls below find out on the device what the arrays hold.  What they cannot do raises a flag and is left undone:
+ *   GOOSE_FLAG_PAGES  no free page is left, an entry of a table or a reference count is out of range, a fork into a sequence
+ *                     that is not empty, a K/V row for a page that is missing or shared, or shared_pages below that are not shared;
+ *   GOOSE_FLAG_CAPACITY  a length below 0, above P_max, or beyond table_ld * 64 with the call's new slots.
+ * Pages named by entries out of range are read as page 0, never out of bounds.  Sequences are given by number (host
+ * integers, 0 <= seq < n_seqs, none twice in a call, at most GOOSE_MAX_REQUESTS of them). */
+enum { GOOSE_PAGE = 64, GOOSE_FLAG_PAGES = 16 };
+typedef struct {
+  void* d_kpool;
+  void* d_vpool;
+  int32_t* d_table;
+  int32_t* d_len;
+  int32_t* d_refs;
+  int32_t n_pages, n_seqs, table_ld;
+} goose_pages;
+
+/* One request of a call on a paged cache.  Every call names the fields that it reads beside seq and B. */
+typedef struct {
+  int32_t seq;              /* its sequence */
+  int32_t B;                /* nodes of its tree, 1..max_B of the context */
+  int32_t P_max;            /* host upper bound of d_len[seq]; P_max + B <= table_ld * 64 */
+  const int32_t* d_tokens;  /* [B] */
+  const int32_t* d_parent;  /* [B] */
+  const uint8_t* d_is_spine;/* [B] or NULL */
+  const uint64_t* d_mask;   /* [B][ceil(B/64)] as goose_build_mask writes it */
+  const int32_t* d_pos;     /* [B] positions */
+  int32_t* d_accept_len;    /* [1] */
+  int32_t* d_path;          /* [B] */
+  int32_t* d_bonus;         /* [1] */
+  int32_t* d_next_root_or_null;
+  int32_t* d_succ_ids_or_null;   /* successor tables [vocab][harvest_k], both or neither */
+  float* d_succ_scores_or_null;
+  int32_t harvest_k;
+} goose_paged_request;
+
+/* All tables empty, all lengths 0, all pages free. */
+int goose_pages_clear(goose_ctx* ctx, const goose_pages* pages, void* stream);
+/* Every sequence of h_dst (empty ones) starts with the first `len` committed slots of sequence src (len < 0: with all of
+ * them): their tables name src's pages, nothing is copied.  One of them that is not empty is left alone (GOOSE_FLAG_PAGES);
+ * a src with fewer than `len` slots leaves all alone (GOOSE_FLAG_CAPACITY). */
+int goose_pages_fork(goose_ctx* ctx, const goose_pages* pages, int src, int len, const int32_t* h_dst, int n, void* stream);
+/* Room for h_new[i] (>= 1) slots behind the committed ones of sequence h_seqs[i]: missing pages are taken from the pool, the free
+ * page with the lowest number first, for the sequences in their order.  Where the page of the first new slot is shared
+ * the sequence gets one of its own: the 32-slot blocks that hold committed slots are copied in every layer, K and V (other slots
+ * of a taken page keep what they held).  All or nothing: if pages do not suffice or a length is out of range, no table changes.
+ * One call takes at most 4096 pages (sum of h_new / 64 + 2 per sequence, else GOOSE_ERR_CAPACITY). */
+int goose_pages_reserve(goose_ctx* ctx, const goose_pages* pages, const int32_t* h_seqs, const int32_t* h_new, int n, void* stream);
+/* goose_compact_kv on pages, for n requests (d_path, d_accept_len): slot P + path[j] -> P + j in every layer, the length becomes
+ * P + L + 1, and reserved pages beyond it are given back.  A path that is not increasing, or leaves the tree, is followed up to there. */
+int goose_pages_commit(goose_ctx* ctx, const goose_pages* pages, const goose_paged_request* reqs, int n, void* stream);
+/* The sequences become empty; pages that no table names any more are free. */
+int goose_pages_free(goose_ctx* ctx, const goose_pages* pages, const int32_t* h_seqs, int n, void* stream);
+
+/* From the q|k|v projection to rotated queries and to K/V rows in the pages, one launch for all requests (d_pos of each).
+ * d_qkv: fp32 [ksplit][rows][ld] as goose_gemm_packed leaves it, slices split_stride elements apart (1 <= ksplit <= 16), columns q
+ * (n_heads * head_dim), k, v (n_kv_heads * head_dim each); rows of a request start at the sum of round_up(B, 32) of the requests
+ * before it.  The slices are added in their order; with d_gq and d_gk (T [head_dim], both or neither) every head of q and k is
+ * normalised, x * rsqrt(mean(x^2) + rms_eps) * g; pairs (j, j + head_dim/2) are rotated by pos * base^(-2j/head_dim), the angle
+ * reduced in 64 bits.  q: T [rows][ldq], in q_terms = 1 or 2 terms (two: hi + lo in groups of eight columns, ldq >= 2 * n_heads *
+ * head_dim; see goose_split_operand); k and v of node i: slot d_len[seq] + i of layer `layer`, whose page must be the
+ * sequence's own (goose_pages_reserve).  Rows between requests are neither read nor written.  ld and split_stride multiples of 4, ldq of 8,
+ * d_qkv and d_q 16-byte aligned. */
+int goose_qk_norm_rope_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const float* d_qkv, int ksplit, size_t split_stride,
+                             size_t ld, const void* d_gq_or_null, const void* d_gk_or_null, const goose_paged_request* reqs, int n,
+                             void* d_q, size_t ldq, int q_terms, void* stream);
+/* Tree attention of n requests over pages of one layer (d_mask of each): a node sees slots [0, P) of its sequence and the slots P + j of the
+ * nodes j of its mask row (bits at or beyond B count as clear), scores / sqrt(head_dim), softmax.  The first shared_pages entries of
+ * all n tables must be the same pages, wholly committed (shared_pages * 64 <= every length): the keys in them are read once for
+ * the rows of all requests.  shared_pages = 0 is always allowed, and the result does not depend on it beyond rounding.
+ * d_q as goose_qk_norm_rope_paged writes it; d_o: 16-bit [rows][ldo] of type o_dtype (GOOSE_DTYPE_BF16 or _F16) in o_terms terms.
+ * Probabilities are rounded to T for the second product, sums and statistics are fp32.  A row that sees nothing but scores of
+ * -infinity, or nothing, is zero; what slots behind a mask hold (NaN, infinities) has no effect; a NaN in what a row sees makes the row NaN,
+ * and so does a score of +infinity.  ldq and ldo multiples of 8, d_q and d_o 16-byte aligned.  Sum of round_up(B, 32) <= max_rows. */
+int goose_attn_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,
+                     const goose_paged_request* reqs, int n, int shared_pages, void* d_o, size_t ldo, int o_dtype, int o_terms,
+                     void* stream);
+/* goose_verify_layer on pages, for the stacked rows of n requests (d_mask, d_pos, P_max of each; d_x fp32 [rows][hidden], rows between
+ * requests finite).  Their slots must be reserved. */
+int goose_verify_layer_paged(goose_ctx* ctx, const void* d_packed_layer, const goose_pages* pages, int layer, float* d_x,
+                             const goose_paged_request* reqs, int n, int shared_pages, void* stream);
+/* goose_verify_step_batched on pages: reserves B slots for every request, runs the pass, walks, commits.  Reads d_tokens, d_parent, d_is_spine, P_max
+ * and the successor tables, writes d_accept_len, d_path, d_bonus, d_next_root_or_null; model->d_kcache_all and d_vcache_all are not used.
+ * The queries keep two terms under bf16 storage (as in goose_verify_layer) and one under fp16. */
+int goose_verify_step_paged(goose_ctx* ctx, const goose_model_ptrs* model, const goose_pages* pages, const goose_paged_request* reqs, int n,
+                            int shared_pages, int32_t* d_argmax_all, void* stream);
+
 /* ---- 7. logit harvest (Sec. 4 stage 2 "verify and harvest"; App. C "adjacency table", tier 1, and
  * "logit harvesting"; Alg. "Decoding Loop", the update of the table from all logits of a cycle) ----
  * For every node i < B -- accepted or not -- row d_tokens[i] of the two dense successor tables

@@ -8,6 +8,8 @@ from .binding import (  # noqa: F401
     GooseError,
     GooseContext,
     ModelDesc,
+    PagedCache,
+    PagedRequests,
     goose_check_parent,
     goose_packed_matrix_bytes,
     goose_pack_matrix,

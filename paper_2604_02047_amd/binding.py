@@ -24,6 +24,8 @@ EXPORTS = [
     "goose_cycle_mode", "goose_verify_step_batched",
     "goose_split_operand", "goose_gemm_packed_ex", "goose_gemm_swiglu_packed_ex",
     "goose_lm_head_argmax_static", "goose_plan_cycle",
+    "goose_pages_clear", "goose_pages_fork", "goose_pages_reserve", "goose_pages_commit", "goose_pages_free",
+    "goose_qk_norm_rope_paged", "goose_attn_paged", "goose_verify_layer_paged", "goose_verify_step_paged",
 ]
 
 GOOSE_DTYPE_BF16, GOOSE_DTYPE_F32, GOOSE_DTYPE_F16 = 0, 1, 2
@@ -64,6 +66,18 @@ class _Request(C.Structure):
                 ("d_accept_len", C.c_void_p), ("d_path", C.c_void_p), ("d_bonus", C.c_void_p),
                 ("d_next_root_or_null", C.c_void_p), ("d_succ_ids_or_null", C.c_void_p),
                 ("d_succ_scores_or_null", C.c_void_p), ("harvest_k", C.c_int32)]
+
+
+class _Pages(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_kpool", "d_vpool", "d_table", "d_len", "d_refs")] + \
+               [(n, C.c_int32) for n in ("n_pages", "n_seqs", "table_ld")]
+
+
+class _PagedRequest(C.Structure):
+    _fields_ = [("seq", C.c_int32), ("B", C.c_int32), ("P_max", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("d_tokens", "d_parent", "d_is_spine", "d_mask", "d_pos", "d_accept_len", "d_path", "d_bonus",
+                                          "d_next_root_or_null", "d_succ_ids_or_null", "d_succ_scores_or_null")] + \
+               [("harvest_k", C.c_int32)]
 
 
 @dataclass
@@ -150,6 +164,16 @@ def load_library():
                                          [C.c_float, C.c_void_p, C.c_void_p])
     lib.goose_gemm_swiglu_packed_ex.argtypes = ([C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p] + [C.c_int] * 4 +
                                                 [C.c_float, C.c_void_p, C.c_int, C.c_void_p])
+    vp, ci, sz, pages, preq = C.c_void_p, C.c_int, C.c_size_t, C.POINTER(_Pages), C.POINTER(_PagedRequest)
+    lib.goose_pages_clear.argtypes = [vp, pages, vp]
+    lib.goose_pages_fork.argtypes = [vp, pages, ci, ci, vp, ci, vp]
+    lib.goose_pages_reserve.argtypes = [vp, pages, vp, vp, ci, vp]
+    lib.goose_pages_commit.argtypes = [vp, pages, preq, ci, vp]
+    lib.goose_pages_free.argtypes = [vp, pages, vp, ci, vp]
+    lib.goose_qk_norm_rope_paged.argtypes = [vp, pages, ci, vp, ci, sz, sz, vp, vp, preq, ci, vp, sz, ci, vp]
+    lib.goose_attn_paged.argtypes = [vp, pages, ci, vp, sz, ci, preq, ci, ci, vp, sz, ci, ci, vp]
+    lib.goose_verify_layer_paged.argtypes = [vp, vp, pages, ci, vp, preq, ci, ci, vp]
+    lib.goose_verify_step_paged.argtypes = [vp, C.POINTER(_ModelPtrs), pages, preq, ci, ci, vp, vp]
     lib.goose_profile_enable.argtypes = [C.c_void_p, C.c_int]
     lib.goose_profile_kinds.argtypes = []
     lib.goose_profile_kind_name.argtypes = [C.c_int]
@@ -240,6 +264,8 @@ def goose_build_spine_tree(anchor, draft, succ_ids, succ_scores, B, r, rho=0.5, 
 
 MODE_AR, MODE_TREE, MODE_BYPASS = 0, 1, 2
 GOOSE_FLAG_BAD_PARENT, GOOSE_FLAG_CAPACITY, GOOSE_FLAG_RANGE, GOOSE_FLAG_WEIGHT_RANGE = 1, 2, 4, 8   # goose_device_flags
+GOOSE_FLAG_PAGES, GOOSE_PAGE = 16, 64
+GOOSE_ERR_ARG, GOOSE_ERR_SHAPE = -1, -2
 GOOSE_ACT_F16, GOOSE_ACT_TWO_TERM = 0, 1
 GOOSE_ERR_CAPACITY, GOOSE_ERR_NOT_TOPOLOGICAL = -3, -4
 
@@ -332,6 +358,58 @@ def goose_lm_head_argmax_static(desc: ModelDesc, packed_head, x, B, argmax, marg
     cd = desc._c()
     _check(load_library().goose_lm_head_argmax_static(C.byref(cd), _ptr(packed_head), _ptr(x), B, _ptr(argmax),
                                                       _ptr(margin), _stream()), "goose_lm_head_argmax_static")
+
+
+class PagedCache:
+    """A paged KV cache (goose_pages): kpool, vpool [n_layers][n_pages][n_kv_heads][64 * head_dim] of the model's 16-bit type in operand
+    order, table int32 [n_seqs][pages a sequence may have], len int32 [n_seqs], refs int32 [n_pages], on one GPU.  Owns nothing but
+    references to the tensors; GooseContext.goose_pages_clear makes a fresh one."""
+
+    def __init__(self, kpool, vpool, table, len, refs):  # noqa: A002
+        self.kpool, self.vpool, self.table, self.len, self.refs = kpool, vpool, table, len, refs
+        t = (kpool, vpool, table, len, refs)
+        import torch
+        ok = (kpool.shape == vpool.shape and kpool.dim() == 4 and kpool.dtype == vpool.dtype
+              and kpool.dtype in (torch.bfloat16, torch.float16) and table.dim() == 2
+              and all(x.dtype == torch.int32 for x in t[2:]) and len.shape == table.shape[:1] and refs.shape == kpool.shape[1:2]
+              and all(x.is_contiguous() and x.device == kpool.device for x in t))
+        if not ok:
+            raise GooseError(GOOSE_ERR_ARG, "PagedCache: shapes, types or devices of the pools and tables do not fit together")
+        self._c = _Pages(*[x.data_ptr() for x in t], refs.shape[0], table.shape[0], table.shape[1])
+
+
+class PagedRequests:
+    """The requests of a paged call, as dicts with seq, B, P_max and the tensors that the call reads (tokens, parent, is_spine, mask, pos,
+    accept_len, path, bonus, next_root, succ_ids, succ_scores).  Build it once for calls that repeat; every call takes a plain
+    list of such dicts as well."""
+
+    def __init__(self, reqs):
+        self.reqs = reqs  # (keeps the tensors alive)
+        self._c = (_PagedRequest * len(reqs))()
+        names = ("tokens", "parent", "is_spine", "mask", "pos", "accept_len", "path", "bonus", "next_root", "succ_ids", "succ_scores")
+        for i, q in enumerate(reqs):
+            ptrs = [None if q.get(n) is None else q[n].data_ptr() for n in names]
+            k = 0 if q.get("succ_ids") is None else int(q["succ_ids"].shape[1])
+            self._c[i] = _PagedRequest(int(q["seq"]), int(q["B"]), int(q.get("P_max", 0)), *ptrs, k)
+
+    def __len__(self):
+        return len(self._c)
+
+
+def _stacked_rows(r):
+    """Rows of the stacked buffers that the requests reach into (each starts at a multiple of 32)."""
+    at = 0
+    for q in r._c[:-1]:
+        at += (q.B + 31) // 32 * 32
+    return at + r._c[len(r) - 1].B if len(r) else 0
+
+
+def _rows_ok(t, rows, cols, dtypes):
+    return t.dim() == 2 and t.dtype in dtypes and t.stride(1) == 1 and t.shape[0] >= rows and t.shape[1] >= cols
+
+
+def _seqs(values):
+    return (C.c_int32 * len(values))(*values)
 
 
 class GooseContext:
@@ -430,6 +508,83 @@ class GooseContext:
                               0 if q.get("succ_ids") is None else int(q["succ_ids"].shape[1]))
         _check(self.lib.goose_verify_step_batched(self._h, C.byref(m), arr, len(requests), _ptr(argmax_all),
                                                   _stream()), "goose_verify_step_batched")
+
+    # ---- paged caches
+    def _pages(self, cache: PagedCache, *tensors):
+        """The descriptor of `cache`, after a look at what the C side cannot see: element types, head layout, devices."""
+        import torch
+        d = self.desc
+        dev, want = cache.kpool.device, {"bf16": torch.bfloat16, "f16": torch.float16}.get(d.dtype)
+        if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+            raise GooseError(GOOSE_ERR_ARG, "the paged cache is not on the current device")
+        if want is not None and (cache.kpool.dtype != want or cache.kpool.shape[2] != d.kv_heads
+                                 or cache.kpool.shape[3] != GOOSE_PAGE * d.head_dim or cache.kpool.shape[0] != d.n_layers):
+            raise GooseError(GOOSE_ERR_ARG, "the paged cache is not one of this model")
+        for t in tensors:
+            if t is not None and t.device != dev:
+                raise GooseError(GOOSE_ERR_ARG, "a tensor of the call is on another device than the paged cache")
+        return C.byref(cache._c)
+
+    @staticmethod
+    def _reqs(reqs):
+        return reqs if isinstance(reqs, PagedRequests) else PagedRequests(reqs)
+
+    def goose_pages_clear(self, cache):
+        _check(self.lib.goose_pages_clear(self._h, self._pages(cache), _stream()), "goose_pages_clear")
+
+    def goose_pages_fork(self, cache, src, dst, length=-1):
+        _check(self.lib.goose_pages_fork(self._h, self._pages(cache), src, length, _seqs(dst), len(dst), _stream()), "goose_pages_fork")
+
+    def goose_pages_reserve(self, cache, seqs, new):
+        if len(seqs) != len(new):
+            raise GooseError(GOOSE_ERR_ARG, "goose_pages_reserve")
+        _check(self.lib.goose_pages_reserve(self._h, self._pages(cache), _seqs(seqs), _seqs(new), len(seqs), _stream()),
+               "goose_pages_reserve")
+
+    def goose_pages_commit(self, cache, reqs):
+        r = self._reqs(reqs)
+        _check(self.lib.goose_pages_commit(self._h, self._pages(cache), r._c, len(r), _stream()), "goose_pages_commit")
+
+    def goose_pages_free(self, cache, seqs):
+        _check(self.lib.goose_pages_free(self._h, self._pages(cache), _seqs(seqs), len(seqs), _stream()), "goose_pages_free")
+
+    def goose_qk_norm_rope_paged(self, cache, layer, qkv, gq, gk, reqs, q, q_terms=1):
+        """qkv: fp32 [ksplit][rows][columns] (strides of the first two dimensions are free), q: [rows][columns] of the cache's type."""
+        r = self._reqs(reqs)
+        pages = self._pages(cache, qkv, gq, gk, q)
+        rows, d = _stacked_rows(r), self.desc
+        import torch
+        if not (qkv.dim() == 3 and qkv.shape[0] > 0
+                and _rows_ok(qkv[0], rows, (d.n_heads + 2 * d.kv_heads) * d.head_dim, (torch.float32,))
+                and _rows_ok(q, rows, d.n_heads * d.head_dim * q_terms, (cache.kpool.dtype,))
+                and all(g is None or (g.dtype == q.dtype and g.is_contiguous() and g.numel() == self.desc.head_dim) for g in (gq, gk))):
+            raise GooseError(GOOSE_ERR_ARG, "goose_qk_norm_rope_paged: rows or types of qkv, q or the gains")
+        _check(self.lib.goose_qk_norm_rope_paged(self._h, pages, layer, _ptr(qkv), qkv.shape[0], qkv.stride(0), qkv.stride(1), _ptr(gq),
+                                                 _ptr(gk), r._c, len(r), _ptr(q), q.stride(0), q_terms, _stream()),
+               "goose_qk_norm_rope_paged")
+
+    def goose_attn_paged(self, cache, layer, q, q_terms, reqs, shared_pages, o, o_terms=1):
+        """q: [rows][columns] of the cache's type; o: [rows][columns], bf16 or fp16."""
+        r = self._reqs(reqs)
+        pages = self._pages(cache, q, o)
+        rows, cols = _stacked_rows(r), self.desc.n_heads * self.desc.head_dim
+        import torch
+        if not (_rows_ok(q, rows, cols * q_terms, (cache.kpool.dtype,))
+                and _rows_ok(o, rows, cols * o_terms, (torch.bfloat16, torch.float16))):
+            raise GooseError(GOOSE_ERR_ARG, "goose_attn_paged: rows or types of q or o")
+        _check(self.lib.goose_attn_paged(self._h, pages, layer, _ptr(q), q.stride(0), q_terms, r._c, len(r), shared_pages, _ptr(o),
+                                         o.stride(0), _dtype_code(o), o_terms, _stream()), "goose_attn_paged")
+
+    def goose_verify_layer_paged(self, packed_layer, cache, layer, x, reqs, shared_pages=0):
+        r = self._reqs(reqs)
+        _check(self.lib.goose_verify_layer_paged(self._h, _ptr(packed_layer), self._pages(cache, x), layer, _ptr(x), r._c, len(r),
+                                                 shared_pages, _stream()), "goose_verify_layer_paged")
+
+    def goose_verify_step_paged(self, model: dict, cache, reqs, shared_pages, argmax_all):
+        m = _ModelPtrs(model["embed"].data_ptr(), model["packed_layers"].data_ptr(), model["packed_head"].data_ptr(), None, None)
+        r = self._reqs(reqs)
+        _check(self.lib.goose_verify_step_paged(self._h, C.byref(m), self._pages(cache, argmax_all), r._c, len(r), shared_pages,
+                                                _ptr(argmax_all), _stream()), "goose_verify_step_paged")
 
     def goose_device_flags(self) -> int:
         out = C.c_int32(0)

@@ -238,6 +238,8 @@ int goose_create_batched(const goose_model_desc* desc, int max_B, int max_rows, 
     A((void**)&c->part, (size_t)c->max_ksplit * c->Bpad * c->part_ld * sizeof(float));
     A((void**)&c->att_o, (size_t)d.n_heads * c->max_splits * c->Bpad * d.head_dim * sizeof(float));
     A((void**)&c->att_ml, (size_t)d.n_heads * c->max_splits * c->Bpad * 2 * sizeof(float));
+    A(&c->q, (size_t)c->Bpad * 2 * c->Kq * es);
+    A(&c->page_copies, GOOSE_MAX_REQUESTS * 16);
   } else {
     A(&c->q, (size_t)c->Bpad * c->Kq * es);
   }
@@ -274,7 +276,7 @@ int goose_create_batched(const goose_model_desc* desc, int max_B, int max_rows, 
 void goose_destroy(goose_ctx* c) {
   if (!c) return;
   void* ptrs[] = {c->xn, c->part, c->q, c->o, c->h, c->att_o, c->att_ml, c->logits, c->top2, c->harvest, c->inv_freq, c->rope_cs,
-                  c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags, c->s_P};
+                  c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags, c->s_P, c->page_copies};
   for (void* p : ptrs)
     if (p) (void)hipFree(p);
   if (c->prof) {
@@ -365,6 +367,9 @@ static int attn_groups() {
   return v;
 }
 
+// partial results that the attention's workspace holds
+static size_t attn_records(const goose_ctx* c) { return (size_t)c->d.n_heads * c->max_splits * c->Bpad; }
+
 static RopeArgs rope_args(const goose_ctx* c, const int32_t* pos, int rows) {
   return RopeArgs{pos, c->inv_freq, (float2*)c->rope_cs, rows, c->d.head_dim / 2};
 }
@@ -452,10 +457,17 @@ static int layer_row(goose_ctx* c, const char* w, float* d_x, const AttnSeg& seg
 // A batch of requests shares every projection (their rows are stacked, each request starting at a
 // multiple of 32 rows); in the attention every request is a slice of the grid with its own caches,
 // mask and length (`segs`; none = the single request given by the plain arguments).
+// `paged`: the requests' keys and values live in a paged cache instead (rotation and K/V rows, then the attention: two stages).
 static_assert(GOOSE_MAX_REQUESTS <= ATTN_MAX_SEGS, "a batch must fit the attention's request table");
+struct PagedPass {
+  const goose_pages* pages;
+  int layer, shared_pages;
+  PagedReqs pos, mask;  // the requests with their positions, and with their masks
+};
 static int layer_impl(goose_ctx* c, const char* w, float* d_x, void* d_kcache, void* d_vcache, int P,
                       const int32_t* dP, int B, const uint64_t* d_mask, hipStream_t st, bool xhat_ready,
-                      const void* g_next, const RopeArgs* rope, const AttnSeg* segs = nullptr, int nseg = 0) {
+                      const void* g_next, const RopeArgs* rope, const AttnSeg* segs = nullptr, int nseg = 0,
+                      const PagedPass* paged = nullptr) {
   int rc = GOOSE_OK;
   const goose_model_desc& d = c->d;
   const size_t pstride = (size_t)c->Bpad * c->part_ld;
@@ -464,7 +476,7 @@ static int layer_impl(goose_ctx* c, const char* w, float* d_x, void* d_kcache, v
   const GemmCfg cq = gemm_cfg(c, "GOOSE_CFG_QKV", Nqkv, c->Kh), co = gemm_cfg(c, "GOOSE_CFG_O", Nh, c->Kq),
                 cd = gemm_cfg(c, "GOOSE_CFG_DOWN", Nh, c->Fpad);
   const AttnSeg whole{0, B, P, d_kcache, d_vcache, dP, d_mask};
-  if (nseg == 0 && one_row(c, B, cq.ks, co.ks, cd.ks))
+  if (nseg == 0 && paged == nullptr && one_row(c, B, cq.ks, co.ks, cd.ks))
     return layer_row(c, w, d_x, whole, cq.ks, co.ks, cd.ks, st, xhat_ready, g_next, rope);
 
   // x_hat = RMSNorm(x) * g1
@@ -483,7 +495,19 @@ static int layer_impl(goose_ctx* c, const char* w, float* d_x, void* d_kcache, v
   if (rc) return rc;
   // rotary embedding of q and k, KV rows of the tree into the cache, tree attention: one kernel
   if (nseg == 0) { segs = &whole; nseg = 1; }
-  { PROF(PK_ATTN);
+  if (paged != nullptr) {
+    PROF(PK_ATTN);
+    // fp16 queries carry 11 bits in one term; bf16 ones need the second (their error is common to all scores of a row)
+    const int q_terms = d.dtype == GOOSE_DTYPE_BF16 ? 2 : 1;
+    const size_t ldq = (size_t)q_terms * Hq;
+    rc = launch_rope_paged(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->inv_freq, d.rms_eps, c->part, ks, pstride,
+                           c->part_ld, d.qk_norm ? w + c->pl.gq : nullptr, d.qk_norm ? w + c->pl.gk : nullptr, paged->pos, c->q, ldq,
+                           q_terms, c->flags, st);
+    if (rc) return rc;
+    rc = launch_attn_paged(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, paged->mask,
+                           paged->shared_pages, c->att_o, c->att_ml, attn_records(c), c->o, c->ld_o, c->act_dtype, T, c->flags, st);
+  } else {
+    PROF(PK_ATTN);
     rc = launch_attn_16(d.dtype, c->part, ks, pstride, c->part_ld, c->rope_cs, d.n_heads, c->n_kv, d.head_dim, c->cap, segs,
                           nseg, attn_splits(), c->max_splits, attn_groups(), d.qk_norm ? w + c->pl.gq : nullptr,
                           d.qk_norm ? w + c->pl.gk : nullptr, d.rms_eps, c->att_o, c->att_ml, c->Bpad, c->o, c->ld_o,
@@ -773,6 +797,222 @@ int goose_verify_step_batched(goose_ctx* c, const goose_model_ptrs* m, const goo
   rc = lm_head_impl(c, m->d_packed_head, c->s_x, rows, d_argmax_all, nullptr, nullptr, st, true, hv);
   if (rc) return rc;
   return launch_batch_end(br, n_req, d_argmax_all, d.n_layers, c->n_kv, c->cap, d.head_dim, c->s_P, c->flags, st);
+}
+
+// ---- paged caches -------------------------------------------------------------------------------
+static int check_pages(const goose_ctx* c, const goose_pages* pg) {
+  if (!c || !pg) return GOOSE_ERR_ARG;
+  if (!is16(c->d.dtype)) return GOOSE_ERR_SHAPE;
+  if (!pg->d_kpool || !pg->d_vpool || !pg->d_table || !pg->d_len || !pg->d_refs) return GOOSE_ERR_ARG;
+  if (((uintptr_t)pg->d_kpool & 15) || ((uintptr_t)pg->d_vpool & 15)) return GOOSE_ERR_ARG;
+  if (pg->n_pages < 1 || pg->n_seqs < 1 || pg->table_ld < 1 || pg->table_ld > INT32_MAX / GOOSE_PAGE) return GOOSE_ERR_ARG;
+  return GOOSE_OK;
+}
+static int check_seqs(const goose_pages* pg, const int32_t* h_seqs, int n) {
+  if (!h_seqs || n < 1 || n > GOOSE_MAX_REQUESTS) return GOOSE_ERR_ARG;
+  for (int i = 0; i < n; ++i) {
+    if (h_seqs[i] < 0 || h_seqs[i] >= pg->n_seqs) return GOOSE_ERR_ARG;
+    for (int j = 0; j < i; ++j)
+      if (h_seqs[j] == h_seqs[i]) return GOOSE_ERR_ARG;
+  }
+  return GOOSE_OK;
+}
+// The requests of a paged call; `field`: what the kernels get of each.  rows: the call works on stacked rows and launches by P_max.
+static int paged_reqs(const goose_ctx* c, const goose_pages* pg, const goose_paged_request* reqs, int n, bool rows, PagedReqs* out,
+                      const void* (*field)(const goose_paged_request&)) {
+  if (!reqs || n < 1 || n > GOOSE_MAX_REQUESTS) return GOOSE_ERR_ARG;
+  int row0 = 0;
+  out->n = n;
+  out->rows = 0;
+  for (int i = 0; i < n; ++i) {
+    const goose_paged_request& q = reqs[i];
+    if (q.seq < 0 || q.seq >= pg->n_seqs || q.B < 1) return GOOSE_ERR_ARG;
+    for (int j = 0; j < i; ++j)
+      if (reqs[j].seq == q.seq) return GOOSE_ERR_ARG;
+    if (q.B > c->max_B) return GOOSE_ERR_CAPACITY;
+    if (rows) {
+      if (q.P_max < 0) return GOOSE_ERR_ARG;
+      if ((long long)q.P_max + q.B > (long long)pg->table_ld * GOOSE_PAGE) return GOOSE_ERR_CAPACITY;
+    }
+    const void* p = field(q);
+    if (!p) return GOOSE_ERR_ARG;
+    out->r[i] = PagedReq{q.seq, q.B, rows ? q.P_max : 0, row0, out->rows, p, q.d_accept_len};
+    out->rows += q.B;
+    row0 += round_up(q.B, 32);
+  }
+  return rows && row0 > c->max_rows ? GOOSE_ERR_CAPACITY : GOOSE_OK;
+}
+static int check_shared(const goose_pages* pg, const PagedReqs& rq, int shared_pages) {
+  if (shared_pages < 0 || shared_pages > pg->table_ld) return GOOSE_ERR_ARG;
+  for (int i = 0; i < rq.n; ++i)
+    if ((long long)shared_pages * GOOSE_PAGE > rq.r[i].P_max) return GOOSE_ERR_CAPACITY;
+  return GOOSE_OK;
+}
+
+int goose_pages_clear(goose_ctx* c, const goose_pages* pg, void* stream) {
+  int rc = check_pages(c, pg);
+  return rc ? rc : launch_pages_clear(*pg, as_stream(stream));
+}
+
+int goose_pages_fork(goose_ctx* c, const goose_pages* pg, int src, int len, const int32_t* h_dst, int n, void* stream) {
+  int rc = check_pages(c, pg);
+  if (!rc) rc = check_seqs(pg, h_dst, n);
+  if (rc) return rc;
+  if (src < 0 || src >= pg->n_seqs) return GOOSE_ERR_ARG;
+  SeqList l{};
+  l.n = n;
+  for (int i = 0; i < n; ++i) {
+    if (h_dst[i] == src) return GOOSE_ERR_ARG;
+    l.seq[i] = h_dst[i];
+  }
+  return launch_pages_fork(*pg, src, len, l, c->flags, as_stream(stream));
+}
+
+int goose_pages_reserve(goose_ctx* c, const goose_pages* pg, const int32_t* h_seqs, const int32_t* h_new, int n, void* stream) {
+  int rc = check_pages(c, pg);
+  if (!rc) rc = check_seqs(pg, h_seqs, n);
+  if (rc) return rc;
+  if (!h_new) return GOOSE_ERR_ARG;
+  SeqList l{};
+  l.n = n;
+  long long pages = 0;
+  for (int i = 0; i < n; ++i) {
+    if (h_new[i] < 1) return GOOSE_ERR_ARG;
+    l.seq[i] = h_seqs[i];
+    l.extra[i] = h_new[i];
+    pages += h_new[i] / GOOSE_PAGE + 2;
+  }
+  if (pages > PAGES_PER_CALL) return GOOSE_ERR_CAPACITY;
+  return launch_pages_reserve(*pg, l, c->d.n_layers, c->n_kv, c->d.head_dim, c->page_copies, c->flags, as_stream(stream));
+}
+
+int goose_pages_commit(goose_ctx* c, const goose_pages* pg, const goose_paged_request* reqs, int n, void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  PagedReqs rq;
+  rc = paged_reqs(c, pg, reqs, n, false, &rq, [](const goose_paged_request& q) -> const void* { return q.d_accept_len ? q.d_path : nullptr; });
+  if (rc) return rc;
+  return launch_pages_commit(*pg, rq, c->d.n_layers, c->n_kv, c->d.head_dim, c->flags, as_stream(stream));
+}
+
+int goose_pages_free(goose_ctx* c, const goose_pages* pg, const int32_t* h_seqs, int n, void* stream) {
+  int rc = check_pages(c, pg);
+  if (!rc) rc = check_seqs(pg, h_seqs, n);
+  if (rc) return rc;
+  SeqList l{};
+  l.n = n;
+  for (int i = 0; i < n; ++i) l.seq[i] = h_seqs[i];
+  return launch_pages_free(*pg, l, c->flags, as_stream(stream));
+}
+
+int goose_qk_norm_rope_paged(goose_ctx* c, const goose_pages* pg, int layer, const float* d_qkv, int ksplit, size_t split_stride, size_t ld,
+                             const void* d_gq, const void* d_gk, const goose_paged_request* reqs, int n, void* d_q, size_t ldq,
+                             int q_terms, void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  if (!d_qkv || !d_q || layer < 0 || layer >= c->d.n_layers || ksplit < 1 || ksplit > c->max_ksplit) return GOOSE_ERR_ARG;
+  if ((q_terms != 1 && q_terms != 2) || (d_gq == nullptr) != (d_gk == nullptr)) return GOOSE_ERR_ARG;
+  if (ld < (size_t)(c->Hq + 2 * c->Hkv) || (ld & 3) || (split_stride & 3) || ldq < (size_t)c->Hq * q_terms || (ldq & 7)) return GOOSE_ERR_ARG;
+  if (((uintptr_t)d_qkv & 15) || ((uintptr_t)d_q & 15)) return GOOSE_ERR_ARG;
+  PagedReqs rq;
+  rc = paged_reqs(c, pg, reqs, n, true, &rq, [](const goose_paged_request& q) -> const void* { return q.d_pos; });
+  if (rc) return rc;
+  return launch_rope_paged(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, c->inv_freq, c->d.rms_eps, d_qkv, ksplit, split_stride,
+                           ld, d_gq, d_gk, rq, d_q, ldq, q_terms, c->flags, as_stream(stream));
+}
+
+int goose_attn_paged(goose_ctx* c, const goose_pages* pg, int layer, const void* d_q, size_t ldq, int q_terms, const goose_paged_request* reqs,
+                     int n, int shared_pages, void* d_o, size_t ldo, int o_dtype, int o_terms, void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  if (!d_q || !d_o || layer < 0 || layer >= c->d.n_layers || !is16(o_dtype)) return GOOSE_ERR_ARG;
+  if ((q_terms != 1 && q_terms != 2) || (o_terms != 1 && o_terms != 2)) return GOOSE_ERR_ARG;
+  if (ldq < (size_t)c->Hq * q_terms || (ldq & 7) || ldo < (size_t)c->Hq * o_terms || (ldo & 7)) return GOOSE_ERR_ARG;
+  if (((uintptr_t)d_q & 15) || ((uintptr_t)d_o & 15)) return GOOSE_ERR_ARG;
+  PagedReqs rq;
+  rc = paged_reqs(c, pg, reqs, n, true, &rq, [](const goose_paged_request& q) -> const void* { return q.d_mask; });
+  if (!rc) rc = check_shared(pg, rq, shared_pages);
+  if (rc) return rc;
+  return launch_attn_paged(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, d_q, ldq, q_terms, rq, shared_pages, c->att_o, c->att_ml,
+                           attn_records(c), d_o, ldo, o_dtype, o_terms, c->flags, as_stream(stream));
+}
+
+int goose_verify_layer_paged(goose_ctx* c, const void* d_packed_layer, const goose_pages* pg, int layer, float* d_x,
+                             const goose_paged_request* reqs, int n, int shared_pages, void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  if (!d_packed_layer || !d_x || layer < 0 || layer >= c->d.n_layers) return GOOSE_ERR_ARG;
+  PagedPass pass;
+  pass.pages = pg;
+  pass.layer = layer;
+  pass.shared_pages = shared_pages;
+  rc = paged_reqs(c, pg, reqs, n, true, &pass.pos, [](const goose_paged_request& q) -> const void* { return q.d_pos; });
+  if (!rc) rc = paged_reqs(c, pg, reqs, n, true, &pass.mask, [](const goose_paged_request& q) -> const void* { return q.d_mask; });
+  if (!rc) rc = check_shared(pg, pass.mask, shared_pages);
+  if (rc) return rc;
+  int rows = pass.pos.r[n - 1].row0 + reqs[n - 1].B;
+  if (n > 1) rows = round_up(rows, 32);
+  return layer_impl(c, (const char*)d_packed_layer, d_x, nullptr, nullptr, 0, nullptr, rows, nullptr, as_stream(stream), false, nullptr, nullptr,
+                    nullptr, 0, &pass);
+}
+
+int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose_pages* pg, const goose_paged_request* reqs, int n,
+                            int shared_pages, int32_t* d_argmax_all, void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  if (!m || !d_argmax_all || !m->d_embed || !m->d_packed_layers || !m->d_packed_head) return GOOSE_ERR_ARG;
+  hipStream_t st = as_stream(stream);
+  const goose_model_desc& d = c->d;
+  PagedPass pass;
+  pass.pages = pg;
+  pass.shared_pages = shared_pages;
+  rc = paged_reqs(c, pg, reqs, n, true, &pass.pos, [](const goose_paged_request& q) -> const void* {
+    const bool all = q.d_tokens && q.d_parent && q.d_accept_len && q.d_path && q.d_bonus;
+    const bool tables = (q.d_succ_ids_or_null == nullptr) == (q.d_succ_scores_or_null == nullptr) &&
+                        (!q.d_succ_ids_or_null || (q.harvest_k >= 1 && q.harvest_k <= 16));
+    return all && tables ? q.d_path : nullptr;
+  });
+  if (!rc) rc = check_shared(pg, pass.pos, shared_pages);
+  if (rc) return rc;
+  pass.mask = pass.pos;
+  PagedReqs commit = pass.pos;
+  SeqList seqs{};
+  BatchReq br[GOOSE_MAX_REQUESTS];
+  HarvestArgs hv;
+  int rows = 0, b_max = 0;
+  seqs.n = n;
+  for (int r = 0; r < n; ++r) {
+    const goose_paged_request& q = reqs[r];
+    seqs.seq[r] = q.seq;
+    seqs.extra[r] = q.B;
+    rows = pass.pos.r[r].row0;
+    pass.pos.r[r].p = c->s_pos + rows;
+    pass.mask.r[r].p = c->s_mask + (size_t)rows * 2;
+    br[r] = BatchReq{q.d_tokens, q.d_parent, q.d_is_spine, q.B, rows, q.P_max, nullptr, nullptr, pg->d_len + q.seq,
+                     q.d_accept_len, q.d_path, q.d_bonus, q.d_next_root_or_null};
+    if (q.d_succ_ids_or_null)
+      hv.req[hv.n++] = HarvestReq{q.d_tokens, q.d_succ_ids_or_null, q.d_succ_scores_or_null, q.B, rows, q.harvest_k};
+    b_max = q.B > b_max ? q.B : b_max;
+    rows += round_up(q.B, 32);
+  }
+  rc = launch_pages_reserve(*pg, seqs, d.n_layers, c->n_kv, d.head_dim, c->page_copies, c->flags, st);
+  if (rc) return rc;
+  rc = launch_batch_begin(d.dtype, br, n, b_max, m->d_embed, d.hidden, d.vocab, c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags,
+                          pg->table_ld * GOOSE_PAGE, st);
+  if (rc) return rc;
+  for (int l = 0; l < d.n_layers; ++l) {
+    const char* w = (const char*)m->d_packed_layers + (size_t)l * c->pl.total;
+    const void* g_next = (l + 1 < d.n_layers) ? (const void*)(w + c->pl.total + c->pl.g1)
+                                              : (const void*)((const char*)m->d_packed_head + c->ph.gf);
+    pass.layer = l;
+    rc = layer_impl(c, w, c->s_x, nullptr, nullptr, 0, nullptr, rows, nullptr, st, l > 0, g_next, nullptr, nullptr, 0, &pass);
+    if (rc) return rc;
+  }
+  rc = lm_head_impl(c, m->d_packed_head, c->s_x, rows, d_argmax_all, nullptr, nullptr, st, true, hv);
+  if (rc) return rc;
+  rc = launch_batch_accept(br, n, d_argmax_all, st);
+  if (rc) return rc;
+  return launch_pages_commit(*pg, commit, d.n_layers, c->n_kv, d.head_dim, c->flags, st);
 }
 
 // ---- the LM head without a context: its workspace is a static device array --------------------

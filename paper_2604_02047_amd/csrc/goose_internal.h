@@ -66,7 +66,7 @@ struct goose_ctx {
   void* xn;        // T [Bpad][ld_xn] normalised activations (GEMM operand; 16-bit models, as part, att_o and att_ml)
   float* part;     // f32 [max_ksplit][Bpad][part_ld]   split-K partials
   size_t part_ld;  // row length of `part`
-  void* q;         // f32 [Bpad][Kq]  rotated queries (fp32 models)
+  void* q;         // rotated queries: f32 [Bpad][Kq] (fp32 models); T [Bpad][2 Kq], passes on a paged cache (16-bit models)
   void* o;         // T [Bpad][ld_o] attention output (GEMM operand)
   void* h;         // T [Bpad][ld_h] SwiGLU output (GEMM operand)
   float* att_o;    // f32 [n_heads][max_splits][Bpad][head_dim]
@@ -83,6 +83,7 @@ struct goose_ctx {
   float* s_x;        // [Bpad][hidden]
   int32_t* flags;    // [1]
   int32_t* s_P;      // [GOOSE_MAX_REQUESTS] a host-supplied P for kernels that read it from memory; the old lengths while a step commits
+  void* page_copies; // int4 [GOOSE_MAX_REQUESTS] what a reservation of pages has to copy (16-bit models)
   goose_prof* prof;  // optional per-kernel event timing
 };
 
@@ -133,6 +134,8 @@ int launch_batch_begin(int dtype, const BatchReq* reqs, int n, int max_B, const 
 // walk, new cache length and compaction of all requests (2 launches); P_old: scratch for the n old lengths
 int launch_batch_end(const BatchReq* reqs, int n, const int32_t* argmax_all, int n_layers, int n_kv_heads, int cap,
                      int head_dim, int32_t* P_old, int32_t* flags, hipStream_t st);
+// the walks alone (lengths stay as they are)
+int launch_batch_accept(const BatchReq* reqs, int n, const int32_t* argmax_all, hipStream_t st);
 int launch_compact(int elem_bytes, void* kall, void* vall, int n_layers, int n_heads, int cap, int head_dim,
                    const int32_t* dP, const int32_t* path, const int32_t* accept_len, int32_t* new_P, int32_t* flags,
                    hipStream_t st);
@@ -264,3 +267,39 @@ int launch_attn_16(int dtype, const float* part, int ks, size_t part_stride, siz
                    float* att_ml, int Bpad, void* o, int ldo, int oterms, int o_dtype, int32_t* flags, hipStream_t st,
                    int* left = nullptr);
 int pick_attn_splits(int n_heads, int keys_max, int max_splits);
+
+// ---- paged caches (pages.hip, rope_paged.hip, attn_paged.hip; 16-bit types)
+enum { PAGES_PER_CALL = 4096 };  // pages that one reservation may take
+// A request of a paged call as the kernels see it.
+struct PagedReq {
+  int32_t seq, B, P_max;
+  int32_t row0;  // its first row of the stacked buffers (multiples of 32)
+  int32_t c0;    // its first row when the rows between requests are left out
+  const void* p; // mask (attention), positions (rotation), path (commit)
+  const int32_t* accept_len;
+};
+struct PagedReqs {
+  int32_t n, rows;  // requests; their nodes in all
+  PagedReq r[GOOSE_MAX_REQUESTS];
+};
+struct SeqList {
+  int32_t n;
+  int32_t seq[GOOSE_MAX_REQUESTS], extra[GOOSE_MAX_REQUESTS];
+};
+int launch_pages_clear(const goose_pages& pg, hipStream_t st);
+int launch_pages_fork(const goose_pages& pg, int src, int len, const SeqList& dst, int32_t* flags, hipStream_t st);
+int launch_pages_reserve(const goose_pages& pg, const SeqList& seqs, int n_layers, int n_kv, int head_dim, void* copies, int32_t* flags,
+                         hipStream_t st);
+int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, int32_t* flags, hipStream_t st);
+int launch_pages_free(const goose_pages& pg, const SeqList& seqs, int32_t* flags, hipStream_t st);
+// base of one layer's part of a pool, in elements
+static inline size_t page_layer_elems(const goose_pages& pg, int n_kv, int head_dim) {
+  return (size_t)pg.n_pages * n_kv * GOOSE_PAGE * head_dim;
+}
+int launch_rope_paged(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const double* inv_freq, float eps,
+                      const float* part, int ks, size_t split_stride, size_t ld, const void* gq, const void* gk, const PagedReqs& rq,
+                      void* q, size_t ldq, int q_terms, int32_t* flags, hipStream_t st);
+// ws_o: f32 [records][head_dim], ws_ml: f32 [records][2]; max_records of them
+int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
+                      const PagedReqs& rq, int shared_pages, float* ws_o, float* ws_ml, size_t max_records, void* o, size_t ldo,
+                      int o_dtype, int o_terms, int32_t* flags, hipStream_t st);

@@ -903,6 +903,14 @@ int launch_batch_end(const BatchReq* reqs, int n, const int32_t* argmax_all, int
   return goose_launch_status();
 }
 
+int launch_batch_accept(const BatchReq* reqs, int n, const int32_t* argmax_all, hipStream_t st) {
+  if (n < 1 || n > GOOSE_MAX_REQUESTS) return GOOSE_ERR_ARG;
+  ReqTable t = req_table(reqs, n);
+  for (int r = 0; r < n; ++r) t.r[r].dP = nullptr;  // (no length is read or written)
+  hipLaunchKernelGGL(k_accept_batch, dim3(n), dim3(128), 0, st, t, argmax_all, (int32_t*)nullptr, 0, (int32_t*)nullptr);
+  return goose_launch_status();
+}
+
 int launch_accept(const int32_t* parent, const int32_t* tokens, const uint8_t* is_spine, const int32_t* argmax, int B,
                   int32_t* accept_len, int32_t* path, int32_t* bonus, int32_t* next_root, int32_t* dP, int32_t* P_old, int cap,
                   int32_t* flags, hipStream_t st) {

@@ -1,0 +1,301 @@
+"""goose_attn_paged against 64-bit attention: head layouts, lengths, shared prefixes, masks, and what lies behind them.
+
+Error bound of one output, u = half a step of the cache's type, u_o of the output's: with A = sum p |v| / sum p,
+  * probabilities are rounded to 16 bits before the second product: u A (fp16: and 2^-25 each below its normals, sum|v| 2^-25 in all, as the
+    largest probability of a row is one in the item that holds it and every rescale only shrinks both);
+  * a score errs by (d + 4) 2^-24 sum|q||k| / sqrt(d) (products exact in 32 bits, d additions, scale), which moves a probability by the same relative
+    amount and the quotient by twice that: 2 A (d + 4) 2^-24 max sum|q||k|/sqrt(d); exponentials and rescales add 2^-20 A;
+  * sums over N keys: N 2^-24 A, twice;
+  * the store: u_o |o| (two terms: u_o^2), fp16 2^-25.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_02047_amd as goose
+from paper_2604_02047_amd import binding as gb
+from paged_ref import PAGE, attention64, mask_words, pack_pages, rows_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = {torch.bfloat16: torch.finfo(torch.bfloat16).eps / 2, torch.float16: torch.finfo(torch.float16).eps / 2}
+
+
+def parents(B, rng):
+    return [-1] + [int(rng.integers(0, i)) if rng.random() < 0.5 else i - 1 for i in range(1, B)]
+
+
+class Case:
+    def __init__(self, nh, nkv, d, dtype, Bs, Ps, S, seed=0, terms=1, o_dtype=torch.float16, o_terms=1, layers=1, layer=0, scale=1.5):
+        self.__dict__.update(locals())
+        rng, g = np.random.default_rng(seed), torch.Generator().manual_seed(seed)
+        self.dt = dt = torch.bfloat16 if dtype == "bf16" else torch.float16
+        n_sh = S // PAGE
+        counts = [(p + b + PAGE - 1) // PAGE for p, b in zip(Ps, Bs)]
+        self.width, n_pages = max(counts) + 1, n_sh + sum(c - n_sh for c in counts) + 2
+        order = torch.randperm(n_pages, generator=g).tolist()
+        self.table, self.refs, at = np.full((len(Bs), self.width), -1, np.int32), np.zeros(n_pages, np.int32), n_sh
+        for r, c in enumerate(counts):
+            row = order[:n_sh] + order[at:at + c - n_sh]
+            at += c - n_sh
+            self.table[r, :c] = row
+            self.refs[row] += 1
+        self.k = torch.randn((layers, n_pages, nkv, PAGE, d), generator=g).to(dt)
+        self.v = torch.randn((layers, n_pages, nkv, PAGE, d), generator=g).to(dt)
+        self.rows = sum((b + 31) // 32 * 32 for b in Bs)
+        self.q32 = torch.randn((self.rows, nh, d), generator=g) * scale
+        self.masks = [mask_words(parents(b, rng)) for b in Bs]
+
+    def q_rows(self):
+        hi = self.q32.to(self.dt)
+        if self.terms == 1:
+            return hi.reshape(self.rows, -1), hi.double()
+        lo = (self.q32 - hi.float()).to(self.dt)
+        n = self.nh * self.d
+        both = torch.stack((hi.view(self.rows, n // 8, 8), lo.view(self.rows, n // 8, 8)), 2)
+        return both.reshape(self.rows, 2 * n), hi.double() + lo.double()
+
+    def run(self, S=None, flags=0):
+        S = self.S if S is None else S
+        q, self.q64 = self.q_rows()
+        desc = goose.ModelDesc(self.layers, 128, self.nh, self.d, 128, 1024, dtype=self.dtype, n_kv_heads=self.nkv)
+        ctx = goose.GooseContext(desc, max(self.Bs), 256, 512)
+        kp, vp = pack_pages(self.k, self.v)
+        self.cache = goose.PagedCache(kp.to(DEV), vp.to(DEV), torch.from_numpy(self.table).to(DEV),
+                                      torch.tensor(self.Ps, dtype=torch.int32, device=DEV), torch.from_numpy(self.refs).to(DEV))
+        o = torch.full((self.rows, self.nh * self.d * self.o_terms + 8), 77.0, dtype=self.o_dtype, device=DEV)
+        reqs = [{"seq": r, "B": b, "P_max": p, "mask": self.masks[r][0].to(DEV)} for r, (b, p) in enumerate(zip(self.Bs, self.Ps))]
+        ctx.goose_attn_paged(self.cache, self.layer, q.to(DEV), self.terms, reqs, S // PAGE, o, self.o_terms)
+        assert ctx.goose_device_flags() == flags
+        ctx.close()
+        o = o.cpu()
+        assert (o[:, self.nh * self.d * self.o_terms:] == 77).all()
+        return o[:, :self.nh * self.d * self.o_terms]
+
+    def check(self, o, nodes=None):
+        at, N = 0, self.nh * self.d
+        u, uo = U[self.dt], U[self.o_dtype] ** self.o_terms
+        for r, (B, P) in enumerate(zip(self.Bs, self.Ps)):
+            k = rows_of(self.k[self.layer], self.table[r], P + B).double()
+            v = rows_of(self.v[self.layer], self.table[r], P + B).double()
+            pick = list(range(B)) if nodes is None or B <= nodes else sorted({0, B - 1, *range(1, B, max(1, B // nodes))})
+            see = np.concatenate([np.ones((B, P), bool), self.masks[r][1]], 1)
+            want, A, qk, vs = attention64(self.q64[at:at + B][pick], k, v, torch.from_numpy(see[pick]))
+            got = o[at:at + B].double()
+            if self.o_terms == 2:
+                got = got.view(B, N // 8, 2, 8).sum(2)
+            got = got.reshape(B, self.nh, self.d)[pick]
+            tol = A * (u + 2 * (self.d + 4) * 2.0 ** -24 * qk.unsqueeze(-1) + 2.0 ** -20 + 2 * (P + B) * 2.0 ** -24) + uo * want.abs() + 2.0 ** -25
+            if self.dt == torch.float16:
+                tol = tol + vs * 2.0 ** -25
+            bad = ~((got - want).abs() <= tol * 1.001) & ~(want.isnan() & got.isnan())
+            assert not bad.any(), (r, bad.nonzero()[0].tolist(), float(got[bad][0]), float(want[bad][0]), float(tol[bad][0]))
+            assert (o[at + B:at + (B + 31) // 32 * 32] == 77).all(), "rows between requests"
+            at += (B + 31) // 32 * 32
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("terms", [1, 2])
+def test_types_and_terms(dtype, d, terms):
+    for o_dtype, o_terms in ((torch.float16, 1), (torch.bfloat16, 2)):
+        c = Case(4, 2, d, dtype, [21, 1, 40], [130, 128, 261], 128, seed=1, terms=terms, o_dtype=o_dtype, o_terms=o_terms)
+        c.check(c.run())
+
+
+@pytest.mark.parametrize("nh,nkv,Bs,Ps,S", [
+    (1, 1, [1], [0], 0), (1, 1, [1], [1], 0), (2, 1, [2], [63], 0), (4, 4, [1], [64], 64), (14, 2, [1, 3], [65, 127], 64), (40, 1, [5], [200], 0),
+    (8, 2, [128], [0], 0), (8, 8, [128, 65], [31, 700], 0), (8, 2, [32] * 16, [192 + 7 * i for i in range(16)], 192),
+    (8, 1, [1] * 16, [320 + i for i in range(16)], 320), (6, 3, [64, 64, 33], [127, 128, 129], 0), (4, 4, [1, 128, 1], [64, 64, 64], 64),
+])
+def test_head_layouts_and_lengths(nh, nkv, Bs, Ps, S):
+    for d, dtype in ((128, "bf16"), (64, "f16")):
+        c = Case(nh, nkv, d, dtype, Bs, Ps, S, seed=nh + len(Bs))
+        c.check(c.run(), nodes=9)
+
+
+def test_the_result_does_not_depend_on_the_sharing():
+    """The same tables with 0 to 5 of the common pages given as shared."""
+    c = Case(8, 2, 128, "bf16", [9, 30, 1], [320, 350, 401], 320, seed=5)
+    for S in (0, 64, 192, 320):
+        c.check(c.run(S), nodes=6)
+
+
+def test_long_prefix_over_many_pages():
+    """A prefix of several splits, each wavefront crossing more than 64 pages."""
+    c = Case(32, 32, 128, "f16", [32] * 16, [20480 + 3 * i for i in range(16)], 20480, seed=6, layers=1)
+    o = c.run()
+    # two requests, a few rows and heads of the whole (the 64-bit form of all of it would take minutes)
+    k = c.k[0][torch.as_tensor(c.table[7, :(c.Ps[7] + 32 + 63) // 64].astype(np.int64))]
+    v = c.v[0][torch.as_tensor(c.table[7, :(c.Ps[7] + 32 + 63) // 64].astype(np.int64))]
+    N = c.Ps[7] + 32
+    for h in (0, 13, 31):
+        kk, vv = k[:, h].reshape(-1, 128)[:N].double(), v[:, h].reshape(-1, 128)[:N].double()
+        see = torch.from_numpy(np.concatenate([np.ones((32, c.Ps[7]), bool), c.masks[7][1]], 1))
+        s = c.q64[7 * 32:8 * 32, h] @ kk.t().contiguous() / math.sqrt(128)
+        p = torch.softmax(s.masked_fill(~see, -math.inf), 1)
+        want = p @ vv
+        qk = (c.q64[7 * 32:8 * 32, h].abs() @ kk.abs().t().contiguous()).max() / math.sqrt(128)
+        tol = (p @ vv.abs()) * (U[torch.float16] + 2 * 132 * 2.0 ** -24 * qk + 2.0 ** -20 + 2 * N * 2.0 ** -24) + want.abs() * 2.0 ** -11 \
+            + 2.0 ** -25 + vv.abs().sum(0) * 2.0 ** -25
+        got = o[7 * 32:8 * 32].view(32, 32, 128)[:, h].double()
+        assert ((got - want).abs() <= tol).all()
+
+
+def test_scores_far_apart():
+    """Scores of thousands, a running maximum that grows with every block, and one key that takes all the weight."""
+    c = Case(4, 2, 128, "bf16", [17], [500], 0, seed=7, scale=200.0)
+    c.check(c.run(), nodes=6)
+    c = Case(2, 1, 64, "f16", [3], [256], 64, seed=8)
+    ramp = torch.arange(256 + 3, dtype=torch.float32) * 0.2
+    for i in range(259):
+        c.k[0, c.table[0, i // 64], 0, i % 64] = ramp[i] * c.q32[0, 0].sign()
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_what_lies_behind_a_mask_has_no_effect(junk, dtype):
+    """Slots behind the tree, siblings' keys and values, mask bits beyond the tree."""
+    for d, Bs, Ps in ((128, [20, 70], [40, 100]), (64, [3, 33], [0, 31])):
+        c = Case(4, 2, d, dtype, Bs, Ps, 0, seed=9)
+        for r, (B, P) in enumerate(zip(Bs, Ps)):
+            for s in range(P + B, (P + B + 63) // 64 * 64):
+                c.k[0, c.table[r, s // 64], :, s % 64] = junk
+                c.v[0, c.table[r, s // 64], :, s % 64] = junk
+            # node 1 is a leaf that only itself sees
+            see = c.masks[r][1]
+            see[2:, 1] = False
+            words = np.zeros((B, (B + 63) // 64), np.uint64)
+            for i in range(B):
+                for j in np.nonzero(see[i])[0]:
+                    words[i, j // 64] |= np.uint64(1) << np.uint64(j % 64)
+                if B % 64:
+                    words[i, -1] |= ~np.uint64(0) << np.uint64(B % 64)  # bits beyond the tree
+            c.masks[r] = (torch.from_numpy(words.view(np.int64)), see)
+            s = P + 1
+            c.v[0, c.table[r, s // 64], :, s % 64, ::3] = junk
+            c.k[0, c.table[r, s // 64], :, s % 64, 5] = junk
+        o = c.run()
+        # rows that see node 1: itself.  Its own row is what IEEE arithmetic makes of it; all others are finite and right
+        at = 0
+        for B in Bs:
+            c.q64[at + 1] = 0
+            at += (B + 31) // 32 * 32
+        at = 0
+        for r, (B, P) in enumerate(zip(Bs, Ps)):
+            keep = [i for i in range(B) if i != 1]
+            k = rows_of(c.k[0], c.table[r], P + B).double()
+            v = rows_of(c.v[0], c.table[r], P + B).double()
+            see = np.concatenate([np.ones((B, P), bool), c.masks[r][1]], 1)[keep]
+            want, A, qk, vs = attention64(c.q64[at:at + B][keep], k, v, torch.from_numpy(see))
+            got = o[at:at + B].double().view(B, 4, d)[keep]
+            u = U[c.dt]
+            tol = A * (u + 2 * (d + 4) * 2.0 ** -24 * qk.unsqueeze(-1) + 2.0 ** -20 + (P + B) * 2.0 ** -23) + want.abs() * 2.0 ** -11 + 2.0 ** -25 + vs * 2.0 ** -25
+            assert ((got - want).abs() <= tol).all(), (r, d)
+            at += (B + 31) // 32 * 32
+
+
+def test_rows_that_see_nothing_and_visible_infinities():
+    c = Case(4, 2, 64, "bf16", [5], [0], 0, seed=10)
+    c.masks[0] = (torch.tensor([[0], [2], [1], [0], [31]]), np.array([[0] * 5, [0, 1, 0, 0, 0], [1, 0, 0, 0, 0], [0] * 5, [1] * 5], bool))
+    o = c.run()
+    assert (o[0] == 0).all() and (o[3] == 0).all()
+    c.check(o)
+    # a key of -infinity scores for every query that sees it (one column, positive queries): no weight; with no other key, zero
+    c = Case(2, 2, 64, "f16", [2], [0], 0, seed=11)
+    c.masks[0] = (torch.tensor([[1], [3]]), np.array([[1, 0], [1, 1]], bool))
+    c.q32 = c.q32.abs() + 0.1
+    c.k[0, c.table[0, 0], :, 0, 3] = -float("inf")
+    o = c.run()
+    assert (o[0] == 0).all()
+    assert torch.equal(o[1].view(2, 64), c.v[0, c.table[0, 0], :, 1])  # the one key with weight
+    c.k[0, c.table[0, 0], :, 0, 3] = float("inf")
+    o = c.run()
+    assert o[:2].isnan().all()
+    c.k[0, c.table[0, 0], :, 0, 3] = float("nan")
+    assert c.run()[:2].isnan().all()
+
+
+def test_offsets_beyond_32_bits():
+    """A pool of more than 2^31 elements: the last pages of the last layer."""
+    nkv, d, n_pages = 32, 128, 4300
+    g = torch.Generator().manual_seed(12)
+    kp = torch.zeros((2, n_pages, nkv, PAGE * d), dtype=torch.bfloat16, device=DEV)
+    vp = torch.zeros_like(kp)
+    k = torch.randn((1, 3, nkv, PAGE, d), generator=g).to(torch.bfloat16)
+    v = torch.randn((1, 3, nkv, PAGE, d), generator=g).to(torch.bfloat16)
+    a, b = pack_pages(k, v)
+    kp[1, n_pages - 3:], vp[1, n_pages - 3:] = a[0].to(DEV), b[0].to(DEV)
+    c = Case(nkv, nkv, d, "bf16", [9], [150], 128, seed=13)
+    c.k, c.v = k, v
+    c.table, c.refs = np.array([[2, 0, 1, -1]], np.int32), np.ones(3, np.int32)
+    q, c.q64 = c.q_rows()
+    ctx = goose.GooseContext(goose.ModelDesc(2, 128, nkv, d, 128, 1024, n_kv_heads=nkv), 32, 256, 512)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    table = torch.tensor([[n_pages - 1, n_pages - 3, n_pages - 2, -1]], **i32)
+    cache = goose.PagedCache(kp, vp, table, torch.tensor([150], **i32), torch.ones(n_pages, **i32))
+    o = torch.full((32, nkv * d), 77.0, dtype=torch.float16, device=DEV)
+    ctx.goose_attn_paged(cache, 1, q.to(DEV), 1, [{"seq": 0, "B": 9, "P_max": 150, "mask": c.masks[0][0].to(DEV)}], 2, o)
+    assert ctx.goose_device_flags() == 0
+    c.check(o.cpu())
+    ctx.close()
+
+
+def test_bad_tables_and_lengths_are_flagged():
+    c = Case(4, 2, 64, "bf16", [3, 4], [70, 75], 64, seed=14)
+    c.table[1, 0] = c.table[1, 1]  # not the shared page
+    c.run(flags=gb.GOOSE_FLAG_PAGES)
+    c = Case(4, 2, 64, "bf16", [3, 4], [70, 75], 64, seed=15)
+    c.table[1, 1] = 99
+    c.run(flags=gb.GOOSE_FLAG_PAGES)
+    c = Case(4, 2, 64, "bf16", [3], [70], 0, seed=16)
+    q, _ = c.q_rows()
+    c.run()
+    ctx = goose.GooseContext(goose.ModelDesc(1, 128, 4, 64, 128, 1024, n_kv_heads=2), 32, 256, 512)
+    o = torch.full((32, 256), 77.0, dtype=torch.float16, device=DEV)
+    req = [{"seq": 0, "B": 3, "P_max": 69, "mask": c.masks[0][0].to(DEV)}]
+    ctx.goose_attn_paged(c.cache, 0, q.to(DEV), 1, req, 0, o)
+    assert ctx.goose_device_flags() == gb.GOOSE_FLAG_CAPACITY
+    req[0]["P_max"] = 100  # a bound above the length is what it is for
+    ctx.goose_attn_paged(c.cache, 0, q.to(DEV), 1, req, 0, o)
+    assert ctx.goose_device_flags() == 0
+    c.check(o.cpu())
+    ctx.close()
+
+
+def test_a_captured_call_follows_the_lengths():
+    """One graph, replayed while the device-resident length grows, with eager calls of the same context in between."""
+    c = Case(8, 2, 128, "bf16", [12, 6], [64, 70], 64, seed=17)
+    long = Case(8, 2, 128, "bf16", [12, 6], [250, 300], 64, seed=17)
+    q, q64 = long.q_rows()
+    long.q64 = q64
+    desc = goose.ModelDesc(1, 128, 8, 128, 128, 1024, n_kv_heads=2)
+    ctx = goose.GooseContext(desc, 32, 256, 512)
+    kp, vp = pack_pages(long.k, long.v)
+    length = torch.tensor([64, 70], dtype=torch.int32, device=DEV)
+    cache = goose.PagedCache(kp.to(DEV), vp.to(DEV), torch.from_numpy(long.table).to(DEV), length, torch.from_numpy(long.refs).to(DEV))
+    o = torch.zeros((64, 1024), dtype=torch.float16, device=DEV)
+    qd = q.to(DEV)
+    reqs = goose.PagedRequests([{"seq": r, "B": b, "P_max": 300, "mask": long.masks[r][0].to(DEV)} for r, b in enumerate([12, 6])])
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        ctx.goose_attn_paged(cache, 0, qd, 1, reqs, 1, o)
+    for Ps in ([64, 70], [100, 64], [250, 300], [127, 128]):
+        length.copy_(torch.tensor(Ps, dtype=torch.int32))
+        o.fill_(77.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        first = o.clone()
+        long.Ps = Ps
+        long.check(first.cpu())
+        ctx.goose_attn_paged(cache, 0, qd, 1, reqs, 1, o)
+        torch.cuda.synchronize()
+        assert torch.equal(first, o)  # the same launch, the same order of sums
+    assert ctx.goose_device_flags() == 0 and c is not None
+    ctx.close()

@@ -1,0 +1,85 @@
+"""Paged caches without a GPU: what the binding and the entry points refuse before anything is launched, and the simulator itself."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_02047_amd as goose
+from paper_2604_02047_amd import binding as gb
+from paged_ref import PAGE, PageSim, mask_words, pack_pages, unpack_pages
+
+
+def tensors(**kw):
+    t = {"kpool": torch.zeros((2, 7, 3, 64 * 64), dtype=torch.bfloat16), "vpool": torch.zeros((2, 7, 3, 64 * 64), dtype=torch.bfloat16),
+         "table": torch.zeros((4, 5), dtype=torch.int32), "len": torch.zeros(4, dtype=torch.int32), "refs": torch.zeros(7, dtype=torch.int32)}
+    t.update(kw)
+    return t
+
+
+def test_the_cache_checks_its_tensors():
+    goose.PagedCache(**tensors())
+    bad = [dict(vpool=torch.zeros((2, 7, 3, 64 * 128), dtype=torch.bfloat16)), dict(vpool=torch.zeros((2, 7, 3, 64 * 64), dtype=torch.float16)),
+           dict(kpool=torch.zeros((2, 7, 3, 64 * 64)), vpool=torch.zeros((2, 7, 3, 64 * 64))), dict(table=torch.zeros((4, 5))),
+           dict(len=torch.zeros(3, dtype=torch.int32)), dict(refs=torch.zeros(8, dtype=torch.int32)),
+           dict(table=torch.zeros((5, 4), dtype=torch.int32).t())]
+    for b in bad:
+        with pytest.raises(goose.GooseError) as e:
+            goose.PagedCache(**tensors(**b))
+        assert e.value.status == gb.GOOSE_ERR_ARG
+
+
+def test_entry_points_refuse_a_missing_context():
+    lib = goose.load_library()
+    import ctypes as C
+    pages = C.byref(goose.PagedCache(**tensors())._c)
+    s = gb._seqs([0])
+    r = goose.PagedRequests([{"seq": 0, "B": 1}])._c
+    assert lib.goose_pages_clear(None, pages, None) == -1
+    assert lib.goose_pages_fork(None, pages, 1, -1, s, 1, None) == -1
+    assert lib.goose_pages_reserve(None, pages, s, s, 1, None) == -1
+    assert lib.goose_pages_commit(None, pages, r, 1, None) == -1
+    assert lib.goose_pages_free(None, pages, s, 1, None) == -1
+    assert lib.goose_qk_norm_rope_paged(None, pages, 0, None, 1, 4, 4, None, None, r, 1, None, 8, 1, None) == -1
+    assert lib.goose_attn_paged(None, pages, 0, None, 8, 1, r, 1, 0, None, 8, 0, 1, None) == -1
+    assert lib.goose_verify_layer_paged(None, None, pages, 0, None, r, 1, 0, None) == -1
+    assert lib.goose_verify_step_paged(None, None, pages, r, 1, 0, None, None) == -1
+
+
+def test_request_structs_match_the_header(tmp_path):
+    """Size and field offsets of the two descriptors as a C compiler lays them out."""
+    import ctypes as C
+    import os
+    import shutil
+    import subprocess
+    gcc = shutil.which("gcc")
+    if gcc is None:
+        pytest.skip("no gcc")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = [("goose_pages", gb._Pages), ("goose_paged_request", gb._PagedRequest)]
+    body = "".join(f'printf("%zu ", sizeof({c}));' + "".join(f'printf("%zu ", offsetof({c}, {f[0]}));' for f in t._fields_) for c, t in names)
+    src = tmp_path / "o.c"
+    src.write_text('#include <stdio.h>\n#include "goose.h"\nint main(void){' + body + "return 0;}\n")
+    subprocess.run([gcc, "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "o")], check=True)
+    got = [int(x) for x in subprocess.run([str(tmp_path / "o")], capture_output=True, text=True).stdout.split()]
+    want = []
+    for _, t in names:
+        want += [C.sizeof(t)] + [getattr(t, f[0]).offset for f in t._fields_]
+    assert got == want
+
+
+def test_simulator_and_layout():
+    k = torch.arange(2 * 3 * 1 * PAGE * 64, dtype=torch.float32).view(2, 3, 1, PAGE, 64)
+    kp, vp = pack_pages(k, -k)
+    a, b = unpack_pages(kp, vp, 64)
+    assert torch.equal(a, k) and torch.equal(b, -k)
+    s = PageSim(4, 3, 5)
+    assert s.reserve([0], [70]) == 0 and list(s.table[0]) == [0, 1, -1]
+    s.len[0] = 70
+    assert s.fork(0, [1, 2]) == 0 and list(s.refs) == [3, 3, 0, 0, 0]
+    assert s.reserve([1, 2, 0], [1, 60, 1]) == 0
+    assert list(s.table[1]) == [0, 2, -1] and list(s.table[2]) == [0, 3, 4] and list(s.table[0]) == [0, 1, -1]
+    assert list(s.refs) == [3, 1, 1, 1, 1] and s.reserve([3], [1]) == 16
+    s.free([2])
+    assert list(s.refs) == [2, 1, 1, 0, 0]
+    words, see = mask_words([-1, 0, 1, 0])
+    assert words.tolist() == [[1], [3], [7], [9]] and see[3].tolist() == [True, False, False, True]
+    assert np.array_equal(see, np.tril(see))
