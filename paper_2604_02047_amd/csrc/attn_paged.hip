@@ -11,6 +11,9 @@
 // 32-wide matrix-instruction tiles: a single token of a grouped-query model fills 4 of 32 columns with its four heads,
 // and sixteen of them share two tiles over the common prefix.  Per 32 keys and 32 rows, as in the contiguous attention:
 // S^T = K Q^T, online softmax with two lanes a row, O^T += V^T P^T, operands straight from the pages' operand order.
+// Under bf16 the probabilities keep two terms for the second product (hi + lo, 2^-17): the output goes on as fp16 or in two terms, and
+// one term of 8 bits would be its largest error by far (16 requests x 1 over 8192 slots: 0.00085 of the output's size, now 0.00021 as
+// the output's own rounding).  fp16 ones have 11 bits and one term.
 #include "mma16.h"
 #include "paged.h"
 
@@ -47,6 +50,7 @@ struct PagedAttnArgs {
   size_t ldq, ldo;
   int32_t table_ld, n_pages, n_heads, n_kv, group, rows, n_req;
   int32_t sh_blocks, sh_tiles, sh_splits;  // shared keys: 32-slot blocks, row tiles, splits
+  int32_t sh_kg, own_kg;                   // k_paged_tiles: key groups of either kind of item
   int32_t direct;                          // every row has one item: it writes o itself
   int32_t o_terms, o_f16;
   AttnReq r[GOOSE_MAX_REQUESTS];
@@ -78,281 +82,678 @@ __device__ inline unsigned window16(uint64_t w0, uint64_t w1, int j0) {
   return (unsigned)x & 0xFFFFu;
 }
 
-// One workgroup = a tile of 32 rows x a range of 32-slot blocks, dealt to four wavefronts in contiguous quarters; every wavefront streams
-// its blocks global -> registers -> matrix cores (no barrier in the loop), the next block's keys and values requested as
-// soon as the current ones have been used.
-template <int D, int TERMS, bool F16>
-__global__ __launch_bounds__(256, 2) void k_attn_paged(const PagedAttnArgs a) {
-  typedef typename Mma16<F16>::T T;
-  typedef typename Mma16<F16>::v8 op8;
-  constexpr int NG = 4, NS = D / 16, QUADS = D / 8, QPW = QUADS / NG;
-  constexpr int WFLOATS = (QUADS + 1) * 256;  // a wavefront's state at the merge
-  constexpr int QL_BYTES = TERMS == 2 ? NS * 1024 : 0;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[NG * WFLOATS * 4 + QL_BYTES];
-  unsigned char* const ql_lds = lds + NG * WFLOATS * 4;
-  const int tid = threadIdx.x, lane = tid & 63, g = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l31 = lane & 31, hh = lane >> 5;
-  const int kvh = blockIdx.x;  // the fast index: where 8 divides the KV heads, all items of a head run on one XCD and find each other's blocks in its L2
-  // ---- the item
-  int y = blockIdx.y, tile, split, nsplit, rec_split, ri = 0, b_first, n_blocks, P = 0, B = 0;
-  const bool shared = y < a.sh_tiles * a.sh_splits;
-  if (shared) {
-    split = (int)((unsigned)y / (unsigned)a.sh_tiles);
-    tile = y - split * a.sh_tiles;
-    nsplit = a.sh_splits;
-    rec_split = split;
+// ---- work items -----------------------------------------------------------------------------------------------------
+struct Item {
+  int ri;        // its request; -1: the shared keys
+  int tile, split, nsplit, rec_split;
+  int seq, B, P; // of the request
+  int b_lo, b_hi;  // its 32-slot blocks, counted from the sequence's start
+  bool first;    // the first item of a request
+};
+__device__ inline Item item_of(const PagedAttnArgs& a, int y, int kvh) {
+  Item it;
+  int n_blocks, b_first;
+  it.ri = -1;
+  it.seq = a.r[0].seq;  // (shared keys: any request's table will do)
+  it.B = it.P = 0;
+  it.first = false;
+  if (y < a.sh_tiles * a.sh_splits) {
+    it.split = __builtin_amdgcn_readfirstlane((int)((unsigned)y / (unsigned)a.sh_tiles));
+    it.tile = y - it.split * a.sh_tiles;
+    it.nsplit = a.sh_splits;
+    it.rec_split = it.split;
     b_first = 0;
     n_blocks = a.sh_blocks;
   } else {
     y -= a.sh_tiles * a.sh_splits;
-    while (y >= a.r[ri].tiles * a.r[ri].splits) { y -= a.r[ri].tiles * a.r[ri].splits; ++ri; }
-    split = (int)((unsigned)y / (unsigned)a.r[ri].tiles);
-    tile = y - split * a.r[ri].tiles;
-    nsplit = a.r[ri].splits;
-    rec_split = a.sh_splits + split;
-    b_first = a.sh_blocks;
-    B = a.r[ri].B;
-    P = a.len[a.r[ri].seq];
-    const int S = a.sh_blocks * 32;
-    if ((P < S || P > a.r[ri].P_max) && tid == 0 && kvh == 0 && y == 0) atomicOr(a.flags, GOOSE_FLAG_CAPACITY);
-    P = min(max(P, S), a.r[ri].P_max);  // (P_max + B <= 64 table_ld, S <= P_max: checked on the host)
-    n_blocks = ((P + B + 31) >> 5) - b_first;
-  }
-  // ---- this lane's row
-  const int rho = tile * 32 + l31;
-  const int node = (int)((unsigned)rho / (unsigned)a.group), hg = rho - node * a.group;
-  int crow, row;
-  bool live;
-  if (shared) {
-    live = node < a.rows;
-    crow = live ? node : 0;
     int r = 0;
-    while (r + 1 < a.n_req && crow >= a.r[r + 1].c0) ++r;
-    row = a.r[r].row0 + crow - a.r[r].c0;
-  } else {
-    live = node < B;
-    crow = a.r[ri].c0 + (live ? node : 0);
-    row = a.r[ri].row0 + (live ? node : 0);
+    while (y >= a.r[r].tiles * a.r[r].splits) { y -= a.r[r].tiles * a.r[r].splits; ++r; }
+    it.ri = r;
+    it.first = y == 0 && kvh == 0;
+    it.split = __builtin_amdgcn_readfirstlane((int)((unsigned)y / (unsigned)a.r[r].tiles));
+    it.tile = y - it.split * a.r[r].tiles;
+    it.nsplit = a.r[r].splits;
+    it.rec_split = a.sh_splits + it.split;
+    it.seq = a.r[r].seq;
+    it.B = a.r[r].B;
+    it.P = __builtin_amdgcn_readfirstlane(a.len[it.seq]);
+    const int S = a.sh_blocks * 32;
+    if ((it.P < S || it.P > a.r[r].P_max) && it.first && threadIdx.x == 0) atomicOr(a.flags, GOOSE_FLAG_CAPACITY);
+    it.P = min(max(it.P, S), a.r[r].P_max);  // (P_max + B <= 64 table_ld, S <= P_max: checked on the host)
+    b_first = a.sh_blocks;
+    n_blocks = ((it.P + it.B + 31) >> 5) - b_first;
   }
-  const int h = kvh * a.group + hg;
-  // ---- the queries
-  op8 qf[NS];
-  {
-    const T* qp = static_cast<const T*>(a.q) + (size_t)row * a.ldq + (size_t)h * D * TERMS + hh * 8 * TERMS;
+  // (divisions go through vector registers: back to uniform ones)
+  it.b_lo = __builtin_amdgcn_readfirstlane(b_first + (int)((unsigned)(n_blocks * it.split) / (unsigned)it.nsplit));
+  it.b_hi = __builtin_amdgcn_readfirstlane(b_first + (int)((unsigned)(n_blocks * (it.split + 1)) / (unsigned)it.nsplit));
+  return it;
+}
+// The shared pages must be the same in all tables: one wavefront a request compares them with the first request's.
+__device__ inline void check_shared(const PagedAttnArgs& a, const Item& it, int lane) {
+  if (!it.first || it.ri <= 0) return;
+  const int32_t* t0 = a.table + (size_t)a.r[0].seq * a.table_ld;
+  const int32_t* t = a.table + (size_t)it.seq * a.table_ld;
+  bool differs = false;
+  for (int i = lane; i < a.sh_blocks / 2; i += 64) differs = differs || t[i] != t0[i];
+  if (differs) atomicOr(a.flags, GOOSE_FLAG_PAGES);
+}
+// Row rho of an item: (node, query head of the group), the heads fastest.
+struct Row {
+  bool live;
+  int node, crow, row, h;
+};
+__device__ inline Row row_of(const PagedAttnArgs& a, const Item& it, int rho, int kvh) {
+  Row w;
+  w.node = (int)((unsigned)rho / (unsigned)a.group);
+  w.h = kvh * a.group + rho - w.node * a.group;
+  if (it.ri < 0) {
+    w.live = w.node < a.rows;
+    w.crow = w.live ? w.node : 0;
+    int r = 0;
+    while (r + 1 < a.n_req && w.crow >= a.r[r + 1].c0) ++r;
+    w.row = a.r[r].row0 + w.crow - a.r[r].c0;
+  } else {
+    w.live = w.node < it.B;
+    const int n = w.live ? w.node : 0;
+    w.crow = a.r[it.ri].c0 + n;
+    w.row = a.r[it.ri].row0 + n;
+  }
+  return w;
+}
+// Page ids of consecutive blocks, 64 of them a register (one a lane); an entry out of range reads page 0 and is flagged.
+struct PageIds {
+  const int32_t* row;
+  int32_t* flags;
+  int base, last, n_pages, ids;
+  __device__ __forceinline__ void load(int lane) {
+    const int e = base + lane;
+    ids = e <= last ? row[e] : 0;
+    if ((unsigned)ids >= (unsigned)n_pages) { atomicOr(flags, GOOSE_FLAG_PAGES); ids = 0; }
+  }
+  // the id of block b's page; b never steps below the window, and block_last bounds it
+  __device__ __forceinline__ int of(int b, int lane) {
+    if ((b >> 1) - base >= 64) { base = b >> 1; load(lane); }
+    return __builtin_amdgcn_readlane(ids, (b >> 1) - base);
+  }
+};
+
+// An empty statement that takes and gives x: it is computed here, neither earlier nor later.
+#if defined(__HIP_DEVICE_COMPILE__)
+#define GOOSE_HERE(x) asm volatile("" : "+v"(x))
+#else
+#define GOOSE_HERE(x) (void)(x)
+#endif
+
+// ---- 32 rows of the softmax ---------------------------------------------------------------------------------------------
+template <int D, int QT, bool F16>
+struct RowTile {
+  static constexpr int NS = D / 16, NDT = D / 32, PT = F16 ? 1 : 2;
+  static constexpr float SLACK = 8.f;
+  typedef typename Mma16<F16>::T T;
+  typedef typename Mma16<F16>::v8 op8;
+  op8 q[NS], ql[QT == 2 ? NS : 1];
+  f32x16 o[NDT];
+  float s[16];  // scores of the block at hand
+  op8 p[2], pl[PT];
+  float m, l, top;   // largest score so far, sum of weights, this block's largest score of this lane
+  float lim, ref, mul;  // see rescale()
+  __device__ __forceinline__ void init(const PagedAttnArgs& a, const Row& w, int hh) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const op8*>(qp + s * 16 * TERMS);
-    if (TERMS == 2) {
-      // the second term in LDS, one copy for the four wavefronts (each brings a quarter)
+    for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-      for (int s = 0; s < NS / NG; ++s)
-        *reinterpret_cast<op8*>(ql_lds + ((g * (NS / NG) + s) * 64 + lane) * 16) =
-            *reinterpret_cast<const op8*>(qp + (g * (NS / NG) + s) * 32 + 8);
-      __syncthreads();
+      for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[j][e] = (T)0.f;
+        pl[j % PT][e] = (T)0.f;
+      }
+    m = lim = -INFINITY;
+    l = ref = 0.f;
+    mul = 1.f;
+    const T* at = static_cast<const T*>(a.q) + (size_t)w.row * a.ldq + ((size_t)w.h * D + hh * 8) * QT;
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+      q[k] = *reinterpret_cast<const op8*>(at + k * 16 * QT);
+      if (QT == 2) ql[k] = *reinterpret_cast<const op8*>(at + k * 32 + 8);
     }
   }
-  uint64_t mw0 = 0, mw1 = 0;
-  if (!shared && live) {
-    const int W = (B + 63) >> 6;
-    mw0 = a.r[ri].mask[(size_t)node * W];
-    if (W > 1) mw1 = a.r[ri].mask[(size_t)node * W + 1];
-    if (B < 64) mw0 &= (1ull << B) - 1;  // bits at or beyond B count as clear
-    if (B < 128) mw1 &= B > 64 ? (1ull << (B - 64)) - 1 : 0;
+  __device__ __forceinline__ void scores(const u32x4 (&k)[NS]) {
+    f32x16 sum;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) sum = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[i]), q[i], sum);
+    if (QT == 2) {
+#pragma unroll
+      for (int i = 0; i < NS; ++i) sum = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[i]), ql[i], sum);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = sum[r];
   }
-  // ---- this wavefront's blocks
-  const int i_lo = (int)((long long)n_blocks * split / nsplit), i_hi = (int)((long long)n_blocks * (split + 1) / nsplit);
-  const int n_wg = i_hi - i_lo;
-  const int b0 = b_first + i_lo + n_wg * g / NG, total = b_first + i_lo + n_wg * (g + 1) / NG - b0;
-  const int32_t* trow = a.table + (size_t)a.r[ri].seq * a.table_ld;  // (shared: any request's table will do)
-  // Page ids, 64 of them a register (one a lane); an entry out of range reads page 0
-  int pg_base = b0 >> 1, pg_ids = 0;
-  const int pg_last = (b0 + total - 1) >> 1;
-  auto load_ids = [&]() {
-    const int e = pg_base + lane;
-    pg_ids = e <= pg_last ? trow[e] : 0;
-    if ((unsigned)pg_ids >= (unsigned)a.n_pages) { atomicOr(a.flags, GOOSE_FLAG_PAGES); pg_ids = 0; }
-  };
-  if (total > 0) load_ids();
-  const size_t head_elems = (size_t)GOOSE_PAGE * D;
-  auto block_at = [&](int idx) -> size_t {  // element offset of block idx in a layer's pool
-    const int b = b0 + idx;
-    if ((b >> 1) - pg_base >= 64) { pg_base = b >> 1; load_ids(); }
-    const int page = __builtin_amdgcn_readlane(pg_ids, (b >> 1) - pg_base);
-    return ((size_t)page * a.n_kv + kvh) * head_elems + (size_t)(b & 1) * 32 * D;
-  };
+  __device__ __forceinline__ void mask(unsigned vis) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = ((vis >> r) & 1u) ? s[r] : -INFINITY;
+  }
+  // This lane's largest score (unscaled, as m is: the scale is positive).
+  __device__ __forceinline__ void maximum() {
+    float t[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) t[r] = fmaxf(fmaxf(s[r], s[r + 4]), fmaxf(s[r + 8], s[r + 12]));
+    top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+  }
+  // m, O and l follow it only where some lane's has grown so far that weights would pass 2^SLACK: weights up to there are as good as
+  // those up to one in floating point (16 bits hold them with room to spare), and with 32 rows in a tile some row's maximum grows by a
+  // little in most blocks (512 rows over 16384 slots: in 3 of 4).
+  // A weight is 2^(s c - ref) in one fused multiply-add, ref = m c rounded; its rounding is the same factor in O and l.  Where products
+  // leave no room for it (2^24 and beyond, infinities), the block's scores become differences to m first.
+  __device__ __forceinline__ void rescale(float c) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > lim) != 0, 0)) {
+      const float m_new = fmaxf(m, fmaxf(top, __shfl_xor(top, 32, 64)));
+      const float old = finite_ref(m), now = finite_ref(m_new);
+      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((old - now) * c);
+      m = m_new;
+      lim = m + SLACK / c;
+      ref = now * c;
+      mul = c;
+      if (__builtin_amdgcn_ballot_w64(!(fabsf(ref) < 16777216.f)) != 0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = (s[r] - now) * c;
+        mul = 1.f;
+        ref = 0.f;
+        lim = -INFINITY;  // (and so will the next block's)
+      }
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+    }
+  }
+  // probabilities of keys 2 i, 2 i + 1 (a masked score is -infinity: zero)
+  __device__ __forceinline__ void weights_of(int i) {
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    typedef float F2 __attribute__((ext_vector_type(2)));
+    const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * i], mul, -ref)), y = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], mul, -ref));
+    l += x;
+    l += y;
+    unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector((F2{x, y}), T2));
+    u32x4 w = __builtin_bit_cast(u32x4, p[i >> 2]);
+    w[i & 3] = h;
+    p[i >> 2] = __builtin_bit_cast(op8, w);
+    if (PT == 2) {
+      const F2 rest = {x - __builtin_bit_cast(float, h << 16), y - __builtin_bit_cast(float, h & 0xFFFF0000u)};
+      unsigned r = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, T2));
+      w = __builtin_bit_cast(u32x4, pl[(i >> 2) % PT]);
+      w[i & 3] = r;
+      pl[(i >> 2) % PT] = __builtin_bit_cast(op8, w);
+    }
+  }
+  __device__ __forceinline__ void weights() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) weights_of(i);
+  }
+  __device__ __forceinline__ void values(const u32x4 (&v)[NS]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), p[j], o[dt]);
+    if (PT == 2) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), pl[j % PT], o[dt]);
+    }
+  }
+  // The second product of a block with a NaN or an infinity in a value that some rows do not see (through the matrix instruction it
+  // would reach them as 0 * NaN): those elements count as zero there, and a product of indicators (is it +inf, -inf, NaN) x (is it visible) tells
+  // which outputs they reach.  Rare.
+  __device__ __forceinline__ void values_odd(const u32x4 (&v)[NS], unsigned vis) {
+    constexpr unsigned short EXP = F16 ? 0x7C00 : 0x7F80;
+    const unsigned short ONE = __builtin_bit_cast(unsigned short, (T)1.f);
+    u16x8 seen[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) seen[r >> 3][r & 7] = ((vis >> r) & 1u) ? ONE : (unsigned short)0;
+#pragma unroll 1
+    for (int c = 0; c < 3; ++c) {
+      const float special = c == 0 ? INFINITY : (c == 1 ? -INFINITY : __builtin_nanf(""));
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        f32x16 hits;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) hits[r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          u32x4 raw = v[dt * 2 + j];
+          asm volatile("" : "+v"(raw));  // (nothing of this may move out of the loop: it would take the registers of the common path)
+          u16x8 e = __builtin_bit_cast(u16x8, raw);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int is = (e[i] & EXP) != EXP ? -1 : (e[i] == EXP ? 0 : (e[i] == (EXP | 0x8000) ? 1 : 2));
+            e[i] = is == c ? ONE : (unsigned short)0;
+          }
+          hits = Mma16<F16>::mfma(__builtin_bit_cast(op8, e), __builtin_bit_cast(op8, seen[j]), hits);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] = hits[r] > 0.f ? o[dt][r] + special : o[dt][r];
+      }
+    }
+    u32x4 w[NS];
+#pragma unroll
+    for (int k = 0; k < NS; ++k) {
+      u16x8 e = __builtin_bit_cast(u16x8, v[k]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = (e[i] & EXP) == EXP ? (unsigned short)0 : e[i];
+      w[k] = __builtin_bit_cast(u32x4, e);
+    }
+    values(w);
+  }
+};
+
+// Mask row of a node, bits at or beyond B cleared.
+struct MaskRow { uint64_t w0, w1; };
+__device__ inline MaskRow mask_of(const PagedAttnArgs& a, const Item& it, const Row& w) {
+  MaskRow k = {0, 0};
+  if (it.ri < 0 || !w.live) return k;
+  const int W = (it.B + 63) >> 6;
+  const uint64_t* p = a.r[it.ri].mask + (size_t)w.node * W;
+  k.w0 = p[0];
+  if (W > 1) k.w1 = p[1];
+  if (it.B < 64) k.w0 &= (1ull << it.B) - 1;
+  if (it.B < 128) k.w1 &= it.B > 64 ? (1ull << (it.B - 64)) - 1 : 0;
+  return k;
+}
+// Slots behind the tree may hold anything: their values (of this lane's 16 keys those from `mine` on) become zero.  True if a NaN or an
+// infinity is left.
+template <bool F16, int NS>
+__device__ __forceinline__ bool clean_values(u32x4 (&v)[NS], int mine) {
+  constexpr unsigned EXP = F16 ? 0x7C00u : 0x7F80u;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {  // keys 2 i, 2 i + 1: dword i % 4 of the pieces with parity i / 4
+    const unsigned keep = 2 * i + 1 < mine ? 0xFFFFFFFFu : (2 * i < mine ? 0xFFFFu : 0u);
+#pragma unroll
+    for (int k = i >> 2; k < NS; k += 2) {
+      const unsigned x = v[k][i & 3] & keep;
+      v[k][i & 3] = x;
+      odd = odd || (x & EXP) == EXP || (x & (EXP << 16)) == (EXP << 16);
+    }
+  }
+  return __builtin_amdgcn_ballot_w64(odd) != 0;
+}
+template <int NS>
+__device__ __forceinline__ void fetch(const void* at, int lane, u32x4 (&dst)[NS]) {
+  const u32x4* p = static_cast<const u32x4*>(at) + lane;
+#pragma unroll
+  for (int s = 0; s < NS; ++s) dst[s] = p[s * 64];
+}
+__device__ inline float softmax_scale(int D) { return 1.4426950408889634f / sqrtf((float)D); }  // log2(e) / sqrt(d): softmax in base 2
+
+// What an item leaves of a row: columns c .. c + 3 of its (m, l, O), or the output itself.  x: sums of weights, x / l the mean
+__device__ inline void leave(const PagedAttnArgs& a, const Item& it, const Row& w, int D, int c, const f32x4& x, float m, float l) {
+  if (a.direct) {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    store_out(a, w.row, w.h * D + c, x * inv);
+  } else {
+    const size_t rec = ((size_t)it.rec_split * a.n_heads + w.h) * a.rows + w.crow;
+    if (c == 0) *reinterpret_cast<float2*>(a.ws_ml + rec * 2) = make_float2(m, l);
+    *reinterpret_cast<f32x4*>(a.ws_o + rec * D + c) = x;
+  }
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------------------------
+// One workgroup = NT tiles of 32 rows x a range of blocks, dealt to four wavefronts in contiguous quarters; every wavefront streams
+// its blocks global -> registers -> matrix cores (no barrier in the loop), the next block's keys and values requested as
+// soon as the current ones have been used.
+template <int D, int QT, bool F16, int NT>
+__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_paged_stream(const PagedAttnArgs a) {
+  typedef RowTile<D, QT, F16> Tile;
+  typedef typename Tile::T T;
+  constexpr int NG = 4, NS = D / 16, QUADS = D / 8, QPW = QUADS / NG;
+  constexpr int WFLOATS = (QUADS + 1) * 256;  // a wavefront's state at the merge
+  __shared__ __attribute__((aligned(16))) float lds[NG * WFLOATS];
+  const int tid = threadIdx.x, lane = tid & 63, g = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l31 = lane & 31, hh = lane >> 5;
+  const int kvh = blockIdx.x;  // the fast index: where 8 divides the KV heads, all items of a head run on one XCD and find each other's blocks in its L2
+  const Item it = item_of(a, blockIdx.y, kvh);
+  const int n_wg = it.b_hi - it.b_lo;
+  const int b0 = it.b_lo + n_wg * g / NG, total = it.b_lo + n_wg * (g + 1) / NG - b0;
+  PageIds pg{a.table + (size_t)it.seq * a.table_ld, a.flags, b0 >> 1, (b0 + total - 1) >> 1, a.n_pages, 0};
   const T* const kp = static_cast<const T*>(a.kpool);
   const T* const vp = static_cast<const T*>(a.vpool);
-  u32x4 kreg[NS], vreg[NS];
-  auto fetch = [&](const T* pool, size_t at, u32x4 (&dst)[NS]) {
-    const u32x4* p = reinterpret_cast<const u32x4*>(pool + at) + lane;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) dst[s] = p[s * 64];
+  auto block_at = [&](int b) -> size_t {
+    return ((size_t)pg.of(b, lane) * a.n_kv + kvh) * (GOOSE_PAGE * D) + (size_t)(b & 1) * 32 * D;
   };
+  u32x4 kreg[NS], vreg[NS];
   size_t at = 0;
   if (total > 0) {
-    at = block_at(0);
-    fetch(kp, at, kreg);
-    fetch(vp, at, vreg);
+    pg.load(lane);
+    at = block_at(b0);
+    fetch(kp + at, lane, kreg);
+    fetch(vp + at, lane, vreg);
   }
-  f32x16 oacc[D / 32];
+  Row row[NT];
+  MaskRow mk[NT];
+  Tile t[NT];
 #pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) oacc[dt][r] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
-  const float scale = 1.4426950408889634f / sqrtf((float)D);  // log2(e) / sqrt(d): softmax in base 2
-
-  for (int idx = 0; idx < total; ++idx) {
-    const size_t here = at;
+  for (int n = 0; n < NT; ++n) {
+    row[n] = row_of(a, it, (it.tile * NT + n) * 32 + l31, kvh);
+    t[n].init(a, row[n], hh);
+    mk[n] = mask_of(a, it, row[n]);
+  }
+  const bool both = NT == 1 || __builtin_amdgcn_ballot_w64(row[NT - 1].live) != 0;  // (the second tile may be empty)
+  const float scale = softmax_scale(D);
+  auto block = [&](int idx, auto tree) {
+    constexpr bool TREE = decltype(tree)::value;
     const int slot0 = (b0 + idx) * 32;
-    const bool tree = !shared && slot0 + 32 > P;  // wavefront-uniform
-    f32x16 s;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-    for (int k = 0; k < NS; ++k) s = Mma16<F16>::mfma(__builtin_bit_cast(op8, kreg[k]), qf[k], s);
-    if (TERMS == 2) {
-#pragma unroll
-      for (int k = 0; k < NS; ++k) {
-        const op8 ql = *reinterpret_cast<const op8*>(ql_lds + (k * 64 + lane) * 16);
-        s = Mma16<F16>::mfma(__builtin_bit_cast(op8, kreg[k]), ql, s);
-      }
-    }
-    if (idx + 1 < total) { at = block_at(idx + 1); fetch(kp, at, kreg); }
-    unsigned vis = 0xFFFFu;
-    if (tree) {
-      vis = window16(mw0, mw1, slot0 + hh * 16 - P);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = ((vis >> r) & 1u) ? s[r] : -INFINITY;
-    }
-    float tmax = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] *= scale;
-      tmax = fmaxf(tmax, s[r]);
-    }
-    tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
-    const bool grew = tmax > m_run;
-    const float m_new = fmaxf(m_run, tmax), ref = finite_ref(m_new);
-    const float alpha = __builtin_amdgcn_exp2f(m_run - ref);
-    m_run = m_new;
-    float psum = 0.f;
-    op8 pf[2];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float p = __builtin_amdgcn_exp2f(s[r] - ref);
-      s[r] = p;
-      psum += p;
-      pf[r >> 3][r & 7] = (T)p;
-    }
-    // the running maximum settles after a few blocks: skip the rescale when no lane's maximum grew
-    if (__builtin_amdgcn_ballot_w64(grew) != 0) {
-      l_run *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[dt][r] *= alpha;
-    }
-    l_run += psum;
+    for (int n = 0; n < NT; ++n)
+      if (n == 0 || both) t[n].scores(kreg);
+    if (idx + 1 < total) { at = block_at(b0 + idx + 1); fetch(kp + at, lane, kreg); }
+    unsigned vis[NT];
     bool odd = false;
-    if (tree) {
-      // slots behind the tree may hold anything: their values become zero.  A NaN or an infinity in the value of a node that
-      // some rows do not see would reach them as 0 * NaN through the matrix instruction.
-      const int mine = P + B - slot0 - hh * 16;  // of this lane's 16 keys, the first `mine` exist
+    if (TREE) {
 #pragma unroll
-      for (int k = 0; k < NS; ++k) {
-        u16x8 e = __builtin_bit_cast(u16x8, vreg[k]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if ((k & 1) * 8 + i >= mine) e[i] = 0;
-          constexpr unsigned short EXP = F16 ? 0x7C00 : 0x7F80;
-          odd = odd || (e[i] & EXP) == EXP;
-        }
-        vreg[k] = __builtin_bit_cast(u32x4, e);
+      for (int n = 0; n < NT; ++n) {
+        vis[n] = window16(mk[n].w0, mk[n].w1, slot0 + hh * 16 - it.P);
+        t[n].mask(vis[n]);
       }
+      odd = clean_values<F16>(vreg, it.P + it.B - slot0 - hh * 16);
     }
-    if (tree && __builtin_amdgcn_ballot_w64(odd) != 0) {
-      // rare: key by key, skipping the pairs that are masked.  The probabilities go through this wavefront's part of the merge buffer.
-      float* const pl = reinterpret_cast<float*>(lds) + (size_t)g * WFLOATS;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) pl[(hh * 16 + r) * 33 + l31] = ((vis >> r) & 1u) ? (float)(T)s[r] : -1.f;
-      const int n_keys = min(32, P + B - slot0);
-      for (int kk = 0; kk < n_keys; ++kk) {
-        const float p = pl[kk * 33 + l31];
-        const T* col = vp + here + (((kk >> 3) & 1) * 64 + 32 * (kk >> 4)) * 8 + (kk & 7);
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float v = (float)col[(dt * 128 + 8 * (r >> 2) + 4 * hh + (r & 3)) * 8];
-            oacc[dt][r] = p >= 0.f || p != p ? fmaf(p, v, oacc[dt][r]) : oacc[dt][r];
-          }
+    for (int n = 0; n < NT; ++n)
+      if (n == 0 || both) {
+        t[n].maximum();
+        t[n].rescale(scale);
+        t[n].weights();
+        if (TREE && odd) t[n].values_odd(vreg, vis[n]);
+        else t[n].values(vreg);
       }
-    } else {
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          oacc[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, vreg[dt * 2 + j]), pf[j], oacc[dt]);
-    }
-    if (idx + 1 < total) fetch(vp, at, vreg);
-  }
+    if (idx + 1 < total) fetch(vp + at, lane, vreg);
+  };
+  // blocks that every row sees whole, then those that the tree reaches into
+  const int full = it.ri < 0 ? total : max(0, min(total, (it.P >> 5) - b0));
+  for (int idx = 0; idx < full; ++idx) block(idx, std::false_type());
+  for (int idx = full; idx < total; ++idx) block(idx, std::true_type());
+  if (g == 0) check_shared(a, it, lane);
 
-  // ---- the four wavefronts' states join in one round through LDS: each leaves its own, then owns a quarter of the columns
-  f32x4 res[QPW];
-  float l_sum = 0.f;
-  {
-    float* dst = reinterpret_cast<float*>(lds) + (size_t)g * WFLOATS + lane * 4;
-    *reinterpret_cast<f32x4*>(dst) = f32x4{m_run, l_run, 0.f, 0.f};
+  // ---- the four wavefronts' states join in one round a tile through LDS: each leaves its own, then owns a quarter of the columns
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    if (n > 0) {
+      if (!both) return;
+      __syncthreads();
+    }
+    float* dst = lds + (size_t)g * WFLOATS + lane * 4;
+    *reinterpret_cast<f32x4*>(dst) = f32x4{t[n].m * scale, t[n].l, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<f32x4*>(dst + 256 * (1 + dt * 4 + q)) =
-            f32x4{oacc[dt][q * 4], oacc[dt][q * 4 + 1], oacc[dt][q * 4 + 2], oacc[dt][q * 4 + 3]};
+            f32x4{t[n].o[dt][q * 4], t[n].o[dt][q * 4 + 1], t[n].o[dt][q * 4 + 2], t[n].o[dt][q * 4 + 3]};
     __syncthreads();
-    const float* src = reinterpret_cast<const float*>(lds) + lane * 4;
-    float mj[NG], lj[NG];
-    m_run = -INFINITY;
+    const float* src = lds + lane * 4;
+    float mj[NG], lj[NG], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
       const f32x4 ml = *reinterpret_cast<const f32x4*>(src + (size_t)j * WFLOATS);
       mj[j] = ml[0];
       lj[j] = ml[1];
-      m_run = fmaxf(m_run, mj[j]);
+      m = fmaxf(m, mj[j]);
     }
-    const float ref = finite_ref(m_run);
+    const float ref = finite_ref(m);
+    f32x4 res[QPW];
 #pragma unroll
     for (int q = 0; q < QPW; ++q) res[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
       const float w = __builtin_amdgcn_exp2f(mj[j] - ref);
-      l_sum += w * lj[j];
+      l += w * lj[j];
 #pragma unroll
       for (int q = 0; q < QPW; ++q)
         res[q] += w * *reinterpret_cast<const f32x4*>(src + (size_t)j * WFLOATS + 256 * (1 + g * QPW + q));
     }
-  }
-  const float l_tot = l_sum + __shfl_xor(l_sum, 32, 64);
-  if (!shared && y == 0 && kvh == 0 && g == 0 && ri > 0) {
-    // the shared pages must be the same in all tables: one wavefront a request compares them with the first request's
-    const int32_t* t0 = a.table + (size_t)a.r[0].seq * a.table_ld;
-    bool differs = false;
-    for (int i = lane; i < a.sh_blocks / 2; i += 64) differs = differs || trow[i] != t0[i];
-    if (differs) atomicOr(a.flags, GOOSE_FLAG_PAGES);
-  }
-  if (!live) return;
-  // quad n of the accumulator = columns 8 n + 4 hh .. + 3
-  if (a.direct) {
-    const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
+    l += __shfl_xor(l, 32, 64);
+    // quad i of the accumulator = columns 8 i + 4 hh .. + 3
+    if (row[n].live) {
 #pragma unroll
-    for (int q = 0; q < QPW; ++q) store_out(a, row, h * D + (g * QPW + q) * 8 + hh * 4, res[q] * inv);
-  } else {
-    const size_t rec = ((size_t)rec_split * a.n_heads + h) * a.rows + crow;
-    if (hh == 0 && g == 0) *reinterpret_cast<float2*>(a.ws_ml + rec * 2) = make_float2(m_run, l_tot);
-    float* dst = a.ws_o + rec * D;
-#pragma unroll
-    for (int q = 0; q < QPW; ++q) *reinterpret_cast<f32x4*>(dst + (g * QPW + q) * 8 + hh * 4) = res[q];
+      for (int q = 0; q < QPW; ++q) leave(a, it, row[n], D, (g * QPW + q) * 8 + hh * 4, res[q], m, l);
+    }
   }
+}
+
+// ---- many rows ----------------------------------------------------------------------------------------------------------
+// One workgroup = eight wavefronts, two on a SIMD, one tile of 32 rows each: 256 rows (items of up to 128 rows: 128, and two key groups) x a
+// range of blocks.  Every block comes into LDS once, global -> LDS without registers, into a ring that runs several blocks ahead.
+// A wavefront alone issues an instruction every five cycles, whatever it is, so the matrix pipe (32 cycles an instruction)
+// and the vector pipe both stay idle in turn; two wavefronts fill each other's gaps.  Within one, the scores of the next block and the
+// outputs of this one are under way while this block's scores become weights and the next block's maximum is taken:
+//     matrix pipe   S = K Q (j+1)         |  O += V P (j)
+//     vector pipe   weights P of block j  |  maximum of S
+// Blocks that need a mask (the tree's, and what is left over) follow without the ring, as in k_paged_stream.
+#define GOOSE_LDS_PTR(p) ((__attribute__((address_space(3))) void*)(p))
+constexpr int vmcnt_imm(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }  // s_waitcnt vmcnt(n) only
+
+template <int CP>
+__device__ __forceinline__ void copy_pieces(const char* src, unsigned char* cp) {
+#if defined(__HIP_DEVICE_COMPILE__)  // (the host pass knows no such builtin and would silently drop the kernel's stub)
+  __builtin_amdgcn_global_load_lds(reinterpret_cast<const u32x4*>(src), GOOSE_LDS_PTR(cp), 16, 0, 0);
+  if (CP == 2) __builtin_amdgcn_global_load_lds(reinterpret_cast<const u32x4*>(src), GOOSE_LDS_PTR(cp), 16, 1024, 0);  // (the offset counts on both sides)
+#endif
+}
+// Step j of a wavefront: scores of block j + 1, outputs of block j.  The operand pieces come from the ring `AHEAD` uses before they are needed; with
+// one key group pc holds the first ones and is left with those of the next step (two units of the ring are then no longer in flight; with two
+// groups that would be all but one).  k1, k2: keys of blocks j + 1 and j + 2, v0: values of block j.  (Pointers that the
+// compiler may take to be distinct memory from cp, where src goes: its reads do not wait for the copies in flight.  What they do wait for is
+// the caller's explicit count and barrier.)  The order is written down: the compiler's own collects the vector work where it waits for the scores.
+template <int D, int QT, bool F16, int CP, int G, int AHEAD>
+__device__ __forceinline__ void ring_step(RowTile<D, QT, F16>& t, u32x4 (&pc)[AHEAD], const u32x4* __restrict__ k1, const u32x4* __restrict__ v0,
+                                          const u32x4* __restrict__ k2, unsigned char* __restrict__ cp, unsigned char* __restrict__ cp2,
+                                          const char* const (&src)[G], bool work, bool more, float scale) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef RowTile<D, QT, F16> Tile;
+  typedef typename Tile::op8 op8;
+  constexpr int NS = Tile::NS, NDT = Tile::NDT, PT = Tile::PT;
+  copy_pieces<CP>(src[0], cp);
+  if (G == 2) copy_pieces<CP>(src[G - 1], cp2);
+  if (!work) return;
+  u32x4 piece[2 * NS + AHEAD];
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n) piece[n] = G == 1 ? pc[n] : k1[n * 64];
+  f32x16 sum;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+#pragma unroll
+  for (int n = 0; n < 2 * NS; ++n) {
+    {
+      const int m = n + AHEAD, x = m - NS;
+      if (m < NS) piece[m] = k1[m * 64];
+      else if (m < 2 * NS) piece[m] = v0[(x % NDT * 2 + x / NDT) * 64];
+      else if (G == 1) piece[m] = k2[(m - 2 * NS) * 64];
+    }
+    const op8 a = __builtin_bit_cast(op8, piece[n]);
+    if (n < NS) {
+      sum = Mma16<F16>::mfma(a, t.q[n], sum);
+      if (QT == 2) sum = Mma16<F16>::mfma(a, t.ql[n % (QT == 2 ? NS : 1)], sum);
+      GOOSE_HERE(sum);
+#pragma unroll
+      for (int w = 8 / NS * n; w < 8 / NS * (n + 1); ++w) t.weights_of(w);
+      GOOSE_HERE(t.l);
+    } else {
+      const int x = n - NS, j = x / NDT, dt = x % NDT;
+      t.o[dt] = Mma16<F16>::mfma(a, t.p[j], t.o[dt]);
+      if (PT == 2) t.o[dt] = Mma16<F16>::mfma(a, t.pl[j % PT], t.o[dt]);
+      GOOSE_HERE(t.o[dt]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) t.s[r] = sum[r];
+  t.maximum();
+  if (more) t.rescale(scale);  // (behind the last block the scores are of a block that is not this loop's)
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n)
+    if (G == 1) pc[n] = piece[2 * NS + n];
+#endif
+}
+
+template <int D, int QT, bool F16>
+__global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
+  typedef RowTile<D, QT, F16> Tile;
+  typedef typename Tile::T T;
+  constexpr int NS = D / 16, QUADS = D / 8;
+  constexpr int BLOCK = 2 * NS * 1024;  // keys and values of 32 slots
+  constexpr int RING = 8;               // blocks
+  constexpr int WFLOATS = (QUADS + 1) * 256;
+  constexpr int CP = 2 * NS / 8;        // pieces of 1 KiB that a wavefront copies of a block
+  constexpr int AHEAD = 4;
+  static_assert(4 * WFLOATS * 4 <= RING * BLOCK, "merge buffer");
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[RING * BLOCK];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l31 = lane & 31, hh = lane >> 5;
+  const int kvh = blockIdx.x;
+  const Item it = item_of(a, blockIdx.y, kvh);
+  // 256 rows in eight tiles, or 128 in four with two key groups
+  const int rows = (it.ri < 0 ? a.rows : it.B) * a.group;
+  const int KG = it.ri < 0 ? a.sh_kg : a.own_kg;
+  const int kg = KG == 1 ? 0 : wave >> 2, rt = KG == 1 ? wave : wave & 3;
+  const int row_first = it.tile * (KG == 1 ? 256 : 128) + rt * 32;
+  const bool work = row_first < rows;
+  // the ring takes units of KG blocks that need no mask; the rest is the tail
+  const int full_end = it.ri < 0 ? it.b_hi : max(it.b_lo, min(it.b_hi, it.P >> 5));
+  const int units = KG == 1 ? full_end - it.b_lo : (full_end - it.b_lo) >> 1;
+  const int tail0 = it.b_lo + units * KG;
+  PageIds pg{a.table + (size_t)it.seq * a.table_ld, a.flags, it.b_lo >> 1, (it.b_hi - 1) >> 1, a.n_pages, 0};
+  if (it.b_hi > it.b_lo) pg.load(lane);
+  const char* const kp = static_cast<const char*>(a.kpool);
+  const char* const vp = static_cast<const char*>(a.vpool);
+  auto block_at = [&](int b) -> size_t {  // bytes (pages times KV heads stays below 2^29: checked on the host)
+    return (size_t)(unsigned)((pg.of(b, lane) * a.n_kv + kvh) * 2 + (b & 1)) * (32 * D * 2);
+  };
+  const Row row = row_of(a, it, row_first + l31, kvh);
+  Tile t;
+  t.init(a, row, hh);
+  const float scale = softmax_scale(D);
+  const int share = wave * CP * 1024;  // this wavefront's pieces of a block: the first four bring keys, the others values
+  const char* const pool = (wave < 4 ? kp : vp) + (wave & 3) * CP * 1024;
+  auto source = [&](int b) -> const char* {  // (behind the range: its last block again, never used)
+    return pool + block_at(min(b, it.b_hi - 1)) + lane * 16;
+  };
+  auto barrier = [&]() {  // (raw: __syncthreads would also drain every copy in flight)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (all that was loaded so far: the counts below are those of the ring's copies)
+  auto through_the_ring = [&](auto kg_c) {
+    constexpr int G = decltype(kg_c)::value;  // key groups
+    constexpr int BU = BLOCK / 16, MASK = RING - 1;
+    for (int i = 0; i < RING - G; ++i) copy_pieces<CP>(source(it.b_lo + i), ring + i * BLOCK + share);  // every unit but the last of the ring
+    __builtin_amdgcn_sched_barrier(0);
+    const u32x4* const base = reinterpret_cast<const u32x4*>(ring) + lane;
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3 * G) * CP));  // units 0 and 1
+    barrier();
+    u32x4 pc[AHEAD];
+    if (work) {
+      u32x4 k[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) k[s] = base[kg * BU + s * 64];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n)
+        if (G == 1) pc[n] = base[BU + n * 64];
+      t.scores(k);
+      t.maximum();
+      t.rescale(scale);
+    }
+    int b = it.b_lo + RING - G;  // the block copied next, into the slots of unit j - 1
+    for (int j = 0; j < units; ++j) {
+      const char* src[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) src[g] = source(b + g);
+      b += G;
+      // unit j + 1 (one key group: j + 2) has landed in every wavefront's share, and unit j - 1 is no longer read
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - (G == 1 ? 4 : 3 * G)) * CP));
+      barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      ring_step<D, QT, F16, CP, G, AHEAD>(t, pc, base + (((j + 1) * G + kg) & MASK) * BU, base + ((j * G + kg) & MASK) * BU + BU / 2,
+                                          base + (((j + 2) * G + kg) & MASK) * BU, ring + ((j * G + RING - G) & MASK) * BLOCK + share,
+                                          ring + ((j * G + RING - 1) & MASK) * BLOCK + share, src, work, j + 1 < units, scale);
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (copies behind the range may still be landing)
+  };
+  if (units > 0) {
+    if (KG == 1) through_the_ring(std::integral_constant<int, 1>());
+    else through_the_ring(std::integral_constant<int, 2>());
+  }
+
+  // ---- blocks without the ring
+  if (work && tail0 + kg < it.b_hi) {
+    const MaskRow mk = mask_of(a, it, row);
+    pg.base = tail0 >> 1;  // (the window may have run ahead)
+    pg.load(lane);
+    for (int b = tail0 + kg; b < it.b_hi; b += KG) {
+      const size_t at = block_at(b);
+      u32x4 k[NS], v[NS];
+      fetch(kp + at, lane, k);
+      fetch(vp + at, lane, v);
+      const int slot0 = b * 32;
+      const bool tree = it.ri >= 0 && slot0 + 32 > it.P;
+      unsigned vis = 0xFFFFu;
+      bool odd = false;
+      t.scores(k);
+      if (tree) {
+        vis = window16(mk.w0, mk.w1, slot0 + hh * 16 - it.P);
+        t.mask(vis);
+        odd = clean_values<F16>(v, it.P + it.B - slot0 - hh * 16);
+      }
+      t.maximum();
+      t.rescale(scale);
+      t.weights();
+      if (odd) t.values_odd(v, vis);
+      else t.values(v);
+    }
+  }
+  if (wave == 0) check_shared(a, it, lane);
+
+  // ---- two key groups join: the second leaves its states in LDS, the first takes them in
+  float m = t.m * scale;
+  if (KG == 2) {
+    __syncthreads();
+    float* const buf = reinterpret_cast<float*>(ring) + (size_t)rt * WFLOATS + lane * 4;
+    if (kg == 1) {
+      *reinterpret_cast<f32x4*>(buf) = f32x4{m, t.l, 0.f, 0.f};
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4*>(buf + 256 * (1 + dt * 4 + q)) =
+              f32x4{t.o[dt][q * 4], t.o[dt][q * 4 + 1], t.o[dt][q * 4 + 2], t.o[dt][q * 4 + 3]};
+    }
+    __syncthreads();
+    if (kg == 1) return;
+    const f32x4 ml = *reinterpret_cast<const f32x4*>(buf);
+    const float both = fmaxf(m, ml[0]), ref = finite_ref(both);
+    const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(ml[0] - ref);
+    m = both;
+    t.l = w0 * t.l + w1 * ml[1];
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(buf + 256 * (1 + dt * 4 + q));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t.o[dt][q * 4 + e] = w0 * t.o[dt][q * 4 + e] + w1 * x[e];
+      }
+  }
+  const float l = t.l + __shfl_xor(t.l, 32, 64);
+  if (!work || !row.live) return;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      leave(a, it, row, D, (dt * 4 + q) * 8 + hh * 4, f32x4{t.o[dt][q * 4], t.o[dt][q * 4 + 1], t.o[dt][q * 4 + 2], t.o[dt][q * 4 + 3]}, m, l);
 }
 
 // Joins the items of a row: D / 4 threads a (row, head), four columns each, records in a fixed order, the loads of eight in flight together.
@@ -396,10 +797,13 @@ __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
   store_out(a, (size_t)a.r[r].row0 + crow - a.r[r].c0, h * D + c, num * inv);
 }
 
-template <int D, int TERMS>
-void launch_t(bool f16, dim3 grid, const PagedAttnArgs& a, hipStream_t st) {
-  if (f16) hipLaunchKernelGGL((k_attn_paged<D, TERMS, true>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_attn_paged<D, TERMS, false>), grid, dim3(256), 0, st, a);
+// which kernel: TILES beyond 64 rows of an item, else tiles of 32 rows a wavefront
+enum { STREAM1, STREAM2, TILES };
+template <int D, int QT, bool F16>
+void launch_t(int kind, dim3 grid, const PagedAttnArgs& a, hipStream_t st) {
+  if (kind == TILES) hipLaunchKernelGGL((k_paged_tiles<D, QT, F16>), grid, dim3(512), 0, st, a);
+  else if (kind == STREAM2) hipLaunchKernelGGL((k_paged_stream<D, QT, F16, 2>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_paged_stream<D, QT, F16, 1>), grid, dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -431,22 +835,31 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.o_terms = o_terms;
   a.o_f16 = o_dtype == GOOSE_DTYPE_F16;
   a.sh_blocks = shared_pages * 2;
-  a.sh_tiles = shared_pages > 0 ? (rq.rows * a.group + 31) / 32 : 0;
-  // Blocks per item: enough items for two workgroups a compute unit, but at least eight blocks each (two a wavefront).
+  int own_max = 0, own_rows = 0;
+  for (int r = 0; r < rq.n; ++r) own_rows = rq.r[r].B > own_rows ? rq.r[r].B : own_rows;
+  own_rows *= a.group;
+  const int sh_rows = shared_pages > 0 ? rq.rows * a.group : 0, most = sh_rows > own_rows ? sh_rows : own_rows;
+  const int kind = most > 64 ? TILES : (most > 32 ? STREAM2 : STREAM1);
+  a.sh_kg = sh_rows <= 128 ? 2 : 1;
+  a.own_kg = own_rows <= 128 ? 2 : 1;
+  const int sh_height = kind == TILES ? 256 / a.sh_kg : (kind == STREAM2 ? 64 : 32);
+  const int own_height = kind == TILES ? 256 / a.own_kg : sh_height;
+  a.sh_tiles = (sh_rows + sh_height - 1) / sh_height;
+  // Blocks per item: one round of workgroups (256 of the tall kernels, 512 of STREAM1), but at least eight blocks each.
   long long work = (long long)a.sh_tiles * a.sh_blocks;
-  int own_max = 0;
   for (int r = 0; r < rq.n; ++r) {
     const PagedReq& s = rq.r[r];
-    a.r[r] = AttnReq{s.seq, s.B, s.P_max, s.row0, s.c0, (s.B * a.group + 31) / 32, 0, (const uint64_t*)s.p};
+    a.r[r] = AttnReq{s.seq, s.B, s.P_max, s.row0, s.c0, (s.B * a.group + own_height - 1) / own_height, 0, (const uint64_t*)s.p};
     const int nb = (s.P_max + s.B + 31) / 32 - a.sh_blocks;
     own_max = nb > own_max ? nb : own_max;
     work += (long long)a.r[r].tiles * nb;
   }
-  long long per = (work * n_kv + 511) / 512;
+  const int slots = kind == STREAM1 ? 512 : 256;
+  long long per = (work * n_kv + slots - 1) / slots;
   if (per < 8) per = 8;
   const size_t step = (size_t)n_heads * rq.rows;  // records of one split
   int own_splits;
-  for (;; per *= 2) {
+  for (;; per += per / 4) {
     a.sh_splits = (int)((a.sh_blocks + per - 1) / per);
     own_splits = (int)((own_max + per - 1) / per);
     if (a.sh_splits + own_splits <= 1 || (size_t)(a.sh_splits + own_splits) * step <= max_records) break;
@@ -462,11 +875,11 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   const dim3 grid(n_kv, items);
   const bool f16 = dtype == GOOSE_DTYPE_F16;
   if (head_dim == 128) {
-    if (q_terms == 2) launch_t<128, 2>(f16, grid, a, st);
-    else launch_t<128, 1>(f16, grid, a, st);
+    if (q_terms == 2) f16 ? launch_t<128, 2, true>(kind, grid, a, st) : launch_t<128, 2, false>(kind, grid, a, st);
+    else f16 ? launch_t<128, 1, true>(kind, grid, a, st) : launch_t<128, 1, false>(kind, grid, a, st);
   } else {
-    if (q_terms == 2) launch_t<64, 2>(f16, grid, a, st);
-    else launch_t<64, 1>(f16, grid, a, st);
+    if (q_terms == 2) f16 ? launch_t<64, 2, true>(kind, grid, a, st) : launch_t<64, 2, false>(kind, grid, a, st);
+    else f16 ? launch_t<64, 1, true>(kind, grid, a, st) : launch_t<64, 1, false>(kind, grid, a, st);
   }
   int rc = goose_launch_status();
   if (rc != GOOSE_OK || a.direct) return rc;

@@ -806,6 +806,7 @@ static int check_pages(const goose_ctx* c, const goose_pages* pg) {
   if (!pg->d_kpool || !pg->d_vpool || !pg->d_table || !pg->d_len || !pg->d_refs) return GOOSE_ERR_ARG;
   if (((uintptr_t)pg->d_kpool & 15) || ((uintptr_t)pg->d_vpool & 15)) return GOOSE_ERR_ARG;
   if (pg->n_pages < 1 || pg->n_seqs < 1 || pg->table_ld < 1 || pg->table_ld > INT32_MAX / GOOSE_PAGE) return GOOSE_ERR_ARG;
+  if ((long long)pg->n_pages * c->n_kv > INT32_MAX / 4) return GOOSE_ERR_ARG;  // (an index inside a layer)
   return GOOSE_OK;
 }
 static int check_seqs(const goose_pages* pg, const int32_t* h_seqs, int n) {

@@ -1,8 +1,8 @@
 """goose_attn_paged against 64-bit attention: head layouts, lengths, shared prefixes, masks, and what lies behind them.
 
-Error bound of one output, u = half a step of the cache's type, u_o of the output's: with A = sum p |v| / sum p,
-  * probabilities are rounded to 16 bits before the second product: u A (fp16: and 2^-25 each below its normals, sum|v| 2^-25 in all, as the
-    largest probability of a row is one in the item that holds it and every rescale only shrinks both);
+Error bound of one output, u_o = half a step of the output's type: with A = sum p |v| / sum p,
+  * probabilities are rounded before the second product: fp16 2^-11 A and 2^-25 each below its normals, sum|v| 2^-25 in all, as the
+    largest probability of a row is one in the item that holds it and every rescale only shrinks both; bf16 in two terms, 2^-16 A;
   * a score errs by (d + 4) 2^-24 sum|q||k| / sqrt(d) (products exact in 32 bits, d additions, scale), which moves a probability by the same relative
     amount and the quotient by twice that: 2 A (d + 4) 2^-24 max sum|q||k|/sqrt(d); exponentials and rescales add 2^-20 A;
   * sums over N keys: N 2^-24 A, twice;
@@ -20,6 +20,7 @@ from paged_ref import PAGE, attention64, mask_words, pack_pages, rows_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
+U_P = {torch.bfloat16: 2.0 ** -16, torch.float16: 2.0 ** -11}
 U = {torch.bfloat16: torch.finfo(torch.bfloat16).eps / 2, torch.float16: torch.finfo(torch.float16).eps / 2}
 
 
@@ -76,7 +77,7 @@ class Case:
 
     def check(self, o, nodes=None):
         at, N = 0, self.nh * self.d
-        u, uo = U[self.dt], U[self.o_dtype] ** self.o_terms
+        u, uo = U_P[self.dt], U[self.o_dtype] ** self.o_terms
         for r, (B, P) in enumerate(zip(self.Bs, self.Ps)):
             k = rows_of(self.k[self.layer], self.table[r], P + B).double()
             v = rows_of(self.v[self.layer], self.table[r], P + B).double()
@@ -192,7 +193,7 @@ def test_what_lies_behind_a_mask_has_no_effect(junk, dtype):
             see = np.concatenate([np.ones((B, P), bool), c.masks[r][1]], 1)[keep]
             want, A, qk, vs = attention64(c.q64[at:at + B][keep], k, v, torch.from_numpy(see))
             got = o[at:at + B].double().view(B, 4, d)[keep]
-            u = U[c.dt]
+            u = U_P[c.dt]
             tol = A * (u + 2 * (d + 4) * 2.0 ** -24 * qk.unsqueeze(-1) + 2.0 ** -20 + (P + B) * 2.0 ** -23) + want.abs() * 2.0 ** -11 + 2.0 ** -25 + vs * 2.0 ** -25
             assert ((got - want).abs() <= tol).all(), (r, d)
             at += (B + 31) // 32 * 32
