@@ -353,6 +353,12 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _raw_stream(device):
+    """The current stream of a device as an integer.  A paged call is a few microseconds of GPU work, and a stream object alone costs two."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def goose_lm_head_argmax_static(desc: ModelDesc, packed_head, x, B, argmax, margin=None):
     """goose_lm_head_argmax without a context and without any allocation (static device workspace)."""
     cd = desc._c()
@@ -376,6 +382,8 @@ class PagedCache:
         if not ok:
             raise GooseError(GOOSE_ERR_ARG, "PagedCache: shapes, types or devices of the pools and tables do not fit together")
         self._c = _Pages(*[x.data_ptr() for x in t], refs.shape[0], table.shape[0], table.shape[1])
+        self._ref, self._device = C.byref(self._c), kpool.get_device()  # (-1 on the CPU)
+        self._shape = (kpool.dtype,) + tuple(kpool.shape[i] for i in (0, 2, 3))
 
 
 class PagedRequests:
@@ -391,17 +399,14 @@ class PagedRequests:
             ptrs = [None if q.get(n) is None else q[n].data_ptr() for n in names]
             k = 0 if q.get("succ_ids") is None else int(q["succ_ids"].shape[1])
             self._c[i] = _PagedRequest(int(q["seq"]), int(q["B"]), int(q.get("P_max", 0)), *ptrs, k)
+        # rows of the stacked buffers that the requests reach into (each starts at a multiple of 32)
+        Bs = [q.B for q in self._c]
+        self.rows = sum((b + 31) // 32 * 32 for b in Bs[:-1]) + (Bs[-1] if Bs else 0)
+        tensors = [q[n] for q in reqs for n in names if q.get(n) is not None]
+        self._devices = {t.get_device() for t in tensors}
 
     def __len__(self):
         return len(self._c)
-
-
-def _stacked_rows(r):
-    """Rows of the stacked buffers that the requests reach into (each starts at a multiple of 32)."""
-    at = 0
-    for q in r._c[:-1]:
-        at += (q.B + 31) // 32 * 32
-    return at + r._c[len(r) - 1].B if len(r) else 0
 
 
 def _rows_ok(t, rows, cols, dtypes):
@@ -427,6 +432,9 @@ class GooseContext:
         else:
             _check(self.lib.goose_create(C.byref(cd), max_B, cap, C.byref(h)), "goose_create")
         self._h = h
+        import torch
+        self._cache_shape = ({"bf16": torch.bfloat16, "f16": torch.float16}.get(desc.dtype), desc.n_layers, desc.kv_heads,
+                             GOOSE_PAGE * desc.head_dim)  # of a paged cache: its type, layers, KV heads, elements of a head's page
 
     def close(self):
         if getattr(self, "_h", None):
@@ -510,81 +518,82 @@ class GooseContext:
                                                   _stream()), "goose_verify_step_batched")
 
     # ---- paged caches
-    def _pages(self, cache: PagedCache, *tensors):
-        """The descriptor of `cache`, after a look at what the C side cannot see: element types, head layout, devices."""
+    def _paged(self, cache, reqs, *tensors):
+        """Descriptor, requests and stream of a paged call, after a look at what the C side cannot see: element types, head layout, devices."""
         import torch
-        d = self.desc
-        dev, want = cache.kpool.device, {"bf16": torch.bfloat16, "f16": torch.float16}.get(d.dtype)
-        if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+        dev = cache._device
+        if dev >= 0 and dev != torch.cuda.current_device():
             raise GooseError(GOOSE_ERR_ARG, "the paged cache is not on the current device")
-        if want is not None and (cache.kpool.dtype != want or cache.kpool.shape[2] != d.kv_heads
-                                 or cache.kpool.shape[3] != GOOSE_PAGE * d.head_dim or cache.kpool.shape[0] != d.n_layers):
+        if cache._shape != self._cache_shape and self.desc.dtype != "f32":
             raise GooseError(GOOSE_ERR_ARG, "the paged cache is not one of this model")
+        r = None
+        if reqs is not None:
+            r = reqs if isinstance(reqs, PagedRequests) else PagedRequests(reqs)
+            if not r._devices <= {dev}:
+                raise GooseError(GOOSE_ERR_ARG, "a tensor of the requests is on another device than the paged cache")
         for t in tensors:
-            if t is not None and t.device != dev:
+            if t is not None and t.get_device() != dev:
                 raise GooseError(GOOSE_ERR_ARG, "a tensor of the call is on another device than the paged cache")
-        return C.byref(cache._c)
-
-    @staticmethod
-    def _reqs(reqs):
-        return reqs if isinstance(reqs, PagedRequests) else PagedRequests(reqs)
+        return r, _raw_stream(dev) if dev >= 0 else None
 
     def goose_pages_clear(self, cache):
-        _check(self.lib.goose_pages_clear(self._h, self._pages(cache), _stream()), "goose_pages_clear")
+        _, st = self._paged(cache, None)
+        _check(self.lib.goose_pages_clear(self._h, cache._ref, st), "goose_pages_clear")
 
     def goose_pages_fork(self, cache, src, dst, length=-1):
-        _check(self.lib.goose_pages_fork(self._h, self._pages(cache), src, length, _seqs(dst), len(dst), _stream()), "goose_pages_fork")
+        _, st = self._paged(cache, None)
+        _check(self.lib.goose_pages_fork(self._h, cache._ref, src, length, _seqs(dst), len(dst), st), "goose_pages_fork")
 
     def goose_pages_reserve(self, cache, seqs, new):
         if len(seqs) != len(new):
             raise GooseError(GOOSE_ERR_ARG, "goose_pages_reserve")
-        _check(self.lib.goose_pages_reserve(self._h, self._pages(cache), _seqs(seqs), _seqs(new), len(seqs), _stream()),
-               "goose_pages_reserve")
+        _, st = self._paged(cache, None)
+        _check(self.lib.goose_pages_reserve(self._h, cache._ref, _seqs(seqs), _seqs(new), len(seqs), st), "goose_pages_reserve")
 
     def goose_pages_commit(self, cache, reqs):
-        r = self._reqs(reqs)
-        _check(self.lib.goose_pages_commit(self._h, self._pages(cache), r._c, len(r), _stream()), "goose_pages_commit")
+        r, st = self._paged(cache, reqs)
+        _check(self.lib.goose_pages_commit(self._h, cache._ref, r._c, len(r), st), "goose_pages_commit")
 
     def goose_pages_free(self, cache, seqs):
-        _check(self.lib.goose_pages_free(self._h, self._pages(cache), _seqs(seqs), len(seqs), _stream()), "goose_pages_free")
+        _, st = self._paged(cache, None)
+        _check(self.lib.goose_pages_free(self._h, cache._ref, _seqs(seqs), len(seqs), st), "goose_pages_free")
 
     def goose_qk_norm_rope_paged(self, cache, layer, qkv, gq, gk, reqs, q, q_terms=1):
         """qkv: fp32 [ksplit][rows][columns] (strides of the first two dimensions are free), q: [rows][columns] of the cache's type."""
-        r = self._reqs(reqs)
-        pages = self._pages(cache, qkv, gq, gk, q)
-        rows, d = _stacked_rows(r), self.desc
+        r, st = self._paged(cache, reqs, qkv, gq, gk, q)
+        d, (ks, rows, cols), (s0, s1, s2) = self.desc, qkv.shape, qkv.stride()
         import torch
-        if not (qkv.dim() == 3 and qkv.shape[0] > 0
-                and _rows_ok(qkv[0], rows, (d.n_heads + 2 * d.kv_heads) * d.head_dim, (torch.float32,))
-                and _rows_ok(q, rows, d.n_heads * d.head_dim * q_terms, (cache.kpool.dtype,))
-                and all(g is None or (g.dtype == q.dtype and g.is_contiguous() and g.numel() == self.desc.head_dim) for g in (gq, gk))):
+        if not (qkv.dtype == torch.float32 and s2 == 1 and rows >= r.rows and cols >= (d.n_heads + 2 * d.kv_heads) * d.head_dim
+                and _rows_ok(q, r.rows, d.n_heads * d.head_dim * q_terms, (cache.kpool.dtype,))
+                and all(g is None or (g.dtype == q.dtype and g.is_contiguous() and g.numel() == d.head_dim) for g in (gq, gk))):
             raise GooseError(GOOSE_ERR_ARG, "goose_qk_norm_rope_paged: rows or types of qkv, q or the gains")
-        _check(self.lib.goose_qk_norm_rope_paged(self._h, pages, layer, _ptr(qkv), qkv.shape[0], qkv.stride(0), qkv.stride(1), _ptr(gq),
-                                                 _ptr(gk), r._c, len(r), _ptr(q), q.stride(0), q_terms, _stream()),
-               "goose_qk_norm_rope_paged")
+        _check(self.lib.goose_qk_norm_rope_paged(self._h, cache._ref, layer, qkv.data_ptr(), ks, s0, s1, gq.data_ptr() if gq is not None else None,
+                                                 gk.data_ptr() if gk is not None else None, r._c, len(r), q.data_ptr(), q.stride(0), q_terms,
+                                                 st), "goose_qk_norm_rope_paged")
 
     def goose_attn_paged(self, cache, layer, q, q_terms, reqs, shared_pages, o, o_terms=1):
         """q: [rows][columns] of the cache's type; o: [rows][columns], bf16 or fp16."""
-        r = self._reqs(reqs)
-        pages = self._pages(cache, q, o)
-        rows, cols = _stacked_rows(r), self.desc.n_heads * self.desc.head_dim
+        r, st = self._paged(cache, reqs, q, o)
+        cols = self.desc.n_heads * self.desc.head_dim
         import torch
-        if not (_rows_ok(q, rows, cols * q_terms, (cache.kpool.dtype,))
-                and _rows_ok(o, rows, cols * o_terms, (torch.bfloat16, torch.float16))):
+        if not (_rows_ok(q, r.rows, cols * q_terms, (cache.kpool.dtype,))
+                and _rows_ok(o, r.rows, cols * o_terms, (torch.bfloat16, torch.float16))):
             raise GooseError(GOOSE_ERR_ARG, "goose_attn_paged: rows or types of q or o")
-        _check(self.lib.goose_attn_paged(self._h, pages, layer, _ptr(q), q.stride(0), q_terms, r._c, len(r), shared_pages, _ptr(o),
-                                         o.stride(0), _dtype_code(o), o_terms, _stream()), "goose_attn_paged")
+        _check(self.lib.goose_attn_paged(self._h, cache._ref, layer, q.data_ptr(), q.stride(0), q_terms, r._c, len(r), shared_pages, o.data_ptr(),
+                                         o.stride(0), _dtype_code(o), o_terms, st), "goose_attn_paged")
 
     def goose_verify_layer_paged(self, packed_layer, cache, layer, x, reqs, shared_pages=0):
-        r = self._reqs(reqs)
-        _check(self.lib.goose_verify_layer_paged(self._h, _ptr(packed_layer), self._pages(cache, x), layer, _ptr(x), r._c, len(r),
-                                                 shared_pages, _stream()), "goose_verify_layer_paged")
+        r, st = self._paged(cache, reqs, packed_layer, x)
+        if not (x.dim() == 2 and x.is_contiguous() and x.shape[0] >= r.rows and x.shape[1] == self.desc.hidden):
+            raise GooseError(GOOSE_ERR_ARG, "goose_verify_layer_paged: rows of x")
+        _check(self.lib.goose_verify_layer_paged(self._h, _ptr(packed_layer), cache._ref, layer, _ptr(x), r._c, len(r), shared_pages, st),
+               "goose_verify_layer_paged")
 
     def goose_verify_step_paged(self, model: dict, cache, reqs, shared_pages, argmax_all):
         m = _ModelPtrs(model["embed"].data_ptr(), model["packed_layers"].data_ptr(), model["packed_head"].data_ptr(), None, None)
-        r = self._reqs(reqs)
-        _check(self.lib.goose_verify_step_paged(self._h, C.byref(m), self._pages(cache, argmax_all), r._c, len(r), shared_pages,
-                                                _ptr(argmax_all), _stream()), "goose_verify_step_paged")
+        r, st = self._paged(cache, reqs, argmax_all)
+        _check(self.lib.goose_verify_step_paged(self._h, C.byref(m), cache._ref, r._c, len(r), shared_pages, _ptr(argmax_all), st),
+               "goose_verify_step_paged")
 
     def goose_device_flags(self) -> int:
         out = C.c_int32(0)

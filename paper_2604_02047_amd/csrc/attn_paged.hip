@@ -403,17 +403,19 @@ __device__ inline void leave(const PagedAttnArgs& a, const Item& it, const Row& 
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------
-// One workgroup = NT tiles of 32 rows x a range of blocks, dealt to four wavefronts in contiguous quarters; every wavefront streams
-// its blocks global -> registers -> matrix cores (no barrier in the loop), the next block's keys and values requested as
-// soon as the current ones have been used.
-template <int D, int QT, bool F16, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_paged_stream(const PagedAttnArgs a) {
+// One workgroup = RT tiles of 32 rows x a range of blocks: eight wavefronts, each with one tile and one of 8 / RT contiguous shares of the
+// range.  A wavefront streams its blocks global -> registers -> matrix cores (no barrier in the loop), the next block's keys
+// and values requested as soon as the current ones have been used; two tiles' wavefronts find each other's blocks in the cache.
+template <int D, int QT, bool F16, int RT>
+__global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) {
   typedef RowTile<D, QT, F16> Tile;
   typedef typename Tile::T T;
-  constexpr int NG = 4, NS = D / 16, QUADS = D / 8, QPW = QUADS / NG;
+  constexpr int NG = 8 / RT, NS = D / 16, QUADS = D / 8, QPW = QUADS / NG;
+  static_assert(QUADS % NG == 0, "register quads must divide over the key groups");
   constexpr int WFLOATS = (QUADS + 1) * 256;  // a wavefront's state at the merge
-  __shared__ __attribute__((aligned(16))) float lds[NG * WFLOATS];
-  const int tid = threadIdx.x, lane = tid & 63, g = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ __attribute__((aligned(16))) float lds[8 * WFLOATS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = wave % NG, rt = wave / NG;
   const int l31 = lane & 31, hh = lane >> 5;
   const int kvh = blockIdx.x;  // the fast index: where 8 divides the KV heads, all items of a head run on one XCD and find each other's blocks in its L2
   const Item it = item_of(a, blockIdx.y, kvh);
@@ -425,103 +427,82 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_paged_stream(const Pag
   auto block_at = [&](int b) -> size_t {
     return ((size_t)pg.of(b, lane) * a.n_kv + kvh) * (GOOSE_PAGE * D) + (size_t)(b & 1) * 32 * D;
   };
+  const Row row = row_of(a, it, (it.tile * RT + rt) * 32 + l31, kvh);
+  const bool work = RT == 1 || __builtin_amdgcn_ballot_w64(row.live) != 0;  // (the second tile may be empty)
   u32x4 kreg[NS], vreg[NS];
   size_t at = 0;
-  if (total > 0) {
+  if (total > 0 && work) {
     pg.load(lane);
     at = block_at(b0);
     fetch(kp + at, lane, kreg);
     fetch(vp + at, lane, vreg);
   }
-  Row row[NT];
-  MaskRow mk[NT];
-  Tile t[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    row[n] = row_of(a, it, (it.tile * NT + n) * 32 + l31, kvh);
-    t[n].init(a, row[n], hh);
-    mk[n] = mask_of(a, it, row[n]);
-  }
-  const bool both = NT == 1 || __builtin_amdgcn_ballot_w64(row[NT - 1].live) != 0;  // (the second tile may be empty)
+  Tile t;
+  t.init(a, row, hh);
   const float scale = softmax_scale(D);
-  auto block = [&](int idx, auto tree) {
-    constexpr bool TREE = decltype(tree)::value;
-    const int slot0 = (b0 + idx) * 32;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-      if (n == 0 || both) t[n].scores(kreg);
-    if (idx + 1 < total) { at = block_at(b0 + idx + 1); fetch(kp + at, lane, kreg); }
-    unsigned vis[NT];
-    bool odd = false;
-    if (TREE) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        vis[n] = window16(mk[n].w0, mk[n].w1, slot0 + hh * 16 - it.P);
-        t[n].mask(vis[n]);
+  if (work) {
+    const MaskRow mk = mask_of(a, it, row);
+    auto block = [&](int idx, auto tree) {
+      constexpr bool TREE = decltype(tree)::value;
+      const int slot0 = (b0 + idx) * 32;
+      t.scores(kreg);
+      if (idx + 1 < total) { at = block_at(b0 + idx + 1); fetch(kp + at, lane, kreg); }
+      unsigned vis = 0xFFFFu;
+      bool odd = false;
+      if (TREE) {
+        vis = window16(mk.w0, mk.w1, slot0 + hh * 16 - it.P);
+        t.mask(vis);
+        odd = clean_values<F16>(vreg, it.P + it.B - slot0 - hh * 16);
       }
-      odd = clean_values<F16>(vreg, it.P + it.B - slot0 - hh * 16);
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-      if (n == 0 || both) {
-        t[n].maximum();
-        t[n].rescale(scale);
-        t[n].weights();
-        if (TREE && odd) t[n].values_odd(vreg, vis[n]);
-        else t[n].values(vreg);
-      }
-    if (idx + 1 < total) fetch(vp + at, lane, vreg);
-  };
-  // blocks that every row sees whole, then those that the tree reaches into
-  const int full = it.ri < 0 ? total : max(0, min(total, (it.P >> 5) - b0));
-  for (int idx = 0; idx < full; ++idx) block(idx, std::false_type());
-  for (int idx = full; idx < total; ++idx) block(idx, std::true_type());
-  if (g == 0) check_shared(a, it, lane);
-
-  // ---- the four wavefronts' states join in one round a tile through LDS: each leaves its own, then owns a quarter of the columns
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    if (n > 0) {
-      if (!both) return;
-      __syncthreads();
-    }
-    float* dst = lds + (size_t)g * WFLOATS + lane * 4;
-    *reinterpret_cast<f32x4*>(dst) = f32x4{t[n].m * scale, t[n].l, 0.f, 0.f};
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4*>(dst + 256 * (1 + dt * 4 + q)) =
-            f32x4{t[n].o[dt][q * 4], t[n].o[dt][q * 4 + 1], t[n].o[dt][q * 4 + 2], t[n].o[dt][q * 4 + 3]};
-    __syncthreads();
-    const float* src = lds + lane * 4;
-    float mj[NG], lj[NG], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int j = 0; j < NG; ++j) {
-      const f32x4 ml = *reinterpret_cast<const f32x4*>(src + (size_t)j * WFLOATS);
-      mj[j] = ml[0];
-      lj[j] = ml[1];
-      m = fmaxf(m, mj[j]);
-    }
-    const float ref = finite_ref(m);
-    f32x4 res[QPW];
-#pragma unroll
-    for (int q = 0; q < QPW; ++q) res[q] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < NG; ++j) {
-      const float w = __builtin_amdgcn_exp2f(mj[j] - ref);
-      l += w * lj[j];
-#pragma unroll
-      for (int q = 0; q < QPW; ++q)
-        res[q] += w * *reinterpret_cast<const f32x4*>(src + (size_t)j * WFLOATS + 256 * (1 + g * QPW + q));
-    }
-    l += __shfl_xor(l, 32, 64);
-    // quad i of the accumulator = columns 8 i + 4 hh .. + 3
-    if (row[n].live) {
-#pragma unroll
-      for (int q = 0; q < QPW; ++q) leave(a, it, row[n], D, (g * QPW + q) * 8 + hh * 4, res[q], m, l);
-    }
+      t.maximum();
+      t.rescale(scale);
+      t.weights();
+      if (TREE && odd) t.values_odd(vreg, vis);
+      else t.values(vreg);
+      if (idx + 1 < total) fetch(vp + at, lane, vreg);
+    };
+    // blocks that every row sees whole, then those that the tree reaches into
+    const int full = it.ri < 0 ? total : max(0, min(total, (it.P >> 5) - b0));
+    for (int idx = 0; idx < full; ++idx) block(idx, std::false_type());
+    for (int idx = full; idx < total; ++idx) block(idx, std::true_type());
   }
+  if (wave == 0) check_shared(a, it, lane);
+
+  // ---- the key groups' states join in one round through LDS: each wavefront leaves its own, then owns some of its tile's columns
+  float* dst = lds + (size_t)wave * WFLOATS + lane * 4;
+  *reinterpret_cast<f32x4*>(dst) = f32x4{t.m * scale, t.l, 0.f, 0.f};
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4*>(dst + 256 * (1 + dt * 4 + q)) = f32x4{t.o[dt][q * 4], t.o[dt][q * 4 + 1], t.o[dt][q * 4 + 2], t.o[dt][q * 4 + 3]};
+  __syncthreads();
+  const float* src = lds + (size_t)rt * NG * WFLOATS + lane * 4;
+  float mj[NG], lj[NG], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    const f32x4 ml = *reinterpret_cast<const f32x4*>(src + (size_t)j * WFLOATS);
+    mj[j] = ml[0];
+    lj[j] = ml[1];
+    m = fmaxf(m, mj[j]);
+  }
+  const float ref = finite_ref(m);
+  f32x4 res[QPW];
+#pragma unroll
+  for (int q = 0; q < QPW; ++q) res[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    const float w = __builtin_amdgcn_exp2f(mj[j] - ref);
+    l += w * lj[j];
+#pragma unroll
+    for (int q = 0; q < QPW; ++q)
+      res[q] += w * *reinterpret_cast<const f32x4*>(src + (size_t)j * WFLOATS + 256 * (1 + g * QPW + q));
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (!row.live) return;
+  // quad i of the accumulator = columns 8 i + 4 hh .. + 3
+#pragma unroll
+  for (int q = 0; q < QPW; ++q) leave(a, it, row, D, (g * QPW + q) * 8 + hh * 4, res[q], m, l);
 }
 
 // ---- many rows ----------------------------------------------------------------------------------------------------------
@@ -757,19 +738,26 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
 }
 
 // Joins the items of a row: D / 4 threads a (row, head), four columns each, records in a fixed order, the loads of eight in flight together.
-template <int D>
+// PARTS = 4: the records of a pair are dealt to four such groups of threads, which join through LDS (many splits mean few rows: one trip to memory
+// instead of four).  The KV head is the fast index as in the kernels above: the records are in that XCD's L2.
+template <int D, int PARTS>
 __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
-  constexpr int TPR = D / 4, CH = 8;
-  const int it = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, c = (threadIdx.x % TPR) * 4;
-  if (it >= a.rows * a.n_heads) return;
-  const int h = (int)((unsigned)it / (unsigned)a.rows), crow = it - h * a.rows;
+  constexpr int TPR = D / 4, CH = 8, PAIRS = 256 / TPR / PARTS;
+  __shared__ f32x4 part_o[PARTS > 1 ? 256 : 1];
+  __shared__ float2 part_ml[PARTS > 1 ? 256 : 1];
+  const int tid = threadIdx.x, c = (tid % TPR) * 4, p = tid / TPR % PARTS;
+  const int pair = blockIdx.y * PAIRS + tid / TPR / PARTS;  // of this KV head: (query head of the group, row)
+  const bool on = pair < a.rows * a.group;
+  const int hg = on ? (int)((unsigned)pair / (unsigned)a.rows) : 0, crow = on ? pair - hg * a.rows : 0;
+  const int h = blockIdx.x * a.group + hg;
   int r = 0;
   while (r + 1 < a.n_req && crow >= a.r[r + 1].c0) ++r;
-  const int n = a.sh_splits + a.r[r].splits;
+  const int all = a.sh_splits + a.r[r].splits;
+  const int s_lo = all * p / PARTS, n = all * (p + 1) / PARTS;
   const size_t base = (size_t)h * a.rows + crow, step = (size_t)a.n_heads * a.rows;
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
   float den = 0.f, m = -INFINITY;
-  for (int s0 = 0; s0 < n; s0 += CH) {
+  for (int s0 = s_lo; s0 < n; s0 += CH) {
     float2 ml[CH];
     f32x4 ov[CH];
 #pragma unroll
@@ -793,17 +781,43 @@ __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
         num += w * ov[k];
       }
   }
+  if (PARTS > 1) {
+    part_o[tid] = num;
+    part_ml[tid] = make_float2(m, den);
+    __syncthreads();
+    if (p != 0) return;
+#pragma unroll
+    for (int k = 1; k < PARTS; ++k) m = fmaxf(m, part_ml[tid + k * TPR].x);
+    const float ref = finite_ref(m);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    den = 0.f;
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) {
+      const float2 ml = part_ml[tid + k * TPR];
+      const float w = __builtin_amdgcn_exp2f(ml.x - ref);
+      den = fmaf(w, ml.y, den);
+      sum += w * part_o[tid + k * TPR];
+    }
+    num = sum;
+  }
+  if (!on) return;
   const float inv = den == 0.f ? 0.f : 1.0f / den;
   store_out(a, (size_t)a.r[r].row0 + crow - a.r[r].c0, h * D + c, num * inv);
 }
 
-// which kernel: TILES beyond 64 rows of an item, else tiles of 32 rows a wavefront
+// which kernel: TILES beyond 64 rows of an item, else STREAM with one or two row tiles
 enum { STREAM1, STREAM2, TILES };
 template <int D, int QT, bool F16>
 void launch_t(int kind, dim3 grid, const PagedAttnArgs& a, hipStream_t st) {
   if (kind == TILES) hipLaunchKernelGGL((k_paged_tiles<D, QT, F16>), grid, dim3(512), 0, st, a);
-  else if (kind == STREAM2) hipLaunchKernelGGL((k_paged_stream<D, QT, F16, 2>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_paged_stream<D, QT, F16, 1>), grid, dim3(256), 0, st, a);
+  else if (kind == STREAM2) hipLaunchKernelGGL((k_paged_stream<D, QT, F16, 2>), grid, dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((k_paged_stream<D, QT, F16, 1>), grid, dim3(512), 0, st, a);
+}
+template <int D>
+void launch_merge(dim3 pairs, int splits, const PagedAttnArgs& a, hipStream_t st) {
+  const int per = 1024 / D;
+  if (splits > 8) hipLaunchKernelGGL((k_paged_merge<D, 4>), dim3(pairs.x, (pairs.y * 4 + per - 1) / per), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_paged_merge<D, 1>), dim3(pairs.x, (pairs.y + per - 1) / per), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -835,40 +849,81 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.o_terms = o_terms;
   a.o_f16 = o_dtype == GOOSE_DTYPE_F16;
   a.sh_blocks = shared_pages * 2;
-  int own_max = 0, own_rows = 0;
+  int own_rows = 0;
   for (int r = 0; r < rq.n; ++r) own_rows = rq.r[r].B > own_rows ? rq.r[r].B : own_rows;
   own_rows *= a.group;
   const int sh_rows = shared_pages > 0 ? rq.rows * a.group : 0, most = sh_rows > own_rows ? sh_rows : own_rows;
   const int kind = most > 64 ? TILES : (most > 32 ? STREAM2 : STREAM1);
-  a.sh_kg = sh_rows <= 128 ? 2 : 1;
-  a.own_kg = own_rows <= 128 ? 2 : 1;
+  // k_paged_tiles: 128 rows with two key groups where that leaves fewer rows of a tile empty
+  auto key_groups = [](int rows) { return (rows + 127) / 128 * 128 < (rows + 255) / 256 * 256 ? 2 : 1; };
+  a.sh_kg = key_groups(sh_rows);
+  a.own_kg = key_groups(own_rows);
   const int sh_height = kind == TILES ? 256 / a.sh_kg : (kind == STREAM2 ? 64 : 32);
   const int own_height = kind == TILES ? 256 / a.own_kg : sh_height;
+  const int sh_mul = kind == TILES ? a.sh_kg : 1, own_mul = kind == TILES ? a.own_kg : 1;  // blocks that an item takes at a time
   a.sh_tiles = (sh_rows + sh_height - 1) / sh_height;
-  // Blocks per item: one round of workgroups (256 of the tall kernels, 512 of STREAM1), but at least eight blocks each.
-  long long work = (long long)a.sh_tiles * a.sh_blocks;
+  int own_blocks[GOOSE_MAX_REQUESTS], own_longest = 0;
   for (int r = 0; r < rq.n; ++r) {
     const PagedReq& s = rq.r[r];
     a.r[r] = AttnReq{s.seq, s.B, s.P_max, s.row0, s.c0, (s.B * a.group + own_height - 1) / own_height, 0, (const uint64_t*)s.p};
-    const int nb = (s.P_max + s.B + 31) / 32 - a.sh_blocks;
-    own_max = nb > own_max ? nb : own_max;
-    work += (long long)a.r[r].tiles * nb;
+    own_blocks[r] = (s.P_max + s.B + 31) / 32 - a.sh_blocks;
+    const int steps = (own_blocks[r] + own_mul - 1) / own_mul;
+    own_longest = steps > own_longest ? steps : own_longest;
   }
-  const int slots = kind == STREAM1 ? 512 : 256;
-  long long per = (work * n_kv + slots - 1) / slots;
-  if (per < 8) per = 8;
+  // Splits: items of at most `per` steps (blocks, or pairs of them).  They run in rounds of 256 workgroups, one a compute unit, the shared keys' items first;
+  // an item costs its steps and a fixed part (FIXED steps: start, first loads, epilogue), a split its records in the merge.  Tried: the smallest
+  // `per` that makes one to four rounds of all items, or of the shared ones; the cheapest is taken.
   const size_t step = (size_t)n_heads * rq.rows;  // records of one split
-  int own_splits;
-  for (;; per += per / 4) {
-    a.sh_splits = (int)((a.sh_blocks + per - 1) / per);
-    own_splits = (int)((own_max + per - 1) / per);
-    if (a.sh_splits + own_splits <= 1 || (size_t)(a.sh_splits + own_splits) * step <= max_records) break;
-    if (per > a.sh_blocks + own_max) return GOOSE_ERR_CAPACITY;
+  struct Plan { long long sh, own; int splits; };
+  auto plan_at = [&](int per) {
+    Plan p{0, 0, 0};
+    const int sh = (a.sh_blocks + per * sh_mul - 1) / (per * sh_mul);
+    p.sh = (long long)a.sh_tiles * sh * n_kv;
+    for (int r = 0; r < rq.n; ++r) {
+      const int n = (own_blocks[r] + per * own_mul - 1) / (per * own_mul);
+      p.own += (long long)a.r[r].tiles * n * n_kv;
+      p.splits = n > p.splits ? n : p.splits;
+    }
+    p.splits += sh;
+    return p;
+  };
+  auto fits = [&](const Plan& p) { return p.splits <= 1 || (size_t)p.splits * step <= max_records; };
+  const int least = kind == TILES ? 4 : 8, fixed = kind == TILES ? 10 : 24, sh_steps = (a.sh_blocks + sh_mul - 1) / sh_mul,
+            longest = sh_steps > own_longest ? sh_steps : own_longest;
+  auto cost_of = [&](const Plan& p, int per) {
+    const long long sh_len = (per < sh_steps ? per : sh_steps) + fixed, own_len = (per < own_longest ? per : own_longest) + fixed;
+    const long long rounds = (p.sh + 255) / 256, room = (rounds * 256 - p.sh) * (sh_len / own_len);  // own items beside the last shared ones
+    const long long left = p.own > room ? p.own - room : 0;
+    return rounds * sh_len + (left + 255) / 256 * own_len + (p.splits > 1 ? (long long)(p.splits * step * head_dim / 1000000) : 0);
+  };
+  const int most_steps = longest > least ? longest : least;
+  int per = most_steps;
+  Plan plan = plan_at(per);
+  if (!fits(plan)) return GOOSE_ERR_CAPACITY;
+  long long best = cost_of(plan, per);
+  auto consider = [&](int cand) {
+    if (cand < least || cand >= most_steps) return;
+    const Plan p = plan_at(cand);
+    const long long cost = cost_of(p, cand);
+    if (fits(p) && cost < best) { best = cost; per = cand; }
+  };
+  for (int rounds = 1; rounds <= 4; ++rounds) {
+    int lo = least, hi = most_steps;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      const Plan p = plan_at(mid);
+      if (p.sh + p.own <= 256 * rounds && fits(p)) hi = mid; else lo = mid + 1;
+    }
+    consider(lo);
+    const int sh = a.sh_tiles > 0 ? 256 * rounds / (a.sh_tiles * n_kv) : 0;
+    if (sh > 0) consider((sh_steps + sh - 1) / sh);
   }
+  a.sh_splits = (a.sh_blocks + per * sh_mul - 1) / (per * sh_mul);
+  int own_splits = 0;
   unsigned items = (unsigned)(a.sh_tiles * a.sh_splits);
   for (int r = 0; r < rq.n; ++r) {
-    const int nb = (rq.r[r].P_max + rq.r[r].B + 31) / 32 - a.sh_blocks;
-    a.r[r].splits = (int)((nb + per - 1) / per);
+    a.r[r].splits = (own_blocks[r] + per * own_mul - 1) / (per * own_mul);
+    own_splits = a.r[r].splits > own_splits ? a.r[r].splits : own_splits;
     items += (unsigned)(a.r[r].tiles * a.r[r].splits);
   }
   a.direct = a.sh_splits + own_splits == 1;
@@ -883,9 +938,8 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   }
   int rc = goose_launch_status();
   if (rc != GOOSE_OK || a.direct) return rc;
-  const int per_wg = 1024 / head_dim;
-  const dim3 mgrid((unsigned)((rq.rows * n_heads + per_wg - 1) / per_wg));
-  if (head_dim == 128) hipLaunchKernelGGL(k_paged_merge<128>, mgrid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_paged_merge<64>, mgrid, dim3(256), 0, st, a);
+  const dim3 pairs(n_kv, rq.rows * a.group);
+  if (head_dim == 128) launch_merge<128>(pairs, a.sh_splits + own_splits, a, st);
+  else launch_merge<64>(pairs, a.sh_splits + own_splits, a, st);
   return goose_launch_status();
 }

@@ -81,7 +81,9 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(const goose_pages pg, cons
   __shared__ int first[GOOSE_MAX_REQUESTS], count[GOOSE_MAX_REQUESTS], entry0[GOOSE_MAX_REQUESTS], leave[GOOSE_MAX_REQUESTS];
   __shared__ int used[GOOSE_MAX_REQUESTS], ws[NT / 64], list[PAGES_PER_CALL], bad;
   const int tid = threadIdx.x;
-  int refs0 = 0;
+  int refs0 = 0, f[4];  // counts of this thread's first four pages: asked for beside the lengths
+#pragma unroll
+  for (int k = 0; k < 4; ++k) f[k] = tid * 4 + k < pg.n_pages ? pg.d_refs[tid * 4 + k] : 1;
   if (tid == 0) bad = 0;
   __syncthreads();
   if (tid < sq.n) {
@@ -142,9 +144,11 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(const goose_pages pg, cons
   int found = 0;
   for (int base = 0; base < pg.n_pages && found < need; base += 4 * NT) {
     const int p0 = base + tid * 4;
-    int f[4], c = 0, sum;
+    int c = 0, sum;
+    if (base > 0) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) f[k] = p0 + k < pg.n_pages ? pg.d_refs[p0 + k] : 1;
+      for (int k = 0; k < 4; ++k) f[k] = p0 + k < pg.n_pages ? pg.d_refs[p0 + k] : 1;
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) c += f[k] == 0;
     int at = found + block_scan(c, ws, &sum);
@@ -204,55 +208,63 @@ __global__ __launch_bounds__(256) void k_pages_copy(const goose_pages pg, const 
 }
 
 // The accepted path, slot P + path[j] -> P + j for j = 1 .. L, in one (layer, head) of a request.  Thread c owns chunk c of the key rows
-// (16 bytes) and column c of the value rows (2 bytes).  Eight moves at a time, all loads before all stores: path[j] >= j and increasing, so
-// no later source lies at or below an earlier destination.
+// (16 bytes) and column c of the value rows (2 bytes).  MOVES moves at a time, all loads before all stores: path[j] >= j and increasing, so
+// no later source lies at or below an earlier destination.  The whole path is fetched at once, an entry a lane, with length, count and page ids
+// beside it: asked for move by move it was a trip to memory each (16 requests, 8 layers of 8 heads: 24 us, now MOVE_NOW).
+constexpr int MOVES = 16;  // (accepted paths are rarely longer)
 template <int D>
 __global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const PagedReqs rq, int n_kv) {
   typedef unsigned short u16;
   const PagedReq& q = rq.r[blockIdx.y];
-  const int layer = blockIdx.x / n_kv, head = blockIdx.x - layer * n_kv, c = threadIdx.x;
+  const int layer = blockIdx.x / n_kv, head = blockIdx.x - layer * n_kv, c = threadIdx.x, lane = c & 63;
   const int32_t* path = static_cast<const int32_t*>(q.p);
-  const int P = pg.d_len[q.seq];
-  int L = *q.accept_len;
+  int p_lo = lane < q.B ? path[lane] : -1, p_hi = lane + 64 < q.B ? path[lane + 64] : -1;
+  const int P = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]);
+  int L = __builtin_amdgcn_readfirstlane(*q.accept_len);
   if (P < 0 || L < 0) return;  // (flagged by k_pages_settle)
   L = min(L, q.B - 1);
+  const int32_t* row = pg.d_table + (size_t)q.seq * pg.table_ld;
+  const int e0 = P >> 6;
+  const int id = lane < 3 && e0 + lane < pg.table_ld ? row[e0 + lane] : -1;  // a tree of 128 nodes reaches into three pages
+  auto at = [&](int j) { return j < 64 ? __builtin_amdgcn_readlane(p_lo, j) : __builtin_amdgcn_readlane(p_hi, j - 64); };
   const size_t layer0 = (size_t)layer * pg.n_pages;
   u16* const kpool = static_cast<u16*>(pg.d_kpool);
   u16* const vpool = static_cast<u16*>(pg.d_vpool);
-  const int32_t* row = pg.d_table + (size_t)q.seq * pg.table_ld;
-  const int e0 = P >> 6;
-  int page[3];  // a tree of 128 nodes reaches into three pages
-#pragma unroll
-  for (int k = 0; k < 3; ++k) page[k] = e0 + k < pg.table_ld ? row[e0 + k] : -1;
   auto head_of = [&](int s) -> long long {  // elements before the head's part of the page of slot s, or -1
-    const int k = (s >> 6) - e0, p = k == 0 ? page[0] : (k == 1 ? page[1] : page[2]);
+    const int p = __builtin_amdgcn_readlane(id, (s >> 6) - e0);
     return (unsigned)p < (unsigned)pg.n_pages ? (long long)(((layer0 + p) * n_kv + head) * (size_t)(GOOSE_PAGE * D)) : -1;
   };
-  for (int j0 = 1; j0 <= L; j0 += 8) {
-    uint4 kr[8];
-    u16 vr[8];
-    int prev = j0 > 1 ? path[j0 - 1] : 0, n = 0;
+  int prev = 0;
+  for (int j0 = 1; j0 <= L; j0 += MOVES) {
+    int n = 0, from[MOVES];  // moves of this round: up to the first entry that is not increasing, leaves the tree or has no page
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int j = j0 + u, s = j <= L ? path[j] : -1;
-      const bool on = n == u && j <= L && s > prev && s < q.B && head_of(P + s) >= 0 && head_of(P + j) >= 0;
-      if (on) {
-        const long long b = head_of(P + s);
-        if (c < D / 8) kr[u] = *reinterpret_cast<const uint4*>(kpool + b + page_k_chunk<D>((P + s) & 63, c));
-        vr[u] = vpool[b + page_v_elem<D>((P + s) & 63, c)];
+    for (int u = 0; u < MOVES; ++u) {
+      const int j = j0 + u, s = j <= L ? at(j) : -1;
+      from[u] = s;
+      if (n == u && s > prev && s < q.B && head_of(P + s) >= 0 && head_of(P + j) >= 0) {
         prev = s;
         n = u + 1;
       }
     }
+    uint4 kr[MOVES];
+    u16 vr[MOVES];
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
+    for (int u = 0; u < MOVES; ++u)
+      if (u < n) {
+        const int s = P + from[u];
+        const long long b = head_of(s);
+        if (c < D / 8) kr[u] = *reinterpret_cast<const uint4*>(kpool + b + page_k_chunk<D>(s & 63, c));
+        vr[u] = vpool[b + page_v_elem<D>(s & 63, c)];
+      }
+#pragma unroll
+    for (int u = 0; u < MOVES; ++u)
       if (u < n) {
         const int d = P + j0 + u;
         const long long b = head_of(d);
         if (c < D / 8) *reinterpret_cast<uint4*>(kpool + b + page_k_chunk<D>(d & 63, c)) = kr[u];
         vpool[b + page_v_elem<D>(d & 63, c)] = vr[u];
       }
-    if (n < 8) break;  // the end, or a malformed path
+    if (n < MOVES) break;  // the end, or a malformed path
   }
 }
 

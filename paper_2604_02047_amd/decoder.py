@@ -9,6 +9,8 @@ the walks' results and the table rows the harvest touched.
 GooseDecoder decodes one request; BatchedGooseDecoder decodes several with one pass over the
 weights per cycle (the batch sweep of App. D), each request with its own KV cache, successor
 tables and adaptive state, and drops a request from the batch as soon as it has its tokens.
+PagedGooseDecoder does the same on one paged cache: what the prompts have in common is prefilled, stored and, in the
+attention, read once for all requests.
 """
 import numpy as np
 import torch
@@ -100,7 +102,8 @@ def _require_room(P, n, cap):
 def _require_clean(flags):
     """The device-side checks of the cycle just run (bad parent array, cache length out of range)."""
     if flags:
-        raise gb.GooseError(gb.GOOSE_ERR_CAPACITY if flags & gb.GOOSE_FLAG_CAPACITY else gb.GOOSE_ERR_NOT_TOPOLOGICAL,
+        full = flags & (gb.GOOSE_FLAG_CAPACITY | gb.GOOSE_FLAG_PAGES)
+        raise gb.GooseError(gb.GOOSE_ERR_CAPACITY if full else gb.GOOSE_ERR_NOT_TOPOLOGICAL,
                             f"the verification kernels flagged the cycle (goose_device_flags = {flags})")
 
 
@@ -164,10 +167,12 @@ class BatchedGooseDecoder:
         assert n_requests * ((max(B, 1 + max_spine) + 31) // 32 * 32) <= gm.ctx.max_rows
         self.gm = gm
         self.o = _Options(gm, B, K, rho, D, min_score, bypass_len, lens, max_spine, alpha)
-        self.reqs = [_Request(gm, K, torch.zeros_like(gm.kcache), torch.zeros_like(gm.vcache))
-                     for _ in range(n_requests)]
+        self.reqs = [self._make_request(gm, K) for _ in range(n_requests)]
         self.argmax_all = torch.zeros(gm.ctx.max_rows, dtype=torch.int32, device=gm.device)
         self.passes = 0
+
+    def _make_request(self, gm, K):
+        return _Request(gm, K, torch.zeros_like(gm.kcache), torch.zeros_like(gm.vcache))
 
     def cycle(self, active):
         """One batched cycle over the requests `active` (indices); returns {index: emitted tokens}."""
@@ -202,4 +207,109 @@ class BatchedGooseDecoder:
             for i, emitted in self.cycle(active).items():
                 outs[i] += emitted
             active = [i for i in active if len(outs[i]) < n_new]
+        return outs
+
+
+class PagedGooseDecoder(BatchedGooseDecoder):
+    """Several requests over one paged cache (goose_verify_step_paged).  Sequence 0 holds the tokens that all prompts begin with; every
+    request's sequence is forked off it, so that the whole pages among them are shared, and gets its own pages from there on.
+    `gm` as for BatchedGooseDecoder; its own contiguous caches are not used.  n_pages: pages of the pool; max_slots: cache slots of a request."""
+
+    def __init__(self, gm: GooseModel, n_requests, n_pages, max_slots, **options):
+        super().__init__(gm, n_requests, **options)
+        self.cache = gm.paged_cache(n_pages, n_requests + 1, max_slots)
+        self.max_slots, self.shared_pages = self.cache.table.shape[1] * gb.GOOSE_PAGE, 0
+        self.mask = torch.zeros(256, dtype=torch.int64, device=gm.device)
+
+    def _make_request(self, gm, K):
+        return _Request(gm, K, kcache=False, vcache=False)  # (no caches of its own)
+
+    def _feed(self, seq, done, tokens, q):
+        """Feeds tokens into a sequence with `done` slots as chain trees (every row kept) and harvests them into q's tables; returns the
+        prediction behind the last one."""
+        gm, c, o = self.gm, self.gm.ctx, 0
+        while o < len(tokens):
+            n = min(gm.max_B, len(tokens) - o)
+            _require_room(done, n, self.max_slots)
+            t, p, _ = gm.stage_tree(tokens[o:o + n], np.arange(-1, n - 1), None)
+            mask = self.mask[:n * ((n + 63) // 64)]
+            accept = torch.full((1,), n - 1, dtype=torch.int32, device=gm.device)
+            path = torch.arange(n, dtype=torch.int32, device=gm.device)
+            req = gb.PagedRequests([{"seq": seq, "B": n, "P_max": done, "mask": mask, "pos": gm.pos, "path": path, "accept_len": accept}])
+            c.goose_pages_reserve(self.cache, [seq], [n])
+            c.goose_build_mask(p, n, done, mask, gm.depth, gm.pos)
+            c.goose_embed(gm.embed, t, n, gm.x)
+            for l in range(gm.desc.n_layers):
+                c.goose_verify_layer_paged(gm.packed_layer(l), self.cache, l, gm.x, req, 0)
+            logits = torch.empty((n, gm.desc.vocab), dtype=torch.float32, device=gm.device)
+            c.goose_lm_head_argmax(gm.packed_head, gm.x, n, gm.argmax, logits, None)
+            c.goose_harvest_topk(logits, gm.desc.vocab, t, n, q.K, q.d_ids, q.d_scores)
+            c.goose_pages_commit(self.cache, req)
+            o, done = o + n, done + n
+        _require_clean(c.goose_device_flags())
+        return int(gm.argmax[n - 1].item())
+
+    def prefill(self, prompts):
+        """The common beginning once, then every prompt's rest; returns the first generated token of each."""
+        prompts = [[int(t) for t in p] for p in prompts]
+        assert len(prompts) == len(self.reqs) and all(prompts)
+        common, most = 0, min(len(p) for p in prompts) - 1   # (every request feeds one token at least: its logits are needed)
+        while common < most and len({p[common] for p in prompts}) == 1:
+            common += 1
+        c, first = self.gm.ctx, self.reqs[0]
+        c.goose_pages_clear(self.cache)
+        for q in self.reqs:                                  # a new round: nothing is left of the tables of the last one
+            q.d_ids.fill_(-1)
+            q.d_scores.zero_()
+            q.h_ids.fill(-1)
+            q.h_scores.fill(0)
+            q.p_hat, q.trace = 0.3, []
+        if common:
+            self._feed(0, 0, prompts[0][:common], first)
+            c.goose_pages_fork(self.cache, 0, list(range(1, len(prompts) + 1)))
+        self.shared_pages = common // gb.GOOSE_PAGE
+        for q in self.reqs[1:]:
+            q.d_ids.copy_(first.d_ids)
+            q.d_scores.copy_(first.d_scores)
+        out = []
+        for r, (q, p) in enumerate(zip(self.reqs, prompts)):
+            q.anchor = self._feed(r + 1, common, p[common:], q)
+            q.P, q.seq = len(p), p + [q.anchor]
+            q.mirror_rows(p)
+            out.append(q.anchor)
+        return out
+
+    def cycle(self, active):
+        """One cycle over the requests `active` (indices); returns {index: emitted tokens}."""
+        gm = self.gm
+        plans, table = [], []
+        for i in active:
+            q = self.reqs[i]
+            tokens, parent, is_spine, mode = q.plan(self.o)
+            _require_room(q.P, len(tokens), self.max_slots)
+            t, p, s = gm.stage_tree(tokens, parent, is_spine)
+            plans.append((tokens, is_spine, mode))
+            table.append({"seq": i + 1, "B": len(tokens), "P_max": q.P, "tokens": t, "parent": p, "is_spine": s,
+                          "accept_len": q.accept_len, "path": q.path, "bonus": q.bonus, "succ_ids": q.d_ids, "succ_scores": q.d_scores})
+        gm.ctx.goose_verify_step_paged(gm.model_ptrs(), self.cache, table, self.shared_pages, self.argmax_all)
+        _require_clean(gm.ctx.goose_device_flags())   # (synchronises the stream)
+        self.passes += 1
+        out = {}
+        for i, (tokens, is_spine, mode) in zip(active, plans):
+            q = self.reqs[i]
+            L = int(q.accept_len.item())
+            out[i] = q.absorb(self.o, tokens, is_spine, mode, L, q.path[:L + 1].cpu().numpy(), int(q.bonus.item()), q.P + L + 1)
+        return out
+
+    def generate(self, prompts, n_new):
+        """As BatchedGooseDecoder.generate; a request that has its tokens gives its pages back."""
+        outs = [[t] for t in self.prefill(prompts)]
+        active = list(range(len(prompts)))
+        while active:
+            for i, emitted in self.cycle(active).items():
+                outs[i] += emitted
+            done = [i for i in active if len(outs[i]) >= n_new]
+            if done:
+                self.gm.ctx.goose_pages_free(self.cache, [i + 1 for i in done])
+            active = [i for i in active if i not in done]
         return outs

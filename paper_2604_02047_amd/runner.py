@@ -8,7 +8,7 @@ import numpy as np
 import torch
 
 from . import layout
-from .binding import GooseContext, ModelDesc
+from .binding import GOOSE_PAGE, GooseContext, ModelDesc, PagedCache
 
 
 def _torch_dtype(name):
@@ -94,6 +94,17 @@ class GooseModel:
     def set_P(self, P: int):
         self.P = int(P)
         self.d_P.fill_(self.P)
+
+    def paged_cache(self, n_pages: int, n_seqs: int, max_slots: int):
+        """An empty paged cache of this model: n_pages pages of 64 slots for all layers, tables for n_seqs sequences of up to max_slots."""
+        d = self.desc
+        pool = (d.n_layers, n_pages, d.kv_heads, GOOSE_PAGE * d.head_dim)
+        i32 = dict(dtype=torch.int32, device=self.device)
+        cache = PagedCache(torch.zeros(pool, dtype=self.dt, device=self.device), torch.zeros(pool, dtype=self.dt, device=self.device),
+                           torch.empty((n_seqs, (max_slots + GOOSE_PAGE - 1) // GOOSE_PAGE), **i32), torch.empty(n_seqs, **i32),
+                           torch.empty(n_pages, **i32))
+        self.ctx.goose_pages_clear(cache)
+        return cache
 
     def model_ptrs(self):
         return {"embed": self.embed, "packed_layers": self.packed_layers, "packed_head": self.packed_head,

@@ -1,0 +1,240 @@
+"""Whole passes on a paged cache: the layer and the step beside their contiguous forms, graphs, and decoding loops that share a prompt."""
+import numpy as np
+import pytest
+import torch
+
+import goose_inputs as gi
+from paged_ref import PAGE, unpack_pages
+from util import gpu_model, torch_model
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _page_rows(cache, table_row, n, d):
+    """Logical K and V rows [layer][head][n][d] of a sequence."""
+    k, v = unpack_pages(cache.kpool, cache.vpool, d)
+    pages = torch.as_tensor(table_row[:(n + PAGE - 1) // PAGE].astype(np.int64), device=cache.kpool.device)
+    out = []
+    for x in (k, v):
+        x = x[:, pages].transpose(1, 2)
+        out.append(x.reshape(x.shape[0], x.shape[1], -1, d)[:, :, :n])
+    return out
+
+
+def _fill(gm, cache, Ps, common, seed):
+    """Random rows for prefixes with `common` equal slots: contiguous caches per request, and the same in pages (sequence r + 1 of a fork)."""
+    from paper_2604_02047_amd import layout
+    d, L, H = gm.desc.head_dim, gm.desc.n_layers, gm.desc.kv_heads
+    g = torch.Generator().manual_seed(seed)
+    base = [torch.randn((L, H, common, d), generator=g).to(gm.dt) for _ in range(2)]
+    rows = [[torch.cat((b, torch.randn((L, H, p - common, d), generator=g).to(gm.dt)), 2).to(DEV) for b in base] for p in Ps]
+    caches = []
+    for k, v in rows:
+        kc, vc = torch.zeros_like(gm.kcache), torch.zeros_like(gm.vcache)
+        s = torch.arange(k.shape[2], device=DEV)
+        kc[:, :, layout.k_offsets(s, d)] = k
+        vc[:, :, layout.v_offsets(s, d)] = v
+        caches.append((kc, vc))
+    c = gm.ctx
+    one = lambda seq, n: {"seq": seq, "B": n, "path": torch.arange(n, dtype=torch.int32, device=DEV),  # noqa: E731
+                          "accept_len": torch.tensor([n - 1], dtype=torch.int32, device=DEV)}
+
+    def grow(seq, n):
+        while n > 0:
+            step = min(n, gm.max_B)
+            c.goose_pages_reserve(cache, [seq], [step])
+            c.goose_pages_commit(cache, [one(seq, step)])
+            n -= step
+
+    if common:
+        grow(0, common)
+        c.goose_pages_fork(cache, 0, list(range(1, len(Ps) + 1)))
+    for r, p in enumerate(Ps):
+        grow(r + 1, p - common)
+    table = cache.table.cpu().numpy()
+    for r, (k, v) in enumerate(rows):
+        for i in range((Ps[r] + PAGE - 1) // PAGE):
+            n = min(PAGE, Ps[r] - i * PAGE)
+            s = torch.arange(n, device=DEV)
+            cache.kpool[:, table[r + 1, i]][:, :, layout.k_offsets(s, d)] = k[:, :, i * PAGE:i * PAGE + n]
+            cache.vpool[:, table[r + 1, i]][:, :, layout.v_offsets(s, d)] = v[:, :, i * PAGE:i * PAGE + n]
+    assert c.goose_device_flags() == 0
+    return caches
+
+
+def _requests(gm, n, B, seed):
+    rng = np.random.default_rng(seed)
+    out = []
+    for r in range(n):
+        parent = np.array([-1] + [int(rng.integers(0, i)) for i in range(1, B[r])], np.int32)
+        tokens = rng.integers(0, gm.desc.vocab, B[r])
+        t, p, s = gm.stage_tree(tokens, parent, np.ones(B[r], np.uint8))
+        i32 = dict(dtype=torch.int32, device=DEV)
+        out.append({"tokens": t, "parent": p, "is_spine": s, "B": B[r], "accept_len": torch.zeros(1, **i32), "path": torch.zeros(128, **i32),
+                    "bonus": torch.zeros(1, **i32), "next_root": torch.zeros(1, **i32)})
+    return out
+
+
+@pytest.mark.parametrize("name,act_mode", [("small_bf16", 0), ("tiny_gqa_bf16", 0), ("small_gqa_qknorm_bf16", 1), ("small_gqa_qknorm_f16", 0)])
+def test_a_step_on_pages_beside_the_batched_step(name, act_mode):
+    import dataclasses
+
+    import paper_2604_02047_amd as goose
+    from paper_2604_02047_amd.runner import GooseModel
+    shape = gi.SHAPES[name]
+    tm = torch_model(shape, seed=3, gain_jitter=0.1)
+    desc = dataclasses.replace(goose.ModelDesc.from_shape(shape), act_mode=act_mode)
+    gm = GooseModel(desc, 64, 512, lambda l: tm["layers"][l], tm["embed"], tm["lm_head"], tm["final_norm"], max_rows=256)
+    Ps, B, common = [150, 201, 129], [33, 7, 64], 129
+    cache = gm.paged_cache(24, 5, 400)
+    caches = _fill(gm, cache, Ps, common, 1)
+    rq = _requests(gm, 3, B, 2)
+    d_P = [torch.tensor([p], dtype=torch.int32, device=DEV) for p in Ps]
+    am0, am1 = torch.zeros(256, dtype=torch.int32, device=DEV), torch.zeros(256, dtype=torch.int32, device=DEV)
+    K = 8
+    tables = [[(torch.full((shape.vocab, K), -1, dtype=torch.int32, device=DEV), torch.zeros((shape.vocab, K), device=DEV))
+               for _ in range(3)] for _ in range(2)]
+    batch = [dict(q, P_max=p, P=dp, kcache=kc, vcache=vc, succ_ids=t[0], succ_scores=t[1])
+             for q, p, dp, (kc, vc), t in zip(rq, Ps, d_P, caches, tables[0])]
+    gm.ctx.goose_verify_step_batched(gm.model_ptrs(), batch, am0)
+    want = [(int(q["accept_len"]), q["path"].clone(), int(q["bonus"])) for q in rq]
+    paged = [dict(q, seq=r + 1, P_max=p, succ_ids=t[0], succ_scores=t[1]) for r, (q, p, t) in enumerate(zip(rq, Ps, tables[1]))]
+    gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, paged, common // PAGE, am1)
+    assert gm.ctx.goose_device_flags() == 0
+    # the softmax weights of the successor tables are logits of the two passes side by side: equal to what 16-bit operands leave open
+    for (i0, s0), (i1, s1) in zip(*tables):
+        assert (i0 == i1).float().mean() > 0.98
+        assert (s0 - s1).abs().max() < 2e-2
+    row0, agree, total = 0, 0, 0
+    for b in B:
+        agree += int((am0[row0:row0 + b] == am1[row0:row0 + b]).sum())
+        total += b
+        row0 += (b + 31) // 32 * 32
+    assert agree >= total - 2
+    table, lens, refs = cache.table.cpu().numpy(), cache.len.cpu().numpy(), cache.refs.cpu().numpy()
+    for r, (q, p) in enumerate(zip(rq, Ps)):
+        L = int(q["accept_len"])
+        assert lens[r + 1] == p + L + 1
+        if want[r][0] != L or not torch.equal(want[r][1], q["path"]):
+            continue  # (a near tie decided otherwise)
+        assert want[r][2] == int(q["bonus"]) == int(q["next_root"])
+        n = p + L + 1
+        k, v = _page_rows(cache, table[r + 1], n, desc.head_dim)
+        from paper_2604_02047_amd import layout
+        s = torch.arange(n, device=DEV)
+        for got, ref in ((k, caches[r][0][:, :, layout.k_offsets(s, desc.head_dim)]), (v, caches[r][1][:, :, layout.v_offsets(s, desc.head_dim)])):
+            assert torch.equal(got[:, :, :p], ref[:, :, :p])                          # the prefix, bit for bit
+            assert (got - ref).abs().max() <= 2e-2 * ref.abs().max()                  # the committed rows
+            assert (got[0] - ref[0]).abs().max() <= torch.finfo(gm.dt).eps * ref[0].abs().max()   # layer 0: the same projection, one rounding
+    # shared pages are held by the prompt and all three; nothing beyond the lengths is held
+    assert list(refs[table[0, :2]]) == [4, 4] and refs.sum() == sum((int(x) + 63) // 64 for x in lens)
+    gm.ctx.close()
+
+
+def test_a_layer_does_not_depend_on_the_sharing():
+    shape = gi.SHAPES["small_bf16"]
+    tm = torch_model(shape, seed=5)
+    gm = gpu_model(shape, tm, max_B=64, cap=512, max_rows=128)
+    cache = gm.paged_cache(20, 3, 320)
+    _fill(gm, cache, [130, 180], 128, 4)
+    B = [20, 40]
+    from paged_ref import mask_words
+    rng = np.random.default_rng(0)
+    masks = [mask_words([-1] + [int(rng.integers(0, i)) for i in range(1, b)]) for b in B]
+    gm.ctx.goose_pages_reserve(cache, [1, 2], B)
+    reqs = []
+    for r, (b, p) in enumerate(zip(B, [130, 180])):
+        depth = masks[r][1].sum(1) - 1
+        reqs.append({"seq": r + 1, "B": b, "P_max": p, "mask": masks[r][0].to(DEV), "pos": torch.tensor(p + depth, dtype=torch.int32, device=DEV)})
+    x0 = torch.randn((96, shape.hidden), generator=torch.Generator().manual_seed(1)).to(DEV)
+    out = []
+    for shared in (0, 1, 2):
+        x = x0.clone()
+        gm.ctx.goose_verify_layer_paged(gm.packed_layer(1), cache, 1, x, reqs, shared)
+        out.append(x)
+    assert gm.ctx.goose_device_flags() == 0
+    scale = (out[0] - x0).abs().max()
+    for x in out[1:]:
+        assert (x - out[0]).abs().max() <= 5e-3 * scale
+        assert torch.equal(x[20:32], out[0][20:32]) or (x[20:32] - out[0][20:32]).abs().max() <= 1e-2 * scale  # rows between requests: finite
+    gm.ctx.close()
+
+
+def test_a_captured_step_follows_pages_and_lengths():
+    """One graph of a whole step; replays advance the sequences, take and give back pages, and equal the eager steps of a second cache."""
+    shape = gi.SHAPES["tiny_gqa_bf16"]
+    tm = torch_model(shape, seed=7, gain_jitter=0.1)
+    gm = gpu_model(shape, tm, max_B=32, cap=512, max_rows=64)
+    c0, c1 = gm.paged_cache(16, 3, 256), gm.paged_cache(16, 3, 256)
+    for c in (c0, c1):
+        _fill(gm, c, [70, 90], 64, 9)
+    rq = _requests(gm, 2, [12, 20], 11)
+    am = [torch.zeros(64, dtype=torch.int32, device=DEV) for _ in range(2)]
+    table = [dict(q, seq=r + 1, P_max=230) for r, q in enumerate(rq)]
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        gm.ctx.goose_verify_step_paged(gm.model_ptrs(), c0, table, 1, am[0])
+    for i in range(8):
+        with torch.cuda.stream(st):
+            graph.replay()
+        st.synchronize()
+        got = [(int(q["accept_len"]), int(q["bonus"])) for q in rq]
+        torch.zeros(1000, device=DEV).sum().item()
+        gm.ctx.goose_verify_step_paged(gm.model_ptrs(), c1, table, 1, am[1])
+        torch.cuda.synchronize()
+        assert got == [(int(q["accept_len"]), int(q["bonus"])) for q in rq], i
+        assert torch.equal(am[0][:12], am[1][:12]) and torch.equal(am[0][32:52], am[1][32:52])
+        for a, b in ((c0.table, c1.table), (c0.len, c1.len), (c0.refs, c1.refs)):
+            assert torch.equal(a, b), i
+    assert torch.equal(c0.kpool, c1.kpool) and torch.equal(c0.vpool, c1.vpool)
+    assert gm.ctx.goose_device_flags() == 0
+    gm.ctx.close()
+
+
+def _prompts(vocab, n, common):
+    pat = gi.prefix_tokens(31, 12, vocab).tolist()
+    head = (pat * (common // 12 + 1))[:common]
+    return [head + gi.prefix_tokens(40 + r, 10 + 7 * r, vocab).tolist() + pat[:6] for r in range(n)]
+
+
+@pytest.mark.parametrize("common", [0, 40, 150])
+def test_paged_decoding_gives_each_request_its_own_tokens(common):
+    """Requests that share a prompt, decoded over one paged cache, against each decoded alone over a contiguous one.  16-bit near-ties may be
+    decided differently where launches differ in shape: long agreement is the check, as for the batched decoder."""
+    from paper_2604_02047_amd.decoder import GooseDecoder, PagedGooseDecoder
+    shape = gi.SHAPES["small_bf16"]
+    tm = torch_model(shape, seed=6, gain_jitter=0.1)
+    prompts = _prompts(shape.vocab, 3, common)
+    gm = gpu_model(shape, tm, max_B=64, cap=512, max_rows=192)
+    pd = PagedGooseDecoder(gm, 3, n_pages=24, max_slots=448, B=40, min_score=0.0)
+    outs = pd.generate(prompts, 60)
+    assert pd.shared_pages == common // 64 and pd.passes < sum(len(o) for o in outs) / 3
+    refs = pd.cache.refs.cpu()
+    assert int(refs.sum()) == (common + 63) // 64      # all requests have given their pages back, the prompt's are held
+    again = pd.generate(prompts, 60)                   # and the pool serves a second round
+    assert again == outs
+    gm.ctx.close()
+    for r, prompt in enumerate(prompts):
+        gm = gpu_model(shape, tm, max_B=64, cap=512)
+        y = GooseDecoder(gm, B=40, min_score=0.0).generate(prompt, 60)
+        gm.ctx.close()
+        n = min(len(y), len(outs[r]))
+        same = next((i for i in range(n) if y[i] != outs[r][i]), n)
+        assert same >= 40, (r, same, y[:same + 2], outs[r][:same + 2])
+
+
+def test_a_full_pool_stops_decoding_with_an_error():
+    from paper_2604_02047_amd.binding import GOOSE_ERR_CAPACITY, GooseError
+    from paper_2604_02047_amd.decoder import PagedGooseDecoder
+    shape = gi.SHAPES["tiny_bf16"]
+    tm = torch_model(shape, seed=4, gain_jitter=0.1)
+    gm = gpu_model(shape, tm, max_B=64, cap=512, max_rows=128)
+    for pages, slots in ((5, 512), (40, 128)):      # the pool, and a sequence's table
+        pd = PagedGooseDecoder(gm, 2, n_pages=pages, max_slots=slots, B=24, min_score=0.0)
+        with pytest.raises(GooseError) as e:
+            pd.generate(_prompts(shape.vocab, 2, 70), 400)
+        assert e.value.status == GOOSE_ERR_CAPACITY
+    gm.ctx.close()
