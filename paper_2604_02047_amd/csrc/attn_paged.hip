@@ -193,7 +193,7 @@ struct RowTile {
   typedef typename Mma16<F16>::v8 op8;
   op8 q[NS], ql[QT == 2 ? NS : 1];
   f32x16 o[NDT];
-  float s[16];  // scores of the block at hand
+  f32x16 s;  // scores of the block at hand
   op8 p[2], pl[PT];
   float m, l, top;   // largest score so far, sum of weights, this block's largest score of this lane
   float lim, ref, mul;  // see rescale()
@@ -212,6 +212,9 @@ struct RowTile {
     m = lim = -INFINITY;
     l = ref = 0.f;
     mul = 1.f;
+    load_q(a, w, hh);
+  }
+  __device__ __forceinline__ void load_q(const PagedAttnArgs& a, const Row& w, int hh) {
     const T* at = static_cast<const T*>(a.q) + (size_t)w.row * a.ldq + ((size_t)w.h * D + hh * 8) * QT;
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
@@ -229,26 +232,31 @@ struct RowTile {
 #pragma unroll
       for (int i = 0; i < NS; ++i) sum = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[i]), ql[i], sum);
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = sum[r];
+    s = sum;
   }
   __device__ __forceinline__ void mask(unsigned vis) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = ((vis >> r) & 1u) ? s[r] : -INFINITY;
   }
-  // This lane's largest score (unscaled, as m is: the scale is positive).
+  // This lane's largest score (unscaled, as m is: the scale is positive), from partial ones: a NaN stays one, and compares as no larger.
+  static __device__ __forceinline__ float partial_max(const f32x16& x, int r) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x[r], x[r + 4]), __builtin_elementwise_maximum(x[r + 8], x[r + 12]));
+  }
+  static __device__ __forceinline__ float join_max(const float (&t)[4]) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(t[0], t[1]), __builtin_elementwise_maximum(t[2], t[3]));
+  }
   __device__ __forceinline__ void maximum() {
-    float t[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) t[r] = fmaxf(fmaxf(s[r], s[r + 4]), fmaxf(s[r + 8], s[r + 12]));
-    top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+    const float t[4] = {partial_max(s, 0), partial_max(s, 1), partial_max(s, 2), partial_max(s, 3)};
+    top = join_max(t);
   }
   // m, O and l follow it only where some lane's has grown so far that weights would pass 2^SLACK: weights up to there are as good as
   // those up to one in floating point (16 bits hold them with room to spare), and with 32 rows in a tile some row's maximum grows by a
   // little in most blocks (512 rows over 16384 slots: in 3 of 4).
   // A weight is 2^(s c - ref) in one fused multiply-add, ref = m c rounded; its rounding is the same factor in O and l.  Where products
   // leave no room for it (2^24 and beyond, infinities), the block's scores become differences to m first.
-  __device__ __forceinline__ void rescale(float c) {
+  // x: the scores; PENDING: weights of an earlier block, in w and wl, are not in O yet and follow too.
+  template <bool PENDING>
+  __device__ __forceinline__ void rescale(float c, f32x16& x, op8 (&w)[2], op8 (&wl)[PT]) {
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > lim) != 0, 0)) {
       const float m_new = fmaxf(m, fmaxf(top, __shfl_xor(top, 32, 64)));
       const float old = finite_ref(m), now = finite_ref(m_new);
@@ -259,7 +267,7 @@ struct RowTile {
       mul = c;
       if (__builtin_amdgcn_ballot_w64(!(fabsf(ref) < 16777216.f)) != 0) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = (s[r] - now) * c;
+        for (int r = 0; r < 16; ++r) x[r] = (x[r] - now) * c;
         mul = 1.f;
         ref = 0.f;
         lim = -INFINITY;  // (and so will the next block's)
@@ -269,30 +277,42 @@ struct RowTile {
       for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+      if (PENDING) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int j = i >> 2, e = 2 * i & 7;
+          if (PT == 2) pair_to(i, ((float)w[j][e] + (float)wl[j % PT][e]) * alpha, ((float)w[j][e + 1] + (float)wl[j % PT][e + 1]) * alpha, w, wl);
+          else pair_to(i, (float)w[j][e] * alpha, (float)w[j][e + 1] * alpha, w, wl);
+        }
+      }
     }
   }
-  // probabilities of keys 2 i, 2 i + 1 (a masked score is -infinity: zero)
-  __device__ __forceinline__ void weights_of(int i) {
+  __device__ __forceinline__ void rescale(float c) { rescale<false>(c, s, p, pl); }
+  // x, y in 16 bits, as weights of keys 2 i, 2 i + 1
+  static __device__ __forceinline__ void pair_to(int i, float x, float y, op8 (&w)[2], op8 (&wl)[PT]) {
     typedef T T2 __attribute__((ext_vector_type(2)));
     typedef float F2 __attribute__((ext_vector_type(2)));
-    const float x = __builtin_amdgcn_exp2f(fmaf(s[2 * i], mul, -ref)), y = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], mul, -ref));
-    l += x;
-    l += y;
-    unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector((F2{x, y}), T2));
-    u32x4 w = __builtin_bit_cast(u32x4, p[i >> 2]);
-    w[i & 3] = h;
-    p[i >> 2] = __builtin_bit_cast(op8, w);
+    const unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector((F2{x, y}), T2));
+    u32x4 v = __builtin_bit_cast(u32x4, w[i >> 2]);
+    v[i & 3] = h;
+    w[i >> 2] = __builtin_bit_cast(op8, v);
     if (PT == 2) {
       const F2 rest = {x - __builtin_bit_cast(float, h << 16), y - __builtin_bit_cast(float, h & 0xFFFF0000u)};
-      unsigned r = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, T2));
-      w = __builtin_bit_cast(u32x4, pl[(i >> 2) % PT]);
-      w[i & 3] = r;
-      pl[(i >> 2) % PT] = __builtin_bit_cast(op8, w);
+      v = __builtin_bit_cast(u32x4, wl[(i >> 2) % PT]);
+      v[i & 3] = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, T2));
+      wl[(i >> 2) % PT] = __builtin_bit_cast(op8, v);
     }
+  }
+  // weights of keys 2 i, 2 i + 1 of the scores in z (a masked score is -infinity: zero)
+  __device__ __forceinline__ void weights_of(int i, const f32x16& z, op8 (&w)[2], op8 (&wl)[PT]) {
+    const float x = __builtin_amdgcn_exp2f(fmaf(z[2 * i], mul, -ref)), y = __builtin_amdgcn_exp2f(fmaf(z[2 * i + 1], mul, -ref));
+    l += x;
+    l += y;
+    pair_to(i, x, y, w, wl);
   }
   __device__ __forceinline__ void weights() {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) weights_of(i);
+    for (int i = 0; i < 8; ++i) weights_of(i, s, p, pl);
   }
   __device__ __forceinline__ void values(const u32x4 (&v)[NS]) {
 #pragma unroll
@@ -509,43 +529,49 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
 // One workgroup = eight wavefronts, two on a SIMD, one tile of 32 rows each: 256 rows (items of up to 128 rows: 128, and two key groups) x a
 // range of blocks.  Every block comes into LDS once, global -> LDS without registers, into a ring that runs several blocks ahead.
 // A wavefront alone issues an instruction every five cycles, whatever it is, so the matrix pipe (32 cycles an instruction)
-// and the vector pipe both stay idle in turn; two wavefronts fill each other's gaps.  Within one, the scores of the next block and the
-// outputs of this one are under way while this block's scores become weights and the next block's maximum is taken:
-//     matrix pipe   S = K Q (j+1)         |  O += V P (j)
-//     vector pipe   weights P of block j  |  maximum of S
+// and the vector pipe both stay idle in turn; two wavefronts fill each other's gaps.  Within one, three blocks are under way at once:
+//     matrix pipe   S = K Q of block j + 1, then O += V P of block j - 1
+//     vector pipe   weights P of block j, then the maximum of S
+// so that no step waits for another one's result, and a weight has two matrix instructions to hide behind (all of them beside S: half as many).
+// What bounds it is power: fp16, 2048 rows a KV head over 16384 slots, a step takes 1680 cycles (1024 of them the matrix pipe's; 1490 without the
+// copies and the raised maxima) at a clock that falls to 1.45 GHz, where the same products on constants run at 1.95.  770 TFLOP/s; with S and
+// P V of neighbouring blocks in one step, weights beside S alone and copies that made each LDS read wait for all: 690.
 // Blocks that need a mask (the tree's, and what is left over) follow without the ring, as in k_paged_stream.
+#define GOOSE_BUFFER_WORD3 0x00020000  // (buffer descriptor: raw 32-bit data)
 #define GOOSE_LDS_PTR(p) ((__attribute__((address_space(3))) void*)(p))
 constexpr int vmcnt_imm(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }  // s_waitcnt vmcnt(n) only
 
+// CP pieces of 1 KiB from src (uniform) to LDS.  Through a buffer descriptor: LDS reads behind a global_load to LDS wait for all reads
+// in flight instead of the ones that they need.
 template <int CP>
-__device__ __forceinline__ void copy_pieces(const char* src, unsigned char* cp) {
+__device__ __forceinline__ void copy_pieces(const char* src, int lane, unsigned char* cp) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host pass knows no such builtin and would silently drop the kernel's stub)
-  __builtin_amdgcn_global_load_lds(reinterpret_cast<const u32x4*>(src), GOOSE_LDS_PTR(cp), 16, 0, 0);
-  if (CP == 2) __builtin_amdgcn_global_load_lds(reinterpret_cast<const u32x4*>(src), GOOSE_LDS_PTR(cp), 16, 1024, 0);  // (the offset counts on both sides)
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, CP * 1024, GOOSE_BUFFER_WORD3);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(cp), 16, lane * 16, 0, 0, 0);
+  if (CP == 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(cp), 16, lane * 16, 0, 1024, 0);  // (the offset counts on both sides)
 #endif
 }
-// Step j of a wavefront: scores of block j + 1, outputs of block j.  The operand pieces come from the ring `AHEAD` uses before they are needed; with
-// one key group pc holds the first ones and is left with those of the next step (two units of the ring are then no longer in flight; with two
-// groups that would be all but one).  k1, k2: keys of blocks j + 1 and j + 2, v0: values of block j.  (Pointers that the
-// compiler may take to be distinct memory from cp, where src goes: its reads do not wait for the copies in flight.  What they do wait for is
-// the caller's explicit count and barrier.)  The order is written down: the compiler's own collects the vector work where it waits for the scores.
-template <int D, int QT, bool F16, int CP, int G, int AHEAD>
+// Step j of a wavefront: scores of block j + 1 (to z1), weights of block j (from z0 to w0), outputs of block j - 1 (its weights in w).  None of the three
+// needs another, so the vector work is dealt out evenly beside the matrix instructions, and the last quarter of them hides the maximum of z1.
+// The operand pieces come from the ring AHEAD uses before they are needed; with
+// one key group pc holds the first ones and is left with those of the next step.  k1, k2: keys of blocks j + 1 and j + 2, v0: values of block j - 1.
+// The order is written down: the compiler's own collects the vector work where it waits for the scores.
+template <int D, int QT, bool F16, int G, int AHEAD>
 __device__ __forceinline__ void ring_step(RowTile<D, QT, F16>& t, u32x4 (&pc)[AHEAD], const u32x4* __restrict__ k1, const u32x4* __restrict__ v0,
-                                          const u32x4* __restrict__ k2, unsigned char* __restrict__ cp, unsigned char* __restrict__ cp2,
-                                          const char* const (&src)[G], bool work, bool more, float scale) {
-#if defined(__HIP_DEVICE_COMPILE__)
+                                          const u32x4* __restrict__ k2, const f32x16& z0, f32x16& z1,
+                                          const typename RowTile<D, QT, F16>::op8 (&w)[2], const typename RowTile<D, QT, F16>::op8 (&wl)[RowTile<D, QT, F16>::PT],
+                                          typename RowTile<D, QT, F16>::op8 (&w0)[2], typename RowTile<D, QT, F16>::op8 (&wl0)[RowTile<D, QT, F16>::PT],
+                                          bool more, float scale) {
   typedef RowTile<D, QT, F16> Tile;
   typedef typename Tile::op8 op8;
-  constexpr int NS = Tile::NS, NDT = Tile::NDT, PT = Tile::PT;
-  copy_pieces<CP>(src[0], cp);
-  if (G == 2) copy_pieces<CP>(src[G - 1], cp2);
-  if (!work) return;
+  constexpr int NS = Tile::NS, NDT = Tile::NDT, PT = Tile::PT, ALL = NS * (QT + PT), SPREAD = ALL * 3 / 4;
   u32x4 piece[2 * NS + AHEAD];
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n) piece[n] = G == 1 ? pc[n] : k1[n * 64];
   f32x16 sum;
 #pragma unroll
   for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+  float part[4];
 #pragma unroll
   for (int n = 0; n < 2 * NS; ++n) {
     {
@@ -559,25 +585,31 @@ __device__ __forceinline__ void ring_step(RowTile<D, QT, F16>& t, u32x4 (&pc)[AH
       sum = Mma16<F16>::mfma(a, t.q[n], sum);
       if (QT == 2) sum = Mma16<F16>::mfma(a, t.ql[n % (QT == 2 ? NS : 1)], sum);
       GOOSE_HERE(sum);
-#pragma unroll
-      for (int w = 8 / NS * n; w < 8 / NS * (n + 1); ++w) t.weights_of(w);
-      GOOSE_HERE(t.l);
     } else {
       const int x = n - NS, j = x / NDT, dt = x % NDT;
-      t.o[dt] = Mma16<F16>::mfma(a, t.p[j], t.o[dt]);
-      if (PT == 2) t.o[dt] = Mma16<F16>::mfma(a, t.pl[j % PT], t.o[dt]);
+      t.o[dt] = Mma16<F16>::mfma(a, w[j], t.o[dt]);
+      if (PT == 2) t.o[dt] = Mma16<F16>::mfma(a, wl[j % PT], t.o[dt]);
       GOOSE_HERE(t.o[dt]);
     }
+    const int before = n < NS ? n * QT : NS * QT + (n - NS) * PT, behind = before + (n < NS ? QT : PT);  // matrix instructions so far
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= 8 * before / SPREAD && i < 8 * behind / SPREAD) t.weights_of(i, z0, w0, wl0);
+    GOOSE_HERE(t.l);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (2 * NS - NS / 2 + r * NS / 8 == n) {
+        part[r] = Tile::partial_max(sum, r);
+        GOOSE_HERE(part[r]);
+      }
     __builtin_amdgcn_sched_barrier(0);
   }
-#pragma unroll
-  for (int r = 0; r < 16; ++r) t.s[r] = sum[r];
-  t.maximum();
-  if (more) t.rescale(scale);  // (behind the last block the scores are of a block that is not this loop's)
+  z1 = sum;
+  t.top = Tile::join_max(part);
+  if (more) t.template rescale<true>(scale, z1, w0, wl0);  // (behind the last block the scores are of a block that is not this loop's)
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n)
     if (G == 1) pc[n] = piece[2 * NS + n];
-#endif
 }
 
 template <int D, int QT, bool F16>
@@ -613,14 +645,15 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
   auto block_at = [&](int b) -> size_t {  // bytes (pages times KV heads stays below 2^29: checked on the host)
     return (size_t)(unsigned)((pg.of(b, lane) * a.n_kv + kvh) * 2 + (b & 1)) * (32 * D * 2);
   };
-  const Row row = row_of(a, it, row_first + l31, kvh);
+  Row row = row_of(a, it, row_first + l31, kvh);
   Tile t;
   t.init(a, row, hh);
   const float scale = softmax_scale(D);
-  const int share = wave * CP * 1024;  // this wavefront's pieces of a block: the first four bring keys, the others values
-  const char* const pool = (wave < 4 ? kp : vp) + (wave & 3) * CP * 1024;
+  const bool keys = wave < 4;  // the first four wavefronts copy keys, the others values
+  const int share = wave * CP * 1024;  // this wavefront's pieces of a block
+  const char* const pool = (keys ? kp : vp) + (wave & 3) * CP * 1024;
   auto source = [&](int b) -> const char* {  // (behind the range: its last block again, never used)
-    return pool + block_at(min(b, it.b_hi - 1)) + lane * 16;
+    return pool + block_at(min(b, it.b_hi - 1));
   };
   auto barrier = [&]() {  // (raw: __syncthreads would also drain every copy in flight)
     asm volatile("" ::: "memory");
@@ -630,39 +663,73 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (all that was loaded so far: the counts below are those of the ring's copies)
   auto through_the_ring = [&](auto kg_c) {
     constexpr int G = decltype(kg_c)::value;  // key groups
-    constexpr int BU = BLOCK / 16, MASK = RING - 1;
-    for (int i = 0; i < RING - G; ++i) copy_pieces<CP>(source(it.b_lo + i), ring + i * BLOCK + share);  // every unit but the last of the ring
+    constexpr int BU = BLOCK / 16, RU = RING / G;
+    auto slot = [](int u) { return (u & (RU - 1)) * G; };
+    int next = 0;  // the unit copied next
+    auto copy = [&]() {
+#pragma unroll
+      for (int g = 0; g < G; ++g) copy_pieces<CP>(source(it.b_lo + next * G + g), lane, ring + (slot(next) + g) * BLOCK + share);
+      ++next;
+    };
+    const int first = keys ? RU : RU - 1;
+    while (next < first) copy();
     __builtin_amdgcn_sched_barrier(0);
     const u32x4* const base = reinterpret_cast<const u32x4*>(ring) + lane;
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3 * G) * CP));  // units 0 and 1
+    auto keys_of = [&](int u) { return base + (slot(u) + kg) * BU; };
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((RU - 3) * G * CP));  // units 0 to 2 (values: 0 and 1); before step 1 below the first of these
     barrier();
     u32x4 pc[AHEAD];
+    f32x16 z1;
+    typename Tile::op8 w1[2], wl1[Tile::PT];
     if (work) {
       u32x4 k[NS];
 #pragma unroll
-      for (int s = 0; s < NS; ++s) k[s] = base[kg * BU + s * 64];
-#pragma unroll
-      for (int n = 0; n < AHEAD; ++n)
-        if (G == 1) pc[n] = base[BU + n * 64];
+      for (int s = 0; s < NS; ++s) k[s] = keys_of(0)[s * 64];
       t.scores(k);
       t.maximum();
       t.rescale(scale);
-    }
-    int b = it.b_lo + RING - G;  // the block copied next, into the slots of unit j - 1
-    for (int j = 0; j < units; ++j) {
-      const char* src[G];
+      t.weights();
 #pragma unroll
-      for (int g = 0; g < G; ++g) src[g] = source(b + g);
-      b += G;
-      // unit j + 1 (one key group: j + 2) has landed in every wavefront's share, and unit j - 1 is no longer read
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - (G == 1 ? 4 : 3 * G)) * CP));
+      for (int s = 0; s < NS; ++s) k[s] = keys_of(1)[s * 64];
+      t.scores(k);
+      t.maximum();
+      if (units > 1) t.template rescale<true>(scale, t.s, t.p, t.pl);
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n)
+        if (G == 1) pc[n] = keys_of(2)[n * 64];
+    }
+    barrier();
+    if (keys) copy();  // (unit RU, where unit 0 was)
+    // Before step j the keys of unit j + 1 (one key group: j + 2) and the values of unit j - 1 have landed in every wavefront's share; keys of unit j and
+    // values of unit j - 2 are no longer read, and make room for those RU units later.
+    auto step = [&](int j, const f32x16& za, f32x16& zb, const auto& w, const auto& wl, auto& wn, auto& wln) {
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm((RU - (G == 1 ? 3 : 2)) * G * CP));
       barrier();
       __builtin_amdgcn_sched_barrier(0);
-      ring_step<D, QT, F16, CP, G, AHEAD>(t, pc, base + (((j + 1) * G + kg) & MASK) * BU, base + ((j * G + kg) & MASK) * BU + BU / 2,
-                                          base + (((j + 2) * G + kg) & MASK) * BU, ring + ((j * G + RING - G) & MASK) * BLOCK + share,
-                                          ring + ((j * G + RING - 1) & MASK) * BLOCK + share, src, work, j + 1 < units, scale);
+      copy();
+      if (work) ring_step<D, QT, F16, G, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale);
+    };
+    int j = 1;
+    for (; j + 1 < units; j += 2) {
+      step(j, t.s, z1, t.p, t.pl, w1, wl1);
+      step(j + 1, z1, t.s, w1, wl1, t.p, t.pl);
     }
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (copies behind the range may still be landing)
+    if (j < units) {
+      step(j, t.s, z1, t.p, t.pl, w1, wl1);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        t.p[i] = w1[i];
+        t.pl[i % Tile::PT] = wl1[i % Tile::PT];
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (the last values, and copies behind the range)
+    barrier();
+    if (work) {
+      u32x4 v[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) v[s] = keys_of(units - 1)[BU / 2 + s * 64];
+      t.values(v);
+    }
   };
   if (units > 0) {
     if (KG == 1) through_the_ring(std::integral_constant<int, 1>());
@@ -670,7 +737,12 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
   }
 
   // ---- blocks without the ring
+  // (the row and its query again: kept over the ring's loop they would take registers that it needs)
+  int rho = row_first + l31;
+  GOOSE_HERE(rho);
+  row = row_of(a, it, rho, kvh);
   if (work && tail0 + kg < it.b_hi) {
+    t.load_q(a, row, hh);
     const MaskRow mk = mask_of(a, it, row);
     pg.base = tail0 >> 1;  // (the window may have run ahead)
     pg.load(lane);

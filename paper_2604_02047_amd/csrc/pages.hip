@@ -210,7 +210,7 @@ __global__ __launch_bounds__(256) void k_pages_copy(const goose_pages pg, const 
 // The accepted path, slot P + path[j] -> P + j for j = 1 .. L, in one (layer, head) of a request.  Thread c owns chunk c of the key rows
 // (16 bytes) and column c of the value rows (2 bytes).  MOVES moves at a time, all loads before all stores: path[j] >= j and increasing, so
 // no later source lies at or below an earlier destination.  The whole path is fetched at once, an entry a lane, with length, count and page ids
-// beside it: asked for move by move it was a trip to memory each (16 requests, 8 layers of 8 heads: 24 us, now MOVE_NOW).
+// beside it: asked for move by move it was a trip to memory each (16 requests, 8 layers of 8 heads: 24 us, now 11).
 constexpr int MOVES = 16;  // (accepted paths are rarely longer)
 template <int D>
 __global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const PagedReqs rq, int n_kv) {
