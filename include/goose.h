@@ -291,7 +291,7 @@ int goose_verify_step_batched(goose_ctx* ctx, const goose_model_ptrs* model, con
  *   GOOSE_FLAG_PAGES  no free page is left, an entry of a table or a reference count is out of range, a fork into a sequence
  *                     that is not empty, a K/V row for a page that is missing or shared, or shared_pages below that are not shared;
  *   GOOSE_FLAG_CAPACITY  a length below 0, above P_max, or beyond table_ld * 64 with the call's new slots.
- * Pages named by entries out of range are read as page 0, never out of bounds.  Sequences are given by number (host
+ * Pages named by entries out of range are read as page 0, never out of bounds.  n_pages * n_kv_heads < 2^29.  Sequences are given by number (host
  * integers, 0 <= seq < n_seqs, none twice in a call, at most GOOSE_MAX_REQUESTS of them). */
 enum { GOOSE_PAGE = 64, GOOSE_FLAG_PAGES = 16 };
 typedef struct {
@@ -357,7 +357,7 @@ int goose_qk_norm_rope_paged(goose_ctx* ctx, const goose_pages* pages, int layer
  * all n tables must be the same pages, wholly committed (shared_pages * 64 <= every length): the keys in them are read once for
  * the rows of all requests.  shared_pages = 0 is always allowed, and the result does not depend on it beyond rounding.
  * d_q as goose_qk_norm_rope_paged writes it; d_o: 16-bit [rows][ldo] of type o_dtype (GOOSE_DTYPE_BF16 or _F16) in o_terms terms.
- * Probabilities are rounded to T for the second product, sums and statistics are fp32.  A row that sees nothing but scores of
+ * Probabilities enter the second product in one term of fp16, or in two of bf16; sums and statistics are fp32.  A row that sees nothing but scores of
  * -infinity, or nothing, is zero; what slots behind a mask hold (NaN, infinities) has no effect; a NaN in what a row sees makes the row NaN,
  * and so does a score of +infinity.  ldq and ldo multiples of 8, d_q and d_o 16-byte aligned.  Sum of round_up(B, 32) <= max_rows. */
 int goose_attn_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,

@@ -389,15 +389,26 @@ class PagedCache:
 class PagedRequests:
     """The requests of a paged call, as dicts with seq, B, P_max and the tensors that the call reads (tokens, parent, is_spine, mask, pos,
     accept_len, path, bonus, next_root, succ_ids, succ_scores).  Build it once for calls that repeat; every call takes a plain
-    list of such dicts as well."""
+    list of such dicts as well.  What the C side cannot see is looked at here: types, layouts, and that the B nodes' entries are there."""
 
     def __init__(self, reqs):
+        import torch
         self.reqs = reqs  # (keeps the tensors alive)
         self._c = (_PagedRequest * len(reqs))()
         names = ("tokens", "parent", "is_spine", "mask", "pos", "accept_len", "path", "bonus", "next_root", "succ_ids", "succ_scores")
         for i, q in enumerate(reqs):
             ptrs = [None if q.get(n) is None else q[n].data_ptr() for n in names]
-            k = 0 if q.get("succ_ids") is None else int(q["succ_ids"].shape[1])
+            B, i32 = max(int(q["B"]), 1), (torch.int32,)
+            fields = {"tokens": (i32, B), "parent": (i32, B), "is_spine": ((torch.uint8, torch.bool), B), "pos": (i32, B), "path": (i32, B),
+                      "mask": ((torch.int64, torch.uint64), B * ((B + 63) // 64)), "accept_len": (i32, 1), "bonus": (i32, 1), "next_root": (i32, 1)}
+            ids, sc = q.get("succ_ids"), q.get("succ_scores")
+            ok = all(q.get(n) is None or (q[n].dtype in t and q[n].is_contiguous() and q[n].numel() >= size) for n, (t, size) in fields.items())
+            if ids is not None and sc is not None:
+                ok = ok and (ids.dtype == torch.int32 and sc.dtype == torch.float32 and ids.dim() == 2 and ids.shape == sc.shape
+                             and ids.is_contiguous() and sc.is_contiguous())
+            if not ok or (ids is None) != (sc is None):
+                raise GooseError(GOOSE_ERR_ARG, f"PagedRequests: type, layout or size of a tensor of request {i}")
+            k = 0 if ids is None else int(ids.shape[1])
             self._c[i] = _PagedRequest(int(q["seq"]), int(q["B"]), int(q.get("P_max", 0)), *ptrs, k)
         # rows of the stacked buffers that the requests reach into (each starts at a multiple of 32)
         Bs = [q.B for q in self._c]
@@ -584,14 +595,19 @@ class GooseContext:
 
     def goose_verify_layer_paged(self, packed_layer, cache, layer, x, reqs, shared_pages=0):
         r, st = self._paged(cache, reqs, packed_layer, x)
-        if not (x.dim() == 2 and x.is_contiguous() and x.shape[0] >= r.rows and x.shape[1] == self.desc.hidden):
-            raise GooseError(GOOSE_ERR_ARG, "goose_verify_layer_paged: rows of x")
+        import torch
+        if not (x.dtype == torch.float32 and x.dim() == 2 and x.is_contiguous() and x.shape[0] >= r.rows and x.shape[1] == self.desc.hidden):
+            raise GooseError(GOOSE_ERR_ARG, "goose_verify_layer_paged: rows or type of x")
         _check(self.lib.goose_verify_layer_paged(self._h, _ptr(packed_layer), cache._ref, layer, _ptr(x), r._c, len(r), shared_pages, st),
                "goose_verify_layer_paged")
 
     def goose_verify_step_paged(self, model: dict, cache, reqs, shared_pages, argmax_all):
         m = _ModelPtrs(model["embed"].data_ptr(), model["packed_layers"].data_ptr(), model["packed_head"].data_ptr(), None, None)
         r, st = self._paged(cache, reqs, argmax_all)
+        import torch
+        if not (argmax_all.dtype == torch.int32 and argmax_all.is_contiguous() and argmax_all.numel() >= r.rows
+                and all(q.get("succ_ids") is None or q["succ_ids"].shape[0] >= self.desc.vocab for q in r.reqs)):
+            raise GooseError(GOOSE_ERR_ARG, "goose_verify_step_paged: argmax_all, or rows of a successor table")
         _check(self.lib.goose_verify_step_paged(self._h, C.byref(m), cache._ref, r._c, len(r), shared_pages, _ptr(argmax_all), st),
                "goose_verify_step_paged")
 

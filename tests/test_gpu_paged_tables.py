@@ -171,8 +171,9 @@ def test_what_cannot_be_done_is_flagged_and_left_undone():
 def test_refusals():
     ctx, cache, _ = make()
     lib, h, pages = ctx.lib, ctx._h, C.byref(cache._c)
-    p1 = torch.zeros(128, dtype=torch.int32, device=DEV)
-    one = [{"seq": 0, "B": 1, "P_max": 0, "path": p1, "accept_len": p1, "pos": p1, "mask": p1}]
+    p1 = torch.zeros(256, dtype=torch.int32, device=DEV)
+    m1 = torch.zeros(1024, dtype=torch.int64, device=DEV)
+    one = [{"seq": 0, "B": 1, "P_max": 0, "path": p1, "accept_len": p1, "pos": p1, "mask": m1}]
 
     def status(fn, *a, **k):
         with pytest.raises(goose.GooseError) as e:
@@ -220,7 +221,7 @@ def test_refusals():
     assert attn(oterms=2) == gb.GOOSE_ERR_ARG and attn(terms=0) == gb.GOOSE_ERR_ARG
     assert attn(o=o.float()) == gb.GOOSE_ERR_ARG and attn(reqs=[dict(one[0], mask=None)]) == gb.GOOSE_ERR_ARG
     assert attn(reqs=[]) == gb.GOOSE_ERR_ARG
-    many = [{"seq": i, "B": 128, "P_max": 0, "mask": p1} for i in range(5)]
+    many = [{"seq": i, "B": 128, "P_max": 0, "mask": m1} for i in range(5)]
     assert attn(q=q.new_zeros((640, 256)), o=o.new_zeros((640, 128)), reqs=many) == gb.GOOSE_ERR_CAPACITY
     # C callers: no context, no descriptor, no arrays
     assert lib.goose_pages_clear(None, pages, None) == gb.GOOSE_ERR_ARG

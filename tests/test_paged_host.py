@@ -27,6 +27,24 @@ def test_the_cache_checks_its_tensors():
         assert e.value.status == gb.GOOSE_ERR_ARG
 
 
+def test_requests_check_their_tensors():
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    good = {"seq": 0, "B": 70, "P_max": 5, "tokens": i32(70), "parent": i32(70), "is_spine": torch.zeros(70, dtype=torch.uint8), "pos": i32(80),
+            "path": i32(128), "mask": torch.zeros((70, 2), dtype=torch.int64), "accept_len": i32(1), "bonus": i32(1), "next_root": i32(1),
+            "succ_ids": torch.zeros((9, 4), dtype=torch.int32), "succ_scores": torch.zeros((9, 4))}
+    r = goose.PagedRequests([good, dict(good, seq=1, B=3, is_spine=None, succ_ids=None, succ_scores=None)])
+    assert len(r) == 2 and r.rows == 96 + 3 and r._c[0].harvest_k == 4 and r._c[1].harvest_k == 0
+    bad = [dict(tokens=i32(69)), dict(tokens=torch.zeros(70, dtype=torch.int64)), dict(parent=i32(140)[::2]), dict(pos=torch.zeros(70)),
+           dict(path=i32(64)), dict(mask=torch.zeros((70, 1), dtype=torch.int64)), dict(mask=i32(280)), dict(is_spine=i32(70)),
+           dict(accept_len=i32(0)), dict(accept_len=torch.zeros(1, dtype=torch.int64)), dict(bonus=torch.zeros(1)), dict(succ_ids=None),
+           dict(succ_scores=None), dict(succ_scores=torch.zeros((9, 5))), dict(succ_ids=torch.zeros((9, 4))),
+           dict(succ_ids=torch.zeros((4, 9), dtype=torch.int32).t())]
+    for b in bad:
+        with pytest.raises(goose.GooseError) as e:
+            goose.PagedRequests([good, dict(good, seq=1, **b)])
+        assert e.value.status == gb.GOOSE_ERR_ARG, b
+
+
 def test_entry_points_refuse_a_missing_context():
     lib = goose.load_library()
     import ctypes as C
