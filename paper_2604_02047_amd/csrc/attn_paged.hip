@@ -196,7 +196,9 @@ struct RowTile {
   f32x16 s;  // scores of the block at hand
   op8 p[2], pl[PT];
   float m, l, top;   // largest score so far, sum of weights, this block's largest score of this lane
-  float lim, ref, mul;  // see rescale()
+  float lim, ref, mul;  // see raise()
+  float late;           // see rescale_later()
+  bool due;
   __device__ __forceinline__ void init(const PagedAttnArgs& a, const Row& w, int hh) {
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt)
@@ -211,7 +213,8 @@ struct RowTile {
       }
     m = lim = -INFINITY;
     l = ref = 0.f;
-    mul = 1.f;
+    mul = late = 1.f;
+    due = false;
     load_q(a, w, hh);
   }
   __device__ __forceinline__ void load_q(const PagedAttnArgs& a, const Row& w, int hh) {
@@ -249,57 +252,68 @@ struct RowTile {
     const float t[4] = {partial_max(s, 0), partial_max(s, 1), partial_max(s, 2), partial_max(s, 3)};
     top = join_max(t);
   }
-  // m, O and l follow it only where some lane's has grown so far that weights would pass 2^SLACK: weights up to there are as good as
-  // those up to one in floating point (16 bits hold them with room to spare), and with 32 rows in a tile some row's maximum grows by a
+  // The exponent that weights, l and O are relative to.
+  __device__ __forceinline__ float reference(float c) const { return finite_ref(m) * c; }
+  __device__ __forceinline__ bool grown() const { return __builtin_amdgcn_ballot_w64(top > lim) != 0; }
+  // m, and with it l and O, follows only where a row's largest score has grown so far that weights would pass 2^SLACK: weights up to there are as
+  // good as those up to one in floating point (16 bits hold them with room to spare), and with 32 rows in a tile some row's maximum grows by a
   // little in most blocks (512 rows over 16384 slots: in 3 of 4).
   // A weight is 2^(s c - ref) in one fused multiply-add, ref = m c rounded; its rounding is the same factor in O and l.  Where products
-  // leave no room for it (2^24 and beyond, infinities), the block's scores become differences to m first.
-  // x: the scores; PENDING: weights of an earlier block, in w and wl, are not in O yet and follow too.
-  template <bool PENDING>
-  __device__ __forceinline__ void rescale(float c, f32x16& x, op8 (&w)[2], op8 (&wl)[PT]) {
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(top > lim) != 0, 0)) {
-      const float m_new = fmaxf(m, fmaxf(top, __shfl_xor(top, 32, 64)));
-      const float old = finite_ref(m), now = finite_ref(m_new);
-      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((old - now) * c);
-      m = m_new;
-      lim = m + SLACK / c;
-      ref = now * c;
-      mul = c;
-      if (__builtin_amdgcn_ballot_w64(!(fabsf(ref) < 16777216.f)) != 0) {
+  // leave no room for it (2^24 and beyond, infinities), the block's scores (x) become differences to m first.
+  // Returns the factor that O has to follow by.
+  __device__ __forceinline__ float raise(float c, f32x16& x) {
+    const float both = fmaxf(top, __shfl_xor(top, 32, 64)), m_new = both > lim ? fmaxf(m, both) : m;
+    const float old = finite_ref(m), now = finite_ref(m_new), before = reference(c);
+    const bool none = m == -INFINITY;
+    m = m_new;
+    ref = reference(c);
+    const bool far = !(fabsf(ref) < 16777216.f);
+    const float alpha = none ? 0.f : __builtin_amdgcn_exp2f(far ? (old - now) * c : before - ref);
+    lim = m + SLACK / c;
+    mul = c;
+    if (__builtin_amdgcn_ballot_w64(far) != 0) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = (x[r] - now) * c;
-        mul = 1.f;
-        ref = 0.f;
-        lim = -INFINITY;  // (and so will the next block's)
-      }
-      l *= alpha;
+      for (int r = 0; r < 16; ++r) x[r] = far ? (x[r] - now) * c : fmaf(x[r], c, -ref);
+      mul = 1.f;
+      ref = 0.f;
+      lim = -INFINITY;  // (and so will the next block's)
+    }
+    l *= alpha;
+    return alpha;
+  }
+  __device__ __forceinline__ void scale_out(float alpha) {
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
+    for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
-      if (PENDING) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int j = i >> 2, e = 2 * i & 7;
-          if (PT == 2) pair_to(i, ((float)w[j][e] + (float)wl[j % PT][e]) * alpha, ((float)w[j][e + 1] + (float)wl[j % PT][e + 1]) * alpha, w, wl);
-          else pair_to(i, (float)w[j][e] * alpha, (float)w[j][e + 1] * alpha, w, wl);
-        }
-      }
+      for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+  }
+  __device__ __forceinline__ void rescale(float c) {
+    if (__builtin_expect(grown(), 0)) scale_out(raise(c, s));
+  }
+  // The same where O still lacks an earlier block, whose weights go by the reference before: its factor waits until that block is in.
+  __device__ __forceinline__ void rescale_later(float c, f32x16& x, bool more) {
+    const bool grows = more && grown();
+    if (__builtin_expect(grows || due, 0)) {
+      if (due) scale_out(late);
+      due = grows;
+      if (grows) late = raise(c, x);
     }
   }
-  __device__ __forceinline__ void rescale(float c) { rescale<false>(c, s, p, pl); }
   // x, y in 16 bits, as weights of keys 2 i, 2 i + 1
   static __device__ __forceinline__ void pair_to(int i, float x, float y, op8 (&w)[2], op8 (&wl)[PT]) {
     typedef T T2 __attribute__((ext_vector_type(2)));
     typedef float F2 __attribute__((ext_vector_type(2)));
-    const unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector((F2{x, y}), T2));
+    unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector((F2{x, y}), T2));
+    GOOSE_HERE(h);  // (the compiler would move it to the next step, which uses it, with no matrix instruction beside it)
     u32x4 v = __builtin_bit_cast(u32x4, w[i >> 2]);
     v[i & 3] = h;
     w[i >> 2] = __builtin_bit_cast(op8, v);
     if (PT == 2) {
       const F2 rest = {x - __builtin_bit_cast(float, h << 16), y - __builtin_bit_cast(float, h & 0xFFFF0000u)};
       v = __builtin_bit_cast(u32x4, wl[(i >> 2) % PT]);
-      v[i & 3] = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, T2));
+      unsigned low = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, T2));
+      GOOSE_HERE(low);
+      v[i & 3] = low;
       wl[(i >> 2) % PT] = __builtin_bit_cast(op8, v);
     }
   }
@@ -490,7 +504,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
 
   // ---- the key groups' states join in one round through LDS: each wavefront leaves its own, then owns some of its tile's columns
   float* dst = lds + (size_t)wave * WFLOATS + lane * 4;
-  *reinterpret_cast<f32x4*>(dst) = f32x4{t.m * scale, t.l, 0.f, 0.f};
+  *reinterpret_cast<f32x4*>(dst) = f32x4{t.m == -INFINITY ? t.m : t.reference(scale), t.l, 0.f, 0.f};
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -606,7 +620,7 @@ __device__ __forceinline__ void ring_step(RowTile<D, QT, F16>& t, u32x4 (&pc)[AH
   }
   z1 = sum;
   t.top = Tile::join_max(part);
-  if (more) t.template rescale<true>(scale, z1, w0, wl0);  // (behind the last block the scores are of a block that is not this loop's)
+  t.rescale_later(scale, z1, more);  // (behind the last block the scores are of a block that is not this loop's)
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n)
     if (G == 1) pc[n] = piece[2 * NS + n];
@@ -693,7 +707,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
       for (int s = 0; s < NS; ++s) k[s] = keys_of(1)[s * 64];
       t.scores(k);
       t.maximum();
-      if (units > 1) t.template rescale<true>(scale, t.s, t.p, t.pl);
+      t.rescale_later(scale, t.s, units > 1);
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n)
         if (G == 1) pc[n] = keys_of(2)[n * 64];
@@ -771,7 +785,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
   if (wave == 0) check_shared(a, it, lane);
 
   // ---- two key groups join: the second leaves its states in LDS, the first takes them in
-  float m = t.m * scale;
+  float m = t.m == -INFINITY ? t.m : t.reference(scale);
   if (KG == 2) {
     __syncthreads();
     float* const buf = reinterpret_cast<float*>(ring) + (size_t)rt * WFLOATS + lane * 4;
@@ -959,7 +973,11 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
     p.splits += sh;
     return p;
   };
-  auto fits = [&](const Plan& p) { return p.splits <= 1 || (size_t)p.splits * step <= max_records; };
+  // (blocks times splits stays a 32-bit number in item_of)
+  const unsigned long long most_blocks = 2ull * (a.sh_blocks > own_longest * own_mul ? a.sh_blocks : own_longest * own_mul);
+  auto fits = [&](const Plan& p) {
+    return p.splits <= 1 || ((size_t)p.splits * step <= max_records && most_blocks * (unsigned)p.splits <= UINT32_MAX);
+  };
   const int least = kind == TILES ? 4 : 8, fixed = kind == TILES ? 10 : 24, sh_steps = (a.sh_blocks + sh_mul - 1) / sh_mul,
             longest = sh_steps > own_longest ? sh_steps : own_longest;
   auto cost_of = [&](const Plan& p, int per) {

@@ -300,3 +300,85 @@ def test_a_captured_call_follows_the_lengths():
         assert torch.equal(first, o)  # the same launch, the same order of sums
     assert ctx.goose_device_flags() == 0 and c is not None
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [128, 256])
+def test_many_rows_over_every_number_of_blocks(dtype, rows):
+    """128 rows a KV head (two key groups) and 256 (one): no whole block, then 1 to 14 of them, with and without a partial one behind."""
+    for n in range(15):
+        P = 32 * n + (0, 0, 17)[n % 3]
+        c = Case(8, 1, 128 if n % 2 else 64, dtype, [rows // 8], [P], 0, seed=40 + n, terms=1 + n // 2 % 2)
+        c.check(c.run(), nodes=4)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [24, 128, 256])
+def test_maxima_that_grow_in_every_block(dtype, rows):
+    """Keys along one direction, longer by the slot: some queries' maxima grow by up to 2^13 a block (others' shrink or stay), from one and from two
+    requests that share the first pages."""
+    B, d = rows // 8, 64
+    c = Case(8, 1, d, dtype, [B, B], [389, 400], 128, seed=60)
+    way = torch.randn(d, generator=torch.Generator().manual_seed(61))
+    turn = torch.linspace(-3.0, 3.0, c.rows * 8).view(c.rows, 8, 1)  # of the queries along it
+    c.q32 = turn * way / way.norm() ** 2 * math.sqrt(d) + 0.05 * c.q32
+    for r in range(2):
+        for s in range(c.Ps[r] + B):
+            c.k[0, c.table[r, s // 64], 0, s % 64] = (0.05 * c.k[0, c.table[r, s // 64], 0, s % 64].float() + way * (s / 11.0)).to(c.dt)
+    c.check(c.run(), nodes=8)
+    c.check(c.run(64), nodes=8)
+
+
+def test_keys_of_minus_infinity_over_whole_blocks():
+    """The first 300 keys score -infinity for queries with a positive entry: rows that first see nothing, block after block; the others see a +infinity."""
+    for rows in (16, 128, 256):
+        c = Case(8, 1, 64, "f16", [rows // 8], [420], 128, seed=70)
+        c.q32[..., 5] = c.q32[..., 5].abs() + 0.1
+        c.q32[1, 3, 5] = -0.5
+        for s in range(300):
+            c.k[0, c.table[0, s // 64], 0, s % 64, 5] = -float("inf")
+        o = c.run()
+        assert o.view(-1, 8, 64)[1, 3].isnan().all()
+        o.view(-1, 8, 64)[1, 3] = float("nan")
+        # against the 64-bit form without those keys: they have no weight
+        k, v = (rows_of(x[0], c.table[0], 420 + rows // 8).double()[:, 300:] for x in (c.k, c.v))
+        see = np.concatenate([np.ones((rows // 8, 120), bool), c.masks[0][1]], 1)
+        want, A, qk, vs = attention64(c.q64[:rows // 8], k, v, torch.from_numpy(see))
+        tol = A * (2.0 ** -11 + 2 * 68 * 2.0 ** -24 * qk.unsqueeze(-1) + 2.0 ** -20 + 2 * 430 * 2.0 ** -24) + want.abs() * 2.0 ** -11 + 2.0 ** -25 + vs * 2.0 ** -25
+        off = (o[:rows // 8].view(-1, 8, 64).double() - want).abs()
+        off[1, 3] = 0
+        assert (off <= tol * 1.001).all()
+
+
+def test_two_graphs_of_one_context():
+    """They share the context's workspace: replayed in turn, between eager calls, each gives what it gave alone."""
+    few, many = (Case(8, 2, 128, "bf16", Bs, Ps, 256, seed=80) for Bs, Ps in (([1] * 5, [2000 + i for i in range(5)]), ([64, 64, 31], [800, 900, 1000])))
+    ctx = goose.GooseContext(goose.ModelDesc(1, 128, 8, 128, 128, 1024, n_kv_heads=2), 64, 256, 512)
+    st, calls = torch.cuda.Stream(), []
+    for c in (few, many):
+        q, c.q64 = c.q_rows()
+        kp, vp = pack_pages(c.k, c.v)
+        cache = goose.PagedCache(kp.to(DEV), vp.to(DEV), torch.from_numpy(c.table).to(DEV), torch.tensor(c.Ps, dtype=torch.int32, device=DEV),
+                                 torch.from_numpy(c.refs).to(DEV))
+        reqs = goose.PagedRequests([{"seq": r, "B": b, "P_max": p, "mask": c.masks[r][0].to(DEV)} for r, (b, p) in enumerate(zip(c.Bs, c.Ps))])
+        o, qd, graph = torch.full((c.rows, 1024), 77.0, dtype=torch.float16, device=DEV), q.to(DEV), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=st):
+            ctx.goose_attn_paged(cache, 0, qd, 1, reqs, 4, o)
+        calls.append((c, graph, o, (cache, 0, qd, 1, reqs, 4, o)))
+    first = [None, None]
+    for turn in range(6):
+        with torch.cuda.stream(st):
+            for _, graph, o, _ in calls:
+                o.fill_(77.0)
+                graph.replay()
+            if turn % 2:
+                ctx.goose_attn_paged(*calls[0][3])
+        st.synchronize()
+        for i, (c, _, o, _) in enumerate(calls):
+            if turn == 0:
+                c.check(o.cpu(), nodes=6)
+                first[i] = o.clone()
+            assert torch.equal(o, first[i]), (turn, i)
+    assert ctx.goose_device_flags() == 0
+    ctx.close()
