@@ -49,7 +49,8 @@ struct PagedAttnArgs {
   int32_t* flags;
   size_t ldq, ldo;
   int32_t table_ld, n_pages, n_heads, n_kv, group, rows, n_req;
-  int32_t sh_blocks, sh_tiles, sh_splits;  // shared keys: 32-slot blocks, row tiles, splits
+  int32_t same_blocks;                     // 32-slot blocks in front that must be the same in all tables
+  int32_t sh_blocks, sh_tiles, sh_splits;  // shared keys with items of their own: blocks (all of those, or none), row tiles, splits
   int32_t sh_kg, own_kg;                   // k_paged_tiles: key groups of either kind of item
   int32_t direct;                          // every row has one item: it writes o itself
   int32_t o_terms, o_f16;
@@ -118,7 +119,7 @@ __device__ inline Item item_of(const PagedAttnArgs& a, int y, int kvh) {
     it.B = a.r[r].B;
     it.P = __builtin_amdgcn_readfirstlane(a.len[it.seq]);
     const int S = a.sh_blocks * 32;
-    if ((it.P < S || it.P > a.r[r].P_max) && it.first && threadIdx.x == 0) atomicOr(a.flags, GOOSE_FLAG_CAPACITY);
+    if ((it.P < a.same_blocks * 32 || it.P < 0 || it.P > a.r[r].P_max) && it.first && threadIdx.x == 0) atomicOr(a.flags, GOOSE_FLAG_CAPACITY);
     it.P = min(max(it.P, S), a.r[r].P_max);  // (P_max + B <= 64 table_ld, S <= P_max: checked on the host)
     b_first = a.sh_blocks;
     n_blocks = ((it.P + it.B + 31) >> 5) - b_first;
@@ -134,7 +135,7 @@ __device__ inline void check_shared(const PagedAttnArgs& a, const Item& it, int 
   const int32_t* t0 = a.table + (size_t)a.r[0].seq * a.table_ld;
   const int32_t* t = a.table + (size_t)it.seq * a.table_ld;
   bool differs = false;
-  for (int i = lane; i < a.sh_blocks / 2; i += 64) differs = differs || t[i] != t0[i];
+  for (int i = lane; i < a.same_blocks / 2; i += 64) differs = differs || t[i] != t0[i];
   if (differs) atomicOr(a.flags, GOOSE_FLAG_PAGES);
 }
 // Row rho of an item: (node, query head of the group), the heads fastest.
@@ -934,87 +935,110 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.n_req = rq.n;
   a.o_terms = o_terms;
   a.o_f16 = o_dtype == GOOSE_DTYPE_F16;
-  a.sh_blocks = shared_pages * 2;
+  a.same_blocks = shared_pages * 2;
   int own_rows = 0;
   for (int r = 0; r < rq.n; ++r) own_rows = rq.r[r].B > own_rows ? rq.r[r].B : own_rows;
   own_rows *= a.group;
-  const int sh_rows = shared_pages > 0 ? rq.rows * a.group : 0, most = sh_rows > own_rows ? sh_rows : own_rows;
-  const int kind = most > 64 ? TILES : (most > 32 ? STREAM2 : STREAM1);
-  // k_paged_tiles: 128 rows with two key groups where that leaves fewer rows of a tile empty
-  auto key_groups = [](int rows) { return (rows + 127) / 128 * 128 < (rows + 255) / 256 * 256 ? 2 : 1; };
-  a.sh_kg = key_groups(sh_rows);
-  a.own_kg = key_groups(own_rows);
-  const int sh_height = kind == TILES ? 256 / a.sh_kg : (kind == STREAM2 ? 64 : 32);
-  const int own_height = kind == TILES ? 256 / a.own_kg : sh_height;
-  const int sh_mul = kind == TILES ? a.sh_kg : 1, own_mul = kind == TILES ? a.own_kg : 1;  // blocks that an item takes at a time
-  a.sh_tiles = (sh_rows + sh_height - 1) / sh_height;
-  int own_blocks[GOOSE_MAX_REQUESTS], own_longest = 0;
-  for (int r = 0; r < rq.n; ++r) {
-    const PagedReq& s = rq.r[r];
-    a.r[r] = AttnReq{s.seq, s.B, s.P_max, s.row0, s.c0, (s.B * a.group + own_height - 1) / own_height, 0, (const uint64_t*)s.p};
-    own_blocks[r] = (s.P_max + s.B + 31) / 32 - a.sh_blocks;
-    const int steps = (own_blocks[r] + own_mul - 1) / own_mul;
-    own_longest = steps > own_longest ? steps : own_longest;
-  }
-  // Splits: items of at most `per` steps (blocks, or pairs of them).  They run in rounds of 256 workgroups, one a compute unit, the shared keys' items first;
-  // an item costs its steps and a fixed part (FIXED steps: start, first loads, epilogue), a split its records in the merge.  Tried: the smallest
-  // `per` that makes one to four rounds of all items, or of the shared ones; the cheapest is taken.
-  const size_t step = (size_t)n_heads * rq.rows;  // records of one split
-  struct Plan { long long sh, own; int splits; };
-  auto plan_at = [&](int per) {
-    Plan p{0, 0, 0};
-    const int sh = (a.sh_blocks + per * sh_mul - 1) / (per * sh_mul);
-    p.sh = (long long)a.sh_tiles * sh * n_kv;
+  const size_t records = (size_t)n_heads * rq.rows;  // of one split
+  // A way to split the work: do the shared keys have items of their own, which kernel, and how many steps (blocks, or pairs of them) an item takes
+  // at most.  Items run in rounds of 256 workgroups, one a compute unit, the shared keys' items first; times in units of 10 ns at head_dim 128, from
+  // runs with 20 calls in a graph: an item's fixed part (start, first loads, epilogue; 5.5 us, with the ring 11) and its steps (0.21 us a
+  // block, 0.4 where two row tiles halve the key groups; with the ring 1.15 us with two products in all, 2.0 with four), the merge 4 us and its records.
+  struct Way {
+    int kind, per, sh_blocks, sh_kg, own_kg, sh_height, own_height;
+    long long cost;
+  };
+  auto cheapest = [&](bool share, Way& best) {  // updates best; false: no way fits the workspace
+    Way w{};
+    w.sh_blocks = share ? a.same_blocks : 0;
+    const int sh_rows = share ? rq.rows * a.group : 0, most = sh_rows > own_rows ? sh_rows : own_rows;
+    w.kind = most > 64 ? TILES : (most > 32 ? STREAM2 : STREAM1);
+    // k_paged_tiles: 128 rows with two key groups where that leaves fewer rows of a tile empty
+    auto key_groups = [](int rows) { return (rows + 127) / 128 * 128 < (rows + 255) / 256 * 256 ? 2 : 1; };
+    w.sh_kg = key_groups(sh_rows);
+    w.own_kg = key_groups(own_rows);
+    const bool ring = w.kind == TILES;
+    w.sh_height = ring ? 256 / w.sh_kg : (w.kind == STREAM2 ? 64 : 32);
+    w.own_height = ring ? 256 / w.own_kg : w.sh_height;
+    const int sh_mul = ring ? w.sh_kg : 1, own_mul = ring ? w.own_kg : 1;  // blocks that a step takes
+    const int sh_tiles = (sh_rows + w.sh_height - 1) / w.sh_height, sh_steps = (w.sh_blocks + sh_mul - 1) / sh_mul;
+    int own_steps[GOOSE_MAX_REQUESTS], own_tiles[GOOSE_MAX_REQUESTS], own_longest = 0;
     for (int r = 0; r < rq.n; ++r) {
-      const int n = (own_blocks[r] + per * own_mul - 1) / (per * own_mul);
-      p.own += (long long)a.r[r].tiles * n * n_kv;
-      p.splits = n > p.splits ? n : p.splits;
+      own_steps[r] = ((rq.r[r].P_max + rq.r[r].B + 31) / 32 - w.sh_blocks + own_mul - 1) / own_mul;
+      own_tiles[r] = (rq.r[r].B * a.group + w.own_height - 1) / w.own_height;
+      own_longest = own_steps[r] > own_longest ? own_steps[r] : own_longest;
     }
-    p.splits += sh;
-    return p;
-  };
-  // (blocks times splits stays a 32-bit number in item_of)
-  const unsigned long long most_blocks = 2ull * (a.sh_blocks > own_longest * own_mul ? a.sh_blocks : own_longest * own_mul);
-  auto fits = [&](const Plan& p) {
-    return p.splits <= 1 || ((size_t)p.splits * step <= max_records && most_blocks * (unsigned)p.splits <= UINT32_MAX);
-  };
-  const int least = kind == TILES ? 4 : 8, fixed = kind == TILES ? 10 : 24, sh_steps = (a.sh_blocks + sh_mul - 1) / sh_mul,
-            longest = sh_steps > own_longest ? sh_steps : own_longest;
-  auto cost_of = [&](const Plan& p, int per) {
-    const long long sh_len = (per < sh_steps ? per : sh_steps) + fixed, own_len = (per < own_longest ? per : own_longest) + fixed;
-    const long long rounds = (p.sh + 255) / 256, room = (rounds * 256 - p.sh) * (sh_len / own_len);  // own items beside the last shared ones
-    const long long left = p.own > room ? p.own - room : 0;
-    return rounds * sh_len + (left + 255) / 256 * own_len + (p.splits > 1 ? (long long)(p.splits * step * head_dim / 1000000) : 0);
-  };
-  const int most_steps = longest > least ? longest : least;
-  int per = most_steps;
-  Plan plan = plan_at(per);
-  if (!fits(plan)) return GOOSE_ERR_CAPACITY;
-  long long best = cost_of(plan, per);
-  auto consider = [&](int cand) {
-    if (cand < least || cand >= most_steps) return;
-    const Plan p = plan_at(cand);
-    const long long cost = cost_of(p, cand);
-    if (fits(p) && cost < best) { best = cost; per = cand; }
-  };
-  for (int rounds = 1; rounds <= 4; ++rounds) {
-    int lo = least, hi = most_steps;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      const Plan p = plan_at(mid);
-      if (p.sh + p.own <= 256 * rounds && fits(p)) hi = mid; else lo = mid + 1;
+    const int least = ring ? 4 : 8, fixed = ring ? 1100 : 550,
+              step = (ring ? 30 + 42 * (q_terms + (dtype == GOOSE_DTYPE_F16 ? 1 : 2)) : (w.kind == STREAM2 ? 40 : 21)) * head_dim / 128;
+    const int longest = sh_steps > own_longest ? sh_steps : own_longest, most_steps = longest > least ? longest : least;
+    struct Plan { long long sh, own; int splits; };  // workgroups, records a row
+    auto plan_at = [&](int per) {
+      Plan p{0, 0, 0};
+      const int sh = (sh_steps + per - 1) / per;
+      p.sh = (long long)sh_tiles * sh * n_kv;
+      for (int r = 0; r < rq.n; ++r) {
+        const int n = (own_steps[r] + per - 1) / per;
+        p.own += (long long)own_tiles[r] * n * n_kv;
+        p.splits = n > p.splits ? n : p.splits;
+      }
+      p.splits += sh;
+      return p;
+    };
+    auto fits = [&](const Plan& p) {  // (blocks times splits stays a 32-bit number in item_of)
+      return p.splits <= 1 || ((size_t)p.splits * records <= max_records && 2ull * longest * 2 * (unsigned)p.splits <= UINT32_MAX);
+    };
+    bool any = false;
+    auto consider = [&](int per) {
+      if (per < least || per > most_steps) return;
+      const Plan p = plan_at(per);
+      if (!fits(p)) return;
+      any = true;
+      const long long sh_len = (long long)(per < sh_steps ? per : sh_steps) * step + fixed,
+                      own_len = (long long)(per < own_longest ? per : own_longest) * step + fixed;
+      const long long rounds = (p.sh + 255) / 256, room = (rounds * 256 - p.sh) * (sh_len / own_len);  // own items beside the last shared ones
+      const long long left = p.own > room ? p.own - room : 0;
+      w.cost = rounds * sh_len + (left + 255) / 256 * own_len +
+               (p.splits > 1 ? 400 + (long long)(p.splits * records * head_dim * 130 / 1000000) : 0);
+      w.per = per;
+      if (w.cost < best.cost) best = w;
+    };
+    // tried: no split, and the smallest `per` that makes one to four rounds of all items, or of the shared ones
+    consider(most_steps);
+    for (int rounds = 1; rounds <= 4; ++rounds) {
+      int lo = least, hi = most_steps;
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        const Plan p = plan_at(mid);
+        if (p.sh + p.own <= 256 * rounds && fits(p)) hi = mid; else lo = mid + 1;
+      }
+      consider(lo);
+      const int sh = sh_tiles > 0 ? 256 * rounds / (sh_tiles * n_kv) : 0;
+      if (sh > 0) consider((sh_steps + sh - 1) / sh);
     }
-    consider(lo);
-    const int sh = a.sh_tiles > 0 ? 256 * rounds / (a.sh_tiles * n_kv) : 0;
-    if (sh > 0) consider((sh_steps + sh - 1) / sh);
-  }
-  a.sh_splits = (a.sh_blocks + per * sh_mul - 1) / (per * sh_mul);
+    return any;
+  };
+  // The shared keys get items of their own where rows of one request leave most of a tile empty, or where many keys meet few rows (16 requests x 1
+  // over 8192 slots: 27 us, by request 54).  Where a request fills its tiles by itself the products are the same either way, the caches serve the
+  // pages to all of them, and one set of items and fewer records win (16 x 32 over 4096 slots, bf16: 95 us, shared 118; over 64: 16 and 24).
+  Way way{};
+  way.cost = INT64_MAX;
+  const bool by_request = cheapest(false, way);
+  if (!(shared_pages > 0 && cheapest(true, way)) && !by_request) return GOOSE_ERR_CAPACITY;
+  const int kind = way.kind, sh_mul = kind == TILES ? way.sh_kg : 1, own_mul = kind == TILES ? way.own_kg : 1;
+  a.sh_blocks = way.sh_blocks;
+  a.sh_kg = way.sh_kg;
+  a.own_kg = way.own_kg;
+  a.sh_tiles = a.sh_blocks > 0 ? (rq.rows * a.group + way.sh_height - 1) / way.sh_height : 0;
+  a.sh_splits = (a.sh_blocks + way.per * sh_mul - 1) / (way.per * sh_mul);
   int own_splits = 0;
   unsigned items = (unsigned)(a.sh_tiles * a.sh_splits);
   for (int r = 0; r < rq.n; ++r) {
-    a.r[r].splits = (own_blocks[r] + per * own_mul - 1) / (per * own_mul);
-    own_splits = a.r[r].splits > own_splits ? a.r[r].splits : own_splits;
-    items += (unsigned)(a.r[r].tiles * a.r[r].splits);
+    const PagedReq& q = rq.r[r];
+    const int blocks = (q.P_max + q.B + 31) / 32 - a.sh_blocks, tiles = (q.B * a.group + way.own_height - 1) / way.own_height,
+              splits = (blocks + way.per * own_mul - 1) / (way.per * own_mul);
+    a.r[r] = AttnReq{q.seq, q.B, q.P_max, q.row0, q.c0, tiles, splits, (const uint64_t*)q.p};
+    own_splits = splits > own_splits ? splits : own_splits;
+    items += (unsigned)(tiles * splits);
   }
   a.direct = a.sh_splits + own_splits == 1;
   const dim3 grid(n_kv, items);
