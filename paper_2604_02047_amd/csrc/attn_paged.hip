@@ -551,7 +551,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
 // What bounds it is power: fp16, 2048 rows a KV head over 16384 slots, a step takes 1680 cycles (1024 of them the matrix pipe's; 1490 without the
 // copies and the raised maxima) at a clock that falls to 1.45 GHz, where the same products on constants run at 1.95.  770 TFLOP/s; with S and
 // P V of neighbouring blocks in one step, weights beside S alone and copies that made each LDS read wait for all: 690.
-// Blocks that need a mask (the tree's, and what is left over) follow without the ring, as in k_paged_stream.
+// Blocks that need a mask (the tree's, and what is left over) follow as in k_paged_stream, from what the ring has copied ahead or from memory.
 #define GOOSE_BUFFER_WORD3 0x00020000  // (buffer descriptor: raw 32-bit data)
 #define GOOSE_LDS_PTR(p) ((__attribute__((address_space(3))) void*)(p))
 constexpr int vmcnt_imm(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }  // s_waitcnt vmcnt(n) only
@@ -761,11 +761,22 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
     const MaskRow mk = mask_of(a, it, row);
     pg.base = tail0 >> 1;  // (the window may have run ahead)
     pg.load(lane);
-    for (int b = tail0 + kg; b < it.b_hi; b += KG) {
-      const size_t at = block_at(b);
+    // the ring's copies have run ahead by RING / KG - 2 units (values; keys by more), so most of these blocks are in LDS already
+    const int units_there = units > 0 ? units + RING / KG - 2 : 0;
+    for (int u = units, b = tail0 + kg; b < it.b_hi; ++u, b += KG) {
       u32x4 k[NS], v[NS];
-      fetch(kp + at, lane, k);
-      fetch(vp + at, lane, v);
+      if (u < units_there) {
+        const u32x4* const at = reinterpret_cast<const u32x4*>(ring + (size_t)((u * KG & (RING - 1)) + kg) * BLOCK) + lane;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          k[s] = at[s * 64];
+          v[s] = at[(NS + s) * 64];
+        }
+      } else {
+        const size_t at = block_at(b);
+        fetch(kp + at, lane, k);
+        fetch(vp + at, lane, v);
+      }
       const int slot0 = b * 32;
       const bool tree = it.ri >= 0 && slot0 + 32 > it.P;
       unsigned vis = 0xFFFFu;
