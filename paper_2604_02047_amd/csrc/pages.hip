@@ -188,29 +188,33 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(const goose_pages pg, cons
 }
 
 // Copies of a reservation: workgroup (2 (layer * n_kv + head) + (K or V), request) moves the 32-slot blocks that hold committed
-// slots, contiguous in the operand order: 1 or 2 x 64 d bytes.
+// slots, contiguous in the operand order: 1 or 2 x 64 d bytes.  Non-temporal stores: pages that stay dirty in the L2s are written back at the
+// kernel's end, with nothing beside it (16 requests, 8 layers of 8 heads, 33.5 MB each way: 21 us, now 8.8; loads non-temporal too: 13; half the
+// bytes a workgroup: level).
 __global__ __launch_bounds__(256) void k_pages_copy(const goose_pages pg, const int4* __restrict__ copies, int n_kv, int D) {
   const int4 c = copies[blockIdx.y];
   if (c.x < 0) return;
   const int lh = blockIdx.x >> 1, layer = lh / n_kv, head = lh - layer * n_kv;
-  uint4* pool = reinterpret_cast<uint4*>((blockIdx.x & 1) ? pg.d_vpool : pg.d_kpool);
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  u32x4* pool = reinterpret_cast<u32x4*>((blockIdx.x & 1) ? pg.d_vpool : pg.d_kpool);
   const size_t per_head = (size_t)GOOSE_PAGE * D / 8;  // 16-byte units
-  const uint4* src = pool + (((size_t)layer * pg.n_pages + c.x) * n_kv + head) * per_head;
-  uint4* dst = pool + (((size_t)layer * pg.n_pages + c.y) * n_kv + head) * per_head;
+  const u32x4* src = pool + (((size_t)layer * pg.n_pages + c.x) * n_kv + head) * per_head;
+  u32x4* dst = pool + (((size_t)layer * pg.n_pages + c.y) * n_kv + head) * per_head;
   const int units = c.z * 32 * D / 8;
-  uint4 v[4];  // (at most 64 * 128 / 8 = 1024 units: four a thread, all loads in flight together)
+  u32x4 v[4];  // (at most 64 * 128 / 8 = 1024 units: four a thread, all loads in flight together)
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     if ((int)threadIdx.x + k * 256 < units) v[k] = src[threadIdx.x + k * 256];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
-    if ((int)threadIdx.x + k * 256 < units) dst[threadIdx.x + k * 256] = v[k];
+    if ((int)threadIdx.x + k * 256 < units) __builtin_nontemporal_store(v[k], dst + threadIdx.x + k * 256);
 }
 
 // The accepted path, slot P + path[j] -> P + j for j = 1 .. L, in one (layer, head) of a request.  Thread c owns chunk c of the key rows
 // (16 bytes) and column c of the value rows (2 bytes).  MOVES moves at a time, all loads before all stores: path[j] >= j and increasing, so
 // no later source lies at or below an earlier destination.  The whole path is fetched at once, an entry a lane, with length, count and page ids
-// beside it: asked for move by move it was a trip to memory each (16 requests, 8 layers of 8 heads: 24 us, now 11).
+// beside it, and the moves of a round are checked by a lane each: asked for move by move it was a trip to memory each (16 requests, 8 layers of 8
+// heads: 24 us), checked one behind the other 11 us; now 9.6, of which the trips (length, entry, loads, stores) are the most.
 constexpr int MOVES = 16;  // (accepted paths are rarely longer)
 template <int D>
 __global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const PagedReqs rq, int n_kv) {
@@ -226,33 +230,31 @@ __global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const Pa
   const int32_t* row = pg.d_table + (size_t)q.seq * pg.table_ld;
   const int e0 = P >> 6;
   const int id = lane < 3 && e0 + lane < pg.table_ld ? row[e0 + lane] : -1;  // a tree of 128 nodes reaches into three pages
-  auto at = [&](int j) { return j < 64 ? __builtin_amdgcn_readlane(p_lo, j) : __builtin_amdgcn_readlane(p_hi, j - 64); };
   const size_t layer0 = (size_t)layer * pg.n_pages;
   u16* const kpool = static_cast<u16*>(pg.d_kpool);
   u16* const vpool = static_cast<u16*>(pg.d_vpool);
-  auto head_of = [&](int s) -> long long {  // elements before the head's part of the page of slot s, or -1
-    const int p = __builtin_amdgcn_readlane(id, (s >> 6) - e0);
-    return (unsigned)p < (unsigned)pg.n_pages ? (long long)(((layer0 + p) * n_kv + head) * (size_t)(GOOSE_PAGE * D)) : -1;
-  };
+  const size_t per_page = (size_t)n_kv * (GOOSE_PAGE * D);
+  const size_t base = layer0 * per_page + (size_t)head * (GOOSE_PAGE * D);
   int prev = 0;
   for (int j0 = 1; j0 <= L; j0 += MOVES) {
-    int n = 0, from[MOVES];  // moves of this round: up to the first entry that is not increasing, leaves the tree or has no page
-#pragma unroll
-    for (int u = 0; u < MOVES; ++u) {
-      const int j = j0 + u, s = j <= L ? at(j) : -1;
-      from[u] = s;
-      if (n == u && s > prev && s < q.B && head_of(P + s) >= 0 && head_of(P + j) >= 0) {
-        prev = s;
-        n = u + 1;
-      }
-    }
+    // Lane u: move j0 + u, from slot P + from to slot P + j0 + u, each with its page.  The round ends at the first entry that is not increasing,
+    // leaves the tree or has no page.
+    const int j = j0 + lane;
+    const int lo = __shfl(p_lo, j & 63, 64), hi = __shfl(p_hi, j & 63, 64), from = j < 64 ? lo : hi;
+    const int up = __shfl_up(from, 1, 64), last = lane == 0 ? prev : up;
+    const int src = P + from, dst = P + j;
+    const int ps = __shfl(id, ((src >> 6) - e0) & 63, 64), pd = __shfl(id, ((dst >> 6) - e0) & 63, 64);
+    const bool good = lane < MOVES && j <= L && from > last && from < q.B && (unsigned)ps < (unsigned)pg.n_pages && (unsigned)pd < (unsigned)pg.n_pages;
+    const int n = __builtin_ctzll(~__builtin_amdgcn_ballot_w64(good));  // (at most MOVES)
+    if (n > 0) prev = __builtin_amdgcn_readlane(from, n - 1);
+    auto part_of = [&](int page, int u) { return base + (size_t)__builtin_amdgcn_readlane(page, u) * per_page; };
     uint4 kr[MOVES];
     u16 vr[MOVES];
 #pragma unroll
     for (int u = 0; u < MOVES; ++u)
       if (u < n) {
-        const int s = P + from[u];
-        const long long b = head_of(s);
+        const int s = __builtin_amdgcn_readlane(src, u);
+        const size_t b = part_of(ps, u);
         if (c < D / 8) kr[u] = *reinterpret_cast<const uint4*>(kpool + b + page_k_chunk<D>(s & 63, c));
         vr[u] = vpool[b + page_v_elem<D>(s & 63, c)];
       }
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const Pa
     for (int u = 0; u < MOVES; ++u)
       if (u < n) {
         const int d = P + j0 + u;
-        const long long b = head_of(d);
+        const size_t b = part_of(pd, u);
         if (c < D / 8) *reinterpret_cast<uint4*>(kpool + b + page_k_chunk<D>(d & 63, c)) = kr[u];
         vpool[b + page_v_elem<D>(d & 63, c)] = vr[u];
       }
