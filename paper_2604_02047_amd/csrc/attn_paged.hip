@@ -954,7 +954,8 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   // A way to split the work: do the shared keys have items of their own, which kernel, and how many steps (blocks, or pairs of them) an item takes
   // at most.  Items run in rounds of 256 workgroups, one a compute unit, the shared keys' items first; times in units of 10 ns at head_dim 128, from
   // runs with 20 calls in a graph: an item's fixed part (start, first loads, epilogue; 5.5 us, with the ring 11) and its steps (0.21 us a
-  // block, 0.4 where two row tiles halve the key groups; with the ring 1.15 us with two products in all, 2.0 with four), the merge 4 us and its records.
+  // block, 0.4 where two row tiles halve the key groups; with the ring 1.15 us with two products in all, 2.0 with four), the merge 4 us and its records;
+  // and no less than what the caches take to serve all items' blocks (8.5 TB/s).
   struct Way {
     int kind, per, sh_blocks, sh_kg, own_kg, sh_height, own_height;
     long long cost;
@@ -974,11 +975,14 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
     const int sh_mul = ring ? w.sh_kg : 1, own_mul = ring ? w.own_kg : 1;  // blocks that a step takes
     const int sh_tiles = (sh_rows + w.sh_height - 1) / w.sh_height, sh_steps = (w.sh_blocks + sh_mul - 1) / sh_mul;
     int own_steps[GOOSE_MAX_REQUESTS], own_tiles[GOOSE_MAX_REQUESTS], own_longest = 0;
+    long long fetched = (long long)sh_tiles * w.sh_blocks;  // blocks, by all items of a KV head
     for (int r = 0; r < rq.n; ++r) {
       own_steps[r] = ((rq.r[r].P_max + rq.r[r].B + 31) / 32 - w.sh_blocks + own_mul - 1) / own_mul;
       own_tiles[r] = (rq.r[r].B * a.group + w.own_height - 1) / w.own_height;
       own_longest = own_steps[r] > own_longest ? own_steps[r] : own_longest;
+      fetched += (long long)own_tiles[r] * own_steps[r] * own_mul;
     }
+    const long long fetch = fetched * n_kv * head_dim * 128 / 85000;
     const int least = ring ? 4 : 8, fixed = ring ? 1100 : 550,
               step = (ring ? 30 + 42 * (q_terms + (dtype == GOOSE_DTYPE_F16 ? 1 : 2)) : (w.kind == STREAM2 ? 40 : 21)) * head_dim / 128;
     const int longest = sh_steps > own_longest ? sh_steps : own_longest, most_steps = longest > least ? longest : least;
@@ -1008,8 +1012,8 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
                       own_len = (long long)(per < own_longest ? per : own_longest) * step + fixed;
       const long long rounds = (p.sh + 255) / 256, room = (rounds * 256 - p.sh) * (sh_len / own_len);  // own items beside the last shared ones
       const long long left = p.own > room ? p.own - room : 0;
-      w.cost = rounds * sh_len + (left + 255) / 256 * own_len +
-               (p.splits > 1 ? 400 + (long long)(p.splits * records * head_dim * 130 / 1000000) : 0);
+      const long long items = rounds * sh_len + (left + 255) / 256 * own_len;
+      w.cost = (items > fetch ? items : fetch) + (p.splits > 1 ? 400 + (long long)(p.splits * records * head_dim * 130 / 1000000) : 0);
       w.per = per;
       if (w.cost < best.cost) best = w;
     };
