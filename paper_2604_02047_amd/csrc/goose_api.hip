@@ -893,7 +893,7 @@ int goose_pages_commit(goose_ctx* c, const goose_pages* pg, const goose_paged_re
   PagedReqs rq;
   rc = paged_reqs(c, pg, reqs, n, false, &rq, [](const goose_paged_request& q) -> const void* { return q.d_accept_len ? q.d_path : nullptr; });
   if (rc) return rc;
-  return launch_pages_commit(*pg, rq, c->d.n_layers, c->n_kv, c->d.head_dim, c->flags, as_stream(stream));
+  return launch_pages_commit(*pg, rq, c->d.n_layers, c->n_kv, c->d.head_dim, nullptr, c->flags, as_stream(stream));
 }
 
 int goose_pages_free(goose_ctx* c, const goose_pages* pg, const int32_t* h_seqs, int n, void* stream) {
@@ -1013,7 +1013,7 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
   if (rc) return rc;
   rc = launch_batch_accept(br, n, d_argmax_all, st);
   if (rc) return rc;
-  return launch_pages_commit(*pg, commit, d.n_layers, c->n_kv, d.head_dim, c->flags, st);
+  return launch_pages_commit(*pg, commit, d.n_layers, c->n_kv, d.head_dim, c->page_copies, c->flags, st);
 }
 
 // ---- the LM head without a context: its workspace is a static device array --------------------

@@ -290,7 +290,9 @@ int launch_pages_clear(const goose_pages& pg, hipStream_t st);
 int launch_pages_fork(const goose_pages& pg, int src, int len, const SeqList& dst, int32_t* flags, hipStream_t st);
 int launch_pages_reserve(const goose_pages& pg, const SeqList& seqs, int n_layers, int n_kv, int head_dim, void* copies, int32_t* flags,
                          hipStream_t st);
-int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, int32_t* flags, hipStream_t st);
+// reservation: null, or the `copies` of a reservation without which nothing is to be committed
+int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, const void* reservation, int32_t* flags,
+                        hipStream_t st);
 int launch_pages_free(const goose_pages& pg, const SeqList& seqs, int32_t* flags, hipStream_t st);
 // base of one layer's part of a pool, in elements
 static inline size_t page_layer_elems(const goose_pages& pg, int n_kv, int head_dim) {

@@ -164,7 +164,10 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(const goose_pages pg, cons
   if (tid == 0 && (found < need || need > PAGES_PER_CALL)) bad |= GOOSE_FLAG_PAGES;
   __syncthreads();
   if (bad) {
-    if (tid == 0) atomicOr(flags, bad);
+    if (tid == 0) {
+      atomicOr(flags, bad);
+      copies[0].w = 1;  // (the reservation has failed)
+    }
     return;
   }
   int done = 0;
@@ -217,7 +220,7 @@ __global__ __launch_bounds__(256) void k_pages_copy(const goose_pages pg, const 
 // heads: 24 us), checked one behind the other 11 us; now 9.6, of which the trips (length, entry, loads, stores) are the most.
 constexpr int MOVES = 16;  // (accepted paths are rarely longer)
 template <int D>
-__global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const PagedReqs rq, int n_kv) {
+__global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const PagedReqs rq, int n_kv, const int4* __restrict__ reservation) {
   typedef unsigned short u16;
   const PagedReq& q = rq.r[blockIdx.y];
   const int layer = blockIdx.x / n_kv, head = blockIdx.x - layer * n_kv, c = threadIdx.x, lane = c & 63;
@@ -226,6 +229,7 @@ __global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const Pa
   const int P = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]);
   int L = __builtin_amdgcn_readfirstlane(*q.accept_len);
   if (P < 0 || L < 0) return;  // (flagged by k_pages_settle)
+  if (reservation && reservation->w) return;
   L = min(L, q.B - 1);
   const int32_t* row = pg.d_table + (size_t)q.seq * pg.table_ld;
   const int e0 = P >> 6;
@@ -281,8 +285,10 @@ __device__ inline void release(const goose_pages& pg, size_t at, int32_t* flags)
   }
 }
 
-// New lengths, and the pages behind them go back.
-__global__ __launch_bounds__(256) void k_pages_settle(const goose_pages pg, const PagedReqs rq, int32_t* __restrict__ flags) {
+// New lengths, and the pages behind them go back.  reservation: where the slots were taken in the same call, and nothing is committed if that failed.
+__global__ __launch_bounds__(256) void k_pages_settle(const goose_pages pg, const PagedReqs rq, const int4* __restrict__ reservation,
+                                                      int32_t* __restrict__ flags) {
+  if (reservation && reservation->w) return;
   const PagedReq& q = rq.r[blockIdx.x];
   const int P = pg.d_len[q.seq], L = *q.accept_len;
   const bool off = P < 0 || L < 0 || L >= q.B || (long long)P + L + 1 > (long long)pg.table_ld * GOOSE_PAGE;
@@ -329,14 +335,16 @@ int launch_pages_reserve(const goose_pages& pg, const SeqList& seqs, int n_layer
   return goose_launch_status();
 }
 
-int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, int32_t* flags, hipStream_t st) {
+int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, const void* reservation, int32_t* flags,
+                        hipStream_t st) {
+  const int4* res = (const int4*)reservation;
   const dim3 grid(n_layers * n_kv, rq.n);
-  if (head_dim == 128) hipLaunchKernelGGL(k_pages_move<128>, grid, dim3(128), 0, st, pg, rq, n_kv);
-  else if (head_dim == 64) hipLaunchKernelGGL(k_pages_move<64>, grid, dim3(64), 0, st, pg, rq, n_kv);
+  if (head_dim == 128) hipLaunchKernelGGL(k_pages_move<128>, grid, dim3(128), 0, st, pg, rq, n_kv, res);
+  else if (head_dim == 64) hipLaunchKernelGGL(k_pages_move<64>, grid, dim3(64), 0, st, pg, rq, n_kv, res);
   else return GOOSE_ERR_SHAPE;
   int rc = goose_launch_status();
   if (rc != GOOSE_OK) return rc;
-  hipLaunchKernelGGL(k_pages_settle, dim3(rq.n), dim3(256), 0, st, pg, rq, flags);
+  hipLaunchKernelGGL(k_pages_settle, dim3(rq.n), dim3(256), 0, st, pg, rq, res, flags);
   return goose_launch_status();
 }
 

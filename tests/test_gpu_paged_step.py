@@ -238,3 +238,31 @@ def test_a_full_pool_stops_decoding_with_an_error():
             pd.generate(_prompts(shape.vocab, 2, 70), 400)
         assert e.value.status == GOOSE_ERR_CAPACITY
     gm.ctx.close()
+
+
+def test_a_step_without_room_is_left_undone_and_can_be_run_again():
+    """Six pages, three of them held by a third sequence, three by the prompt and the requests: the step finds no room for one request, commits nothing for either, and after the third has given
+    its pages back it does what it does in a pool with room."""
+    from paper_2604_02047_amd import binding as gb
+    shape = gi.SHAPES["tiny_gqa_bf16"]
+    tm = torch_model(shape, seed=7, gain_jitter=0.1)
+    gm = gpu_model(shape, tm, max_B=32, cap=512, max_rows=64)
+    rq = _requests(gm, 2, [12, 20], 13)
+    am = torch.zeros(64, dtype=torch.int32, device=DEV)
+    seen = []
+    for pages in (6, 16):
+        cache = gm.paged_cache(pages, 4, 256)
+        _fill(gm, cache, [50, 60], 40, 12)                 # one page each, the prompt's page beside them
+        if pages == 6:
+            gm.ctx.goose_pages_reserve(cache, [3], [3 * PAGE])
+            before = [x.clone() for x in (cache.table, cache.len, cache.refs)]
+            table = [dict(q, seq=r + 1, P_max=p) for r, (q, p) in enumerate(zip(rq, (50, 60)))]
+            gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, table, 0, am)
+            assert gm.ctx.goose_device_flags() & gb.GOOSE_FLAG_PAGES
+            assert all(torch.equal(a, b) for a, b in zip(before, (cache.table, cache.len, cache.refs)))
+            gm.ctx.goose_pages_free(cache, [3])
+        gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, table, 0, am)
+        assert gm.ctx.goose_device_flags() == 0
+        seen.append(([(int(q["accept_len"]), int(q["bonus"])) for q in rq], cache.len.tolist(), am[:12].clone(), am[32:52].clone()))
+    assert seen[0][:2] == seen[1][:2] and torch.equal(seen[0][2], seen[1][2]) and torch.equal(seen[0][3], seen[1][3])
+    gm.ctx.close()
