@@ -354,8 +354,8 @@ int goose_qk_norm_rope_paged(goose_ctx* ctx, const goose_pages* pages, int layer
                              void* d_q, size_t ldq, int q_terms, void* stream);
 /* Tree attention of n requests over pages of one layer (d_mask of each): a node sees slots [0, P) of its sequence and the slots P + j of the
  * nodes j of its mask row (bits at or beyond B count as clear), scores / sqrt(head_dim), softmax.  The first shared_pages entries of
- * all n tables must be the same pages, wholly committed (shared_pages * 64 <= every length): the keys in them are read once for
- * the rows of all requests.  shared_pages = 0 is always allowed, and the result does not depend on it beyond rounding.
+ * all n tables must be the same pages, wholly committed (shared_pages * 64 <= every length): where it is cheaper the keys in them are read
+ * once for the rows of all requests.  shared_pages = 0 is always allowed, and the result does not depend on it beyond rounding.
  * d_q as goose_qk_norm_rope_paged writes it; d_o: 16-bit [rows][ldo] of type o_dtype (GOOSE_DTYPE_BF16 or _F16) in o_terms terms.
  * Probabilities enter the second product in one term of fp16, or in two of bf16; sums and statistics are fp32.  A row that sees nothing but scores of
  * -infinity, or nothing, is zero; what slots behind a mask hold (NaN, infinities) has no effect; a NaN in what a row sees makes the row NaN,

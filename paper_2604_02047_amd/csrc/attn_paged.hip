@@ -1,10 +1,10 @@
-// Tree attention of up to 16 requests over a paged cache; the pages that all of them share are read once for the rows of all.
+// Tree attention of up to 16 requests over a paged cache; pages that all of them share can be read once for the rows of all.
 //
 //   o[row, h] = sum_k softmax_k(q[row, h] . K[k] / sqrt(d)) V[k],   k over the slots that the row sees.
 //
 // Softmax is associative over sets of keys: with (m, l, O) = (max, sum of 2^(s - m), sum of 2^(s - m) V) of a set, two sets join as
-// m = max(m1, m2), l = 2^(m1 - m) l1 + 2^(m2 - m) l2, O likewise.  So the shared keys and a request's own ones are
-// separate work items, and either kind is split along the keys as far as it takes to fill the card; k_paged_merge joins what
+// m = max(m1, m2), l = 2^(m1 - m) l1 + 2^(m2 - m) l2, O likewise.  So the shared keys and a request's own ones can be
+// separate work items (where that is cheaper: the rule is at launch_attn_paged), and either kind is split along the keys as far as it takes to fill the card; k_paged_merge joins what
 // the items of a row left, in a fixed order.
 //
 // The rows of one KV head -- (node, query head of the group), for the shared keys of all requests one behind the other -- are the columns of
@@ -549,8 +549,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
 //     vector pipe   weights P of block j, then the maximum of S
 // so that no step waits for another one's result, and a weight has two matrix instructions to hide behind (all of them beside S: half as many).
 // What bounds it is power: fp16, 2048 rows a KV head over 16384 slots, a step takes 1680 cycles (1024 of them the matrix pipe's; 1490 without the
-// copies and the raised maxima) at a clock that falls to 1.45 GHz, where the same products on constants run at 1.95.  770 TFLOP/s; with S and
-// P V of neighbouring blocks in one step, weights beside S alone and copies that made each LDS read wait for all: 690.
+// copies and the raised maxima) at a clock that falls to 1.45 GHz, where the same products on constants run at 1.95.  880 TFLOP/s; a tenth less with S
+// and P V of neighbouring blocks in one step, weights beside S alone and copies that made each LDS read wait for all.
 // Blocks that need a mask (the tree's, and what is left over) follow as in k_paged_stream, from what the ring has copied ahead or from memory.
 #define GOOSE_BUFFER_WORD3 0x00020000  // (buffer descriptor: raw 32-bit data)
 #define GOOSE_LDS_PTR(p) ((__attribute__((address_space(3))) void*)(p))
@@ -903,7 +903,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
   store_out(a, (size_t)a.r[r].row0 + crow - a.r[r].c0, h * D + c, num * inv);
 }
 
-// which kernel: TILES beyond 64 rows of an item, else STREAM with one or two row tiles
+// which kernel: k_paged_stream with one or two row tiles, or k_paged_tiles
 enum { STREAM1, STREAM2, TILES };
 template <int D, int QT, bool F16>
 void launch_t(int kind, dim3 grid, const PagedAttnArgs& a, hipStream_t st) {
@@ -953,18 +953,18 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   const size_t records = (size_t)n_heads * rq.rows;  // of one split
   // A way to split the work: do the shared keys have items of their own, which kernel, and how many steps (blocks, or pairs of them) an item takes
   // at most.  Items run in rounds of 256 workgroups, one a compute unit, the shared keys' items first; times in units of 10 ns at head_dim 128, from
-  // runs with 20 calls in a graph: an item's fixed part (start, first loads, epilogue; 5.5 us, with the ring 11) and its steps (0.21 us a
-  // block, 0.4 where two row tiles halve the key groups; with the ring 1.15 us with two products in all, 2.0 with four), the merge 4 us and its records;
-  // and no less than what the caches take to serve all items' blocks (8.5 TB/s).
+  // runs with 20 calls in a graph: an item's fixed part (start, first loads, epilogue; 5.5 us, with the ring 10.5) and its steps (fp16: 0.21 us a
+  // block, 0.43 where two row tiles halve the key groups, with the ring 1.02; more with more terms), the merge 6 us and its records;
+  // and no less than what the caches take to serve all items' blocks (10.5 TB/s).
   struct Way {
     int kind, per, sh_blocks, sh_kg, own_kg, sh_height, own_height;
     long long cost;
   };
-  auto cheapest = [&](bool share, Way& best) {  // updates best; false: no way fits the workspace
+  auto cheapest = [&](bool share, int kind, Way& best) {  // updates best
     Way w{};
+    w.kind = kind;
     w.sh_blocks = share ? a.same_blocks : 0;
-    const int sh_rows = share ? rq.rows * a.group : 0, most = sh_rows > own_rows ? sh_rows : own_rows;
-    w.kind = most > 64 ? TILES : (most > 32 ? STREAM2 : STREAM1);
+    const int sh_rows = share ? rq.rows * a.group : 0;
     // k_paged_tiles: 128 rows with two key groups where that leaves fewer rows of a tile empty
     auto key_groups = [](int rows) { return (rows + 127) / 128 * 128 < (rows + 255) / 256 * 256 ? 2 : 1; };
     w.sh_kg = key_groups(sh_rows);
@@ -975,70 +975,71 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
     const int sh_mul = ring ? w.sh_kg : 1, own_mul = ring ? w.own_kg : 1;  // blocks that a step takes
     const int sh_tiles = (sh_rows + w.sh_height - 1) / w.sh_height, sh_steps = (w.sh_blocks + sh_mul - 1) / sh_mul;
     int own_steps[GOOSE_MAX_REQUESTS], own_tiles[GOOSE_MAX_REQUESTS], own_longest = 0;
-    long long fetched = (long long)sh_tiles * w.sh_blocks;  // blocks, by all items of a KV head
+    long long fetched = (long long)sh_tiles * w.sh_blocks, all_steps = (long long)sh_tiles * sh_steps;  // of a KV head: blocks, steps
     for (int r = 0; r < rq.n; ++r) {
       own_steps[r] = ((rq.r[r].P_max + rq.r[r].B + 31) / 32 - w.sh_blocks + own_mul - 1) / own_mul;
       own_tiles[r] = (rq.r[r].B * a.group + w.own_height - 1) / w.own_height;
       own_longest = own_steps[r] > own_longest ? own_steps[r] : own_longest;
       fetched += (long long)own_tiles[r] * own_steps[r] * own_mul;
+      all_steps += (long long)own_tiles[r] * own_steps[r];
     }
-    const long long fetch = fetched * n_kv * head_dim * 128 / 85000;
-    const int least = ring ? 4 : 8, fixed = ring ? 1100 : 550,
-              step = (ring ? 30 + 42 * (q_terms + (dtype == GOOSE_DTYPE_F16 ? 1 : 2)) : (w.kind == STREAM2 ? 40 : 21)) * head_dim / 128;
+    const long long fetch = fetched * n_kv * head_dim * 128 / 105000;
+    const int least = ring ? 4 : 8, fixed = ring ? 1050 : 550,
+              products = q_terms + (dtype == GOOSE_DTYPE_F16 ? 1 : 2),
+              step = (ring ? 38 + 32 * products : (w.kind == STREAM2 ? 29 + 7 * products : 15 + 3 * products)) * head_dim / 128;
+    const long long work = fixed + all_steps * n_kv * step / 256;
+    if ((work > fetch ? work : fetch) >= best.cost) return;  // (no way of this kind is cheaper)
     const int longest = sh_steps > own_longest ? sh_steps : own_longest, most_steps = longest > least ? longest : least;
-    struct Plan { long long sh, own; int splits; };  // workgroups, records a row
-    auto plan_at = [&](int per) {
-      Plan p{0, 0, 0};
+    auto consider = [&](int per) {  // returns the workgroups that it makes
+      per = per < least ? least : (per > most_steps ? most_steps : per);
       const int sh = (sh_steps + per - 1) / per;
-      p.sh = (long long)sh_tiles * sh * n_kv;
+      int own = 0, splits = 0;
       for (int r = 0; r < rq.n; ++r) {
         const int n = (own_steps[r] + per - 1) / per;
-        p.own += (long long)own_tiles[r] * n * n_kv;
-        p.splits = n > p.splits ? n : p.splits;
+        own += own_tiles[r] * n;
+        splits = n > splits ? n : splits;
       }
-      p.splits += sh;
-      return p;
+      splits += sh;
+      const long long sh_items = (long long)sh_tiles * sh * n_kv, own_items = (long long)own * n_kv;
+      // (blocks times splits stays a 32-bit number in item_of)
+      if (splits <= 1 || ((size_t)splits * records <= max_records && 4ull * longest * (unsigned)splits <= UINT32_MAX)) {
+        const long long sh_len = (long long)(per < sh_steps ? per : sh_steps) * step + fixed,
+                        own_len = (long long)(per < own_longest ? per : own_longest) * step + fixed;
+        const long long rounds = (sh_items + 255) / 256, room = (rounds * 256 - sh_items) * (sh_len / own_len);  // own items beside the last shared ones
+        const long long left = own_items > room ? own_items - room : 0, time = rounds * sh_len + (left + 255) / 256 * own_len;
+        w.cost = (time > fetch ? time : fetch) + (splits > 1 ? 600 + (long long)(splits * records * head_dim * 150 / 1000000) : 0);
+        w.per = per;
+        if (w.cost < best.cost) best = w;
+      }
+      return sh_items + own_items;
     };
-    auto fits = [&](const Plan& p) {  // (blocks times splits stays a 32-bit number in item_of)
-      return p.splits <= 1 || ((size_t)p.splits * records <= max_records && 2ull * longest * 2 * (unsigned)p.splits <= UINT32_MAX);
-    };
-    bool any = false;
-    auto consider = [&](int per) {
-      if (per < least || per > most_steps) return;
-      const Plan p = plan_at(per);
-      if (!fits(p)) return;
-      any = true;
-      const long long sh_len = (long long)(per < sh_steps ? per : sh_steps) * step + fixed,
-                      own_len = (long long)(per < own_longest ? per : own_longest) * step + fixed;
-      const long long rounds = (p.sh + 255) / 256, room = (rounds * 256 - p.sh) * (sh_len / own_len);  // own items beside the last shared ones
-      const long long left = p.own > room ? p.own - room : 0;
-      const long long items = rounds * sh_len + (left + 255) / 256 * own_len;
-      w.cost = (items > fetch ? items : fetch) + (p.splits > 1 ? 400 + (long long)(p.splits * records * head_dim * 130 / 1000000) : 0);
-      w.per = per;
-      if (w.cost < best.cost) best = w;
-    };
-    // tried: no split, and the smallest `per` that makes one to four rounds of all items, or of the shared ones
+    // tried: no split, and about the smallest `per` that makes one to three rounds of all items, or of the shared ones
     consider(most_steps);
-    for (int rounds = 1; rounds <= 4; ++rounds) {
-      int lo = least, hi = most_steps;
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        const Plan p = plan_at(mid);
-        if (p.sh + p.own <= 256 * rounds && fits(p)) hi = mid; else lo = mid + 1;
+    for (int rounds = 1; rounds <= 3; ++rounds) {
+      long long per = (all_steps * n_kv + 256 * rounds - 1) / (256 * rounds);
+      for (int k = 0; k < 3 && per < most_steps; ++k) {
+        const long long made = consider((int)per);
+        if (made <= 256 * rounds) break;
+        per = (per < least ? least : per) * made / (256 * rounds) + 1;
       }
-      consider(lo);
       const int sh = sh_tiles > 0 ? 256 * rounds / (sh_tiles * n_kv) : 0;
       if (sh > 0) consider((sh_steps + sh - 1) / sh);
     }
-    return any;
   };
   // The shared keys get items of their own where rows of one request leave most of a tile empty, or where many keys meet few rows (16 requests x 1
   // over 8192 slots: 27 us, by request 54).  Where a request fills its tiles by itself the products are the same either way, the caches serve the
   // pages to all of them, and one set of items and fewer records win (16 x 32 over 4096 slots, bf16: 95 us, shared 118; over 64: 16 and 24).
+  // Which kernel: one row tile where there is no second one; the ring where rows fill it (7B, 2 requests x 100 over 4096: 37 us, two row tiles 46; 8 x 30
+  // of 4 heads over 64: 14 and 12); two row tiles or one between (16 x 16 of 4 heads over 4096 slots: 42 and 52 us, x 12 over 2048: 37 and 30).
   Way way{};
   way.cost = INT64_MAX;
-  const bool by_request = cheapest(false, way);
-  if (!(shared_pages > 0 && cheapest(true, way)) && !by_request) return GOOSE_ERR_CAPACITY;
+  for (int share = 0; share <= (shared_pages > 0 ? 1 : 0); ++share) {
+    const int most = share ? rq.rows * a.group : own_rows;
+    if (most > 64) cheapest(share, TILES, way);
+    if (most > 32) cheapest(share, STREAM2, way);
+    cheapest(share, STREAM1, way);
+  }
+  if (way.cost == INT64_MAX) return GOOSE_ERR_CAPACITY;
   const int kind = way.kind, sh_mul = kind == TILES ? way.sh_kg : 1, own_mul = kind == TILES ? way.own_kg : 1;
   a.sh_blocks = way.sh_blocks;
   a.sh_kg = way.sh_kg;

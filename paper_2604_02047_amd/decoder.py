@@ -9,8 +9,8 @@ the walks' results and the table rows the harvest touched.
 GooseDecoder decodes one request; BatchedGooseDecoder decodes several with one pass over the
 weights per cycle (the batch sweep of App. D), each request with its own KV cache, successor
 tables and adaptive state, and drops a request from the batch as soon as it has its tokens.
-PagedGooseDecoder does the same on one paged cache: what the prompts have in common is prefilled, stored and, in the
-attention, read once for all requests.
+PagedGooseDecoder does the same on one paged cache: what the prompts have in common is prefilled and stored once, and read
+once for all requests by the attention where that is cheaper.
 """
 import numpy as np
 import torch
