@@ -837,7 +837,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
 
 // Joins the items of a row: D / 4 threads a (row, head), four columns each, records in a fixed order, the loads of eight in flight together.
 // PARTS = 4: the records of a pair are dealt to four such groups of threads, which join through LDS (many splits mean few rows: one trip to memory
-// instead of four).  The KV head is the fast index as in the kernels above: the records are in that XCD's L2.
+// instead of four; 16 x 1 over 8192 slots in 17 splits: 8 us, now 6.3).  The KV head is the fast index as in the kernels above: the records are in that XCD's L2.
 template <int D, int PARTS>
 __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
   constexpr int TPR = D / 4, CH = 8, PAIRS = 256 / TPR / PARTS;
@@ -1027,10 +1027,10 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
     }
   };
   // The shared keys get items of their own where rows of one request leave most of a tile empty, or where many keys meet few rows (16 requests x 1
-  // over 8192 slots: 27 us, by request 54).  Where a request fills its tiles by itself the products are the same either way, the caches serve the
-  // pages to all of them, and one set of items and fewer records win (16 x 32 over 4096 slots, bf16: 95 us, shared 118; over 64: 16 and 24).
-  // Which kernel: one row tile where there is no second one; the ring where rows fill it (7B, 2 requests x 100 over 4096: 37 us, two row tiles 46; 8 x 30
-  // of 4 heads over 64: 14 and 12); two row tiles or one between (16 x 16 of 4 heads over 4096 slots: 42 and 52 us, x 12 over 2048: 37 and 30).
+  // over 8192 slots: 24 us, by request 51).  Where a request fills its tiles by itself the products are the same either way, the caches serve the
+  // pages to all of them, and one set of items and fewer records win (16 x 32 over 4096 slots, bf16: 86 us, shared 102; over 64: 15 and 24).
+  // Which kernel: the ring where rows fill it and keys are many (7B, 2 requests x 100 over 4096: 38 us, two row tiles 46; 8 x 30 of 4 heads over 64: 14
+  // and 12); two row tiles where the caches bound one (16 x 16 of 4 heads over 4096 slots: 42 and 52 us), one where two leave units idle (x 12 over 2048: 37 and 30).
   Way way{};
   way.cost = INT64_MAX;
   for (int share = 0; share <= (shared_pages > 0 ? 1 : 0); ++share) {

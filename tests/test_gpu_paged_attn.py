@@ -58,16 +58,21 @@ class Case:
         both = torch.stack((hi.view(self.rows, n // 8, 8), lo.view(self.rows, n // 8, 8)), 2)
         return both.reshape(self.rows, 2 * n), hi.double() + lo.double()
 
-    def run(self, S=None, flags=0):
+    def run(self, S=None, flags=0, bound=None):
+        """bound: P_max of all requests instead of their lengths (launches go by it; the tables are widened to hold it)."""
         S = self.S if S is None else S
+        table = self.table
+        if bound is not None:
+            table = np.full((len(self.Bs), (bound + max(self.Bs)) // PAGE + 1), -1, np.int32)
+            table[:, :self.width] = self.table
         q, self.q64 = self.q_rows()
         desc = goose.ModelDesc(self.layers, 128, self.nh, self.d, 128, 1024, dtype=self.dtype, n_kv_heads=self.nkv)
         ctx = goose.GooseContext(desc, max(self.Bs), 256, 512)
         kp, vp = pack_pages(self.k, self.v)
-        self.cache = goose.PagedCache(kp.to(DEV), vp.to(DEV), torch.from_numpy(self.table).to(DEV),
+        self.cache = goose.PagedCache(kp.to(DEV), vp.to(DEV), torch.from_numpy(table).to(DEV),
                                       torch.tensor(self.Ps, dtype=torch.int32, device=DEV), torch.from_numpy(self.refs).to(DEV))
         o = torch.full((self.rows, self.nh * self.d * self.o_terms + 8), 77.0, dtype=self.o_dtype, device=DEV)
-        reqs = [{"seq": r, "B": b, "P_max": p, "mask": self.masks[r][0].to(DEV)} for r, (b, p) in enumerate(zip(self.Bs, self.Ps))]
+        reqs = [{"seq": r, "B": b, "P_max": bound or p, "mask": self.masks[r][0].to(DEV)} for r, (b, p) in enumerate(zip(self.Bs, self.Ps))]
         ctx.goose_attn_paged(self.cache, self.layer, q.to(DEV), self.terms, reqs, S // PAGE, o, self.o_terms)
         assert ctx.goose_device_flags() == flags
         ctx.close()
@@ -382,3 +387,55 @@ def test_two_graphs_of_one_context():
             assert torch.equal(o, first[i]), (turn, i)
     assert ctx.goose_device_flags() == 0
     ctx.close()
+
+
+# Sixteen requests that may have 16384 slots are many rows over many keys, so that the ring takes them; their real lengths give its items (two of a
+# request, each half the keys) from no block to some thirty.
+RING = dict(Bs=[32] * 16, Ps=[0, 31, 32, 33, 64, 95, 130, 200, 300, 420, 555, 700, 901, 1111, 1500, 2050])
+
+
+@pytest.mark.parametrize("dtype,terms", [("bf16", 1), ("bf16", 2), ("f16", 1), ("f16", 2)])
+@pytest.mark.parametrize("nh", [32, 64])
+def test_the_ring_over_every_number_of_blocks(dtype, terms, nh):
+    """128 rows a KV head (two key groups) and 256 (one)."""
+    for d in (128, 64):
+        c = Case(nh, 8, d, dtype, S=0, seed=90 + nh, terms=terms, **RING)
+        c.check(c.run(bound=16384), nodes=3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("nh", [32, 64])
+def test_the_ring_with_maxima_that_grow_and_keys_of_minus_infinity(dtype, nh):
+    """As test_maxima_that_grow_in_every_block; the odd requests' first 200 keys score -infinity."""
+    c = Case(nh, 8, 64, dtype, S=0, seed=95, **RING)
+    way = torch.randn(64, generator=torch.Generator().manual_seed(96))
+    way[5] = 0
+    turn = torch.linspace(-3.0, 3.0, c.rows * nh).view(c.rows, nh, 1)
+    c.q32 = turn * way / way.norm() ** 2 * 8 + 0.05 * c.q32
+    c.q32[..., 5] = 0.25
+    for r, P in enumerate(c.Ps):
+        for s in range(P + 32):
+            at = (0, c.table[r, s // 64], slice(None), s % 64)
+            c.k[at] = (0.05 * c.k[at].float() + way * (s % 450 / 11.0)).to(c.dt)
+            c.k[at][:, 5] = -float("inf") if r % 2 and s < min(P, 200) else 0.0
+    o, N, at = c.run(bound=16384), nh * 64, 0
+    for r, P in enumerate(c.Ps):
+        skip = min(P, 200) if r % 2 else 0   # (keys without weight: the 64-bit form goes without them)
+        k, v = (rows_of(x[0], c.table[r], P + 32).double()[:, skip:] for x in (c.k, c.v))
+        pick = [0, 1, 17, 31]
+        see = np.concatenate([np.ones((32, P - skip), bool), c.masks[r][1]], 1)[pick]
+        want, A, qk, vs = attention64(c.q64[at:at + 32][pick], k, v, torch.from_numpy(see))
+        tol = A * (U_P[c.dt] + 2 * 68 * 2.0 ** -24 * qk.unsqueeze(-1) + 2.0 ** -20 + 2 * (P + 32) * 2.0 ** -24) + want.abs() * 2.0 ** -11 + 2.0 ** -25
+        if dtype == "f16":
+            tol = tol + vs * 2.0 ** -25
+        got = o[at:at + 32][pick].double().view(4, nh, 64)
+        assert ((got - want).abs() <= tol * 1.001).all(), (r, float(((got - want).abs() / tol).max()))
+        at += 32
+
+
+@pytest.mark.parametrize("nh,nkv,B,S,dtype,terms", [(32, 32, 16, 8192, "f16", 1), (32, 32, 16, 8192, "bf16", 2), (16, 2, 1, 4096, "bf16", 2),
+                                                    (16, 2, 4, 4096, "f16", 1), (8, 8, 3, 4096, "bf16", 1)])
+def test_long_shared_prefixes_by_items_of_their_own(nh, nkv, B, S, dtype, terms):
+    """Few rows of a request over many shared keys, where the shared keys are worked on once for all sixteen: 256 rows of them, 128, 64 and 48."""
+    c = Case(nh, nkv, 64, dtype, [B] * 16, [S + 5 * i + (i == 3) * 200 for i in range(16)], S, seed=100 + B, terms=terms)
+    c.check(c.run(), nodes=1 if nh == 32 else 2)
