@@ -444,6 +444,7 @@ class GooseContext:
             _check(self.lib.goose_create(C.byref(cd), max_B, cap, C.byref(h)), "goose_create")
         self._h = h
         import torch
+        self._device = torch.cuda.current_device()
         self._cache_shape = ({"bf16": torch.bfloat16, "f16": torch.float16}.get(desc.dtype), desc.n_layers, desc.kv_heads,
                              GOOSE_PAGE * desc.head_dim)  # of a paged cache: its type, layers, KV heads, elements of a head's page
 
@@ -533,8 +534,8 @@ class GooseContext:
         """Descriptor, requests and stream of a paged call, after a look at what the C side cannot see: element types, head layout, devices."""
         import torch
         dev = cache._device
-        if dev >= 0 and dev != torch.cuda.current_device():
-            raise GooseError(GOOSE_ERR_ARG, "the paged cache is not on the current device")
+        if dev != self._device or dev != torch.cuda.current_device():  # (-1: in host memory)
+            raise GooseError(GOOSE_ERR_ARG, "the paged cache is not on the context's device, or that is not the current one")
         if cache._shape != self._cache_shape and self.desc.dtype != "f32":
             raise GooseError(GOOSE_ERR_ARG, "the paged cache is not one of this model")
         r = None
@@ -545,7 +546,7 @@ class GooseContext:
         for t in tensors:
             if t is not None and t.get_device() != dev:
                 raise GooseError(GOOSE_ERR_ARG, "a tensor of the call is on another device than the paged cache")
-        return r, _raw_stream(dev) if dev >= 0 else None
+        return r, _raw_stream(dev)
 
     def goose_pages_clear(self, cache):
         _, st = self._paged(cache, None)

@@ -45,6 +45,23 @@ def test_requests_check_their_tensors():
         assert e.value.status == gb.GOOSE_ERR_ARG, b
 
 
+def test_a_cache_in_host_memory_or_on_another_device_is_refused(monkeypatch):
+    """Before the library is called: the context here has none."""
+    ctx = object.__new__(goose.GooseContext)
+    ctx._device = 0
+    ctx.desc = goose.ModelDesc(2, 192, 3, 64, 128, 1024)
+    ctx._cache_shape = (torch.bfloat16, 2, 3, 64 * 64)
+    cache = goose.PagedCache(**tensors())
+    for device, current in ((-1, 0), (1, 0), (1, 1), (0, 1)):
+        cache._device = device
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+        for call in (lambda: ctx.goose_pages_clear(cache), lambda: ctx.goose_pages_free(cache, [0]), lambda: ctx.goose_pages_fork(cache, 0, [1]),
+                     lambda: ctx.goose_pages_reserve(cache, [0], [1]), lambda: ctx.goose_pages_commit(cache, [{"seq": 0, "B": 1}])):
+            with pytest.raises(goose.GooseError) as e:
+                call()
+            assert e.value.status == gb.GOOSE_ERR_ARG
+
+
 def test_entry_points_refuse_a_missing_context():
     lib = goose.load_library()
     import ctypes as C
