@@ -439,3 +439,41 @@ def test_long_shared_prefixes_by_items_of_their_own(nh, nkv, B, S, dtype, terms)
     """Few rows of a request over many shared keys, where the shared keys are worked on once for all sixteen: 256 rows of them, 128, 64 and 48."""
     c = Case(nh, nkv, 64, dtype, [B] * 16, [S + 5 * i + (i == 3) * 200 for i in range(16)], S, seed=100 + B, terms=terms)
     c.check(c.run(), nodes=1 if nh == 32 else 2)
+
+
+@pytest.mark.parametrize("junk", [float("nan"), float("inf")])
+@pytest.mark.parametrize("nh,d,dtype", [(32, 128, "bf16"), (32, 64, "f16"), (64, 128, "f16"), (64, 64, "bf16")])
+def test_the_ring_and_what_lies_behind_a_mask(junk, nh, d, dtype):
+    """As test_what_lies_behind_a_mask_has_no_effect: stale slots, a node that only itself sees, mask bits beyond the tree."""
+    c = Case(nh, 8, d, dtype, S=0, seed=97, **RING)
+    for r, P in enumerate(c.Ps):
+        for s in range(P + 32, (P + 32 + 63) // 64 * 64):
+            c.k[0, c.table[r, s // 64], :, s % 64] = junk
+            c.v[0, c.table[r, s // 64], :, s % 64] = junk
+        see = c.masks[r][1]
+        see[2:, 1] = False
+        words = np.full((32, 1), 0xFFFFFFFF00000000, np.uint64)
+        for i in range(32):
+            for j in np.nonzero(see[i])[0]:
+                words[i, 0] |= np.uint64(1) << np.uint64(j)
+        c.masks[r] = (torch.from_numpy(words.view(np.int64)), see)
+        s = P + 1
+        c.v[0, c.table[r, s // 64], :, s % 64, ::3] = junk
+        c.k[0, c.table[r, s // 64], :, s % 64, 5] = junk
+    o = c.run(bound=16384)
+    pick = [0, 2, 9, 31]
+    for r, P in enumerate(c.Ps):
+        k, v = (rows_of(x[0], c.table[r], P + 32).double() for x in (c.k, c.v))
+        see = np.concatenate([np.ones((32, P), bool), c.masks[r][1]], 1)[pick]
+        want, A, qk, vs = attention64(c.q64[r * 32:r * 32 + 32][pick], k, v, torch.from_numpy(see))
+        got = o[r * 32:r * 32 + 32].double().view(32, nh, d)[pick]
+        tol = A * (U_P[c.dt] + 2 * (d + 4) * 2.0 ** -24 * qk.unsqueeze(-1) + 2.0 ** -20 + (P + 32) * 2.0 ** -23) + want.abs() * 2.0 ** -11 + 2.0 ** -25 + vs * 2.0 ** -25
+        assert ((got - want).abs() <= tol).all(), (r, P)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_the_ring_with_the_largest_trees(dtype):
+    """Trees of 128 nodes reach over five blocks, with an odd whole one in front six: more than the ring has copied ahead."""
+    for nh, d in ((32, 128), (64, 64)):
+        c = Case(nh, 32, d, dtype, [128] * 4, [45, 100, 333, 610], 0, seed=110 + nh)
+        c.check(c.run(bound=16384), nodes=5)
