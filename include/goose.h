@@ -357,7 +357,7 @@ int goose_qk_norm_rope_paged(goose_ctx* ctx, const goose_pages* pages, int layer
  * all n tables must be the same pages, wholly committed (shared_pages * 64 <= every length): where it is cheaper the keys in them are read
  * once for the rows of all requests.  shared_pages = 0 is always allowed, and the result does not depend on it beyond rounding.
  * d_q as goose_qk_norm_rope_paged writes it; d_o: 16-bit [rows][ldo] of type o_dtype (GOOSE_DTYPE_BF16 or _F16) in o_terms terms.
- * Probabilities enter the second product in one term of fp16, or in two of bf16; sums and statistics are fp32.  A row that sees nothing but scores of
+ * Probabilities enter the second product in two terms of the cache's type; sums and statistics are fp32.  A row that sees nothing but scores of
  * -infinity, or nothing, is zero; what slots behind a mask hold (NaN, infinities) has no effect; a NaN in what a row sees makes the row NaN,
  * and so does a score of +infinity.  ldq and ldo multiples of 8, d_q and d_o 16-byte aligned.  Sum of round_up(B, 32) <= max_rows. */
 int goose_attn_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,

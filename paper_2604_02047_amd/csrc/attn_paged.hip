@@ -11,9 +11,11 @@
 // 32-wide matrix-instruction tiles: a single token of a grouped-query model fills 4 of 32 columns with its four heads,
 // and sixteen of them share two tiles over the common prefix.  Per 32 keys and 32 rows, as in the contiguous attention:
 // S^T = K Q^T, online softmax with two lanes a row, O^T += V^T P^T, operands straight from the pages' operand order.
-// Under bf16 the probabilities keep two terms for the second product (hi + lo, 2^-17): the output goes on as fp16 or in two terms, and
-// one term of 8 bits would be its largest error by far (16 requests x 1 over 8192 slots: 0.00085 of the output's size, now 0.00021 as
-// the output's own rounding).  fp16 ones have 11 bits and one term.
+// The probabilities keep two terms for the second product (hi + lo: 2^-17 under bf16, 2^-22 under fp16), as the plain form keeps them in
+// 32 bits.  The output goes on as fp16 or in two terms: one bf16 term of 8 bits would be its largest error by far (16 requests x 1 over 8192
+// slots: 0.00085 of the output's size, with two 0.00021 as the output's own rounding), one fp16 term of 11 bits an error as large as the output's own
+// rounding (16 x 32 over 16384: 0.00029, with two 0.00021; more for a row that one key with a weight above one dominates, see raise()).  The second fp16
+// term costs half the matrix instructions again: 161 us before, now 210; 7B, 5 ragged requests over 1984 slots 25, now 28.
 #include "mma16.h"
 #include "paged.h"
 
@@ -188,14 +190,14 @@ struct PageIds {
 // ---- 32 rows of the softmax ---------------------------------------------------------------------------------------------
 template <int D, int QT, bool F16>
 struct RowTile {
-  static constexpr int NS = D / 16, NDT = D / 32, PT = F16 ? 1 : 2;
+  static constexpr int NS = D / 16, NDT = D / 32;
   static constexpr float SLACK = 8.f;
   typedef typename Mma16<F16>::T T;
   typedef typename Mma16<F16>::v8 op8;
   op8 q[NS], ql[QT == 2 ? NS : 1];
   f32x16 o[NDT];
   f32x16 s;  // scores of the block at hand
-  op8 p[2], pl[PT];
+  op8 p[2], pl[2];  // weights of the block at hand: leading and second terms
   float m, l, top;   // largest score so far, sum of weights, this block's largest score of this lane
   float lim, ref, mul;  // see raise()
   float late;           // see rescale_later()
@@ -210,7 +212,7 @@ struct RowTile {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         p[j][e] = (T)0.f;
-        pl[j % PT][e] = (T)0.f;
+        pl[j][e] = (T)0.f;
       }
     m = lim = -INFINITY;
     l = ref = 0.f;
@@ -257,7 +259,8 @@ struct RowTile {
   __device__ __forceinline__ float reference(float c) const { return finite_ref(m) * c; }
   __device__ __forceinline__ bool grown() const { return __builtin_amdgcn_ballot_w64(top > lim) != 0; }
   // m, and with it l and O, follows only where a row's largest score has grown so far that weights would pass 2^SLACK: weights up to there are as
-  // good as those up to one in floating point (16 bits hold them with room to spare), and with 32 rows in a tile some row's maximum grows by a
+  // good as those up to one (in two terms, of which 16 bits hold both with room to spare: a weight other than one is rounded for the second product and not in
+  // l, so with one term a row that a single key dominates would be off by that term's rounding), and with 32 rows in a tile some row's maximum grows by a
   // little in most blocks (512 rows over 16384 slots: in 3 of 4).
   // A weight is 2^(s c - ref) in one fused multiply-add, ref = m c rounded; its rounding is the same factor in O and l.  Where products
   // leave no room for it (2^24 and beyond, infinities), the block's scores (x) become differences to m first.
@@ -300,8 +303,8 @@ struct RowTile {
       if (grows) late = raise(c, x);
     }
   }
-  // x, y in 16 bits, as weights of keys 2 i, 2 i + 1
-  static __device__ __forceinline__ void pair_to(int i, float x, float y, op8 (&w)[2], op8 (&wl)[PT]) {
+  // x, y in two 16-bit terms, as weights of keys 2 i, 2 i + 1
+  static __device__ __forceinline__ void pair_to(int i, float x, float y, op8 (&w)[2], op8 (&wl)[2]) {
     typedef T T2 __attribute__((ext_vector_type(2)));
     typedef float F2 __attribute__((ext_vector_type(2)));
     unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector((F2{x, y}), T2));
@@ -309,17 +312,21 @@ struct RowTile {
     u32x4 v = __builtin_bit_cast(u32x4, w[i >> 2]);
     v[i & 3] = h;
     w[i >> 2] = __builtin_bit_cast(op8, v);
-    if (PT == 2) {
-      const F2 rest = {x - __builtin_bit_cast(float, h << 16), y - __builtin_bit_cast(float, h & 0xFFFF0000u)};
-      v = __builtin_bit_cast(u32x4, wl[(i >> 2) % PT]);
-      unsigned low = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, T2));
-      GOOSE_HERE(low);
-      v[i & 3] = low;
-      wl[(i >> 2) % PT] = __builtin_bit_cast(op8, v);
+    F2 rest;
+    if constexpr (F16) {
+      const T2 t = __builtin_bit_cast(T2, h);
+      rest = F2{x - (float)t[0], y - (float)t[1]};
+    } else {
+      rest = F2{x - __builtin_bit_cast(float, h << 16), y - __builtin_bit_cast(float, h & 0xFFFF0000u)};
     }
+    v = __builtin_bit_cast(u32x4, wl[i >> 2]);
+    unsigned low = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, T2));
+    GOOSE_HERE(low);
+    v[i & 3] = low;
+    wl[i >> 2] = __builtin_bit_cast(op8, v);
   }
   // weights of keys 2 i, 2 i + 1 of the scores in z (a masked score is -infinity: zero)
-  __device__ __forceinline__ void weights_of(int i, const f32x16& z, op8 (&w)[2], op8 (&wl)[PT]) {
+  __device__ __forceinline__ void weights_of(int i, const f32x16& z, op8 (&w)[2], op8 (&wl)[2]) {
     const float x = __builtin_amdgcn_exp2f(fmaf(z[2 * i], mul, -ref)), y = __builtin_amdgcn_exp2f(fmaf(z[2 * i + 1], mul, -ref));
     l += x;
     l += y;
@@ -334,12 +341,10 @@ struct RowTile {
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), p[j], o[dt]);
-    if (PT == 2) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), pl[j % PT], o[dt]);
-    }
+      for (int dt = 0; dt < NDT; ++dt) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), pl[j], o[dt]);
   }
   // The second product of a block with a NaN or an infinity in a value that some rows do not see (through the matrix instruction it
   // would reach them as 0 * NaN): those elements count as zero there, and a product of indicators (is it +inf, -inf, NaN) x (is it visible) tells
@@ -548,9 +553,9 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
 //     matrix pipe   S = K Q of block j + 1, then O += V P of block j - 1
 //     vector pipe   weights P of block j, then the maximum of S
 // so that no step waits for another one's result, and a weight has two matrix instructions to hide behind (all of them beside S: half as many).
-// What bounds it is power: fp16, 2048 rows a KV head over 16384 slots, a step takes 1680 cycles (1024 of them the matrix pipe's; 1490 without the
-// copies and the raised maxima) at a clock that falls to 1.45 GHz, where the same products on constants run at 1.95.  880 TFLOP/s; a tenth less with S
-// and P V of neighbouring blocks in one step, weights beside S alone and copies that made each LDS read wait for all.
+// 16 requests x 32 of 4 heads over 16384 slots, fp16, one query term: 210 us (1536 cycles of the matrix pipe a step).
+// Measured on the form with one term of weights (1024 cycles): a step took 1680 cycles, 1490 without the copies and the raised maxima, at a clock that fell to
+// 1.45 GHz under this load; a tenth more with S and P V of neighbouring blocks in one step, weights beside S alone and copies that made each LDS read wait for all.
 // Blocks that need a mask (the tree's, and what is left over) follow as in k_paged_stream, from what the ring has copied ahead or from memory.
 #define GOOSE_BUFFER_WORD3 0x00020000  // (buffer descriptor: raw 32-bit data)
 #define GOOSE_LDS_PTR(p) ((__attribute__((address_space(3))) void*)(p))
@@ -574,12 +579,12 @@ __device__ __forceinline__ void copy_pieces(const char* src, int lane, unsigned 
 template <int D, int QT, bool F16, int G, int AHEAD>
 __device__ __forceinline__ void ring_step(RowTile<D, QT, F16>& t, u32x4 (&pc)[AHEAD], const u32x4* __restrict__ k1, const u32x4* __restrict__ v0,
                                           const u32x4* __restrict__ k2, const f32x16& z0, f32x16& z1,
-                                          const typename RowTile<D, QT, F16>::op8 (&w)[2], const typename RowTile<D, QT, F16>::op8 (&wl)[RowTile<D, QT, F16>::PT],
-                                          typename RowTile<D, QT, F16>::op8 (&w0)[2], typename RowTile<D, QT, F16>::op8 (&wl0)[RowTile<D, QT, F16>::PT],
+                                          const typename RowTile<D, QT, F16>::op8 (&w)[2], const typename RowTile<D, QT, F16>::op8 (&wl)[2],
+                                          typename RowTile<D, QT, F16>::op8 (&w0)[2], typename RowTile<D, QT, F16>::op8 (&wl0)[2],
                                           bool more, float scale) {
   typedef RowTile<D, QT, F16> Tile;
   typedef typename Tile::op8 op8;
-  constexpr int NS = Tile::NS, NDT = Tile::NDT, PT = Tile::PT, ALL = NS * (QT + PT), SPREAD = ALL * 3 / 4;
+  constexpr int NS = Tile::NS, NDT = Tile::NDT, ALL = NS * (QT + 2), SPREAD = ALL * 3 / 4;
   u32x4 piece[2 * NS + AHEAD];
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n) piece[n] = G == 1 ? pc[n] : k1[n * 64];
@@ -603,10 +608,10 @@ __device__ __forceinline__ void ring_step(RowTile<D, QT, F16>& t, u32x4 (&pc)[AH
     } else {
       const int x = n - NS, j = x / NDT, dt = x % NDT;
       t.o[dt] = Mma16<F16>::mfma(a, w[j], t.o[dt]);
-      if (PT == 2) t.o[dt] = Mma16<F16>::mfma(a, wl[j % PT], t.o[dt]);
+      t.o[dt] = Mma16<F16>::mfma(a, wl[j], t.o[dt]);
       GOOSE_HERE(t.o[dt]);
     }
-    const int before = n < NS ? n * QT : NS * QT + (n - NS) * PT, behind = before + (n < NS ? QT : PT);  // matrix instructions so far
+    const int before = n < NS ? n * QT : NS * QT + (n - NS) * 2, behind = before + (n < NS ? QT : 2);  // matrix instructions so far
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i >= 8 * before / SPREAD && i < 8 * behind / SPREAD) t.weights_of(i, z0, w0, wl0);
@@ -695,7 +700,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
     barrier();
     u32x4 pc[AHEAD];
     f32x16 z1;
-    typename Tile::op8 w1[2], wl1[Tile::PT];
+    typename Tile::op8 w1[2], wl1[2];
     if (work) {
       u32x4 k[NS];
 #pragma unroll
@@ -734,7 +739,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         t.p[i] = w1[i];
-        t.pl[i % Tile::PT] = wl1[i % Tile::PT];
+        t.pl[i] = wl1[i];
       }
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (the last values, and copies behind the range)
@@ -956,8 +961,8 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   const size_t records = (size_t)n_heads * rq.rows;  // of one split
   // A way to split the work: do the shared keys have items of their own, which kernel, and how many steps (blocks, or pairs of them) an item takes
   // at most.  Items run in rounds of 256 workgroups, one a compute unit, the shared keys' items first; times in units of 10 ns at head_dim 128, from
-  // runs with 20 calls in a graph: an item's fixed part (start, first loads, epilogue; 5.5 us, with the ring 10.5) and its steps (fp16: 0.21 us a
-  // block, 0.43 where two row tiles halve the key groups, with the ring 1.02; more with more terms), the merge 6 us and its records;
+  // runs with 20 calls in a graph: an item's fixed part (start, first loads, epilogue; 5.5 us, with the ring 10.5) and its steps (one query term: 0.24 us a
+  // block, 0.50 where two row tiles halve the key groups, with the ring 1.34; more with two), the merge 6 us and its records;
   // and no less than what the caches take to serve all items' blocks (10.5 TB/s).
   struct Way {
     int kind, per, sh_blocks, sh_kg, own_kg, sh_height, own_height;
@@ -988,7 +993,7 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
     }
     const long long fetch = fetched * n_kv * head_dim * 128 / 105000;
     const int least = ring ? 4 : 8, fixed = ring ? 1050 : 550,
-              products = q_terms + (dtype == GOOSE_DTYPE_F16 ? 1 : 2),
+              products = q_terms + 2,
               step = (ring ? 38 + 32 * products : (w.kind == STREAM2 ? 29 + 7 * products : 15 + 3 * products)) * head_dim / 128;
     const long long work = fixed + all_steps * n_kv * step / 256;
     if ((work > fetch ? work : fetch) >= best.cost) return;  // (no way of this kind is cheaper)

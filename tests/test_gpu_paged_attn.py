@@ -477,3 +477,34 @@ def test_the_ring_with_the_largest_trees(dtype):
     for nh, d in ((32, 128), (64, 64)):
         c = Case(nh, 32, d, dtype, [128] * 4, [45, 100, 333, 610], 0, seed=110 + nh)
         c.check(c.run(bound=16384), nodes=5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("nh,nkv,Bs,bound", [(8, 4, [7], None), (16, 4, [12, 9], None), (32, 8, [32] * 16, 16384), (64, 8, [32] * 16, 16384)])
+def test_a_weight_above_one_keeps_its_bits(dtype, nh, nkv, Bs, bound):
+    """All scores are zero but one key's, t < 8 ln 2 in a later block than a wavefront's first: its weight e^t is not one, as the reference stays at the
+    first maximum.  All other values are zero, so the output is p v of that key and what is lost of the weight is lost of it.  One product makes a score,
+    so it errs by its scale's and the reference's rounding only (4 steps of 2^-24 t); p in two terms (fp16 2^-21, bf16 2^-16); sums, exponential, store as above."""
+    d, P = 64, 560
+    c = Case(nh, nkv, d, dtype, Bs, [P] * len(Bs), 0, seed=120, o_dtype=torch.float16, o_terms=2)
+    c.k.zero_()
+    c.v.mul_(0)
+    values = torch.randn((nkv, d), generator=torch.Generator().manual_seed(121)).to(c.dt)
+    c.q32 = torch.linspace(0.5, 5.4, c.rows * nh).view(c.rows, nh, 1) * torch.eye(d)[5]
+    for r in range(len(Bs)):
+        for h in range(nkv):
+            s = 40 + 32 * h
+            c.k[0, c.table[r, s // 64], h, s % 64, 5] = 8.0
+            c.v[0, c.table[r, s // 64], h, s % 64] = values[h]
+    o, at = c.run(bound=bound).double(), 0
+    o = o.view(c.rows, nh * d // 8, 2, 8).sum(2).view(c.rows, nh, d)
+    u = 2.0 ** -21 if dtype == "f16" else 2.0 ** -16
+    v = values.double().repeat_interleave(nh // nkv, 0)
+    for B, (_, see) in zip(Bs, c.masks):
+        t = c.q64[at:at + B, :, 5:6]                                             # (the key's 8 over sqrt(64))
+        N = torch.from_numpy(P + see.sum(1)).view(B, 1, 1)
+        want = torch.exp(t) / (N - 1 + torch.exp(t)) * v
+        tol = want.abs() * (u + 8 * 2.0 ** -24 * t + 2.0 ** -20 + 2 * N * 2.0 ** -24 + 2.0 ** -22) + 2.0 ** -24 + v.abs() * 2.0 ** -25
+        off = (o[at:at + B] - want).abs() / tol
+        assert off.max() <= 1, (float(off.max()), off.argmax())
+        at += (B + 31) // 32 * 32
