@@ -363,8 +363,9 @@ int goose_qk_norm_rope_paged(goose_ctx* ctx, const goose_pages* pages, int layer
 int goose_attn_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,
                      const goose_paged_request* reqs, int n, int shared_pages, void* d_o, size_t ldo, int o_dtype, int o_terms,
                      void* stream);
-/* goose_verify_layer on pages, for the stacked rows of n requests (d_mask, d_pos, P_max of each; d_x fp32 [rows][hidden], rows between
- * requests finite).  Their slots must be reserved. */
+/* goose_verify_layer on pages, for the stacked rows of n requests (d_mask, d_pos, P_max of each).  d_x: fp32 [rows][hidden], rows = the sum of
+ * round_up(B, 32) of the requests before the last one plus its B; rows between requests must be finite, and hold other finite values afterwards.
+ * The requests' slots must be reserved. */
 int goose_verify_layer_paged(goose_ctx* ctx, const void* d_packed_layer, const goose_pages* pages, int layer, float* d_x,
                              const goose_paged_request* reqs, int n, int shared_pages, void* stream);
 /* goose_verify_step_batched on pages: reserves B slots for every request, runs the pass, walks, commits.  Reads d_tokens, d_parent, d_is_spine, P_max

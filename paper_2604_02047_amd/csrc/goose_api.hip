@@ -951,8 +951,7 @@ int goose_verify_layer_paged(goose_ctx* c, const void* d_packed_layer, const goo
   if (!rc) rc = paged_reqs(c, pg, reqs, n, true, &pass.mask, [](const goose_paged_request& q) -> const void* { return q.d_mask; });
   if (!rc) rc = check_shared(pg, pass.mask, shared_pages);
   if (rc) return rc;
-  int rows = pass.pos.r[n - 1].row0 + reqs[n - 1].B;
-  if (n > 1) rows = round_up(rows, 32);
+  const int rows = pass.pos.r[n - 1].row0 + reqs[n - 1].B;  // (d_x ends with the last request's last node)
   return layer_impl(c, (const char*)d_packed_layer, d_x, nullptr, nullptr, 0, nullptr, rows, nullptr, as_stream(stream), false, nullptr, nullptr,
                     nullptr, 0, &pass);
 }

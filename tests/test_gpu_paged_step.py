@@ -266,3 +266,34 @@ def test_a_step_without_room_is_left_undone_and_can_be_run_again():
         seen.append(([(int(q["accept_len"]), int(q["bonus"])) for q in rq], cache.len.tolist(), am[:12].clone(), am[32:52].clone()))
     assert seen[0][:2] == seen[1][:2] and torch.equal(seen[0][2], seen[1][2]) and torch.equal(seen[0][3], seen[1][3])
     gm.ctx.close()
+
+
+def _layer_requests(Bs, Ps, seed=0):
+    from paged_ref import mask_words
+    rng = np.random.default_rng(seed)
+    reqs = []
+    for r, (b, p) in enumerate(zip(Bs, Ps)):
+        words, see = mask_words([-1] + [int(rng.integers(0, i)) for i in range(1, b)])
+        reqs.append({"seq": r + 1, "B": b, "P_max": p, "mask": words.to(DEV), "pos": torch.tensor(p + see.sum(1) - 1, dtype=torch.int32, device=DEV)})
+    return reqs
+
+
+@pytest.mark.parametrize("Bs", [[5], [5, 5], [20, 40], [64, 64, 33], [33, 1]])
+def test_a_layer_writes_no_row_behind_the_last_request(Bs):
+    """x of exactly the rows that the call asks for, at the front of a larger allocation whose rest must stay."""
+    shape = gi.SHAPES["small_bf16"]
+    gm = gpu_model(shape, torch_model(shape, seed=5), max_B=64, cap=512, max_rows=256)
+    cache = gm.paged_cache(24, len(Bs) + 1, 320)
+    Ps = [130 + 9 * r for r in range(len(Bs))]
+    _fill(gm, cache, Ps, 128, 4)
+    gm.ctx.goose_pages_reserve(cache, list(range(1, len(Bs) + 1)), Bs)
+    reqs = _layer_requests(Bs, Ps)
+    rows = sum((b + 31) // 32 * 32 for b in Bs[:-1]) + Bs[-1]
+    x0 = torch.randn((256, shape.hidden), generator=torch.Generator().manual_seed(1)).to(DEV)
+    big, exact = x0.clone(), x0.clone()
+    gm.ctx.goose_verify_layer_paged(gm.packed_layer(1), cache, 1, big, reqs, 2)
+    gm.ctx.goose_verify_layer_paged(gm.packed_layer(1), cache, 1, exact[:rows], reqs, 2)
+    assert gm.ctx.goose_device_flags() == 0
+    assert torch.equal(exact[rows:], x0[rows:]) and torch.equal(big[rows:], x0[rows:])
+    assert torch.equal(exact, big) and not torch.equal(exact[rows - 1], x0[rows - 1]) and exact[:rows].isfinite().all()
+    gm.ctx.close()
