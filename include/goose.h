@@ -370,6 +370,8 @@ int goose_verify_layer_paged(goose_ctx* ctx, const void* d_packed_layer, const g
                              const goose_paged_request* reqs, int n, int shared_pages, void* stream);
 /* goose_verify_step_batched on pages: reserves B slots for every request, runs the pass, walks, commits.  Reads d_tokens, d_parent, d_is_spine, P_max
  * and the successor tables, writes d_accept_len, d_path, d_bonus, d_next_root_or_null; model->d_kcache_all and d_vcache_all are not used.
+ * d_argmax_all: int32 [rows], rows as for goose_verify_layer_paged; request r's rows start at the sum of round_up(B, 32) of those before it, entries
+ * between requests mean nothing.
  * The queries keep two terms under bf16 storage (as in goose_verify_layer) and one under fp16.  If the slots cannot be reserved (a flag is
  * raised) the other outputs mean nothing, and tables and lengths stay as they were: the step can be run again once there is room. */
 int goose_verify_step_paged(goose_ctx* ctx, const goose_model_ptrs* model, const goose_pages* pages, const goose_paged_request* reqs, int n,

@@ -993,8 +993,8 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
     if (q.d_succ_ids_or_null)
       hv.req[hv.n++] = HarvestReq{q.d_tokens, q.d_succ_ids_or_null, q.d_succ_scores_or_null, q.B, rows, q.harvest_k};
     b_max = q.B > b_max ? q.B : b_max;
-    rows += round_up(q.B, 32);
   }
+  rows += reqs[n - 1].B;  // the last row of the pass: d_argmax_all ends there
   rc = launch_pages_reserve(*pg, seqs, d.n_layers, c->n_kv, d.head_dim, c->page_copies, c->flags, st);
   if (rc) return rc;
   rc = launch_batch_begin(d.dtype, br, n, b_max, m->d_embed, d.hidden, d.vocab, c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags,

@@ -297,3 +297,31 @@ def test_a_layer_writes_no_row_behind_the_last_request(Bs):
     assert torch.equal(exact[rows:], x0[rows:]) and torch.equal(big[rows:], x0[rows:])
     assert torch.equal(exact, big) and not torch.equal(exact[rows - 1], x0[rows - 1]) and exact[:rows].isfinite().all()
     gm.ctx.close()
+
+
+@pytest.mark.parametrize("Bs", [[1], [5], [20, 12], [64, 64, 33], [33, 1]])
+def test_a_step_writes_no_prediction_behind_the_last_request(Bs):
+    """argmax_all of exactly the entries that the call asks for, at the front of a larger allocation whose rest must stay."""
+    shape = gi.SHAPES["small_bf16"]
+    gm = gpu_model(shape, torch_model(shape, seed=5), max_B=64, cap=512, max_rows=256)
+    n = len(Bs)
+    rows = sum((b + 31) // 32 * 32 for b in Bs[:-1]) + Bs[-1]
+    Ps, seen = [130 + 9 * r for r in range(n)], []
+    rq = _requests(gm, n, Bs, 3)
+    for size in (256, rows):
+        cache = gm.paged_cache(24, n + 1, 320)
+        _fill(gm, cache, Ps, 128, 4)
+        am = torch.full((256,), -9, dtype=torch.int32, device=DEV)
+        gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, [dict(q, seq=r + 1, P_max=p) for r, (q, p) in enumerate(zip(rq, Ps))], 2, am[:size])
+        assert gm.ctx.goose_device_flags() == 0
+        assert (am[rows:] == -9).all()
+        seen.append((am.clone(), [(int(q["accept_len"]), int(q["bonus"])) for q in rq]))
+    at = 0
+    for b in Bs:
+        assert (seen[0][0][at:at + b] >= 0).all() and torch.equal(seen[0][0][at:at + b], seen[1][0][at:at + b])
+        at += (b + 31) // 32 * 32
+    assert seen[0][1] == seen[1][1]
+    with pytest.raises(Exception) as e:
+        gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, [dict(q, seq=r + 1, P_max=p) for r, (q, p) in enumerate(zip(rq, Ps))], 2, am[:rows - 1])
+    assert e.value.status == -1
+    gm.ctx.close()
