@@ -334,8 +334,11 @@ int goose_pages_fork(goose_ctx* ctx, const goose_pages* pages, int src, int len,
  * of a taken page keep what they held).  All or nothing: if pages do not suffice or a length is out of range, no table changes.
  * One call takes at most 4096 pages (sum of h_new / 64 + 2 per sequence, else GOOSE_ERR_CAPACITY). */
 int goose_pages_reserve(goose_ctx* ctx, const goose_pages* pages, const int32_t* h_seqs, const int32_t* h_new, int n, void* stream);
-/* goose_compact_kv on pages, for n requests (d_path, d_accept_len): slot P + path[j] -> P + j in every layer, the length becomes
- * P + L + 1, and reserved pages beyond it are given back.  A path that is not increasing, or leaves the tree, is followed up to there. */
+/* goose_compact_kv on pages, for n requests whose slots are reserved (d_path, d_accept_len): slot P + path[j] -> P + j in every layer, the length becomes
+ * P + L + 1, and reserved pages beyond it are given back.  A path that is not increasing, or leaves the tree, is followed up to there.
+ * A request is committed as a whole or not at all: with accept_len outside 0 .. B - 1 or beyond the table (GOOSE_FLAG_CAPACITY), or with a page from slot P to the
+ * last one read or committed that is missing or in another table too (GOOSE_FLAG_PAGES: slots that were not reserved, or a fork taken between the
+ * reservation and the commit), its rows, length and table stay as they are. */
 int goose_pages_commit(goose_ctx* ctx, const goose_pages* pages, const goose_paged_request* reqs, int n, void* stream);
 /* The sequences become empty; pages that no table names any more are free. */
 int goose_pages_free(goose_ctx* ctx, const goose_pages* pages, const int32_t* h_seqs, int n, void* stream);

@@ -239,7 +239,7 @@ int goose_create_batched(const goose_model_desc* desc, int max_B, int max_rows, 
     A((void**)&c->att_o, (size_t)d.n_heads * c->max_splits * c->Bpad * d.head_dim * sizeof(float));
     A((void**)&c->att_ml, (size_t)d.n_heads * c->max_splits * c->Bpad * 2 * sizeof(float));
     A(&c->q, (size_t)c->Bpad * 2 * c->Kq * es);
-    A(&c->page_copies, GOOSE_MAX_REQUESTS * 16);
+    A((void**)&c->pages, sizeof(PageScratch));
   } else {
     A(&c->q, (size_t)c->Bpad * c->Kq * es);
   }
@@ -276,7 +276,7 @@ int goose_create_batched(const goose_model_desc* desc, int max_B, int max_rows, 
 void goose_destroy(goose_ctx* c) {
   if (!c) return;
   void* ptrs[] = {c->xn, c->part, c->q, c->o, c->h, c->att_o, c->att_ml, c->logits, c->top2, c->harvest, c->inv_freq, c->rope_cs,
-                  c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags, c->s_P, c->page_copies};
+                  c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags, c->s_P, c->pages};
   for (void* p : ptrs)
     if (p) (void)hipFree(p);
   if (c->prof) {
@@ -884,7 +884,7 @@ int goose_pages_reserve(goose_ctx* c, const goose_pages* pg, const int32_t* h_se
     pages += h_new[i] / GOOSE_PAGE + 2;
   }
   if (pages > PAGES_PER_CALL) return GOOSE_ERR_CAPACITY;
-  return launch_pages_reserve(*pg, l, c->d.n_layers, c->n_kv, c->d.head_dim, c->page_copies, c->flags, as_stream(stream));
+  return launch_pages_reserve(*pg, l, c->d.n_layers, c->n_kv, c->d.head_dim, c->pages, c->flags, as_stream(stream));
 }
 
 int goose_pages_commit(goose_ctx* c, const goose_pages* pg, const goose_paged_request* reqs, int n, void* stream) {
@@ -893,7 +893,7 @@ int goose_pages_commit(goose_ctx* c, const goose_pages* pg, const goose_paged_re
   PagedReqs rq;
   rc = paged_reqs(c, pg, reqs, n, false, &rq, [](const goose_paged_request& q) -> const void* { return q.d_accept_len ? q.d_path : nullptr; });
   if (rc) return rc;
-  return launch_pages_commit(*pg, rq, c->d.n_layers, c->n_kv, c->d.head_dim, nullptr, c->flags, as_stream(stream));
+  return launch_pages_commit(*pg, rq, c->d.n_layers, c->n_kv, c->d.head_dim, c->pages, false, c->flags, as_stream(stream));
 }
 
 int goose_pages_free(goose_ctx* c, const goose_pages* pg, const int32_t* h_seqs, int n, void* stream) {
@@ -995,7 +995,7 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
     b_max = q.B > b_max ? q.B : b_max;
   }
   rows += reqs[n - 1].B;  // the last row of the pass: d_argmax_all ends there
-  rc = launch_pages_reserve(*pg, seqs, d.n_layers, c->n_kv, d.head_dim, c->page_copies, c->flags, st);
+  rc = launch_pages_reserve(*pg, seqs, d.n_layers, c->n_kv, d.head_dim, c->pages, c->flags, st);
   if (rc) return rc;
   rc = launch_batch_begin(d.dtype, br, n, b_max, m->d_embed, d.hidden, d.vocab, c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags,
                           pg->table_ld * GOOSE_PAGE, st);
@@ -1012,7 +1012,7 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
   if (rc) return rc;
   rc = launch_batch_accept(br, n, d_argmax_all, st);
   if (rc) return rc;
-  return launch_pages_commit(*pg, commit, d.n_layers, c->n_kv, d.head_dim, c->page_copies, c->flags, st);
+  return launch_pages_commit(*pg, commit, d.n_layers, c->n_kv, d.head_dim, c->pages, true, c->flags, st);
 }
 
 // ---- the LM head without a context: its workspace is a static device array --------------------

@@ -83,7 +83,7 @@ struct goose_ctx {
   float* s_x;        // [Bpad][hidden]
   int32_t* flags;    // [1]
   int32_t* s_P;      // [GOOSE_MAX_REQUESTS] a host-supplied P for kernels that read it from memory; the old lengths while a step commits
-  void* page_copies; // int4 [GOOSE_MAX_REQUESTS] what a reservation of pages has to copy (16-bit models)
+  struct PageScratch* pages;  // what the kernels of a paged call tell each other (16-bit models)
   goose_prof* prof;  // optional per-kernel event timing
 };
 
@@ -286,13 +286,18 @@ struct SeqList {
   int32_t n;
   int32_t seq[GOOSE_MAX_REQUESTS], extra[GOOSE_MAX_REQUESTS];
 };
+// Device memory of the context through which the kernels of a paged call tell each other what they found.
+struct PageScratch {
+  int4 copies[GOOSE_MAX_REQUESTS];      // of a reservation: page to copy (-1: none), its copy, 32-slot blocks; w of the first: it has failed
+  int32_t verdict[GOOSE_MAX_REQUESTS];  // of a commit: flags that a request raises instead of being done
+};
 int launch_pages_clear(const goose_pages& pg, hipStream_t st);
 int launch_pages_fork(const goose_pages& pg, int src, int len, const SeqList& dst, int32_t* flags, hipStream_t st);
-int launch_pages_reserve(const goose_pages& pg, const SeqList& seqs, int n_layers, int n_kv, int head_dim, void* copies, int32_t* flags,
+int launch_pages_reserve(const goose_pages& pg, const SeqList& seqs, int n_layers, int n_kv, int head_dim, PageScratch* scratch, int32_t* flags,
                          hipStream_t st);
-// reservation: null, or the `copies` of a reservation without which nothing is to be committed
-int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, const void* reservation, int32_t* flags,
-                        hipStream_t st);
+// reserved: the slots were taken by a reservation of the same call, without which nothing is to be committed
+int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, PageScratch* scratch, bool reserved,
+                        int32_t* flags, hipStream_t st);
 int launch_pages_free(const goose_pages& pg, const SeqList& seqs, int32_t* flags, hipStream_t st);
 // base of one layer's part of a pool, in elements
 static inline size_t page_layer_elems(const goose_pages& pg, int n_kv, int head_dim) {

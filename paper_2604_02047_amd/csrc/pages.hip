@@ -216,41 +216,50 @@ __global__ __launch_bounds__(256) void k_pages_copy(const goose_pages pg, const 
 // The accepted path, slot P + path[j] -> P + j for j = 1 .. L, in one (layer, head) of a request.  Thread c owns chunk c of the key rows
 // (16 bytes) and column c of the value rows (2 bytes).  MOVES moves at a time, all loads before all stores: path[j] >= j and increasing, so
 // no later source lies at or below an earlier destination.  The whole path is fetched at once, an entry a lane, with length, count and page ids
-// beside it, and the moves of a round are checked by a lane each: asked for move by move it was a trip to memory each (16 requests, 8 layers of 8
+// beside it, and the moves are checked by a lane each: asked for move by move it was a trip to memory each (16 requests, 8 layers of 8
 // heads: 24 us), checked one behind the other 11 us; now 9.6, of which the trips (length, entry, loads, stores) are the most.
+//
+// A commit is done as a whole or not at all: L must leave the sequence inside its tree and table, and every page from slot P to the last slot that is read or
+// committed must be there and be the sequence's own (one that other tables name too may hold their committed rows in these slots).  Every workgroup
+// comes to the same verdict, as this launch changes no table, length or count; k_pages_settle does, and goes by verdict[request] (the flags to raise, 0: done).
+// The counts are asked for beside the first round's rows, and nothing is stored before they are there.
 constexpr int MOVES = 16;  // (accepted paths are rarely longer)
 template <int D>
-__global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const PagedReqs rq, int n_kv, const int4* __restrict__ reservation) {
+__global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const PagedReqs rq, int n_kv, const int4* __restrict__ reservation,
+                                                  int32_t* __restrict__ verdict) {
   typedef unsigned short u16;
   const PagedReq& q = rq.r[blockIdx.y];
   const int layer = blockIdx.x / n_kv, head = blockIdx.x - layer * n_kv, c = threadIdx.x, lane = c & 63;
   const int32_t* path = static_cast<const int32_t*>(q.p);
-  int p_lo = lane < q.B ? path[lane] : -1, p_hi = lane + 64 < q.B ? path[lane + 64] : -1;
-  const int P = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]);
-  int L = __builtin_amdgcn_readfirstlane(*q.accept_len);
-  if (P < 0 || L < 0) return;  // (flagged by k_pages_settle)
+  const int p_lo = lane < q.B ? path[lane] : -1, p_hi = lane + 64 < q.B ? path[lane + 64] : -1;
+  const int P = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]), L = __builtin_amdgcn_readfirstlane(*q.accept_len);
   if (reservation && reservation->w) return;
-  L = min(L, q.B - 1);
-  const int32_t* row = pg.d_table + (size_t)q.seq * pg.table_ld;
+  int bad = 0;
+  if (P < 0 || L < 0 || L >= q.B || (long long)P + L + 1 > (long long)pg.table_ld * GOOSE_PAGE) bad = GOOSE_FLAG_CAPACITY;
+  // lane u: is path[u], path[u + 64] a move (increasing from 0 at the root on, inside the tree)?  The path is followed up to the first that is none.
+  const int up_lo = __shfl_up(p_lo, 1, 64), up_hi = __shfl_up(p_hi, 1, 64), end_lo = __shfl(p_lo, 63, 64);
+  const bool go_lo = lane == 0 || (lane <= L && p_lo > (lane == 1 ? 0 : up_lo) && p_lo < q.B);
+  const bool go_hi = lane + 64 <= L && p_hi > (lane == 0 ? end_lo : up_hi) && p_hi < q.B;
+  const uint64_t stop_lo = ~__builtin_amdgcn_ballot_w64(go_lo), stop_hi = ~__builtin_amdgcn_ballot_w64(go_hi);
+  const int moves = (stop_lo ? __builtin_ctzll(stop_lo) : 64 + (stop_hi ? __builtin_ctzll(stop_hi) : 64)) - 1;
+  const int last = moves < 64 ? __builtin_amdgcn_readlane(p_lo, moves) : __builtin_amdgcn_readlane(p_hi, moves - 64);
+  const int reach = moves > 0 ? max(L, last) : L;  // slots P .. P + reach are read or committed: in three pages at most
   const int e0 = P >> 6;
-  const int id = lane < 3 && e0 + lane < pg.table_ld ? row[e0 + lane] : -1;  // a tree of 128 nodes reaches into three pages
+  const bool needed = !bad && lane < 3 && e0 + lane <= (int)((unsigned)(P + reach) >> 6);
+  const int id = needed && e0 + lane < pg.table_ld ? pg.d_table[(size_t)q.seq * pg.table_ld + e0 + lane] : -1;
+  if (__builtin_amdgcn_ballot_w64(needed && (unsigned)id >= (unsigned)pg.n_pages) != 0) bad = GOOSE_FLAG_PAGES;
+  const int count = needed && !bad ? pg.d_refs[id] : 1;
   const size_t layer0 = (size_t)layer * pg.n_pages;
   u16* const kpool = static_cast<u16*>(pg.d_kpool);
   u16* const vpool = static_cast<u16*>(pg.d_vpool);
   const size_t per_page = (size_t)n_kv * (GOOSE_PAGE * D);
   const size_t base = layer0 * per_page + (size_t)head * (GOOSE_PAGE * D);
-  int prev = 0;
-  for (int j0 = 1; j0 <= L; j0 += MOVES) {
-    // Lane u: move j0 + u, from slot P + from to slot P + j0 + u, each with its page.  The round ends at the first entry that is not increasing,
-    // leaves the tree or has no page.
-    const int j = j0 + lane;
+  for (int j0 = 1; !bad && j0 <= moves; j0 += MOVES) {
+    // Lane u: move j0 + u, from slot P + from to slot P + j0 + u, each with its page.
+    const int j = j0 + lane, n = min(MOVES, moves - j0 + 1);
     const int lo = __shfl(p_lo, j & 63, 64), hi = __shfl(p_hi, j & 63, 64), from = j < 64 ? lo : hi;
-    const int up = __shfl_up(from, 1, 64), last = lane == 0 ? prev : up;
     const int src = P + from, dst = P + j;
     const int ps = __shfl(id, ((src >> 6) - e0) & 63, 64), pd = __shfl(id, ((dst >> 6) - e0) & 63, 64);
-    const bool good = lane < MOVES && j <= L && from > last && from < q.B && (unsigned)ps < (unsigned)pg.n_pages && (unsigned)pd < (unsigned)pg.n_pages;
-    const int n = __builtin_ctzll(~__builtin_amdgcn_ballot_w64(good));  // (at most MOVES)
-    if (n > 0) prev = __builtin_amdgcn_readlane(from, n - 1);
     auto part_of = [&](int page, int u) { return base + (size_t)__builtin_amdgcn_readlane(page, u) * per_page; };
     uint4 kr[MOVES];
     u16 vr[MOVES];
@@ -262,6 +271,7 @@ __global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const Pa
         if (c < D / 8) kr[u] = *reinterpret_cast<const uint4*>(kpool + b + page_k_chunk<D>(s & 63, c));
         vr[u] = vpool[b + page_v_elem<D>(s & 63, c)];
       }
+    if (__builtin_amdgcn_ballot_w64(count != 1) != 0) break;
 #pragma unroll
     for (int u = 0; u < MOVES; ++u)
       if (u < n) {
@@ -270,8 +280,9 @@ __global__ __launch_bounds__(D) void k_pages_move(const goose_pages pg, const Pa
         if (c < D / 8) *reinterpret_cast<uint4*>(kpool + b + page_k_chunk<D>(d & 63, c)) = kr[u];
         vpool[b + page_v_elem<D>(d & 63, c)] = vr[u];
       }
-    if (n < MOVES) break;  // the end, or a malformed path
   }
+  if (__builtin_amdgcn_ballot_w64(count != 1) != 0) bad = GOOSE_FLAG_PAGES;
+  if (blockIdx.x == 0 && c == 0) verdict[blockIdx.y] = bad;
 }
 
 __device__ inline void release(const goose_pages& pg, size_t at, int32_t* flags) {
@@ -285,25 +296,21 @@ __device__ inline void release(const goose_pages& pg, size_t at, int32_t* flags)
   }
 }
 
-// New lengths, and the pages behind them go back.  reservation: where the slots were taken in the same call, and nothing is committed if that failed.
+// New lengths, and the pages behind them go back; a request whose verdict (k_pages_move) is not 0 stays as it is.
+// reservation: where the slots were taken in the same call, and nothing is committed if that failed.
 __global__ __launch_bounds__(256) void k_pages_settle(const goose_pages pg, const PagedReqs rq, const int4* __restrict__ reservation,
-                                                      int32_t* __restrict__ flags) {
+                                                      const int32_t* __restrict__ verdict, int32_t* __restrict__ flags) {
   if (reservation && reservation->w) return;
   const PagedReq& q = rq.r[blockIdx.x];
-  const int P = pg.d_len[q.seq], L = *q.accept_len;
-  const bool off = P < 0 || L < 0 || L >= q.B || (long long)P + L + 1 > (long long)pg.table_ld * GOOSE_PAGE;
+  const int bad = verdict[blockIdx.x], len = pg.d_len[q.seq] + *q.accept_len + 1;
   __syncthreads();  // every thread has the old length
-  if (off) {
-    if (threadIdx.x == 0) atomicOr(flags, GOOSE_FLAG_CAPACITY);
+  if (bad) {
+    if (threadIdx.x == 0) atomicOr(flags, bad);
     return;
   }
-  const int len = P + L + 1;
   const size_t row = (size_t)q.seq * pg.table_ld;
   for (int i = (len + GOOSE_PAGE - 1) / GOOSE_PAGE + threadIdx.x; i < pg.table_ld; i += 256) release(pg, row + i, flags);
-  if (threadIdx.x == 0) {
-    pg.d_len[q.seq] = len;
-    if (pg.d_table[row + ((len - 1) >> 6)] < 0) atomicOr(flags, GOOSE_FLAG_PAGES);  // slots that were never reserved
-  }
+  if (threadIdx.x == 0) pg.d_len[q.seq] = len;
 }
 
 __global__ __launch_bounds__(256) void k_pages_free(const goose_pages pg, const SeqList sq, int32_t* __restrict__ flags) {
@@ -326,25 +333,25 @@ int launch_pages_fork(const goose_pages& pg, int src, int len, const SeqList& ds
   return goose_launch_status();
 }
 
-int launch_pages_reserve(const goose_pages& pg, const SeqList& seqs, int n_layers, int n_kv, int head_dim, void* copies, int32_t* flags,
+int launch_pages_reserve(const goose_pages& pg, const SeqList& seqs, int n_layers, int n_kv, int head_dim, PageScratch* scratch, int32_t* flags,
                          hipStream_t st) {
-  hipLaunchKernelGGL(k_pages_reserve, dim3(1), dim3(NT), 0, st, pg, seqs, (int4*)copies, flags);
+  hipLaunchKernelGGL(k_pages_reserve, dim3(1), dim3(NT), 0, st, pg, seqs, scratch->copies, flags);
   int rc = goose_launch_status();
   if (rc != GOOSE_OK) return rc;
-  hipLaunchKernelGGL(k_pages_copy, dim3(2 * n_layers * n_kv, seqs.n), dim3(256), 0, st, pg, (const int4*)copies, n_kv, head_dim);
+  hipLaunchKernelGGL(k_pages_copy, dim3(2 * n_layers * n_kv, seqs.n), dim3(256), 0, st, pg, (const int4*)scratch->copies, n_kv, head_dim);
   return goose_launch_status();
 }
 
-int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, const void* reservation, int32_t* flags,
-                        hipStream_t st) {
-  const int4* res = (const int4*)reservation;
+int launch_pages_commit(const goose_pages& pg, const PagedReqs& rq, int n_layers, int n_kv, int head_dim, PageScratch* scratch, bool reserved,
+                        int32_t* flags, hipStream_t st) {
+  const int4* res = reserved ? scratch->copies : nullptr;
   const dim3 grid(n_layers * n_kv, rq.n);
-  if (head_dim == 128) hipLaunchKernelGGL(k_pages_move<128>, grid, dim3(128), 0, st, pg, rq, n_kv, res);
-  else if (head_dim == 64) hipLaunchKernelGGL(k_pages_move<64>, grid, dim3(64), 0, st, pg, rq, n_kv, res);
+  if (head_dim == 128) hipLaunchKernelGGL(k_pages_move<128>, grid, dim3(128), 0, st, pg, rq, n_kv, res, scratch->verdict);
+  else if (head_dim == 64) hipLaunchKernelGGL(k_pages_move<64>, grid, dim3(64), 0, st, pg, rq, n_kv, res, scratch->verdict);
   else return GOOSE_ERR_SHAPE;
   int rc = goose_launch_status();
   if (rc != GOOSE_OK) return rc;
-  hipLaunchKernelGGL(k_pages_settle, dim3(rq.n), dim3(256), 0, st, pg, rq, res, flags);
+  hipLaunchKernelGGL(k_pages_settle, dim3(rq.n), dim3(256), 0, st, pg, rq, res, scratch->verdict, flags);
   return goose_launch_status();
 }
 

@@ -266,3 +266,68 @@ def test_two_streams_and_a_graph():
     same(cache, sim)
     assert ctx.goose_device_flags() == 0
     ctx.close()
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "f16")])
+def test_a_commit_is_done_as_a_whole_or_not_at_all(d, dtype):
+    """Slots that were not reserved, in a page of another sequence or in none, paths longer than the tree: rows, lengths and tables stay, also those of the
+    sequence that shares the page; a request beside them is committed."""
+    ctx, cache, sim = make(d=d, dtype=dtype)
+    ctx.goose_pages_reserve(cache, [0], [100])
+    sim.reserve([0], [100])
+    commit(ctx, cache, sim, [0], [list(range(100))], [100])
+    ctx.goose_pages_fork(cache, 0, [1], 70)
+    sim.fork(0, [1], 70)
+    ctx.goose_pages_reserve(cache, [2], [40])
+    sim.reserve([2], [40])
+    ctx.goose_pages_fork(cache, 0, [3], 64)
+    sim.fork(0, [3], 64)
+    same(cache, sim, "before")
+    assert ctx.goose_device_flags() == 0
+
+    def refused(seq, path, B, L, flag):
+        p = torch.full((128,), -1, dtype=torch.int32)
+        p[:len(path)] = torch.tensor(path)
+        ctx.goose_pages_commit(cache, [{"seq": seq, "B": B, "path": p.to(DEV), "accept_len": torch.tensor([L], dtype=torch.int32, device=DEV)}])
+        same(cache, sim, (seq, path, B, L))
+        assert ctx.goose_device_flags() == flag, (seq, path, B, L)
+
+    refused(1, [0, 5], 8, 1, gb.GOOSE_FLAG_PAGES)                  # slot 75 over 71 of a page that sequence 0 has committed rows in
+    refused(1, [0], 1, 0, gb.GOOSE_FLAG_PAGES)                     # nothing moves, but slot 70 is sequence 0's
+    refused(0, [0, 1, 2], 3, 2, gb.GOOSE_FLAG_PAGES)               # and the other way round
+    refused(3, [0, 2], 5, 1, gb.GOOSE_FLAG_PAGES)                  # no page at slot 64
+    refused(2, [0] + list(range(70, 128)), 128, 30, gb.GOOSE_FLAG_PAGES)   # destinations reserved, sources not
+    refused(2, [0, 3, 9], 2, 2, gb.GOOSE_FLAG_CAPACITY)            # longer than the tree
+    refused(2, [0, 3], 9, -1, gb.GOOSE_FLAG_CAPACITY)
+    refused(0, list(range(128)), 128, 127, gb.GOOSE_FLAG_PAGES)
+    # a refused one beside one that can be done
+    path = torch.tensor([[0, 5] + [-1] * 126, [0, 2, 7, 30] + [-1] * 124], dtype=torch.int32, device=DEV)
+    L = torch.tensor([1, 3], dtype=torch.int32, device=DEV)
+    ctx.goose_pages_commit(cache, [{"seq": 1, "B": 8, "path": path[0], "accept_len": L}, {"seq": 2, "B": 40, "path": path[1], "accept_len": L[1:]}])
+    sim.commit([2], [[0, 2, 7, 30]])
+    same(cache, sim, "beside")
+    assert ctx.goose_device_flags() == gb.GOOSE_FLAG_PAGES
+    # a fork taken between the reservation and the commit shares the page again: refused until slots are reserved anew
+    ctx.goose_pages_reserve(cache, [2], [10])
+    sim.reserve([2], [10])
+    ctx.goose_pages_fork(cache, 2, [4])
+    sim.fork(2, [4])
+    refused(2, [0, 3], 10, 1, gb.GOOSE_FLAG_PAGES)
+    ctx.goose_pages_reserve(cache, [2], [10])
+    sim.reserve([2], [10])
+    commit(ctx, cache, sim, [2], [[0, 3]], [10])
+    same(cache, sim, "reserved anew")
+    # a path that leaves the order is followed up to there
+    ctx.goose_pages_reserve(cache, [1], [128])
+    sim.reserve([1], [128])
+    p = torch.tensor([0, 4, 9, 9, 20] + [-1] * 123, dtype=torch.int32, device=DEV)
+    ctx.goose_pages_commit(cache, [{"seq": 1, "B": 128, "path": p, "accept_len": torch.tensor([4], dtype=torch.int32, device=DEV)}])
+    sim.commit([1], [[0, 4, 9, 3, 4]])
+    same(cache, sim, "malformed")
+    ctx.goose_pages_reserve(cache, [1], [128])
+    sim.reserve([1], [128])
+    long = [0, 2] + list(range(4, 66)) + list(range(67, 126))      # over both halves of the path, into the third page
+    commit(ctx, cache, sim, [1], [long], [128])
+    same(cache, sim, "long")
+    assert ctx.goose_device_flags() == 0
+    ctx.close()
