@@ -375,8 +375,10 @@ int goose_verify_layer_paged(goose_ctx* ctx, const void* d_packed_layer, const g
  * and the successor tables, writes d_accept_len, d_path, d_bonus, d_next_root_or_null; model->d_kcache_all and d_vcache_all are not used.
  * d_argmax_all: int32 [rows], rows as for goose_verify_layer_paged; request r's rows start at the sum of round_up(B, 32) of those before it, entries
  * between requests mean nothing.
- * The queries keep two terms under bf16 storage (as in goose_verify_layer) and one under fp16.  If the slots cannot be reserved (a flag is
- * raised) the other outputs mean nothing, and tables and lengths stay as they were: the step can be run again once there is room. */
+ * The queries keep two terms under bf16 storage (as in goose_verify_layer) and one under fp16.  The step is left undone, with a flag, if the slots cannot be
+ * reserved, if a length is above P_max or the first shared_pages entries are not wholly committed (GOOSE_FLAG_CAPACITY), or if they differ or a table names a page
+ * out of range (GOOSE_FLAG_PAGES): the other outputs then mean nothing, and tables, lengths and committed rows stay as they were: it can be run again
+ * once there is room, or with arguments that fit. */
 int goose_verify_step_paged(goose_ctx* ctx, const goose_model_ptrs* model, const goose_pages* pages, const goose_paged_request* reqs, int n,
                             int shared_pages, int32_t* d_argmax_all, void* stream);
 

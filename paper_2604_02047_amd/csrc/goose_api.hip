@@ -981,10 +981,13 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
   HarvestArgs hv;
   int rows = 0, b_max = 0;
   seqs.n = n;
+  seqs.step = 1;
+  seqs.shared_pages = shared_pages;
   for (int r = 0; r < n; ++r) {
     const goose_paged_request& q = reqs[r];
     seqs.seq[r] = q.seq;
     seqs.extra[r] = q.B;
+    seqs.most[r] = q.P_max;
     rows = pass.pos.r[r].row0;
     pass.pos.r[r].p = c->s_pos + rows;
     pass.mask.r[r].p = c->s_mask + (size_t)rows * 2;

@@ -285,6 +285,9 @@ struct PagedReqs {
 struct SeqList {
   int32_t n;
   int32_t seq[GOOSE_MAX_REQUESTS], extra[GOOSE_MAX_REQUESTS];
+  // a reservation for a whole step: what the kernels behind it rely on is looked at as well
+  int32_t step, shared_pages;          // step != 0; entries that all tables must have in common, wholly committed
+  int32_t most[GOOSE_MAX_REQUESTS];    // P_max of the requests
 };
 // Device memory of the context through which the kernels of a paged call tell each other what they found.
 struct PageScratch {

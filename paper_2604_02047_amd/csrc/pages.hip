@@ -76,6 +76,10 @@ __device__ inline int block_scan(int v, int* ws, int* total) {
 // Items = (request, page that its new slots touch), requests in order, pages ascending.  An item takes a page where its entry is
 // missing, or where it is the first one and shared.  Of several requests of the call that share a page, the last may keep it: the
 // i-th of them leaves while refs - i > 1.  The k-th item that takes a page gets the k-th free page.
+//
+// Of a step (sq.step) the reservation is what decides whether it is done: it also fails where a length is above the request's P_max or below the
+// shared pages, where a table names a page out of range in front of its length, or where the shared entries differ.  The kernels behind it would only raise a
+// flag for these and leave rows unwritten, or read other keys, and the commit would then keep them.
 __global__ __launch_bounds__(NT) void k_pages_reserve(const goose_pages pg, const SeqList sq, int4* __restrict__ copies,
                                                       int32_t* __restrict__ flags) {
   __shared__ int first[GOOSE_MAX_REQUESTS], count[GOOSE_MAX_REQUESTS], entry0[GOOSE_MAX_REQUESTS], leave[GOOSE_MAX_REQUESTS];
@@ -92,7 +96,7 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(const goose_pages pg, cons
     const long long end = (long long)len + sq.extra[tid];
     copies[tid] = make_int4(-1, -1, 0, 0);
     int e = -1, cnt = 0;
-    if (len < 0 || end > (long long)pg.table_ld * GOOSE_PAGE) {
+    if (len < 0 || end > (long long)pg.table_ld * GOOSE_PAGE || (sq.step && (len > sq.most[tid] || len < sq.shared_pages * GOOSE_PAGE))) {
       atomicOr(&bad, GOOSE_FLAG_CAPACITY);
     } else {
       cnt = (int)((end - 1) >> 6) - lo + 1;
@@ -101,12 +105,25 @@ __global__ __launch_bounds__(NT) void k_pages_reserve(const goose_pages pg, cons
       else if (e >= 0) refs0 = pg.d_refs[e];
       if (e == -1 && (len & 63) != 0) atomicOr(&bad, GOOSE_FLAG_PAGES);  // committed slots without a page
     }
-    first[tid] = lo;
+    first[tid] = cnt > 0 ? lo : 0;
     count[tid] = cnt;
     entry0[tid] = e;
     used[tid] = ((len & 63) + 31) >> 5;  // 32-slot blocks of that page with committed slots
   }
   __syncthreads();
+  if (sq.step) {  // a wavefront a request: the entries of its whole committed pages
+    static_assert(NT / 64 >= GOOSE_MAX_REQUESTS, "a wavefront for every request");
+    const int r = tid >> 6;
+    const int32_t* row = pg.d_table + (size_t)sq.seq[r < sq.n ? r : 0] * pg.table_ld;
+    const int32_t* row0 = pg.d_table + (size_t)sq.seq[0] * pg.table_ld;
+    bool wrong = false;
+    const int n = r < sq.n ? first[r] : 0;
+    for (int i = tid & 63; i < n; i += 64) {
+      const int e = row[i];
+      wrong = wrong || (unsigned)e >= (unsigned)pg.n_pages || (i < sq.shared_pages && e != row0[i]);
+    }
+    if (wrong) atomicOr(&bad, GOOSE_FLAG_PAGES);
+  }
   if (tid < sq.n) {
     int before = 0;
     for (int r = 0; r < tid; ++r) before += entry0[r] == entry0[tid];

@@ -325,3 +325,63 @@ def test_a_step_writes_no_prediction_behind_the_last_request(Bs):
         gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, [dict(q, seq=r + 1, P_max=p) for r, (q, p) in enumerate(zip(rq, Ps))], 2, am[:rows - 1])
     assert e.value.status == -1
     gm.ctx.close()
+
+
+def _state(cache):
+    torch.cuda.synchronize()
+    return [x.clone() for x in (cache.table, cache.len, cache.refs)]
+
+
+@pytest.mark.parametrize("what", ["P_max", "shared_len", "shared_more", "shared_pages", "hole", "P_max in a graph"])
+def test_a_step_that_its_arguments_do_not_fit_is_left_undone(what):
+    """A length above P_max, shared pages beyond a length, tables that differ in them, an entry out of range: flagged; tables, lengths, counts and committed
+    rows stay, and with arguments that fit the step does what it does in a fresh cache."""
+    from paper_2604_02047_amd import binding as gb
+    shape = gi.SHAPES["tiny_gqa_bf16"]
+    gm = gpu_model(shape, torch_model(shape, seed=7, gain_jitter=0.1), max_B=32, cap=512, max_rows=64)
+    rq = _requests(gm, 2, [12, 20], 11)
+    am = torch.zeros(64, dtype=torch.int32, device=DEV)
+    Ps, seen = [140, 170], []
+    for trial in range(2):
+        cache = gm.paged_cache(24, 3, 320)
+        _fill(gm, cache, Ps, 130, 9)
+        table = [dict(q, seq=r + 1, P_max=p) for r, (q, p) in enumerate(zip(rq, Ps))]
+        if trial == 0:
+            bad, shared, flag, entry = [dict(q) for q in table], 2, gb.GOOSE_FLAG_CAPACITY, None
+            if what.startswith("P_max"):
+                bad[1]["P_max"] = 169
+            elif what == "shared_len":
+                cache.len[1] = 127
+            elif what == "shared_more":   # three pages of 140 and 170 slots
+                shared = 3
+                bad[0]["P_max"] = bad[1]["P_max"] = 200
+            else:
+                flag, entry = gb.GOOSE_FLAG_PAGES, (2, 0, 7 if what == "shared_pages" else -1)
+                shared = 2 if what == "shared_pages" else 0
+            if entry:
+                kept = int(cache.table[entry[:2]])
+                cache.table[entry[:2]] = entry[2]
+            before, rows = _state(cache), [x.clone() for x in _page_rows(cache, cache.table[1].cpu().numpy(), 127, 64)]
+            if what.endswith("graph"):
+                st, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+                torch.cuda.synchronize()
+                with torch.cuda.graph(graph, stream=st):
+                    gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, bad, shared, am)
+                for _ in range(3):
+                    graph.replay()
+            else:
+                gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, bad, shared, am)
+            torch.cuda.synchronize()
+            assert gm.ctx.goose_device_flags() & flag
+            assert all(torch.equal(a, b) for a, b in zip(before, _state(cache)))
+            assert all(torch.equal(a, b) for a, b in zip(rows, _page_rows(cache, cache.table[1].cpu().numpy(), 127, 64)))
+            if what == "shared_len":
+                break   # (rows behind the length that it was given here, 127, are nobody's: the undone step may have written there)
+            if entry:
+                cache.table[entry[:2]] = kept
+        gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, table, 2, am)
+        assert gm.ctx.goose_device_flags() == 0
+        seen.append(([(int(q["accept_len"]), int(q["bonus"])) for q in rq], cache.len.tolist(), am[:12].clone(), am[32:52].clone()))
+    if seen:
+        assert seen[0][:2] == seen[1][:2] and torch.equal(seen[0][2], seen[1][2]) and torch.equal(seen[0][3], seen[1][3])
+    gm.ctx.close()
