@@ -377,8 +377,8 @@ int goose_verify_layer_paged(goose_ctx* ctx, const void* d_packed_layer, const g
  * between requests mean nothing.
  * The queries keep two terms under bf16 storage (as in goose_verify_layer) and one under fp16.  The step is left undone, with a flag, if the slots cannot be
  * reserved, if a length is above P_max or the first shared_pages entries are not wholly committed (GOOSE_FLAG_CAPACITY), or if they differ or a table names a page
- * out of range (GOOSE_FLAG_PAGES): the other outputs then mean nothing, and tables, lengths and committed rows stay as they were: it can be run again
- * once there is room, or with arguments that fit. */
+ * out of range (GOOSE_FLAG_PAGES): d_argmax_all then means nothing, and everything else stays as it was (tables, lengths, committed rows, the
+ * requests' outputs, next roots and successor tables): it can be run again once there is room, or with arguments that fit. */
 int goose_verify_step_paged(goose_ctx* ctx, const goose_model_ptrs* model, const goose_pages* pages, const goose_paged_request* reqs, int n,
                             int shared_pages, int32_t* d_argmax_all, void* stream);
 

@@ -580,6 +580,7 @@ int goose_verify_layer(goose_ctx* c, const void* d_packed_layer, float* d_x, voi
 struct HarvestArgs {  // optional harvest of the logits into the requests' successor tables
   HarvestReq req[GOOSE_MAX_REQUESTS];
   int n = 0;
+  const int32_t* undone = nullptr;  // null, or where a 1 on the device leaves the tables alone
 };
 static int lm_head_impl(goose_ctx* c, const void* d_packed_head, const float* d_x, int B, int32_t* d_argmax,
                         float* d_logits_or_null, float* d_margin_or_null, hipStream_t st, bool xhat_ready,
@@ -626,7 +627,7 @@ static int lm_head_impl(goose_ctx* c, const void* d_packed_head, const float* d_
       rc = launch_argmax_top2(c->top2, groups, B, d_argmax, d_margin_or_null, st); }
     if (rc || hv.n == 0) return rc;
     PROF(PK_HARVEST);
-    return launch_harvest_topk(out, ld, d.vocab, hv.req, hv.n, c->harvest, st);
+    return launch_harvest_topk(out, ld, d.vocab, hv.req, hv.n, c->harvest, st, hv.undone);
   }
   float* logits = d_logits_or_null ? d_logits_or_null : c->logits;
   const size_t ld = d_logits_or_null ? (size_t)d.vocab : (size_t)c->Vpad;
@@ -980,6 +981,8 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
   BatchReq br[GOOSE_MAX_REQUESTS];
   HarvestArgs hv;
   int rows = 0, b_max = 0;
+  const int32_t* undone = &c->pages->copies[0].w;  // (what the reservation found)
+  hv.undone = undone;
   seqs.n = n;
   seqs.step = 1;
   seqs.shared_pages = shared_pages;
@@ -1013,7 +1016,7 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
   }
   rc = lm_head_impl(c, m->d_packed_head, c->s_x, rows, d_argmax_all, nullptr, nullptr, st, true, hv);
   if (rc) return rc;
-  rc = launch_batch_accept(br, n, d_argmax_all, st);
+  rc = launch_batch_accept(br, n, d_argmax_all, undone, st);
   if (rc) return rc;
   return launch_pages_commit(*pg, commit, d.n_layers, c->n_kv, d.head_dim, c->pages, true, c->flags, st);
 }

@@ -134,8 +134,8 @@ int launch_batch_begin(int dtype, const BatchReq* reqs, int n, int max_B, const 
 // walk, new cache length and compaction of all requests (2 launches); P_old: scratch for the n old lengths
 int launch_batch_end(const BatchReq* reqs, int n, const int32_t* argmax_all, int n_layers, int n_kv_heads, int cap,
                      int head_dim, int32_t* P_old, int32_t* flags, hipStream_t st);
-// the walks alone (lengths stay as they are)
-int launch_batch_accept(const BatchReq* reqs, int n, const int32_t* argmax_all, hipStream_t st);
+// the walks alone (lengths stay as they are); undone: where a 1 on the device leaves the requests' outputs alone
+int launch_batch_accept(const BatchReq* reqs, int n, const int32_t* argmax_all, const int32_t* undone, hipStream_t st);
 int launch_compact(int elem_bytes, void* kall, void* vall, int n_layers, int n_heads, int cap, int head_dim,
                    const int32_t* dP, const int32_t* path, const int32_t* accept_len, int32_t* new_P, int32_t* flags,
                    hipStream_t st);
@@ -237,7 +237,9 @@ enum { GOOSE_HARVEST_CHUNK = 8192, GOOSE_HARVEST_KMAX = 16 };
 static inline size_t goose_harvest_ws_bytes(int V, int rows) {  // per (row, chunk): (max, sum) and KMAX (value, id) pairs
   return (size_t)rows * ((V + GOOSE_HARVEST_CHUNK - 1) / GOOSE_HARVEST_CHUNK) * (GOOSE_HARVEST_KMAX + 1) * 8;
 }
-int launch_harvest_topk(const float* logits, size_t ld, int V, const HarvestReq* reqs, int n, void* ws, hipStream_t st);
+// undone: null, or where a 1 on the device leaves the tables alone.
+int launch_harvest_topk(const float* logits, size_t ld, int V, const HarvestReq* reqs, int n, void* ws, hipStream_t st,
+                        const int32_t* undone = nullptr);
 int launch_split_operand(int dtype, const float* src, int rows, int cols, int ld_src, void* dst, int ld_dst,
                          hipStream_t st);
 int launch_copy_probe(const void* src, void* dst, size_t bytes, hipStream_t st);

@@ -321,7 +321,10 @@ constexpr int HARVEST_VPT = 32, HARVEST_CHUNK = 256 * HARVEST_VPT, HARVEST_KMAX 
 constexpr int HARVEST_MERGE = 1024;  // pairs a merge round ranks
 static_assert(HARVEST_CHUNK == GOOSE_HARVEST_CHUNK && HARVEST_KMAX == GOOSE_HARVEST_KMAX, "the workspace is sized for these");
 
-struct HarvestTable { HarvestReq r[GOOSE_MAX_REQUESTS]; };
+struct HarvestTable {
+  HarvestReq r[GOOSE_MAX_REQUESTS];
+  const int32_t* undone;  // null, or where a 1 leaves the tables alone
+};
 
 // `n` pairs in LDS -> out(0 ..), the best `keep` of them in order.  All 256 threads call it.
 template <typename Out>
@@ -405,7 +408,7 @@ __global__ __launch_bounds__(256) void k_harvest_part(const float* __restrict__ 
   }
   if (WHOLE) {
     const bool dup = __syncthreads_or(tid > m && tid < q.B && tok_t == tok);  // a later node carries the same token
-    if (tok < 0 || tok >= V || dup) return;
+    if (tok < 0 || tok >= V || dup || (t.undone && *t.undone)) return;
     const int n = n_s;
     const float S = fabsf(M) == INFINITY ? NAN : red[4] + red[5] + red[6] + red[7];
     int32_t* ids = q.ids + (size_t)tok * K;
@@ -480,7 +483,7 @@ __global__ __launch_bounds__(256) void k_harvest_merge(int chunks, int table_row
   float S = fabsf(M) == INFINITY ? NAN : 0.f;
 #pragma unroll
   for (int w = 0; w < 4; ++w) S += red[4 + w] * exp_below(red[w], M);
-  if (tid < q.K && tok >= 0 && tok < table_rows && !dup) {
+  if (tid < q.K && tok >= 0 && tok < table_rows && !dup && !(t.undone && *t.undone)) {
     const hkey p = top[tid];
     q.ids[(size_t)tok * q.K + tid] = p != 0 ? harvest_id(p) : -1;
     q.scores[(size_t)tok * q.K + tid] = p != 0 ? exp_below(harvest_value(p), M) / S : 0.f;
@@ -564,7 +567,9 @@ __global__ __launch_bounds__(128) void k_accept(const int32_t* __restrict__ pare
 }
 
 __global__ __launch_bounds__(128) void k_accept_batch(const ReqTable t, const int32_t* __restrict__ argmax_all,
-                                                      int32_t* __restrict__ P_old, int cap, int32_t* __restrict__ flags) {
+                                                      int32_t* __restrict__ P_old, int cap, int32_t* __restrict__ flags,
+                                                      const int32_t* __restrict__ undone) {
+  if (undone && *undone) return;
   const BatchReq& q = t.r[blockIdx.x];
   accept_body(q.parent, q.tokens, q.is_spine, argmax_all + q.row0, q.B, q.accept_len, q.path, q.bonus, q.next_root, q.dP,
               P_old + blockIdx.x, cap, flags);
@@ -814,9 +819,11 @@ static void launch_harvest_whole(const float* logits, size_t ld, int V, const Ha
 // launch of k_harvest_merge fills them all; where two of them overlap (requests that share a table) they are filled one
 // request after the other, so that the later request wins.  A vocabulary of one chunk needs no merge: the K best of its rows
 // are known in k_harvest_part (launch_harvest_whole).
-int launch_harvest_topk(const float* logits, size_t ld, int V, const HarvestReq* reqs, int n, void* ws, hipStream_t st) {
+int launch_harvest_topk(const float* logits, size_t ld, int V, const HarvestReq* reqs, int n, void* ws, hipStream_t st,
+                        const int32_t* undone) {
   if (n < 1 || n > GOOSE_MAX_REQUESTS || ws == nullptr || V < 1) return GOOSE_ERR_ARG;
   HarvestTable t{};
+  t.undone = undone;
   int k_max = 0, b_max = 0;
   size_t rows = 0;
   bool overlap = false;
@@ -853,6 +860,7 @@ int launch_harvest_topk(const float* logits, size_t ld, int V, const HarvestReq*
   if (!overlap) return fill(t, b_max, n);
   for (int r = 0; r < n; ++r) {
     HarvestTable one{};
+    one.undone = undone;
     one.r[0] = reqs[r];
     rc = fill(one, reqs[r].B, 1);
     if (rc != GOOSE_OK) return rc;
@@ -890,7 +898,7 @@ int launch_batch_end(const BatchReq* reqs, int n, const int32_t* argmax_all, int
                      int head_dim, int32_t* P_old, int32_t* flags, hipStream_t st) {
   if (n < 1 || n > GOOSE_MAX_REQUESTS) return GOOSE_ERR_ARG;
   ReqTable t = req_table(reqs, n);
-  hipLaunchKernelGGL(k_accept_batch, dim3(n), dim3(128), 0, st, t, argmax_all, P_old, cap, flags);
+  hipLaunchKernelGGL(k_accept_batch, dim3(n), dim3(128), 0, st, t, argmax_all, P_old, cap, flags, (const int32_t*)nullptr);
   int rc = goose_launch_status();
   if (rc != GOOSE_OK) return rc;
   for (int r = 0; r < n; ++r) t.r[r].dP = P_old + r;  // the walk replaced the lengths
@@ -903,11 +911,11 @@ int launch_batch_end(const BatchReq* reqs, int n, const int32_t* argmax_all, int
   return goose_launch_status();
 }
 
-int launch_batch_accept(const BatchReq* reqs, int n, const int32_t* argmax_all, hipStream_t st) {
+int launch_batch_accept(const BatchReq* reqs, int n, const int32_t* argmax_all, const int32_t* undone, hipStream_t st) {
   if (n < 1 || n > GOOSE_MAX_REQUESTS) return GOOSE_ERR_ARG;
   ReqTable t = req_table(reqs, n);
   for (int r = 0; r < n; ++r) t.r[r].dP = nullptr;  // (no length is read or written)
-  hipLaunchKernelGGL(k_accept_batch, dim3(n), dim3(128), 0, st, t, argmax_all, (int32_t*)nullptr, 0, (int32_t*)nullptr);
+  hipLaunchKernelGGL(k_accept_batch, dim3(n), dim3(128), 0, st, t, argmax_all, (int32_t*)nullptr, 0, (int32_t*)nullptr, undone);
   return goose_launch_status();
 }
 

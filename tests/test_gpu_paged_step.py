@@ -385,3 +385,41 @@ def test_a_step_that_its_arguments_do_not_fit_is_left_undone(what):
     if seen:
         assert seen[0][:2] == seen[1][:2] and torch.equal(seen[0][2], seen[1][2]) and torch.equal(seen[0][3], seen[1][3])
     gm.ctx.close()
+
+
+@pytest.mark.parametrize("vocab_chunks", [1, 2])
+def test_an_undone_step_touches_neither_roots_nor_successor_tables(vocab_chunks):
+    """No room for one of two requests: next roots (which may be the trees' own first tokens), paths, accept lengths and the harvested tables stay as they
+    were for both, with a vocabulary of one chunk of the harvest and of several; with room, a second step over the same buffers writes them."""
+    import dataclasses
+
+    import paper_2604_02047_amd as goose
+    from paper_2604_02047_amd import binding as gb
+    from paper_2604_02047_amd.runner import GooseModel
+    shape = dataclasses.replace(gi.SHAPES["tiny_gqa_bf16"], vocab=1024 if vocab_chunks == 1 else 9000)
+    tm = torch_model(shape, seed=7, gain_jitter=0.1)
+    gm = GooseModel(goose.ModelDesc.from_shape(shape), 32, 512, lambda l: tm["layers"][l], tm["embed"], tm["lm_head"], tm["final_norm"], max_rows=64)
+    rq, K = _requests(gm, 2, [12, 20], 13), 4
+    cache = gm.paged_cache(6, 4, 256)
+    _fill(gm, cache, [50, 60], 40, 12)
+    gm.ctx.goose_pages_reserve(cache, [3], [3 * PAGE])             # (two pages held, the prompt's and three: none is left)
+    g = torch.Generator().manual_seed(1)
+    reqs, kept = [], []
+    for r, q in enumerate(rq):
+        ids = torch.randint(0, shape.vocab, (shape.vocab, K), generator=g).to(torch.int32).to(DEV)
+        scores = torch.rand((shape.vocab, K), generator=g).to(DEV)
+        for name in ("accept_len", "path", "bonus"):
+            q[name].fill_(-77)
+        reqs.append(dict(q, seq=r + 1, P_max=50 + 10 * r, succ_ids=ids, succ_scores=scores, next_root=q["tokens"][:1]))
+        kept.append([reqs[r][k].clone() for k in ("tokens", "accept_len", "path", "bonus", "succ_ids", "succ_scores")])
+    am = torch.zeros(64, dtype=torch.int32, device=DEV)
+    for room in (False, True):
+        if room:
+            gm.ctx.goose_pages_free(cache, [3])
+        gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, reqs, 0, am)
+        flags = gm.ctx.goose_device_flags()
+        assert flags == 0 if room else flags & gb.GOOSE_FLAG_PAGES
+        for q, before in zip(reqs, kept):
+            for k, x in zip(("tokens", "accept_len", "path", "bonus", "succ_ids", "succ_scores"), before):
+                assert torch.equal(q[k], x) == (not room) or (room and k == "tokens" and int(q["bonus"]) == int(x[0])), (room, k)
+    gm.ctx.close()
