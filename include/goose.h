@@ -325,8 +325,8 @@ typedef struct {
 /* All tables empty, all lengths 0, all pages free. */
 int goose_pages_clear(goose_ctx* ctx, const goose_pages* pages, void* stream);
 /* Every sequence of h_dst (empty ones) starts with the first `len` committed slots of sequence src (len < 0: with all of
- * them): their tables name src's pages, nothing is copied.  One of them that is not empty is left alone (GOOSE_FLAG_PAGES);
- * a src with fewer than `len` slots leaves all alone (GOOSE_FLAG_CAPACITY). */
+ * them): their tables name src's pages, nothing is copied.  One of them that is not empty is left alone (GOOSE_FLAG_PAGES); a src with fewer than
+ * `len` slots (GOOSE_FLAG_CAPACITY), or with a page among them that is missing, out of range or counted as free (GOOSE_FLAG_PAGES), leaves all alone. */
 int goose_pages_fork(goose_ctx* ctx, const goose_pages* pages, int src, int len, const int32_t* h_dst, int n, void* stream);
 /* Room for h_new[i] (>= 1) slots behind the committed ones of sequence h_seqs[i]: missing pages are taken from the pool, the free
  * page with the lowest number first, for the sequences in their order.  Where the page of the first new slot is shared

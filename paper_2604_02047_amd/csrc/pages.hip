@@ -34,15 +34,20 @@ __global__ __launch_bounds__(NT) void k_pages_fork(const goose_pages pg, int src
     ok[tid] = empty;
     if (!empty) atomicOr(flags, GOOSE_FLAG_PAGES);
   }
-  __syncthreads();
+  // a hole in the source, or a page of it that counts as free: nothing is shared
+  bool hole = false;
+  for (int i = tid; i < np; i += NT) {
+    const int e = pg.d_table[(size_t)src * pg.table_ld + i];
+    hole = hole || (unsigned)e >= (unsigned)pg.n_pages || pg.d_refs[e] < 1;
+  }
+  if (__syncthreads_or(hole)) {
+    if (tid == 0) atomicOr(flags, GOOSE_FLAG_PAGES);
+    return;
+  }
   int forks = 0;
   for (int r = 0; r < dst.n; ++r) forks += ok[r];
   for (int i = tid; i < np; i += NT) {
     const int e = pg.d_table[(size_t)src * pg.table_ld + i];
-    if ((unsigned)e >= (unsigned)pg.n_pages) {  // a hole in the source: nothing to share there
-      atomicOr(flags, GOOSE_FLAG_PAGES);
-      continue;
-    }
     for (int r = 0; r < dst.n; ++r)
       if (ok[r]) pg.d_table[(size_t)dst.seq[r] * pg.table_ld + i] = e;
     atomicAdd(&pg.d_refs[e], forks);  // (integers: the order does not matter)

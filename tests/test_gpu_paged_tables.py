@@ -331,3 +331,32 @@ def test_a_commit_is_done_as_a_whole_or_not_at_all(d, dtype):
     same(cache, sim, "long")
     assert ctx.goose_device_flags() == 0
     ctx.close()
+
+
+def test_a_fork_over_a_hole_is_left_undone():
+    """A source with a page missing, out of range or counted as free among its committed ones: no sequence gets any of them; up to the hole it can be forked."""
+    ctx, cache, sim = make(width=40, n_pages=60)
+    ctx.goose_pages_reserve(cache, [0], [2300])
+    sim.reserve([0], [2300])
+    cache.len[0] = 2300
+    sim.len[0] = 2300
+    same(cache, sim)
+    for at, value in ((0, -1), (17, 60), (35, -5)):
+        good = int(sim.table[0, at])
+        cache.table[0, at] = sim.table[0, at] = value
+        ctx.goose_pages_fork(cache, 0, [1, 3])
+        same(cache, sim, (at, value))
+        assert ctx.goose_device_flags() == gb.GOOSE_FLAG_PAGES
+        ctx.goose_pages_fork(cache, 0, [1], at * 64)
+        sim.fork(0, [1], at * 64)
+        same(cache, sim, (at, value, "up to there"))
+        assert ctx.goose_device_flags() == 0
+        ctx.goose_pages_free(cache, [1])
+        sim.free([1])
+        cache.table[0, at] = sim.table[0, at] = good
+    cache.refs[int(sim.table[0, 20])] = 0
+    sim.refs[sim.table[0, 20]] = 0
+    ctx.goose_pages_fork(cache, 0, [2])
+    same(cache, sim, "count")
+    assert ctx.goose_device_flags() == gb.GOOSE_FLAG_PAGES
+    ctx.close()
