@@ -46,7 +46,7 @@ struct PagedAttnArgs {
   const int32_t* len;
   const void* q;
   float* ws_o;    // [split][head][row][d]; splits of the shared keys first
-  float* ws_ml;   // [split][head][row][2]
+  float* ws_ml;   // [split][head][row][2]: largest score (unscaled), sum of weights
   unsigned short* o;
   int32_t* flags;
   size_t ldq, ldo;
@@ -74,6 +74,19 @@ __device__ inline void store_out(const PagedAttnArgs& a, size_t row, int col, co
 
 // The maximum as the exponent's reference: a row that has seen nothing (or only scores of -infinity) takes 0, so that 2^(-inf - 0) = 0.
 __device__ inline float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
+// Scores are unscaled; c = log2(e) / sqrt(d).  Weights are 2^(s c - ref), ref = m c rounded once.
+__device__ __forceinline__ float reference_of(float m, float c) {
+#pragma clang fp contract(off)
+  return finite_ref(m) * c;
+}
+// From 2^24 on such products leave no room for the fraction: there (and for infinities) differences of scores are scaled instead.
+__device__ __forceinline__ bool far_out(float ref) { return !(fabsf(ref) < 16777216.f); }
+// What the sums of a set of keys with the maximum m0 are multiplied by where the maximum becomes m >= m0.
+__device__ __forceinline__ float join_factor(float m0, float m, float c) {
+#pragma clang fp contract(off)
+  const float ref = reference_of(m, c);
+  return m0 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(far_out(ref) ? (m0 - finite_ref(m)) * c : m0 * c - ref);
+}
 
 // Which keys of the 16 from tree node j0 on (negative: committed slots, visible) a mask row shows.
 __device__ inline unsigned window16(uint64_t w0, uint64_t w1, int j0) {
@@ -255,24 +268,20 @@ struct RowTile {
     const float t[4] = {partial_max(s, 0), partial_max(s, 1), partial_max(s, 2), partial_max(s, 3)};
     top = join_max(t);
   }
-  // The exponent that weights, l and O are relative to.
-  __device__ __forceinline__ float reference(float c) const { return finite_ref(m) * c; }
   __device__ __forceinline__ bool grown() const { return __builtin_amdgcn_ballot_w64(top > lim) != 0; }
   // m, and with it l and O, follows only where a row's largest score has grown so far that weights would pass 2^SLACK: weights up to there are as
   // good as those up to one (in two terms, of which 16 bits hold both with room to spare: a weight other than one is rounded for the second product and not in
   // l, so with one term a row that a single key dominates would be off by that term's rounding), and with 32 rows in a tile some row's maximum grows by a
   // little in most blocks (512 rows over 16384 slots: in 3 of 4).
-  // A weight is 2^(s c - ref) in one fused multiply-add, ref = m c rounded; its rounding is the same factor in O and l.  Where products
-  // leave no room for it (2^24 and beyond, infinities), the block's scores (x) become differences to m first.
+  // A weight is 2^(s c - ref) in one fused multiply-add; the rounding of ref is the same factor in O and l.  Far out
+  // the block's scores (x) become differences to m first.
   // Returns the factor that O has to follow by.
   __device__ __forceinline__ float raise(float c, f32x16& x) {
     const float both = fmaxf(top, __shfl_xor(top, 32, 64)), m_new = both > lim ? fmaxf(m, both) : m;
-    const float old = finite_ref(m), now = finite_ref(m_new), before = reference(c);
-    const bool none = m == -INFINITY;
+    const float now = finite_ref(m_new), alpha = join_factor(m, m_new, c);
     m = m_new;
-    ref = reference(c);
-    const bool far = !(fabsf(ref) < 16777216.f);
-    const float alpha = none ? 0.f : __builtin_amdgcn_exp2f(far ? (old - now) * c : before - ref);
+    ref = reference_of(m, c);
+    const bool far = far_out(ref);
     lim = m + SLACK / c;
     mul = c;
     if (__builtin_amdgcn_ballot_w64(far) != 0) {
@@ -510,7 +519,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
 
   // ---- the key groups' states join in one round through LDS: each wavefront leaves its own, then owns some of its tile's columns
   float* dst = lds + (size_t)wave * WFLOATS + lane * 4;
-  *reinterpret_cast<f32x4*>(dst) = f32x4{t.m == -INFINITY ? t.m : t.reference(scale), t.l, 0.f, 0.f};
+  *reinterpret_cast<f32x4*>(dst) = f32x4{t.m, t.l, 0.f, 0.f};
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -526,13 +535,12 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
     lj[j] = ml[1];
     m = fmaxf(m, mj[j]);
   }
-  const float ref = finite_ref(m);
   f32x4 res[QPW];
 #pragma unroll
   for (int q = 0; q < QPW; ++q) res[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
-    const float w = __builtin_amdgcn_exp2f(mj[j] - ref);
+    const float w = join_factor(mj[j], m, scale);
     l += w * lj[j];
 #pragma unroll
     for (int q = 0; q < QPW; ++q)
@@ -802,7 +810,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
   if (wave == 0) check_shared(a, it, lane);
 
   // ---- two key groups join: the second leaves its states in LDS, the first takes them in
-  float m = t.m == -INFINITY ? t.m : t.reference(scale);
+  float m = t.m;
   if (KG == 2) {
     __syncthreads();
     float* const buf = reinterpret_cast<float*>(ring) + (size_t)rt * WFLOATS + lane * 4;
@@ -818,8 +826,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
     __syncthreads();
     if (kg == 1) return;
     const f32x4 ml = *reinterpret_cast<const f32x4*>(buf);
-    const float both = fmaxf(m, ml[0]), ref = finite_ref(both);
-    const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(ml[0] - ref);
+    const float both = fmaxf(m, ml[0]);
+    const float w0 = join_factor(m, both, scale), w1 = join_factor(ml[0], both, scale);
     m = both;
     t.l = w0 * t.l + w1 * ml[1];
 #pragma unroll
@@ -859,6 +867,7 @@ __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
   const int all = a.sh_splits + a.r[r].splits;
   const int s_lo = all * p / PARTS, n = all * (p + 1) / PARTS;
   const size_t base = (size_t)h * a.rows + crow, step = (size_t)a.n_heads * a.rows;
+  const float scale = softmax_scale(D);
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
   float den = 0.f, m = -INFINITY;
   for (int s0 = s_lo; s0 < n; s0 += CH) {
@@ -873,14 +882,14 @@ __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
     float m_new = m;
 #pragma unroll
     for (int k = 0; k < CH; ++k) m_new = fmaxf(m_new, ml[k].x);
-    const float ref = finite_ref(m_new), w0 = __builtin_amdgcn_exp2f(m - ref);
+    const float w0 = join_factor(m, m_new, scale);
     den *= w0;
     num *= w0;
     m = m_new;
 #pragma unroll
     for (int k = 0; k < CH; ++k)
       if (s0 + k < n) {
-        const float w = __builtin_amdgcn_exp2f(ml[k].x - ref);
+        const float w = join_factor(ml[k].x, m, scale);
         den = fmaf(w, ml[k].y, den);
         num += w * ov[k];
       }
@@ -892,13 +901,12 @@ __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
     if (p != 0) return;
 #pragma unroll
     for (int k = 1; k < PARTS; ++k) m = fmaxf(m, part_ml[tid + k * TPR].x);
-    const float ref = finite_ref(m);
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     den = 0.f;
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) {
       const float2 ml = part_ml[tid + k * TPR];
-      const float w = __builtin_amdgcn_exp2f(ml.x - ref);
+      const float w = join_factor(ml.x, m, scale);
       den = fmaf(w, ml.y, den);
       sum += w * part_o[tid + k * TPR];
     }

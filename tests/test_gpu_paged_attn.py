@@ -508,3 +508,35 @@ def test_a_weight_above_one_keeps_its_bits(dtype, nh, nkv, Bs, bound):
         off = (o[at:at + B] - want).abs() / tol
         assert off.max() <= 1, (float(off.max()), off.argmax())
         at += (B + 31) // 32 * 32
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("nh,nkv,Bs,P,S,bound", [(8, 4, [7], 600, 0, None), (16, 4, [12, 9], 600, 0, None), (32, 8, [32] * 16, 600, 0, 16384),
+                                                 (64, 8, [32] * 16, 600, 0, 16384), (8, 4, [1] * 8, 4500, 4096, None), (8, 4, [2], 9000, 0, None)])
+def test_large_scores_join_by_their_differences(dtype, nh, nkv, Bs, P, S, bound):
+    """Two keys score 2^27 and 2^27 + 16 (over sqrt(64): 2 apart), all others 0, wherever the two lie: in one block, one wavefront's share, two of them, two
+    splits, or the shared pages and a request's own.  The sums of products are multiples of 16 up to 2^27 + 16, so exact in 32 bits in any order; the difference is exact too, and
+    its scale and exponential err by 2^-21 and 2^-22 of the weight: with p, output (one term) and store tol = |v| sums (u + 2^-19) + u_o |o| + 2^-25."""
+    d = 64
+    c = Case(nh, nkv, d, dtype, Bs, [P + i for i in range(len(Bs))], S, seed=130)
+    c.k.zero_()
+    c.v.mul_(0.5)
+    c.q32.zero_()
+    c.q32[..., 3], c.q32[..., 9] = 2.0 ** 13, 4.0
+    first = [[40 if h == 0 else (P - 33 * h if S else 40 + (P // 16 * h)) for h in range(nkv)], [20 + 3 * h for h in range(nkv)]]
+    for r in range(len(Bs)):
+        for h in range(nkv):
+            for s, nine in ((first[1][h], 0.0), (first[0][h], 4.0)):
+                c.k[0, c.table[r, s // 64], h, s % 64, 3] = 2.0 ** 14
+                c.k[0, c.table[r, s // 64], h, s % 64, 9] = nine
+    o, at, u = c.run().double() if bound is None else c.run(bound=bound).double(), 0, U_P[c.dt]
+    for r, B in enumerate(Bs):
+        got = o[at:at + B].view(B, nh, d)
+        for h in range(nkv):
+            lo, hi = (c.v[0, c.table[r, s // 64], h, s % 64].double() for s in (first[1][h], first[0][h]))
+            w = math.exp(2.0)
+            want, mag = (lo + w * hi) / (1 + w), (lo.abs() + w * hi.abs()) / (1 + w)
+            tol = mag * (u + 2.0 ** -19) + U[torch.float16] * want.abs() + 2.0 ** -25
+            off = (got[:, h * nh // nkv:(h + 1) * nh // nkv] - want).abs() / tol
+            assert off.max() <= 1, (r, h, float(off.max()))
+        at += (B + 31) // 32 * 32
