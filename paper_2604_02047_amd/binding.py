@@ -409,7 +409,7 @@ class PagedRequests:
             if not ok or (ids is None) != (sc is None):
                 raise GooseError(GOOSE_ERR_ARG, f"PagedRequests: type, layout or size of a tensor of request {i}")
             k = 0 if ids is None else int(ids.shape[1])
-            self._c[i] = _PagedRequest(int(q["seq"]), int(q["B"]), int(q.get("P_max", 0)), *ptrs, k)
+            self._c[i] = _PagedRequest(_i32(q["seq"]), _i32(q["B"]), _i32(q.get("P_max", 0)), *ptrs, k)
         # rows of the stacked buffers that the requests reach into (each starts at a multiple of 32)
         Bs = [q.B for q in self._c]
         self.rows = sum((b + 31) // 32 * 32 for b in Bs[:-1]) + (Bs[-1] if Bs else 0)
@@ -424,8 +424,16 @@ def _rows_ok(t, rows, cols, dtypes):
     return t.dim() == 2 and t.dtype in dtypes and t.stride(1) == 1 and t.shape[0] >= rows and t.shape[1] >= cols
 
 
+def _i32(x):
+    """A host integer as the C side takes it.  ctypes would cut off the upper bits: sequence 2^32 would be sequence 0."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise GooseError(GOOSE_ERR_ARG, f"{x} does not fit the C entry points' 32-bit integers")
+    return x
+
+
 def _seqs(values):
-    return (C.c_int32 * len(values))(*values)
+    return (C.c_int32 * len(values))(*[_i32(x) for x in values])
 
 
 class GooseContext:
@@ -554,7 +562,7 @@ class GooseContext:
 
     def goose_pages_fork(self, cache, src, dst, length=-1):
         _, st = self._paged(cache, None)
-        _check(self.lib.goose_pages_fork(self._h, cache._ref, src, length, _seqs(dst), len(dst), st), "goose_pages_fork")
+        _check(self.lib.goose_pages_fork(self._h, cache._ref, _i32(src), _i32(length), _seqs(dst), len(dst), st), "goose_pages_fork")
 
     def goose_pages_reserve(self, cache, seqs, new):
         if len(seqs) != len(new):
@@ -579,7 +587,7 @@ class GooseContext:
                 and _rows_ok(q, r.rows, d.n_heads * d.head_dim * q_terms, (cache.kpool.dtype,))
                 and all(g is None or (g.dtype == q.dtype and g.is_contiguous() and g.numel() == d.head_dim) for g in (gq, gk))):
             raise GooseError(GOOSE_ERR_ARG, "goose_qk_norm_rope_paged: rows or types of qkv, q or the gains")
-        _check(self.lib.goose_qk_norm_rope_paged(self._h, cache._ref, layer, qkv.data_ptr(), ks, s0, s1, gq.data_ptr() if gq is not None else None,
+        _check(self.lib.goose_qk_norm_rope_paged(self._h, cache._ref, _i32(layer), qkv.data_ptr(), ks, s0, s1, gq.data_ptr() if gq is not None else None,
                                                  gk.data_ptr() if gk is not None else None, r._c, len(r), q.data_ptr(), q.stride(0), q_terms,
                                                  st), "goose_qk_norm_rope_paged")
 
@@ -591,7 +599,7 @@ class GooseContext:
         if not (_rows_ok(q, r.rows, cols * q_terms, (cache.kpool.dtype,))
                 and _rows_ok(o, r.rows, cols * o_terms, (torch.bfloat16, torch.float16))):
             raise GooseError(GOOSE_ERR_ARG, "goose_attn_paged: rows or types of q or o")
-        _check(self.lib.goose_attn_paged(self._h, cache._ref, layer, q.data_ptr(), q.stride(0), q_terms, r._c, len(r), shared_pages, o.data_ptr(),
+        _check(self.lib.goose_attn_paged(self._h, cache._ref, _i32(layer), q.data_ptr(), q.stride(0), q_terms, r._c, len(r), _i32(shared_pages), o.data_ptr(),
                                          o.stride(0), _dtype_code(o), o_terms, st), "goose_attn_paged")
 
     def goose_verify_layer_paged(self, packed_layer, cache, layer, x, reqs, shared_pages=0):
@@ -599,7 +607,7 @@ class GooseContext:
         import torch
         if not (x.dtype == torch.float32 and x.dim() == 2 and x.is_contiguous() and x.shape[0] >= r.rows and x.shape[1] == self.desc.hidden):
             raise GooseError(GOOSE_ERR_ARG, "goose_verify_layer_paged: rows or type of x")
-        _check(self.lib.goose_verify_layer_paged(self._h, _ptr(packed_layer), cache._ref, layer, _ptr(x), r._c, len(r), shared_pages, st),
+        _check(self.lib.goose_verify_layer_paged(self._h, _ptr(packed_layer), cache._ref, _i32(layer), _ptr(x), r._c, len(r), _i32(shared_pages), st),
                "goose_verify_layer_paged")
 
     def goose_verify_step_paged(self, model: dict, cache, reqs, shared_pages, argmax_all):
@@ -609,7 +617,7 @@ class GooseContext:
         if not (argmax_all.dtype == torch.int32 and argmax_all.is_contiguous() and argmax_all.numel() >= r.rows
                 and all(q.get("succ_ids") is None or q["succ_ids"].shape[0] >= self.desc.vocab for q in r.reqs)):
             raise GooseError(GOOSE_ERR_ARG, "goose_verify_step_paged: argmax_all, or rows of a successor table")
-        _check(self.lib.goose_verify_step_paged(self._h, C.byref(m), cache._ref, r._c, len(r), shared_pages, _ptr(argmax_all), st),
+        _check(self.lib.goose_verify_step_paged(self._h, C.byref(m), cache._ref, r._c, len(r), _i32(shared_pages), _ptr(argmax_all), st),
                "goose_verify_step_paged")
 
     def goose_device_flags(self) -> int:

@@ -118,3 +118,46 @@ def test_simulator_and_layout():
     words, see = mask_words([-1, 0, 1, 0])
     assert words.tolist() == [[1], [3], [7], [9]] and see[3].tolist() == [True, False, False, True]
     assert np.array_equal(see, np.tril(see))
+
+
+class AnyCall:
+    """A library that does whatever it is told."""
+
+    def __getattr__(self, name):
+        return lambda *a: 0
+
+
+def test_integers_beyond_32_bits_are_refused(monkeypatch):
+    """Sequence 2^32 is not sequence 0, nor a layer, a length or a count of shared pages the rest of its division by 2^32."""
+    path = torch.zeros(128, dtype=torch.int32)
+    far = (1 << 32, (1 << 32) + 1, 1 << 31, -(1 << 31) - 1, (1 << 64) - 1)
+
+    def refused(call):
+        with pytest.raises(goose.GooseError) as e:
+            call()
+        assert e.value.status == gb.GOOSE_ERR_ARG
+
+    ctx = object.__new__(goose.GooseContext)
+    ctx._h, ctx._device, ctx.desc = None, 0, goose.ModelDesc(2, 192, 3, 64, 128, 1024)
+    ctx._cache_shape, ctx.lib = (torch.bfloat16, 2, 3, 64 * 64), AnyCall()
+    cache = goose.PagedCache(**tensors())
+    cache._device = 0
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(gb, "_raw_stream", lambda device: 0)
+    monkeypatch.setattr(gb.GooseContext, "_paged", lambda self, cache, reqs, *t: (reqs, 0))
+    rows = torch.zeros((32, 9 * 64), dtype=torch.bfloat16)
+    reqs = goose.PagedRequests([{"seq": 0, "B": 1}])
+    for x in far:
+        refused(lambda: goose.PagedRequests([{"seq": x, "B": 1, "path": path}]))
+        refused(lambda: goose.PagedRequests([{"seq": 0, "B": 1, "P_max": x, "path": path}]))
+        refused(lambda: goose.PagedRequests([{"seq": 0, "B": x}]))
+        refused(lambda: gb._seqs([0, x]))
+        refused(lambda: ctx.goose_pages_free(cache, [x]))
+        refused(lambda: ctx.goose_pages_reserve(cache, [0], [x]))
+        refused(lambda: ctx.goose_pages_fork(cache, x, [1]))
+        refused(lambda: ctx.goose_pages_fork(cache, 0, [1], x))
+        refused(lambda: ctx.goose_attn_paged(cache, x, rows, 1, reqs, 0, rows))
+        refused(lambda: ctx.goose_attn_paged(cache, 0, rows, 1, reqs, x, rows))
+        refused(lambda: ctx.goose_qk_norm_rope_paged(cache, x, torch.zeros((1, 32, 9 * 64)), None, None, reqs, rows))
+        refused(lambda: ctx.goose_verify_layer_paged(rows, cache, x, torch.zeros((32, 192)), reqs))
+    assert list(gb._seqs([0, 2 ** 31 - 1, -2 ** 31])) == [0, 2 ** 31 - 1, -2 ** 31]
