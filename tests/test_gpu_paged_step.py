@@ -423,3 +423,58 @@ def test_an_undone_step_touches_neither_roots_nor_successor_tables(vocab_chunks)
             for k, x in zip(("tokens", "accept_len", "path", "bonus", "succ_ids", "succ_scores"), before):
                 assert torch.equal(q[k], x) == (not room) or (room and k == "tokens" and int(q["bonus"]) == int(x[0])), (room, k)
     gm.ctx.close()
+
+
+@pytest.mark.parametrize("name", ["small_bf16", "small_gqa_qknorm_f16"])
+def test_committed_rows_of_accepted_paths(name):
+    """Trees whose path 0, 3, 8, 14, 21 carries the model's own predictions, so that it is accepted; the committed rows begin in one page and end in the
+    next.  They are compared for every request with those of the batched step: the walk must be the same, with at least four nodes accepted."""
+    from paper_2604_02047_amd import layout
+    shape = gi.SHAPES[name]
+    tm = torch_model(shape, seed=3, gain_jitter=0.1)
+    gm = gpu_model(shape, tm, max_B=64, cap=512, max_rows=256)
+    d, Ps, B, way = gm.desc.head_dim, [190, 254, 318], [24, 33, 40], [0, 3, 8, 14, 21]
+    cache = gm.paged_cache(24, 4, 448)
+    caches = _fill(gm, cache, Ps, 129, 1)
+    rq = _requests(gm, 3, B, 2)
+    am = torch.zeros(256, dtype=torch.int32, device=DEV)
+    for q, b in zip(rq, B):
+        for up, node in zip(way, way[1:]):
+            q["parent"][node] = up
+        for node in range(1, b):    # (a child of the path that is not on it must not be accepted before its turn)
+            if node not in way and int(q["parent"][node]) in way:
+                q["parent"][node] = 1 if node > 2 else 0
+
+    def batched():
+        d_P = [torch.tensor([p], dtype=torch.int32, device=DEV) for p in Ps]
+        gm.ctx.goose_verify_step_batched(gm.model_ptrs(), [dict(q, P_max=p, P=dp, kcache=kc, vcache=vc)
+                                                            for q, p, dp, (kc, vc) in zip(rq, Ps, d_P, caches)], am)
+        torch.cuda.synchronize()
+
+    start = [(kc.clone(), vc.clone()) for kc, vc in caches]
+    for up, node in zip(way, way[1:]):
+        batched()
+        at = 0
+        for q, b in zip(rq, B):
+            q["tokens"][node] = am[at + up]
+            at += (b + 31) // 32 * 32
+    for (kc, vc), (k0, v0) in zip(caches, start):
+        kc.copy_(k0)
+        vc.copy_(v0)
+    batched()
+    want = [(int(q["accept_len"]), q["path"].clone(), int(q["bonus"])) for q in rq]
+    gm.ctx.goose_verify_step_paged(gm.model_ptrs(), cache, [dict(q, seq=r + 1, P_max=p) for r, (q, p) in enumerate(zip(rq, Ps))], 2, am)
+    assert gm.ctx.goose_device_flags() == 0
+    table = cache.table.cpu().numpy()
+    for r, (q, p) in enumerate(zip(rq, Ps)):
+        L = int(q["accept_len"])
+        assert L >= 4 and want[r][0] == L and torch.equal(want[r][1][:L + 1], q["path"][:L + 1]) and want[r][2] == int(q["bonus"])
+        assert q["path"][:5].tolist() == way and int(cache.len[r + 1]) == p + L + 1
+        n = p + L + 1
+        s = torch.arange(n, device=DEV)
+        k, v = _page_rows(cache, table[r + 1], n, d)
+        for got, ref in ((k, caches[r][0][:, :, layout.k_offsets(s, d)]), (v, caches[r][1][:, :, layout.v_offsets(s, d)])):
+            assert torch.equal(got[:, :, :p], ref[:, :, :p])
+            assert (got - ref).abs().max() <= 2e-2 * ref.abs().max()
+            assert (got[0] - ref[0]).abs().max() <= torch.finfo(gm.dt).eps * ref[0].abs().max()
+    gm.ctx.close()
