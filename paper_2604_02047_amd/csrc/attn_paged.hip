@@ -15,7 +15,7 @@
 // 32 bits.  The output goes on as fp16 or in two terms: one bf16 term of 8 bits would be its largest error by far (16 requests x 1 over 8192
 // slots: 0.00085 of the output's size, with two 0.00021 as the output's own rounding), one fp16 term of 11 bits an error as large as the output's own
 // rounding (16 x 32 over 16384: 0.00029, with two 0.00021; more for a row that one key with a weight above one dominates, see raise()).  The second fp16
-// term costs half the matrix instructions again: 161 us before, now 210; 7B, 5 ragged requests over 1984 slots 25, now 28.
+// term costs half the matrix instructions again: 162 us before, now 207; 7B, 5 ragged requests over 1984 slots 26, now 29.
 #include "mma16.h"
 #include "paged.h"
 
@@ -561,7 +561,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
 //     matrix pipe   S = K Q of block j + 1, then O += V P of block j - 1
 //     vector pipe   weights P of block j, then the maximum of S
 // so that no step waits for another one's result, and a weight has two matrix instructions to hide behind (all of them beside S: half as many).
-// 16 requests x 32 of 4 heads over 16384 slots, fp16, one query term: 210 us (1536 cycles of the matrix pipe a step).
+// 16 requests x 32 of 4 heads over 16384 slots, fp16, one query term: 206 us (1536 cycles of the matrix pipe a step).
 // Measured on the form with one term of weights (1024 cycles): a step took 1680 cycles, 1490 without the copies and the raised maxima, at a clock that fell to
 // 1.45 GHz under this load; a tenth more with S and P V of neighbouring blocks in one step, weights beside S alone and copies that made each LDS read wait for all.
 // Blocks that need a mask (the tree's, and what is left over) follow as in k_paged_stream, from what the ring has copied ahead or from memory.
@@ -971,6 +971,8 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   // at most.  Items run in rounds of 256 workgroups, one a compute unit, the shared keys' items first; times in units of 10 ns at head_dim 128, from
   // runs with 20 calls in a graph: an item's fixed part (start, first loads, epilogue; 5.5 us, with the ring 10.5) and its steps (one query term: 0.24 us a
   // block, 0.50 where two row tiles halve the key groups, with the ring 1.34; more with two), the merge 6 us and its records;
+  // own items of two units or fewer hardly pay the ring's start (33B, 16 x 8 over 8192 shared slots and 64 of their own: 84 us; counted
+  // with it, two row tiles looked cheaper and took 149);
   // and no less than what the caches take to serve all items' blocks (10.5 TB/s).
   struct Way {
     int kind, per, sh_blocks, sh_kg, own_kg, sh_height, own_height;
@@ -990,20 +992,22 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
     w.own_height = ring ? 256 / w.own_kg : w.sh_height;
     const int sh_mul = ring ? w.sh_kg : 1, own_mul = ring ? w.own_kg : 1;  // blocks that a step takes
     const int sh_tiles = (sh_rows + w.sh_height - 1) / w.sh_height, sh_steps = (w.sh_blocks + sh_mul - 1) / sh_mul;
-    int own_steps[GOOSE_MAX_REQUESTS], own_tiles[GOOSE_MAX_REQUESTS], own_longest = 0;
+    int own_steps[GOOSE_MAX_REQUESTS], own_tiles[GOOSE_MAX_REQUESTS], own_longest = 0, own_units = 0;
     long long fetched = (long long)sh_tiles * w.sh_blocks, all_steps = (long long)sh_tiles * sh_steps;  // of a KV head: blocks, steps
     for (int r = 0; r < rq.n; ++r) {
       own_steps[r] = ((rq.r[r].P_max + rq.r[r].B + 31) / 32 - w.sh_blocks + own_mul - 1) / own_mul;
       own_tiles[r] = (rq.r[r].B * a.group + w.own_height - 1) / w.own_height;
       own_longest = own_steps[r] > own_longest ? own_steps[r] : own_longest;
+      const int units = (rq.r[r].P_max / 32 - w.sh_blocks) / own_mul;  // of the ring
+      own_units = units > own_units ? units : own_units;
       fetched += (long long)own_tiles[r] * own_steps[r] * own_mul;
       all_steps += (long long)own_tiles[r] * own_steps[r];
     }
     const long long fetch = fetched * n_kv * head_dim * 128 / 105000;
-    const int least = ring ? 4 : 8, fixed = ring ? 1050 : 550,
+    const int least = ring ? 4 : 8, fixed = ring ? 1050 : 550, own_fixed = own_units > 2 ? fixed : 550,
               products = q_terms + 2,
               step = (ring ? 38 + 32 * products : (w.kind == STREAM2 ? 29 + 7 * products : 15 + 3 * products)) * head_dim / 128;
-    const long long work = fixed + all_steps * n_kv * step / 256;
+    const long long work = own_fixed + all_steps * n_kv * step / 256;
     if ((work > fetch ? work : fetch) >= best.cost) return;  // (no way of this kind is cheaper)
     const int longest = sh_steps > own_longest ? sh_steps : own_longest, most_steps = longest > least ? longest : least;
     auto consider = [&](int per) {  // returns the workgroups that it makes
@@ -1020,7 +1024,7 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
       // (blocks times splits stays a 32-bit number in item_of)
       if (splits <= 1 || ((size_t)splits * records <= max_records && 4ull * longest * (unsigned)splits <= UINT32_MAX)) {
         const long long sh_len = (long long)(per < sh_steps ? per : sh_steps) * step + fixed,
-                        own_len = (long long)(per < own_longest ? per : own_longest) * step + fixed;
+                        own_len = (long long)(per < own_longest ? per : own_longest) * step + own_fixed;
         const long long rounds = (sh_items + 255) / 256, room = (rounds * 256 - sh_items) * (sh_len / own_len);  // own items beside the last shared ones
         const long long left = own_items > room ? own_items - room : 0, time = rounds * sh_len + (left + 255) / 256 * own_len;
         w.cost = (time > fetch ? time : fetch) + (splits > 1 ? 600 + (long long)(splits * records * head_dim * 150 / 1000000) : 0);
@@ -1043,10 +1047,11 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
     }
   };
   // The shared keys get items of their own where rows of one request leave most of a tile empty, or where many keys meet few rows (16 requests x 1
-  // over 8192 slots: 24 us, by request 51).  Where a request fills its tiles by itself the products are the same either way, the caches serve the
-  // pages to all of them, and one set of items and fewer records win (16 x 32 over 4096 slots, bf16: 86 us, shared 102; over 64: 15 and 24).
-  // Which kernel: the ring where rows fill it and keys are many (7B, 2 requests x 100 over 4096: 38 us, two row tiles 46; 8 x 30 of 4 heads over 64: 14
-  // and 12); two row tiles where the caches bound one (16 x 16 of 4 heads over 4096 slots: 42 and 52 us), one where two leave units idle (x 12 over 2048: 37 and 30).
+  // over 8192 slots: 24 us, by request 50).  Where a request fills its tiles by itself the products are the same either way, the caches serve the
+  // pages to all of them, and one set of items and fewer records win (16 x 32 over 4096 slots, bf16: 86 us, shared 102; over 64, fp16: 16 and 24).
+  // Which kernel (fp16): the ring where rows fill it and keys are many (7B, 2 requests x 100 over 4096: 42 us, two row tiles 49; 8 x 30 of 4 heads over 64: 15
+  // and, with one, 11.5); two row tiles where the caches bound one (7B, 5 x 61 over 1984: 42 and 51), one where two leave units idle (16 x 12 of 4 heads over
+  // 2048: 24 and 32).  Over 160 cases (named ones, and drawn ones of every model) what it chooses takes 2.8 % longer than the best of all ways on average, 40 % at most.
   Way way{};
   way.cost = INT64_MAX;
   for (int share = 0; share <= (shared_pages > 0 ? 1 : 0); ++share) {
