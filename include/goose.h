@@ -362,7 +362,8 @@ int goose_qk_norm_rope_paged(goose_ctx* ctx, const goose_pages* pages, int layer
  * d_q as goose_qk_norm_rope_paged writes it; d_o: 16-bit [rows][ldo] of type o_dtype (GOOSE_DTYPE_BF16 or _F16) in o_terms terms.
  * Probabilities enter the second product in two terms of the cache's type; sums and statistics are fp32.  A row that sees nothing but scores of
  * -infinity, or nothing, is zero; what slots behind a mask hold (NaN, infinities) has no effect; a NaN in what a row sees makes the row NaN,
- * and so does a score of +infinity.  ldq and ldo multiples of 8, d_q and d_o 16-byte aligned.  Sum of round_up(B, 32) <= max_rows. */
+ * and so does a score of +infinity; an infinity among the values of committed slots makes its columns infinite or NaN.  With a flag raised d_o means nothing.
+ * ldq and ldo multiples of 8, d_q and d_o 16-byte aligned.  Sum of round_up(B, 32) <= max_rows. */
 int goose_attn_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,
                      const goose_paged_request* reqs, int n, int shared_pages, void* d_o, size_t ldo, int o_dtype, int o_terms,
                      void* stream);
@@ -378,7 +379,9 @@ int goose_verify_layer_paged(goose_ctx* ctx, const void* d_packed_layer, const g
  * The queries keep two terms under bf16 storage (as in goose_verify_layer) and one under fp16.  The step is left undone, with a flag, if the slots cannot be
  * reserved, if a length is above P_max or the first shared_pages entries are not wholly committed (GOOSE_FLAG_CAPACITY), or if they differ or a table names a page
  * out of range (GOOSE_FLAG_PAGES): d_argmax_all then means nothing, and everything else stays as it was (tables, lengths, committed rows, the
- * requests' outputs, next roots and successor tables): it can be run again once there is room, or with arguments that fit. */
+ * requests' outputs, next roots and successor tables): it can be run again once there is room, or with arguments that fit.
+ * Scores that are not finite are goose_attn_paged's matter: a NaN makes its row NaN, a row of -infinity only is zero (the contiguous kernels take the
+ * one as the lowest score, and the mean of the row's values for the other). */
 int goose_verify_step_paged(goose_ctx* ctx, const goose_model_ptrs* model, const goose_pages* pages, const goose_paged_request* reqs, int n,
                             int shared_pages, int32_t* d_argmax_all, void* stream);
 

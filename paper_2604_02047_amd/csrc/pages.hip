@@ -4,7 +4,8 @@
 // committed slots; a page is free when its count is 0, and there is no other list of free pages that could disagree with the
 // counts.  Everything is decided on the device from that state, so the calls can be recorded into a graph whose replays allocate
 // and release different pages.  The tables are a few KiB: those kernels are chains of dependent loads (length -> entry -> count ->
-// stores) in one workgroup, about 1 us a link; only the copies move data, at one workgroup per (layer, K or V, head).
+// stores) in one workgroup, about 1 us a link (fork 3 us, reserve 6, free and settle 2 to 4); only copies and moves touch data, at one workgroup
+// per (layer, K or V, head).
 #include "goose_internal.h"
 #include "paged.h"
 
@@ -239,7 +240,8 @@ __global__ __launch_bounds__(256) void k_pages_copy(const goose_pages pg, const 
 // (16 bytes) and column c of the value rows (2 bytes).  MOVES moves at a time, all loads before all stores: path[j] >= j and increasing, so
 // no later source lies at or below an earlier destination.  The whole path is fetched at once, an entry a lane, with length, count and page ids
 // beside it, and the moves are checked by a lane each: asked for move by move it was a trip to memory each (16 requests, 8 layers of 8
-// heads: 24 us), checked one behind the other 11 us; now 9.6, of which the trips (length, entry, loads, stores) are the most.
+// heads: 24 us), checked one behind the other 11 us; now 9.6 in passes among others (13.8 in a kernel trace), of which the trips (length, entry, loads,
+// stores) are the most.
 //
 // A commit is done as a whole or not at all: L must leave the sequence inside its tree and table, and every page from slot P to the last slot that is read or
 // committed must be there and be the sequence's own (one that other tables name too may hold their committed rows in these slots).  Every workgroup

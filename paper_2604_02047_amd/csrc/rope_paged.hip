@@ -7,7 +7,8 @@
 // when there are many rows, and one trip to memory (plus the table's: length -> entry -> count) when there are few.  Two kinds of
 // workgroups: 16 query heads of one row; and one KV head of eight slots that begin at a multiple of eight, because in the
 // operand order eight consecutive slots of a value column are 16 contiguous bytes and the key chunks of four are 64.
-// Measured (kernel trace): 16 requests x 32, 32 + 2 x 8 heads of 128, 4 slices: 11.3 us (57 MB: 5.0 TB/s); one row: 4.4 us (latency).
+// Measured (kernel trace): 16 requests x 32, 32 + 2 x 8 heads of 128, 4 slices: 11.3 us (57 MB: 5.0 TB/s); one row: 4.4 us (latency);
+// 5 ragged requests of 7B heads, 2 slices: 6.5 us (4.5 at a large copy's rate; the K and V rows are asked for behind length, entry and count).
 #include "mma16.h"
 #include "paged.h"
 
