@@ -385,6 +385,70 @@ int goose_verify_layer_paged(goose_ctx* ctx, const void* d_packed_layer, const g
 int goose_verify_step_paged(goose_ctx* ctx, const goose_model_ptrs* model, const goose_pages* pages, const goose_paged_request* reqs, int n,
                             int shared_pages, int32_t* d_argmax_all, void* stream);
 
+/* ---- 6d. prompts on a paged cache: chunks of new tokens, what they look at, and eviction (16-bit models only) -----------------
+ * A chunk is C consecutive tokens of a sequence behind its d_len[seq] = P committed slots: token i becomes slot P + i and sees slots [0, P + i].
+ * Its slots are reserved (goose_pages_reserve), every layer writes its K/V rows and attends (goose_chunk_layer_paged; goose_attn_chunk_paged
+ * alone), and goose_pages_append commits it.  Rows of a chunk are stacked like those of a tree: they start at the sum of round_up(C, 32) of the
+ * chunks before it.  Every call names the fields that it reads beside seq and C. */
+enum { GOOSE_MAX_CHUNK = 32768 };
+typedef struct {
+  int32_t seq;            /* its sequence, none twice in a call */
+  int32_t C;              /* new tokens, 1 .. GOOSE_MAX_CHUNK */
+  int32_t P_max;          /* host upper bound of d_len[seq]; P_max + C <= table_ld * 64 */
+  int32_t first;          /* tokens before it leave no weight (0 .. C - 1) */
+  const int32_t* d_pos;   /* [C] positions of the rotation, NULL: P + i */
+} goose_chunk;
+
+/* Attention of n chunks over pages of one layer (P_max of each): scores / sqrt(head_dim), softmax over the slots that a token sees.
+ * d_q as goose_qk_norm_rope_paged writes it (q_terms = 1 or 2); d_o: 16-bit [rows][ldo] of type o_dtype in o_terms terms; d_lse (or NULL):
+ * fp32 [n_heads][ld_lse], the natural logarithm of every row's sum of exp(score), ld_lse at least the rows.  Rows between chunks and
+ * behind the last one are neither read nor written.  Sums and statistics are fp32; probabilities enter the second product in one term of the
+ * cache's type where the output keeps no more bits than that, else in two (o_terms = 2; fp16 output over a bf16 cache).
+ * What slots behind a token hold (NaN, infinities) has no effect on it; a NaN in what a row sees makes the row NaN, and so does a score of
+ * +infinity; an infinity among the values of committed slots makes its columns infinite or NaN; a row of scores of -infinity only is zero,
+ * its logarithm -infinity.  With a flag raised (GOOSE_FLAG_CAPACITY, GOOSE_FLAG_PAGES) d_o and d_lse mean nothing.
+ * ldq and ldo multiples of 8, d_q and d_o 16-byte aligned.  Chunks may be longer than the context's max_rows. */
+int goose_attn_chunk_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,
+                           const goose_chunk* chunks, int n, void* d_o, size_t ldo, int o_dtype, int o_terms, float* d_lse_or_null,
+                           size_t ld_lse, void* stream);
+/* What the slots of n sequences weigh: d_weight fp32 [n_layers][n_seqs][n_kv_heads][table_ld * 64].  For layer `layer` and every KV head,
+ *   w[s] = decay * w[s] + sum over tokens i >= first with s <= P + i and over the head's query heads of exp(score - lse),   s < P,
+ * and the sum alone for the chunk's own slots P <= s < P + C; other entries stay as they are.  With decay = 0 what was there is not
+ * read.  d_q, d_lse: as for and from goose_attn_chunk_paged (P_max, first of each chunk); rows before `first` are not read.  0 <= decay, finite.
+ * A row whose lse is -infinity weighs nothing; a NaN in a token's score or lse makes the slots NaN that it concerns.  The sums are
+ * formed in a fixed order.  A sequence whose length is out of range, slots of pages out of range: flagged and left alone. */
+int goose_attn_weight_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,
+                            const goose_chunk* chunks, int n, const float* d_lse, size_t ld_lse, float decay, float* d_weight, void* stream);
+/* Commits n chunks whose slots are reserved: lengths become P + C, pages behind them are given back.  A chunk is committed as a whole or not at
+ * all: beyond the table (GOOSE_FLAG_CAPACITY), or with a page of its slots that is missing or in another table too (GOOSE_FLAG_PAGES), its
+ * sequence stays as it is. */
+int goose_pages_append(goose_ctx* ctx, const goose_pages* pages, const goose_chunk* chunks, int n, void* stream);
+
+/* Cuts sequences of more than `keep` committed slots down to `keep`: in every layer and KV head its first `sink` slots stay, its last `recent`
+ * ones, and of the others the keep - sink - recent with the largest weights (d_weight as above; equal weights: the lower slot; a NaN is
+ * below every number).  Kept slots move to the front in their order, K and V rows and weights; slots from `keep` on hold what they held, in the
+ * weights too; pages behind the new length are given back.  reposition != 0: a key that moves from slot s to t is turned by the
+ * rotary angle of position t - s (rounded once), so that slot and position stay the same thing for every call that comes after; 0: rows are exact
+ * copies, and positions are the caller's (d_pos).
+ * d_kept uint64 [n][n_layers][n_kv_heads][table_ld]: bit s % 64 of word s / 64 set iff slot s was kept (all committed slots where nothing had to go).
+ * A sequence is cut as a whole or not at all: with a length out of range (GOOSE_FLAG_CAPACITY), a page in front of it that is missing or out
+ * of range, or one that keeps slots behind `sink` and is in another table too (GOOSE_FLAG_PAGES), it stays as it is, its words of d_kept
+ * too.  (Shared pages can only stay where they are: the whole of a shared prompt among the `sink` slots.) */
+typedef struct {
+  int32_t seq;    /* its sequence, none twice in a call */
+  int32_t keep;   /* >= 1 */
+  int32_t sink;   /* >= 0 */
+  int32_t recent; /* >= 0, sink + recent <= keep */
+} goose_eviction;
+int goose_pages_evict(goose_ctx* ctx, const goose_pages* pages, const goose_eviction* evictions, int n, float* d_weight, uint64_t* d_kept,
+                      int reposition, void* stream);
+/* One decoder layer over the stacked rows of n chunks (P_max, d_pos, and with weights first, of each): goose_verify_layer_paged with
+ * goose_attn_chunk_paged for its attention, and goose_attn_weight_paged where d_weight is not NULL.  d_x: fp32 [rows][hidden], updated in
+ * place; rows between chunks must be finite, and hold other finite values afterwards.  The chunks' slots must be reserved.
+ * Sum of round_up(C, 32) <= max_rows. */
+int goose_chunk_layer_paged(goose_ctx* ctx, const void* d_packed_layer, const goose_pages* pages, int layer, float* d_x,
+                            const goose_chunk* chunks, int n, float* d_weight_or_null, float decay, void* stream);
+
 /* ---- 7. logit harvest (Sec. 4 stage 2 "verify and harvest"; App. C "adjacency table", tier 1, and
  * "logit harvesting"; Alg. "Decoding Loop", the update of the table from all logits of a cycle) ----
  * For every node i < B -- accepted or not -- row d_tokens[i] of the two dense successor tables

@@ -9,6 +9,7 @@ from .binding import (  # noqa: F401
     GooseContext,
     ModelDesc,
     PagedCache,
+    PagedChunks,
     PagedRequests,
     goose_check_parent,
     goose_packed_matrix_bytes,

@@ -26,6 +26,7 @@ EXPORTS = [
     "goose_lm_head_argmax_static", "goose_plan_cycle",
     "goose_pages_clear", "goose_pages_fork", "goose_pages_reserve", "goose_pages_commit", "goose_pages_free",
     "goose_qk_norm_rope_paged", "goose_attn_paged", "goose_verify_layer_paged", "goose_verify_step_paged",
+    "goose_attn_chunk_paged", "goose_attn_weight_paged", "goose_pages_append", "goose_pages_evict", "goose_chunk_layer_paged",
 ]
 
 GOOSE_DTYPE_BF16, GOOSE_DTYPE_F32, GOOSE_DTYPE_F16 = 0, 1, 2
@@ -78,6 +79,14 @@ class _PagedRequest(C.Structure):
                [(n, C.c_void_p) for n in ("d_tokens", "d_parent", "d_is_spine", "d_mask", "d_pos", "d_accept_len", "d_path", "d_bonus",
                                           "d_next_root_or_null", "d_succ_ids_or_null", "d_succ_scores_or_null")] + \
                [("harvest_k", C.c_int32)]
+
+
+class _Chunk(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("seq", "C", "P_max", "first")] + [("d_pos", C.c_void_p)]
+
+
+class _Eviction(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("seq", "keep", "sink", "recent")]
 
 
 @dataclass
@@ -173,6 +182,12 @@ def load_library():
     lib.goose_qk_norm_rope_paged.argtypes = [vp, pages, ci, vp, ci, sz, sz, vp, vp, preq, ci, vp, sz, ci, vp]
     lib.goose_attn_paged.argtypes = [vp, pages, ci, vp, sz, ci, preq, ci, ci, vp, sz, ci, ci, vp]
     lib.goose_verify_layer_paged.argtypes = [vp, vp, pages, ci, vp, preq, ci, ci, vp]
+    chunk = C.POINTER(_Chunk)
+    lib.goose_attn_chunk_paged.argtypes = [vp, pages, ci, vp, sz, ci, chunk, ci, vp, sz, ci, ci, vp, sz, vp]
+    lib.goose_attn_weight_paged.argtypes = [vp, pages, ci, vp, sz, ci, chunk, ci, vp, sz, C.c_float, vp, vp]
+    lib.goose_pages_append.argtypes = [vp, pages, chunk, ci, vp]
+    lib.goose_pages_evict.argtypes = [vp, pages, C.POINTER(_Eviction), ci, vp, vp, ci, vp]
+    lib.goose_chunk_layer_paged.argtypes = [vp, vp, pages, ci, vp, chunk, ci, vp, C.c_float, vp]
     lib.goose_verify_step_paged.argtypes = [vp, C.POINTER(_ModelPtrs), pages, preq, ci, ci, vp, vp]
     lib.goose_profile_enable.argtypes = [C.c_void_p, C.c_int]
     lib.goose_profile_kinds.argtypes = []
@@ -420,6 +435,28 @@ class PagedRequests:
         return len(self._c)
 
 
+class PagedChunks:
+    """The chunks of new tokens of a paged call, as dicts with seq, C, P_max and, where wanted, first and pos (int32 [C]).  Build it once for
+    calls that repeat; every call takes a plain list of such dicts as well."""
+
+    def __init__(self, chunks):
+        import torch
+        self.chunks = chunks  # (keeps the tensors alive)
+        self._c = (_Chunk * len(chunks))()
+        self._devices, self.rows, at = set(), 0, 0
+        for i, q in enumerate(chunks):
+            n, pos = _i32(q["C"]), q.get("pos")
+            if pos is not None:
+                if not (pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() >= n):
+                    raise GooseError(GOOSE_ERR_ARG, f"PagedChunks: type, layout or size of the positions of chunk {i}")
+                self._devices.add(pos.get_device())
+            self._c[i] = _Chunk(_i32(q["seq"]), n, _i32(q.get("P_max", 0)), _i32(q.get("first", 0)), None if pos is None else pos.data_ptr())
+            self.rows, at = at + max(n, 0), at + (max(n, 0) + 31) // 32 * 32
+
+    def __len__(self):
+        return len(self._c)
+
+
 def _rows_ok(t, rows, cols, dtypes):
     return t.dim() == 2 and t.dtype in dtypes and t.stride(1) == 1 and t.shape[0] >= rows and t.shape[1] >= cols
 
@@ -538,7 +575,7 @@ class GooseContext:
                                                   _stream()), "goose_verify_step_batched")
 
     # ---- paged caches
-    def _paged(self, cache, reqs, *tensors):
+    def _paged(self, cache, reqs, *tensors, kind=PagedRequests):
         """Descriptor, requests and stream of a paged call, after a look at what the C side cannot see: element types, head layout, devices."""
         import torch
         dev = cache._device
@@ -548,7 +585,9 @@ class GooseContext:
             raise GooseError(GOOSE_ERR_ARG, "the paged cache is not one of this model")
         r = None
         if reqs is not None:
-            r = reqs if isinstance(reqs, PagedRequests) else PagedRequests(reqs)
+            r = reqs if isinstance(reqs, (PagedRequests, PagedChunks)) else kind(reqs)
+            if not isinstance(r, kind):
+                raise GooseError(GOOSE_ERR_ARG, f"this call takes {kind.__name__}")
             if not r._devices <= {dev}:
                 raise GooseError(GOOSE_ERR_ARG, "a tensor of the requests is on another device than the paged cache")
         for t in tensors:
@@ -619,6 +658,61 @@ class GooseContext:
             raise GooseError(GOOSE_ERR_ARG, "goose_verify_step_paged: argmax_all, or rows of a successor table")
         _check(self.lib.goose_verify_step_paged(self._h, C.byref(m), cache._ref, r._c, len(r), _i32(shared_pages), _ptr(argmax_all), st),
                "goose_verify_step_paged")
+
+    def goose_attn_chunk_paged(self, cache, layer, q, q_terms, chunks, o, o_terms=1, lse=None):
+        """q: [rows][columns] of the cache's type; o: [rows][columns], bf16 or fp16; lse: fp32 [n_heads][rows], or None."""
+        r, st = self._paged(cache, chunks, q, o, lse, kind=PagedChunks)
+        cols = self.desc.n_heads * self.desc.head_dim
+        import torch
+        if not (_rows_ok(q, r.rows, cols * q_terms, (cache.kpool.dtype,)) and _rows_ok(o, r.rows, cols * o_terms, (torch.bfloat16, torch.float16))
+                and (lse is None or _rows_ok(lse, self.desc.n_heads, r.rows, (torch.float32,)))):
+            raise GooseError(GOOSE_ERR_ARG, "goose_attn_chunk_paged: rows or types of q, o or lse")
+        _check(self.lib.goose_attn_chunk_paged(self._h, cache._ref, _i32(layer), q.data_ptr(), q.stride(0), q_terms, r._c, len(r), o.data_ptr(),
+                                               o.stride(0), _dtype_code(o), o_terms, None if lse is None else lse.data_ptr(),
+                                               0 if lse is None else lse.stride(0), st), "goose_attn_chunk_paged")
+
+    def _weights_ok(self, cache, weight):
+        import torch
+        s, n = cache._shape, cache.table.shape
+        return weight.dtype == torch.float32 and weight.is_contiguous() and weight.shape == (s[1], n[0], s[2], n[1] * GOOSE_PAGE)
+
+    def goose_attn_weight_paged(self, cache, layer, q, q_terms, chunks, lse, weight, decay=1.0):
+        """q, lse: as for goose_attn_chunk_paged; weight: fp32 [n_layers][n_seqs][n_kv_heads][slots of a table], updated."""
+        r, st = self._paged(cache, chunks, q, lse, weight, kind=PagedChunks)
+        import torch
+        if not (_rows_ok(q, r.rows, self.desc.n_heads * self.desc.head_dim * q_terms, (cache.kpool.dtype,))
+                and _rows_ok(lse, self.desc.n_heads, r.rows, (torch.float32,)) and self._weights_ok(cache, weight)):
+            raise GooseError(GOOSE_ERR_ARG, "goose_attn_weight_paged: rows, shapes or types of q, lse or weight")
+        _check(self.lib.goose_attn_weight_paged(self._h, cache._ref, _i32(layer), q.data_ptr(), q.stride(0), q_terms, r._c, len(r), lse.data_ptr(),
+                                                lse.stride(0), float(decay), weight.data_ptr(), st), "goose_attn_weight_paged")
+
+    def goose_pages_append(self, cache, chunks):
+        r, st = self._paged(cache, chunks, kind=PagedChunks)
+        _check(self.lib.goose_pages_append(self._h, cache._ref, r._c, len(r), st), "goose_pages_append")
+
+    def goose_pages_evict(self, cache, evictions, weight, kept, reposition=True):
+        """evictions: dicts with seq, keep and, where wanted, sink and recent; weight: as for goose_attn_weight_paged; kept: int64 or uint64
+        [len(evictions)][n_layers][n_kv_heads][pages of a table], receives the bits of the kept slots."""
+        _, st = self._paged(cache, None, weight, kept)
+        import torch
+        s = cache._shape
+        if not (self._weights_ok(cache, weight) and kept.dtype in (torch.int64, torch.uint64) and kept.is_contiguous()
+                and kept.shape == (len(evictions), s[1], s[2], cache.table.shape[1])):
+            raise GooseError(GOOSE_ERR_ARG, "goose_pages_evict: shapes or types of weight or kept")
+        c = (_Eviction * len(evictions))(*[_Eviction(_i32(q["seq"]), _i32(q["keep"]), _i32(q.get("sink", 0)), _i32(q.get("recent", 0)))
+                                           for q in evictions])
+        _check(self.lib.goose_pages_evict(self._h, cache._ref, c, len(c), weight.data_ptr(), kept.data_ptr(), int(bool(reposition)), st),
+               "goose_pages_evict")
+
+    def goose_chunk_layer_paged(self, packed_layer, cache, layer, x, chunks, weight=None, decay=1.0):
+        """x: fp32 [rows][hidden], updated; weight: as for goose_attn_weight_paged, or None."""
+        r, st = self._paged(cache, chunks, packed_layer, x, weight, kind=PagedChunks)
+        import torch
+        if not (x.dtype == torch.float32 and x.dim() == 2 and x.is_contiguous() and x.shape[0] >= r.rows and x.shape[1] == self.desc.hidden
+                and (weight is None or self._weights_ok(cache, weight))):
+            raise GooseError(GOOSE_ERR_ARG, "goose_chunk_layer_paged: rows or type of x, or the weights' shape")
+        _check(self.lib.goose_chunk_layer_paged(self._h, _ptr(packed_layer), cache._ref, _i32(layer), _ptr(x), r._c, len(r), _ptr(weight), float(decay),
+                                                st), "goose_chunk_layer_paged")
 
     def goose_device_flags(self) -> int:
         out = C.c_int32(0)

@@ -8,7 +8,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libgoose.so")
 SOURCES = ["goose_api.hip", "kernels_small.hip", "f32_path.hip", "gemm_bf16.hip", "gemm_rows_bf16.hip", "gemm_row_bf16.hip", "attn_bf16.hip", "pages.hip",
-           "rope_paged.hip", "attn_paged.hip", "draft_host.cpp"]
+           "rope_paged.hip", "attn_paged.hip", "attn_chunk.hip", "attn_weight.hip", "pages_evict.hip", "draft_host.cpp"]
 
 
 def build(verbose: bool = False) -> str:

@@ -1,4 +1,5 @@
 // C ABI of the tree-verification library: argument checks, workspace, kernel sequencing.
+#include <float.h>
 #include <math.h>
 #include <stdlib.h>
 #include <string.h>
@@ -240,6 +241,7 @@ int goose_create_batched(const goose_model_desc* desc, int max_B, int max_rows, 
     A((void**)&c->att_ml, (size_t)d.n_heads * c->max_splits * c->Bpad * 2 * sizeof(float));
     A(&c->q, (size_t)c->Bpad * 2 * c->Kq * es);
     A((void**)&c->pages, sizeof(PageScratch));
+    A((void**)&c->lse, (size_t)d.n_heads * c->Bpad * sizeof(float));
   } else {
     A(&c->q, (size_t)c->Bpad * c->Kq * es);
   }
@@ -276,7 +278,7 @@ int goose_create_batched(const goose_model_desc* desc, int max_B, int max_rows, 
 void goose_destroy(goose_ctx* c) {
   if (!c) return;
   void* ptrs[] = {c->xn, c->part, c->q, c->o, c->h, c->att_o, c->att_ml, c->logits, c->top2, c->harvest, c->inv_freq, c->rope_cs,
-                  c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags, c->s_P, c->pages};
+                  c->s_mask, c->s_depth, c->s_pos, c->s_x, c->flags, c->s_P, c->pages, c->lse};
   for (void* p : ptrs)
     if (p) (void)hipFree(p);
   if (c->prof) {
@@ -463,6 +465,9 @@ struct PagedPass {
   const goose_pages* pages;
   int layer, shared_pages;
   PagedReqs pos, mask;  // the requests with their positions, and with their masks
+  const ChunkReqs* chunks = nullptr;  // the requests are chunks of new tokens instead (no masks); weight: their slots' weights grow, unless null
+  float* weight = nullptr;
+  float decay = 0.f;
 };
 static int layer_impl(goose_ctx* c, const char* w, float* d_x, void* d_kcache, void* d_vcache, int P,
                       const int32_t* dP, int B, const uint64_t* d_mask, hipStream_t st, bool xhat_ready,
@@ -504,8 +509,16 @@ static int layer_impl(goose_ctx* c, const char* w, float* d_x, void* d_kcache, v
                            c->part_ld, d.qk_norm ? w + c->pl.gq : nullptr, d.qk_norm ? w + c->pl.gk : nullptr, paged->pos, c->q, ldq,
                            q_terms, c->flags, st);
     if (rc) return rc;
-    rc = launch_attn_paged(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, paged->mask,
-                           paged->shared_pages, c->att_o, c->att_ml, attn_records(c), c->o, c->ld_o, c->act_dtype, T, c->flags, st);
+    if (paged->chunks) {
+      rc = launch_attn_chunk(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, *paged->chunks, c->o, c->ld_o,
+                             c->act_dtype, T, paged->weight ? c->lse : nullptr, c->Bpad, c->flags, st);
+      if (!rc && paged->weight)
+        rc = launch_attn_weight(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, *paged->chunks, c->lse,
+                                c->Bpad, paged->decay, paged->weight, c->flags, st);
+    } else {
+      rc = launch_attn_paged(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, paged->mask,
+                             paged->shared_pages, c->att_o, c->att_ml, attn_records(c), c->o, c->ld_o, c->act_dtype, T, c->flags, st);
+    }
   } else {
     PROF(PK_ATTN);
     rc = launch_attn_16(d.dtype, c->part, ks, pstride, c->part_ld, c->rope_cs, d.n_heads, c->n_kv, d.head_dim, c->cap, segs,
@@ -1019,6 +1032,118 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
   rc = launch_batch_accept(br, n, d_argmax_all, undone, st);
   if (rc) return rc;
   return launch_pages_commit(*pg, commit, d.n_layers, c->n_kv, d.head_dim, c->pages, true, c->flags, st);
+}
+
+// ---- chunks of new tokens, eviction
+// rows: the call works on stacked rows and launches by P_max.
+static int chunk_reqs(const goose_pages* pg, const goose_chunk* chunks, int n, bool rows, ChunkReqs* out) {
+  if (!chunks || n < 1 || n > GOOSE_MAX_REQUESTS) return GOOSE_ERR_ARG;
+  int row0 = 0;
+  out->n = n;
+  for (int i = 0; i < n; ++i) {
+    const goose_chunk& q = chunks[i];
+    if (q.seq < 0 || q.seq >= pg->n_seqs || q.C < 1 || q.C > GOOSE_MAX_CHUNK) return GOOSE_ERR_ARG;
+    for (int j = 0; j < i; ++j)
+      if (chunks[j].seq == q.seq) return GOOSE_ERR_ARG;
+    if (rows) {
+      if (q.P_max < 0) return GOOSE_ERR_ARG;
+      if ((long long)q.P_max + q.C > (long long)pg->table_ld * GOOSE_PAGE) return GOOSE_ERR_CAPACITY;
+    }
+    out->r[i] = ChunkReq{q.seq, q.C, rows ? q.P_max : 0, q.first, row0, q.d_pos};
+    out->rows = row0 + q.C;
+    row0 += round_up(q.C, 32);
+  }
+  return GOOSE_OK;
+}
+static int check_first(const ChunkReqs& ck) {
+  for (int i = 0; i < ck.n; ++i)
+    if (ck.r[i].first < 0 || ck.r[i].first >= ck.r[i].C) return GOOSE_ERR_ARG;
+  return GOOSE_OK;
+}
+static bool decay_ok(float decay) { return decay >= 0.f && decay <= FLT_MAX; }
+
+int goose_attn_chunk_paged(goose_ctx* c, const goose_pages* pg, int layer, const void* d_q, size_t ldq, int q_terms, const goose_chunk* chunks,
+                           int n, void* d_o, size_t ldo, int o_dtype, int o_terms, float* d_lse, size_t ld_lse, void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  if (!d_q || !d_o || layer < 0 || layer >= c->d.n_layers || !is16(o_dtype)) return GOOSE_ERR_ARG;
+  if ((q_terms != 1 && q_terms != 2) || (o_terms != 1 && o_terms != 2)) return GOOSE_ERR_ARG;
+  if (ldq < (size_t)c->Hq * q_terms || (ldq & 7) || ldo < (size_t)c->Hq * o_terms || (ldo & 7)) return GOOSE_ERR_ARG;
+  if (((uintptr_t)d_q & 15) || ((uintptr_t)d_o & 15) || ((uintptr_t)d_lse & 3)) return GOOSE_ERR_ARG;
+  ChunkReqs ck;
+  rc = chunk_reqs(pg, chunks, n, true, &ck);
+  if (rc) return rc;
+  if (d_lse && ld_lse < (size_t)ck.rows) return GOOSE_ERR_ARG;
+  return launch_attn_chunk(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, d_q, ldq, q_terms, ck, d_o, ldo, o_dtype, o_terms, d_lse,
+                           ld_lse, c->flags, as_stream(stream));
+}
+
+int goose_attn_weight_paged(goose_ctx* c, const goose_pages* pg, int layer, const void* d_q, size_t ldq, int q_terms, const goose_chunk* chunks,
+                            int n, const float* d_lse, size_t ld_lse, float decay, float* d_weight, void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  if (!d_q || !d_lse || !d_weight || layer < 0 || layer >= c->d.n_layers || (q_terms != 1 && q_terms != 2) || !decay_ok(decay)) return GOOSE_ERR_ARG;
+  if (ldq < (size_t)c->Hq * q_terms || (ldq & 7) || ((uintptr_t)d_q & 15) || ((uintptr_t)d_lse & 3) || ((uintptr_t)d_weight & 3)) return GOOSE_ERR_ARG;
+  ChunkReqs ck;
+  rc = chunk_reqs(pg, chunks, n, true, &ck);
+  if (!rc) rc = check_first(ck);
+  if (rc) return rc;
+  if (ld_lse < (size_t)ck.rows) return GOOSE_ERR_ARG;
+  return launch_attn_weight(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, d_q, ldq, q_terms, ck, d_lse, ld_lse, decay, d_weight,
+                            c->flags, as_stream(stream));
+}
+
+int goose_pages_append(goose_ctx* c, const goose_pages* pg, const goose_chunk* chunks, int n, void* stream) {
+  int rc = check_pages(c, pg);
+  ChunkReqs ck;
+  if (!rc) rc = chunk_reqs(pg, chunks, n, false, &ck);
+  return rc ? rc : launch_pages_append(*pg, ck, c->flags, as_stream(stream));
+}
+
+int goose_pages_evict(goose_ctx* c, const goose_pages* pg, const goose_eviction* evictions, int n, float* d_weight, uint64_t* d_kept, int reposition,
+                      void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  if (!evictions || n < 1 || n > GOOSE_MAX_REQUESTS || !d_weight || !d_kept || ((uintptr_t)d_weight & 3) || ((uintptr_t)d_kept & 7)) return GOOSE_ERR_ARG;
+  Evictions ev;
+  ev.n = n;
+  for (int i = 0; i < n; ++i) {
+    const goose_eviction& q = evictions[i];
+    if (q.seq < 0 || q.seq >= pg->n_seqs || q.keep < 1 || q.sink < 0 || q.recent < 0 || (long long)q.sink + q.recent > q.keep) return GOOSE_ERR_ARG;
+    for (int j = 0; j < i; ++j)
+      if (evictions[j].seq == q.seq) return GOOSE_ERR_ARG;
+    ev.r[i] = q;
+  }
+  return launch_pages_evict(c->d.dtype, *pg, ev, c->d.n_layers, c->n_kv, c->d.head_dim, c->inv_freq, d_weight, d_kept, reposition != 0, c->pages,
+                            c->flags, as_stream(stream));
+}
+
+int goose_chunk_layer_paged(goose_ctx* c, const void* d_packed_layer, const goose_pages* pg, int layer, float* d_x, const goose_chunk* chunks, int n,
+                            float* d_weight, float decay, void* stream) {
+  int rc = check_pages(c, pg);
+  if (rc) return rc;
+  if (!d_packed_layer || !d_x || layer < 0 || layer >= c->d.n_layers) return GOOSE_ERR_ARG;
+  if (d_weight && (((uintptr_t)d_weight & 3) || !decay_ok(decay))) return GOOSE_ERR_ARG;
+  PagedPass pass{};
+  pass.pages = pg;
+  pass.layer = layer;
+  pass.weight = d_weight;
+  pass.decay = decay;
+  ChunkReqs ck;
+  rc = chunk_reqs(pg, chunks, n, true, &ck);
+  if (!rc && d_weight) rc = check_first(ck);
+  if (rc) return rc;
+  if (round_up(ck.rows, 32) > c->max_rows) return GOOSE_ERR_CAPACITY;
+  pass.chunks = &ck;
+  pass.pos.n = n;
+  pass.pos.rows = 0;
+  for (int i = 0; i < n; ++i) {
+    const ChunkReq& q = ck.r[i];
+    pass.pos.r[i] = PagedReq{q.seq, q.C, q.P_max, q.row0, pass.pos.rows, q.pos, nullptr};
+    pass.pos.rows += q.C;
+  }
+  return layer_impl(c, (const char*)d_packed_layer, d_x, nullptr, nullptr, 0, nullptr, ck.rows, nullptr, as_stream(stream), false, nullptr, nullptr,
+                    nullptr, 0, &pass);
 }
 
 // ---- the LM head without a context: its workspace is a static device array --------------------

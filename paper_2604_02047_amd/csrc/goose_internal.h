@@ -84,6 +84,7 @@ struct goose_ctx {
   int32_t* flags;    // [1]
   int32_t* s_P;      // [GOOSE_MAX_REQUESTS] a host-supplied P for kernels that read it from memory; the old lengths while a step commits
   struct PageScratch* pages;  // what the kernels of a paged call tell each other (16-bit models)
+  float* lse;        // f32 [n_heads][Bpad] logarithms of the softmax sums of a chunk (16-bit models)
   goose_prof* prof;  // optional per-kernel event timing
 };
 
@@ -277,7 +278,7 @@ struct PagedReq {
   int32_t seq, B, P_max;
   int32_t row0;  // its first row of the stacked buffers (multiples of 32)
   int32_t c0;    // its first row when the rows between requests are left out
-  const void* p; // mask (attention), positions (rotation), path (commit)
+  const void* p; // mask (attention), positions (rotation; null: P + node), path (commit)
   const int32_t* accept_len;
 };
 struct PagedReqs {
@@ -315,3 +316,26 @@ int launch_rope_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
 int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
                       const PagedReqs& rq, int shared_pages, float* ws_o, float* ws_ml, size_t max_records, void* o, size_t ldo,
                       int o_dtype, int o_terms, int32_t* flags, hipStream_t st);
+
+// ---- chunks of new tokens on a paged cache, eviction (attn_chunk.hip, attn_weight.hip, pages_evict.hip; 16-bit types)
+struct ChunkReq {
+  int32_t seq, C, P_max, first;
+  int32_t row0;        // its first row of the stacked buffers (multiples of 32)
+  const int32_t* pos;  // or null
+};
+struct ChunkReqs {
+  int32_t n, rows;  // chunks; rows that they reach into
+  ChunkReq r[GOOSE_MAX_REQUESTS];
+};
+int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
+                      const ChunkReqs& ck, void* o, size_t ldo, int o_dtype, int o_terms, float* lse, size_t ld_lse, int32_t* flags,
+                      hipStream_t st);
+int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
+                       const ChunkReqs& ck, const float* lse, size_t ld_lse, float decay, float* weight, int32_t* flags, hipStream_t st);
+int launch_pages_append(const goose_pages& pg, const ChunkReqs& ck, int32_t* flags, hipStream_t st);
+struct Evictions {
+  int32_t n;
+  goose_eviction r[GOOSE_MAX_REQUESTS];
+};
+int launch_pages_evict(int dtype, const goose_pages& pg, const Evictions& ev, int n_layers, int n_kv, int head_dim, const double* inv_freq,
+                       float* weight, uint64_t* kept, bool reposition, PageScratch* scratch, int32_t* flags, hipStream_t st);

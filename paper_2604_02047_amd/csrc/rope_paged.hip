@@ -108,7 +108,8 @@ __global__ __launch_bounds__(2 * D) void k_rope_paged(const RopePagedArgs a, con
     const int h = part * Q_HEADS + tid / TPH;
     f32x4 lo, hi;
     const int hc = h < a.n_heads ? h : a.n_heads - 1;  // (threads behind the last head: loads stay inside, nothing is stored)
-    const int pos = static_cast<const int32_t*>(rq.r[r].p)[node];
+    const int32_t* const at = static_cast<const int32_t*>(rq.r[r].p);
+    const int pos = at ? at[node] : a.len[rq.r[r].seq] + node;
     sum_slices(a.part + row * a.ld + hc * D + j0, a.split_stride, a.ks, HALF, lo, hi);
     if (tid < HALF) cs[0][tid] = angle(pos, a.inv_freq[tid]);
     __syncthreads();
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(2 * D) void k_rope_paged(const RopePagedArgs a, con
   }
   for (int t = tid; t < 8 * HALF; t += 2 * D) {
     const int i = i0 + t / HALF;
-    if (i >= 0 && i < q.B) cs[t / HALF][t % HALF] = angle(pos[i], a.inv_freq[t % HALF]);
+    if (i >= 0 && i < q.B) cs[t / HALF][t % HALF] = angle(pos ? pos[i] : P + i, a.inv_freq[t % HALF]);
   }
   const size_t head = page_head<D>(page, a.n_kv, kvh);
   const int kcol = (a.n_heads + kvh) * D, vcol = kcol + a.n_kv * D;

@@ -213,13 +213,20 @@ class BatchedGooseDecoder:
 class PagedGooseDecoder(BatchedGooseDecoder):
     """Several requests over one paged cache (goose_verify_step_paged).  Sequence 0 holds the tokens that all prompts begin with; every
     request's sequence is forked off it, so that the whole pages among them are shared, and gets its own pages from there on.
-    `gm` as for BatchedGooseDecoder; its own contiguous caches are not used.  n_pages: pages of the pool; max_slots: cache slots of a request."""
+    `gm` as for BatchedGooseDecoder; its own contiguous caches are not used.  n_pages: pages of the pool; max_slots: cache slots of a request.
+    prompt_rows > 0: prompts are fed in chunks of up to that many tokens (goose_chunk_layer_paged; at most gm's max_rows) instead of chain trees of
+    max_B nodes.  keep > 0 (with prompt_rows): a request whose prompt has more than `keep` tokens goes on with that many cache slots
+    (goose_pages_evict): the first `sink` and whatever it shares, the last `recent`, and those that its prompt's attention weighs most.  Its output is then no longer
+    that of greedy decoding over the whole prompt."""
 
-    def __init__(self, gm: GooseModel, n_requests, n_pages, max_slots, **options):
+    def __init__(self, gm: GooseModel, n_requests, n_pages, max_slots, prompt_rows=0, keep=0, sink=4, recent=64, **options):
         super().__init__(gm, n_requests, **options)
         self.cache = gm.paged_cache(n_pages, n_requests + 1, max_slots)
         self.max_slots, self.shared_pages = self.cache.table.shape[1] * gb.GOOSE_PAGE, 0
         self.mask = torch.zeros(256, dtype=torch.int64, device=gm.device)
+        assert 0 <= prompt_rows <= gm.ctx.max_rows and (keep == 0 or prompt_rows > 0) and keep >= 0 and sink >= 0 and recent >= 0
+        self.prompt_rows, self.keep, self.sink, self.recent = prompt_rows, keep, sink, recent
+        self.weight = gm.slot_weights(self.cache) if keep else None
 
     def _make_request(self, gm, K):
         return _Request(gm, K, kcache=False, vcache=False)  # (no caches of its own)
@@ -249,6 +256,45 @@ class PagedGooseDecoder(BatchedGooseDecoder):
         _require_clean(c.goose_device_flags())
         return int(gm.argmax[n - 1].item())
 
+    def _feed_chunks(self, seq, done, tokens, q):
+        """_feed in chunks of prompt_rows tokens."""
+        gm, c, H = self.gm, self.gm.ctx, self.gm.desc.hidden
+        x = torch.empty((self.prompt_rows, H), dtype=torch.float32, device=gm.device)
+        t = torch.as_tensor(np.asarray(tokens, np.int32), device=gm.device)
+        for o in range(0, len(tokens), self.prompt_rows):
+            n = min(self.prompt_rows, len(tokens) - o)
+            _require_room(done, n, self.max_slots)
+            parts = [(a, min(gm.max_B, n - a)) for a in range(0, n, gm.max_B)]
+            chunk = gb.PagedChunks([{"seq": seq, "C": n, "P_max": done}])
+            c.goose_pages_reserve(self.cache, [seq], [n])
+            for a, b in parts:
+                c.goose_embed(gm.embed, t[o + a:], b, x[a:])
+            for l in range(gm.desc.n_layers):
+                c.goose_chunk_layer_paged(gm.packed_layer(l), self.cache, l, x, chunk, self.weight)
+            for a, b in parts:
+                logits = torch.empty((b, gm.desc.vocab), dtype=torch.float32, device=gm.device)
+                c.goose_lm_head_argmax(gm.packed_head, x[a:], b, gm.argmax, logits, None)
+                c.goose_harvest_topk(logits, gm.desc.vocab, t[o + a:], b, q.K, q.d_ids, q.d_scores)
+            c.goose_pages_append(self.cache, chunk)
+            done += n
+        _require_clean(c.goose_device_flags())
+        return int(gm.argmax[b - 1].item())
+
+    def _cut(self):
+        """Every request down to `keep` slots; what it shares with the others stays where it is."""
+        n, sink = len(self.reqs), max(self.sink, self.shared_pages * gb.GOOSE_PAGE)
+        if any(q.P > self.keep for q in self.reqs) and sink + self.recent > self.keep:
+            raise gb.GooseError(gb.GOOSE_ERR_ARG, f"{self.keep} slots do not hold the {sink} first and the {self.recent} last ones")
+        cut = [r for r, q in enumerate(self.reqs) if q.P > self.keep]
+        if not cut:
+            return
+        d = self.gm.desc
+        kept = torch.empty((len(cut), d.n_layers, d.kv_heads, self.cache.table.shape[1]), dtype=torch.int64, device=self.gm.device)
+        self.gm.ctx.goose_pages_evict(self.cache, [{"seq": r + 1, "keep": self.keep, "sink": sink, "recent": self.recent} for r in cut], self.weight, kept)
+        _require_clean(self.gm.ctx.goose_device_flags())
+        for r in cut:
+            self.reqs[r].P = self.keep
+
     def prefill(self, prompts):
         """The common beginning once, then every prompt's rest; returns the first generated token of each."""
         prompts = [[int(t) for t in p] for p in prompts]
@@ -264,19 +310,24 @@ class PagedGooseDecoder(BatchedGooseDecoder):
             q.h_ids.fill(-1)
             q.h_scores.fill(0)
             q.p_hat, q.trace = 0.3, []
+        feed = self._feed_chunks if self.prompt_rows else self._feed
         if common:
-            self._feed(0, 0, prompts[0][:common], first)
+            feed(0, 0, prompts[0][:common], first)
             c.goose_pages_fork(self.cache, 0, list(range(1, len(prompts) + 1)))
+            if self.weight is not None:
+                self.weight[:, 1:] = self.weight[:, :1]
         self.shared_pages = common // gb.GOOSE_PAGE
         for q in self.reqs[1:]:
             q.d_ids.copy_(first.d_ids)
             q.d_scores.copy_(first.d_scores)
         out = []
         for r, (q, p) in enumerate(zip(self.reqs, prompts)):
-            q.anchor = self._feed(r + 1, common, p[common:], q)
+            q.anchor = feed(r + 1, common, p[common:], q)
             q.P, q.seq = len(p), p + [q.anchor]
             q.mirror_rows(p)
             out.append(q.anchor)
+        if self.keep:
+            self._cut()
         return out
 
     def cycle(self, active):

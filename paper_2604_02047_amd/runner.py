@@ -106,6 +106,11 @@ class GooseModel:
         self.ctx.goose_pages_clear(cache)
         return cache
 
+    def slot_weights(self, cache: PagedCache):
+        """What goose_attn_weight_paged writes for a paged cache of this model, all zero."""
+        shape = (self.desc.n_layers, cache.table.shape[0], self.desc.kv_heads, cache.table.shape[1] * GOOSE_PAGE)
+        return torch.zeros(shape, dtype=torch.float32, device=self.device)
+
     def model_ptrs(self):
         return {"embed": self.embed, "packed_layers": self.packed_layers, "packed_head": self.packed_head,
                 "kcache": self.kcache, "vcache": self.vcache}
