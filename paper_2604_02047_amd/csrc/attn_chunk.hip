@@ -4,111 +4,314 @@
 //
 // The rows of one KV head are (token, query head of the group), the heads fastest, so that a group's heads share what is read of the
 // pages.  Per 32 keys and 32 rows: S^T = K Q^T, online softmax with two lanes a row, O^T += V^T P^T, operands straight from the pages'
-// operand order.  A workgroup takes 128 rows, a wavefront 32 of them, and streams the blocks that its tokens see.
+// operand order.
 #include "chunk.h"
 
 namespace {
 
+struct ChunkItems {
+  int32_t tiles, splits;  // work items: tiles of 256 rows x ranges of their blocks, for every KV head
+  int32_t pair0;          // its first (token, head) pair in the merge
+  uint32_t rec0;          // its first record
+};
 struct ChunkArgs {
   const void* kpool;  // of the layer
   const void* vpool;
   const int32_t* table;
   const int32_t* len;
   const void* q;
+  float* ws_o;    // [record][d]; records of a chunk: [split][token][head]
+  float* ws_ml;   // [record][2]: largest score (unscaled), sum of weights
   unsigned short* o;
   float* lse;
   int32_t* flags;
   size_t ldq, ldo, ld_lse;
-  int32_t table_ld, n_pages, n_kv, group, n;
+  int32_t table_ld, n_pages, n_heads, n_kv, group, n;
   int32_t o_terms, o_f16;
-  int32_t tiles[GOOSE_MAX_REQUESTS];
+  ChunkItems it[GOOSE_MAX_REQUESTS];
   ChunkReq r[GOOSE_MAX_REQUESTS];
 };
 
-template <int D, int QT, bool F16>
-__global__ __launch_bounds__(256, 2) void k_chunk_stream(const ChunkArgs a) {
-  typedef RowTile<D, QT, F16> Tile;
+__device__ __forceinline__ void finish(const ChunkArgs& a, size_t row, int h, int D, int c, const f32x4& x, float m, float l) {
+  store_columns(a.o + row * a.ldo, a.o_terms, a.o_f16, h * D + c, x * (l == 0.f ? 0.f : 1.0f / l));
+  if (a.lse != nullptr && c == 0) a.lse[(size_t)h * a.ld_lse + row] = log_of_sum(m, l, softmax_scale(D));
+}
+
+// One workgroup = eight wavefronts, two on a SIMD, 32 rows each x a range of blocks.  Every block comes into LDS once, global -> LDS without
+// registers, into a ring that runs several blocks ahead; a wavefront has three blocks under way at once (ring_step).  Blocks that a
+// wavefront's rows do not see whole are masked on the way, and behind the last one that it sees it only goes on copying.
+// A weight of zero does not keep a NaN or an infinity of an unseen slot's values out of the matrix instruction: a wavefront that has such a thing in its
+// outputs at the end starts again, block by block with values_odd.  The block that the chunk ends in, whose other slots may hold anything, follows that way always.
+template <int D, int QT, bool F16, int PT>
+__global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
+  typedef RowTile<D, QT, F16, PT> Tile;
   typedef typename Tile::T T;
   constexpr int NS = D / 16;
+  constexpr int BLOCK = 2 * NS * 1024, BU = BLOCK / 16;  // keys and values of 32 slots: bytes, 16-byte units
+  constexpr int RING = 8;                                // blocks
+  constexpr int CP = 2 * NS / 8;                         // pieces of 1 KiB that a wavefront copies of a block
+  constexpr int AHEAD = 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[RING * BLOCK];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l31 = lane & 31, hh = lane >> 5;
   int y = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)a.n_kv));
-  const int kvh = (int)blockIdx.x - y * a.n_kv;
+  const int kvh = (int)blockIdx.x - y * a.n_kv;  // the fast index: where 8 divides the KV heads, all items of a head run on one XCD
   int ri = 0;
-  while (y >= a.tiles[ri]) y -= a.tiles[ri++];
+  while (y >= a.it[ri].tiles * a.it[ri].splits) { y -= a.it[ri].tiles * a.it[ri].splits; ++ri; }
   const ChunkReq& rq = a.r[ri];
+  const ChunkItems& ci = a.it[ri];
   const int P = chunk_length(a.len, rq, a.flags, tid == 0 && y == 0 && kvh == 0);
-  const int rows = rq.C * a.group, row_first = y * 128 + wave * 32;
-  if (row_first >= rows) return;
-  const int rho = min(row_first + l31, rows - 1);
-  const int tok = (int)((unsigned)rho / (unsigned)a.group), h = kvh * a.group + rho - tok * a.group;
-  const int tok_lo = __builtin_amdgcn_readfirstlane((int)((unsigned)row_first / (unsigned)a.group));
-  const int tok_hi = __builtin_amdgcn_readfirstlane((int)((unsigned)min(row_first + 31, rows - 1) / (unsigned)a.group));
-  const int total = (P + tok_hi) / 32 + 1, full = (P + tok_lo + 1) / 32;  // blocks that a row sees, that all rows see whole
-  PageIds pg{a.table + (size_t)rq.seq * a.table_ld, a.flags, 0, (total - 1) >> 1, a.n_pages, 0};
-  pg.load(lane);
-  const T* const kp = static_cast<const T*>(a.kpool);
-  const T* const vp = static_cast<const T*>(a.vpool);
-  auto block_at = [&](int b) -> size_t {
-    return ((size_t)pg.of(b, lane) * a.n_kv + kvh) * (GOOSE_PAGE * D) + (size_t)(b & 1) * 32 * D;
+  const int split = __builtin_amdgcn_readfirstlane((int)((unsigned)y / (unsigned)ci.tiles));
+  const int tile = ci.tiles - 1 - (y - split * ci.tiles);  // (the longest first)
+  const int rows = rq.C * a.group, wg_first = tile * 256, row_first = wg_first + wave * 32;
+  auto token_of = [&](int rho) { return __builtin_amdgcn_readfirstlane((int)((unsigned)min(rho, rows - 1) / (unsigned)a.group)); };
+  auto clamp = [](int x, int lo, int hi) { return min(max(x, lo), hi); };
+  // blocks that the tile's last row sees, this item's range of them, and the blocks of it in front of the chunk's end
+  const int total = (P + token_of(wg_first + 255)) / 32 + 1;
+  const int b_lo = __builtin_amdgcn_readfirstlane((int)((unsigned)(total * split) / (unsigned)ci.splits));
+  const int b_hi = __builtin_amdgcn_readfirstlane((int)((unsigned)(total * (split + 1)) / (unsigned)ci.splits));
+  const int units = clamp((P + rq.C) / 32 - b_lo, 0, b_hi - b_lo);
+  // of the ring's units: from `whole` on some rows of this wavefront do not see all of it, from `seen` on none sees any
+  const int whole = (P + token_of(row_first) + 1) / 32 - b_lo, seen = row_first < rows ? clamp((P + token_of(row_first + 31)) / 32 + 1 - b_lo, 0, units) : -1;
+  PageIds pg{a.table + (size_t)rq.seq * a.table_ld, a.flags, b_lo >> 1, (b_hi - 1) >> 1, a.n_pages, 0};
+  if (b_hi > b_lo) pg.load(lane);
+  const char* const kp = static_cast<const char*>(a.kpool);
+  const char* const vp = static_cast<const char*>(a.vpool);
+  auto block_at = [&](int b) -> size_t {  // bytes (pages times KV heads stays below 2^29: checked on the host)
+    return (size_t)(unsigned)((pg.of(b, lane) * a.n_kv + kvh) * 2 + (b & 1)) * (32 * D * 2);
   };
-  u32x4 kreg[NS], vreg[NS];
-  size_t at = block_at(0);
-  fetch(kp + at, lane, kreg);
-  fetch(vp + at, lane, vreg);
+  const int last = P + (int)((unsigned)min(row_first + l31, rows - 1) / (unsigned)a.group) - b_lo * 32 - hh * 16;  // the last slot that this lane's row sees
+  auto query = [&](int rho) -> const T* {
+    const int at = min(rho, rows - 1), tok = (int)((unsigned)at / (unsigned)a.group), h = kvh * a.group + at - tok * a.group;
+    return static_cast<const T*>(a.q) + ((size_t)rq.row0 + tok) * a.ldq + ((size_t)h * D + hh * 8) * QT;
+  };
   Tile t;
-  const size_t row = (size_t)rq.row0 + tok;
-  t.init(static_cast<const T*>(a.q) + row * a.ldq + ((size_t)h * D + hh * 8) * QT);
+  t.init(query(row_first + l31));
   const float scale = softmax_scale(D);
-  auto block = [&](int b, auto edge) {
-    constexpr bool EDGE = decltype(edge)::value;
-    t.scores(kreg);
-    if (b + 1 < total) { at = block_at(b + 1); fetch(kp + at, lane, kreg); }
-    unsigned vis = 0xFFFFu;
-    bool odd = false;
-    if (EDGE) {
-      vis = seen16(P + tok - b * 32 - hh * 16);
-      t.mask(vis);
-      odd = clean_values<F16>(vreg, P + rq.C - b * 32 - hh * 16);
-    }
-    t.maximum();
-    t.rescale(scale);
-    t.weights();
-    if (EDGE && odd) t.values_odd(vreg, vis);
-    else t.values(vreg);
-    if (b + 1 < total) fetch(vp + at, lane, vreg);
+  const bool keys = wave < 4;          // the first four wavefronts copy keys, the others values
+  const int share = wave * CP * 1024;  // this wavefront's pieces of a block
+  const char* const pool = (keys ? kp : vp) + (wave & 3) * CP * 1024;
+  auto barrier = [&]() {  // (raw: __syncthreads would also drain every copy in flight)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
-  for (int b = 0; b < full; ++b) block(b, std::false_type());
-  for (int b = full; b < total; ++b) block(b, std::true_type());
-
-  const float l = t.l + __shfl_xor(t.l, 32, 64);
-  if (row_first + l31 >= rows) return;
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const u32x4* const base = reinterpret_cast<const u32x4*>(ring) + lane;
+  auto keys_of = [&](int u) { return base + (u & (RING - 1)) * BU; };
+  if (units > 0) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (all that was loaded so far: the counts below are those of the ring's copies)
+    int next = 0;  // the unit copied next
+    auto copy = [&]() {  // (behind the range: its last block again, never used)
+      copy_pieces<CP>(pool + block_at(min(b_lo + next, b_hi - 1)), lane, ring + (next & (RING - 1)) * BLOCK + share);
+      ++next;
+    };
+    const int first = keys ? RING : RING - 1;
+    while (next < first) copy();
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3) * CP));  // units 0 to 2 (values: 0 and 1)
+    barrier();
+    u32x4 pc[AHEAD];
+    f32x16 z1;
+    typename Tile::op8 w1[2], wl1[2];
+    if (seen > 0) {
+      u32x4 k[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) k[s] = keys_of(0)[s * 64];
+      t.scores(k);
+      if (whole <= 0) t.mask(seen16(last));
+      t.maximum();
+      t.rescale(scale);
+      t.weights();
+#pragma unroll
+      for (int s = 0; s < NS; ++s) k[s] = keys_of(1)[s * 64];
+      t.scores(k);
+      if (whole <= 1) t.mask(seen16(last - 32));
+      t.maximum();
+      t.rescale_later(scale, t.s, units > 1);
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) pc[n] = keys_of(2)[n * 64];
+    }
+    barrier();
+    if (keys) copy();  // (unit RING, where unit 0 was)
+    // Before step j the keys of unit j + 2 and the values of unit j - 1 have landed in every wavefront's share; keys of unit j and values of
+    // unit j - 2 are no longer read, and make room for those RING units later.
+    auto step = [&](int j, const f32x16& za, f32x16& zb, const auto& w, const auto& wl, auto& wn, auto& wln) {
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3) * CP));
+      barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      copy();
+      if (j > seen || seen == 0) return;
+      ring_step<D, QT, F16, PT, 1, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale,
+                                          [&](f32x16& s) {
+                                            if (j + 1 >= whole) {
+                                              const unsigned vis = seen16(last - (j + 1) * 32);
+#pragma unroll
+                                              for (int r = 0; r < 16; ++r) s[r] = ((vis >> r) & 1u) ? s[r] : -INFINITY;
+                                            }
+                                          });
+    };
+    int j = 1;
+    for (; j + 1 < units; j += 2) {
+      step(j, t.s, z1, t.p, t.pl, w1, wl1);
+      step(j + 1, z1, t.s, w1, wl1, t.p, t.pl);
+    }
+    if (j < units) {
+      step(j, t.s, z1, t.p, t.pl, w1, wl1);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        t.p[i] = w1[i];
+        t.pl[i] = wl1[i];
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // (the last values, and copies behind the range)
+    barrier();
+    if (seen == units) {
+      u32x4 v[NS];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) v[s] = keys_of(units - 1)[BU / 2 + s * 64];
+      t.values(v);
+    }
+  }
+  if (row_first >= rows) return;
+  // ---- the block that the chunk ends in (in LDS already where the ring ran), or all of them again from memory
+  // (the row and its query again: kept over the ring's loop they would take registers that it needs)
+  int rho = row_first + l31;
+  GOOSE_HERE(rho);
+  const int tok = (int)((unsigned)min(rho, rows - 1) / (unsigned)a.group), h = kvh * a.group + rho - tok * a.group;
+  const int end = min(b_hi, (P + token_of(row_first + 31)) / 32 + 1);
+  float odd_out = 0.f;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      store_columns(a.o + row * a.ldo, a.o_terms, a.o_f16, h * D + (dt * 4 + q) * 8 + hh * 4,
-                    f32x4{t.o[dt][q * 4], t.o[dt][q * 4 + 1], t.o[dt][q * 4 + 2], t.o[dt][q * 4 + 3]} * inv);
-  if (a.lse && hh == 0) a.lse[(size_t)h * a.ld_lse + row] = log_of_sum(t.m, l, scale);
+    for (int r = 0; r < 16; ++r) odd_out = fmaf(t.o[dt][r], 0.f, odd_out);
+  const bool again = units > 0 && __builtin_amdgcn_ballot_w64(odd_out != 0.f) != 0;
+  if (again || b_lo + units < end) {
+    if (again) t.init(query(rho));
+    else t.load_q(query(rho));
+    pg.base = (again ? b_lo : b_lo + units) >> 1;  // (the window may have run ahead)
+    pg.load(lane);
+#pragma unroll 1
+    for (int u = again ? 0 : units, b = b_lo + u; b < end; ++u, ++b) {
+      u32x4 k[NS], v[NS];
+      if (u == units && units > 0) {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          k[s] = keys_of(u)[s * 64];
+          v[s] = keys_of(u)[BU / 2 + s * 64];
+        }
+      } else {
+        const size_t at = block_at(b);
+        fetch(kp + at, lane, k);
+        fetch(vp + at, lane, v);
+      }
+      const unsigned vis = seen16(P + tok - b * 32 - hh * 16);
+      t.scores(k);
+      t.mask(vis);
+      const bool odd = clean_values<F16>(v, P + rq.C - b * 32 - hh * 16);
+      t.maximum();
+      t.rescale(scale);
+      t.weights();
+      if (odd) t.values_odd(v, vis);
+      else t.values(v);
+    }
+  }
+  const float l = t.l + __shfl_xor(t.l, 32, 64);
+  if (rho >= rows) return;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 x = {t.o[dt][q * 4], t.o[dt][q * 4 + 1], t.o[dt][q * 4 + 2], t.o[dt][q * 4 + 3]};
+      const int c = (dt * 4 + q) * 8 + hh * 4;
+      if (ci.splits == 1) {
+        finish(a, (size_t)rq.row0 + tok, h, D, c, x, t.m, l);
+      } else {
+        const size_t rec = ci.rec0 + ((size_t)split * rq.C + tok) * a.n_heads + h;
+        if (c == 0) *reinterpret_cast<float2*>(a.ws_ml + rec * 2) = make_float2(t.m, l);
+        *reinterpret_cast<f32x4*>(a.ws_o + rec * D + c) = x;
+      }
+    }
 }
 
+// Joins the splits of a row: D / 4 threads a (token, head), four columns each, records in their order, four in flight together.
 template <int D>
-void launch_d(bool f16, int q_terms, dim3 grid, const ChunkArgs& a, hipStream_t st) {
-  if (q_terms == 2) {
-    if (f16) hipLaunchKernelGGL((k_chunk_stream<D, 2, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_chunk_stream<D, 2, false>), grid, dim3(256), 0, st, a);
-  } else {
-    if (f16) hipLaunchKernelGGL((k_chunk_stream<D, 1, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_chunk_stream<D, 1, false>), grid, dim3(256), 0, st, a);
+__global__ __launch_bounds__(256) void k_chunk_merge(const ChunkArgs a, int pairs) {
+  constexpr int TPR = D / 4;
+  const int tid = threadIdx.x, c = (tid % TPR) * 4;
+  int pair = blockIdx.x * (256 / TPR) + tid / TPR;
+  if (pair >= pairs) return;
+  int r = 0;
+  while (r + 1 < a.n && pair >= a.it[r + 1].pair0) ++r;
+  pair -= a.it[r].pair0;
+  const size_t step = (size_t)a.r[r].C * a.n_heads, rec0 = a.it[r].rec0 + (size_t)pair;
+  const int n = a.it[r].splits;
+  const float scale = softmax_scale(D);
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  float den = 0.f, m = -INFINITY;
+  for (int s0 = 0; s0 < n; s0 += 4) {
+    float2 ml[4];
+    f32x4 ov[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const size_t rec = rec0 + (size_t)min(s0 + k, n - 1) * step;
+      ml[k] = *reinterpret_cast<const float2*>(a.ws_ml + rec * 2);
+      ov[k] = *reinterpret_cast<const f32x4*>(a.ws_o + rec * D + c);
+    }
+    float m_new = m;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m_new = fmaxf(m_new, ml[k].x);
+    const float w0 = join_factor(m, m_new, scale);
+    den *= w0;
+    num *= w0;
+    m = m_new;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (s0 + k < n) {
+        const float w = join_factor(ml[k].x, m, scale);
+        den = fmaf(w, ml[k].y, den);
+        num += w * ov[k];
+      }
   }
+  const int tok = (int)((unsigned)pair / (unsigned)a.n_heads);
+  finish(a, (size_t)a.r[r].row0 + tok, pair - tok * a.n_heads, D, c, num, m, den);
+}
+
+template <int D, int QT, bool F16>
+void launch_t(int p_terms, dim3 grid, const ChunkArgs& a, hipStream_t st) {
+  if (p_terms == 1) hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, 1>), grid, dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, 2>), grid, dim3(512), 0, st, a);
+}
+template <int D>
+void launch_d(bool f16, int q_terms, int p_terms, dim3 grid, const ChunkArgs& a, hipStream_t st) {
+  if (q_terms == 2) f16 ? launch_t<D, 2, true>(p_terms, grid, a, st) : launch_t<D, 2, false>(p_terms, grid, a, st);
+  else f16 ? launch_t<D, 1, true>(p_terms, grid, a, st) : launch_t<D, 1, false>(p_terms, grid, a, st);
 }
 
 }  // namespace
 
 int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
-                      const ChunkReqs& ck, void* o, size_t ldo, int o_dtype, int o_terms, float* lse, size_t ld_lse, int32_t* flags,
-                      hipStream_t st) {
+                      const ChunkReqs& ck, float* ws_o, float* ws_ml, size_t max_records, void* o, size_t ldo, int o_dtype, int o_terms, float* lse,
+                      size_t ld_lse, int32_t* flags, hipStream_t st) {
+  if (head_dim != 64 && head_dim != 128) return GOOSE_ERR_SHAPE;
+  const int group = n_heads / n_kv;
+  // Chunks of few rows are chains of nodes for the tree kernels, which have shapes for them.
+  PagedReqs few{};
+  ChunkReqs many{};
+  const int few_rows = 128;
+  for (int i = 0; i < ck.n; ++i) {
+    const ChunkReq& c = ck.r[i];
+    if (c.C <= GOOSE_MAX_B && c.C * group <= few_rows) {
+      few.r[few.n++] = PagedReq{c.seq, c.C, c.P_max, c.row0, few.rows, nullptr, nullptr};
+      few.rows += c.C;
+    } else {
+      many.r[many.n++] = c;
+    }
+  }
+  if (few.n > 0) {
+    const int rc = launch_attn_paged(dtype, pg, layer, n_heads, n_kv, head_dim, q, ldq, q_terms, few, 0, ws_o, ws_ml, max_records, o, ldo, o_dtype,
+                                     o_terms, flags, st, lse, ld_lse);
+    if (rc != GOOSE_OK || many.n == 0) return rc;
+  }
   const size_t layer0 = (size_t)layer * page_layer_elems(pg, n_kv, head_dim) * 2;  // bytes
   ChunkArgs a{};
   a.kpool = static_cast<const char*>(pg.d_kpool) + layer0;
@@ -116,6 +319,8 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.table = pg.d_table;
   a.len = pg.d_len;
   a.q = q;
+  a.ws_o = ws_o;
+  a.ws_ml = ws_ml;
   a.o = (unsigned short*)o;
   a.lse = lse;
   a.flags = flags;
@@ -124,22 +329,66 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.ld_lse = ld_lse;
   a.table_ld = pg.table_ld;
   a.n_pages = pg.n_pages;
+  a.n_heads = n_heads;
   a.n_kv = n_kv;
-  a.group = n_heads / n_kv;
-  a.n = ck.n;
+  a.group = group;
+  a.n = many.n;
   a.o_terms = o_terms;
   a.o_f16 = o_dtype == GOOSE_DTYPE_F16;
-  unsigned items = 0;
-  for (int i = 0; i < ck.n; ++i) {
-    a.r[i] = ck.r[i];
-    a.tiles[i] = (ck.r[i].C * a.group + 127) / 128;
-    items += (unsigned)a.tiles[i];
+  // a weight carries as many bits as the output keeps
+  const int p_terms = o_terms == 1 && (o_dtype == GOOSE_DTYPE_BF16 || dtype == GOOSE_DTYPE_F16) ? 1 : 2;
+  // Work items run in rounds of 256 workgroups, the longest first.  In units of 10 ns: an item's fixed part, a block of it, the merge and its records.
+  const long long fixed = 700, step = (30 + 34 * (q_terms + p_terms)) * (head_dim + 64) / 192;
+  long long best = INT64_MAX;
+  int best_per = 0;
+  int longest = 0;
+  for (int i = 0; i < many.n; ++i) {
+    const int blocks = (many.r[i].P_max + many.r[i].C + 31) / 32;
+    longest = blocks > longest ? blocks : longest;
   }
-  if ((unsigned long long)items * n_kv > INT32_MAX) return GOOSE_ERR_CAPACITY;
-  const dim3 grid(items * (unsigned)n_kv);
+  auto splits_of = [](int blocks, int per) { return (blocks + per - 1) / per; };
+  for (int parts = 1; parts <= 32 && parts <= longest; ++parts) {
+    const int per = splits_of(longest, parts);
+    long long work = 0, items = 0, most = 0, records = 0;
+    for (int i = 0; i < many.n; ++i) {
+      const ChunkReq& c = many.r[i];
+      const long long tiles = ((long long)c.C * group + 255) / 256;
+      const int blocks = (c.P_max + c.C + 31) / 32, splits = splits_of(blocks, per);
+      const long long sum = tiles * (2ll * c.P_max + c.C) / 64 + 2 * tiles;  // blocks of all tiles
+      work += (sum * step + tiles * splits * fixed) * n_kv;
+      items += tiles * splits * n_kv;
+      const long long len = splits_of(blocks, splits) * step + fixed;
+      most = len > most ? len : most;
+      if (splits > 1) records += (long long)splits * c.C * n_heads;
+    }
+    if (records > (long long)max_records || records > UINT32_MAX) continue;
+    const long long rounds = (items + 255) / 256, time = rounds * (work / items);
+    const long long cost = (time > most ? time : most) + (records > 0 ? 600 + records * head_dim * 8 / 50000 : 0);
+    if (cost < best) { best = cost; best_per = per; }
+  }
+  if (best_per == 0) best_per = longest;
+  size_t records = 0, pairs = 0;
+  long long items = 0;
+  for (int i = 0; i < many.n; ++i) {
+    const ChunkReq& c = many.r[i];
+    const int tiles = (c.C * group + 255) / 256, splits = splits_of((c.P_max + c.C + 31) / 32, best_per);
+    a.it[i] = ChunkItems{tiles, splits, (int32_t)pairs, (uint32_t)records};
+    if (splits > 1) {
+      records += (size_t)splits * c.C * n_heads;
+      pairs += (size_t)c.C * n_heads;
+    }
+    a.r[i] = c;
+    items += (long long)tiles * splits * n_kv;
+  }
+  if (items > INT32_MAX || pairs > INT32_MAX) return GOOSE_ERR_CAPACITY;
   const bool f16 = dtype == GOOSE_DTYPE_F16;
-  if (head_dim == 128) launch_d<128>(f16, q_terms, grid, a, st);
-  else if (head_dim == 64) launch_d<64>(f16, q_terms, grid, a, st);
-  else return GOOSE_ERR_SHAPE;
+  if (head_dim == 128) launch_d<128>(f16, q_terms, p_terms, dim3((unsigned)items), a, st);
+  else launch_d<64>(f16, q_terms, p_terms, dim3((unsigned)items), a, st);
+  const int rc = goose_launch_status();
+  if (rc != GOOSE_OK || pairs == 0) return rc;
+  const unsigned per_wg = 1024u / (unsigned)head_dim;
+  const dim3 grid((unsigned)((pairs + per_wg - 1) / per_wg));
+  if (head_dim == 128) hipLaunchKernelGGL(k_chunk_merge<128>, grid, dim3(256), 0, st, a, (int)pairs);
+  else hipLaunchKernelGGL(k_chunk_merge<64>, grid, dim3(256), 0, st, a, (int)pairs);
   return goose_launch_status();
 }

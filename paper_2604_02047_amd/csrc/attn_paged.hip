@@ -23,7 +23,7 @@ namespace {
 struct AttnReq {
   int32_t seq, B, P_max, row0, c0;
   int32_t tiles, splits;  // work items over its own keys: tiles x splits, for every KV head
-  const uint64_t* mask;
+  const uint64_t* mask;   // null: a chain, node i sees nodes 0 .. i
 };
 struct PagedAttnArgs {
   const void* kpool;  // of the layer
@@ -34,8 +34,9 @@ struct PagedAttnArgs {
   float* ws_o;    // [split][head][row][d]; splits of the shared keys first
   float* ws_ml;   // [split][head][row][2]: largest score (unscaled), sum of weights
   unsigned short* o;
+  float* lse;     // [n_heads][ld_lse], or null
   int32_t* flags;
-  size_t ldq, ldo;
+  size_t ldq, ldo, ld_lse;
   int32_t table_ld, n_pages, n_heads, n_kv, group, rows, n_req;
   int32_t same_blocks;                     // 32-slot blocks in front that must be the same in all tables
   int32_t sh_blocks, sh_tiles, sh_splits;  // shared keys with items of their own: blocks (all of those, or none), row tiles, splits
@@ -149,6 +150,11 @@ struct MaskRow { uint64_t w0, w1; };
 __device__ inline MaskRow mask_of(const PagedAttnArgs& a, const Item& it, const Row& w) {
   MaskRow k = {0, 0};
   if (it.ri < 0 || !w.live) return k;
+  if (a.r[it.ri].mask == nullptr) {
+    k.w0 = w.node >= 63 ? ~0ull : (2ull << w.node) - 1;
+    k.w1 = w.node >= 127 ? ~0ull : (w.node >= 64 ? (2ull << (w.node - 64)) - 1 : 0);
+    return k;
+  }
   const int W = (it.B + 63) >> 6;
   const uint64_t* p = a.r[it.ri].mask + (size_t)w.node * W;
   k.w0 = p[0];
@@ -162,6 +168,7 @@ __device__ inline void leave(const PagedAttnArgs& a, const Item& it, const Row& 
   if (a.direct) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     store_out(a, w.row, w.h * D + c, x * inv);
+    if (a.lse != nullptr && c == 0) a.lse[(size_t)w.h * a.ld_lse + w.row] = log_of_sum(m, l, softmax_scale(D));
   } else {
     const size_t rec = ((size_t)it.rec_split * a.n_heads + w.h) * a.rows + w.crow;
     if (c == 0) *reinterpret_cast<float2*>(a.ws_ml + rec * 2) = make_float2(m, l);
@@ -283,67 +290,6 @@ __global__ __launch_bounds__(512, 2) void k_paged_stream(const PagedAttnArgs a) 
 // Measured on the form with one term of weights (1024 cycles): a step took 1680 cycles, 1490 without the copies and the raised maxima, at a clock that fell to
 // 1.45 GHz under this load; a tenth more with S and P V of neighbouring blocks in one step, weights beside S alone and copies that made each LDS read wait for all.
 // Blocks that need a mask (the tree's, and what is left over) follow as in k_paged_stream, from what the ring has copied ahead or from memory.
-// Step j of a wavefront: scores of block j + 1 (to z1), weights of block j (from z0 to w0), outputs of block j - 1 (its weights in w).  None of the three
-// needs another, so the vector work is dealt out evenly beside the matrix instructions, and the last quarter of them hides the maximum of z1.
-// The operand pieces come from the ring AHEAD uses before they are needed; with
-// one key group pc holds the first ones and is left with those of the next step.  k1, k2: keys of blocks j + 1 and j + 2, v0: values of block j - 1.
-// The order is written down: the compiler's own collects the vector work where it waits for the scores.
-template <int D, int QT, bool F16, int G, int AHEAD>
-__device__ __forceinline__ void ring_step(RowTile<D, QT, F16>& t, u32x4 (&pc)[AHEAD], const u32x4* __restrict__ k1, const u32x4* __restrict__ v0,
-                                          const u32x4* __restrict__ k2, const f32x16& z0, f32x16& z1,
-                                          const typename RowTile<D, QT, F16>::op8 (&w)[2], const typename RowTile<D, QT, F16>::op8 (&wl)[2],
-                                          typename RowTile<D, QT, F16>::op8 (&w0)[2], typename RowTile<D, QT, F16>::op8 (&wl0)[2],
-                                          bool more, float scale) {
-  typedef RowTile<D, QT, F16> Tile;
-  typedef typename Tile::op8 op8;
-  constexpr int NS = Tile::NS, NDT = Tile::NDT, ALL = NS * (QT + 2), SPREAD = ALL * 3 / 4;
-  u32x4 piece[2 * NS + AHEAD];
-#pragma unroll
-  for (int n = 0; n < AHEAD; ++n) piece[n] = G == 1 ? pc[n] : k1[n * 64];
-  f32x16 sum;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) sum[r] = 0.f;
-  float part[4];
-#pragma unroll
-  for (int n = 0; n < 2 * NS; ++n) {
-    {
-      const int m = n + AHEAD, x = m - NS;
-      if (m < NS) piece[m] = k1[m * 64];
-      else if (m < 2 * NS) piece[m] = v0[(x % NDT * 2 + x / NDT) * 64];
-      else if (G == 1) piece[m] = k2[(m - 2 * NS) * 64];
-    }
-    const op8 a = __builtin_bit_cast(op8, piece[n]);
-    if (n < NS) {
-      sum = Mma16<F16>::mfma(a, t.q[n], sum);
-      if (QT == 2) sum = Mma16<F16>::mfma(a, t.ql[n % (QT == 2 ? NS : 1)], sum);
-      GOOSE_HERE(sum);
-    } else {
-      const int x = n - NS, j = x / NDT, dt = x % NDT;
-      t.o[dt] = Mma16<F16>::mfma(a, w[j], t.o[dt]);
-      t.o[dt] = Mma16<F16>::mfma(a, wl[j], t.o[dt]);
-      GOOSE_HERE(t.o[dt]);
-    }
-    const int before = n < NS ? n * QT : NS * QT + (n - NS) * 2, behind = before + (n < NS ? QT : 2);  // matrix instructions so far
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i >= 8 * before / SPREAD && i < 8 * behind / SPREAD) t.weights_of(i, z0, w0, wl0);
-    GOOSE_HERE(t.l);
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (2 * NS - NS / 2 + r * NS / 8 == n) {
-        part[r] = Tile::partial_max(sum, r);
-        GOOSE_HERE(part[r]);
-      }
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  z1 = sum;
-  t.top = Tile::join_max(part);
-  t.rescale_later(scale, z1, more);  // (behind the last block the scores are of a block that is not this loop's)
-#pragma unroll
-  for (int n = 0; n < AHEAD; ++n)
-    if (G == 1) pc[n] = piece[2 * NS + n];
-}
-
 template <int D, int QT, bool F16>
 __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
   typedef RowTile<D, QT, F16> Tile;
@@ -439,7 +385,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
       barrier();
       __builtin_amdgcn_sched_barrier(0);
       copy();
-      if (work) ring_step<D, QT, F16, G, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale);
+      if (work) ring_step<D, QT, F16, 2, G, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale, [](f32x16&) {});
     };
     int j = 1;
     for (; j + 1 < units; j += 2) {
@@ -618,7 +564,9 @@ __global__ __launch_bounds__(256) void k_paged_merge(const PagedAttnArgs a) {
   }
   if (!on) return;
   const float inv = den == 0.f ? 0.f : 1.0f / den;
-  store_out(a, (size_t)a.r[r].row0 + crow - a.r[r].c0, h * D + c, num * inv);
+  const size_t row = (size_t)a.r[r].row0 + crow - a.r[r].c0;
+  store_out(a, row, h * D + c, num * inv);
+  if (a.lse != nullptr && c == 0) a.lse[(size_t)h * a.ld_lse + row] = log_of_sum(m, den, scale);
 }
 
 // which kernel: k_paged_stream with one or two row tiles, or k_paged_tiles
@@ -642,7 +590,7 @@ void launch_merge(dim3 pairs, int splits, const PagedAttnArgs& a, hipStream_t st
 
 int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
                       const PagedReqs& rq, int shared_pages, float* ws_o, float* ws_ml, size_t max_records, void* o, size_t ldo,
-                      int o_dtype, int o_terms, int32_t* flags, hipStream_t st) {
+                      int o_dtype, int o_terms, int32_t* flags, hipStream_t st, float* lse, size_t ld_lse) {
   if (head_dim != 64 && head_dim != 128) return GOOSE_ERR_SHAPE;
   const size_t layer0 = (size_t)layer * page_layer_elems(pg, n_kv, head_dim) * 2;  // bytes
   PagedAttnArgs a{};
@@ -654,6 +602,8 @@ int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.ws_o = ws_o;
   a.ws_ml = ws_ml;
   a.o = (unsigned short*)o;
+  a.lse = lse;
+  a.ld_lse = ld_lse;
   a.flags = flags;
   a.ldq = ldq;
   a.ldo = ldo;

@@ -77,8 +77,8 @@ struct PageIds {
 #define GOOSE_HERE(x) (void)(x)
 #endif
 
-// ---- 32 rows of the softmax ---------------------------------------------------------------------------------------------
-template <int D, int QT, bool F16>
+// ---- 32 rows of the softmax; weights enter the second product in PT terms --------------------------------------------------
+template <int D, int QT, bool F16, int PT = 2>
 struct RowTile {
   static constexpr int NS = D / 16, NDT = D / 32;
   static constexpr float SLACK = 8.f;
@@ -189,7 +189,7 @@ struct RowTile {
       if (grows) late = raise(c, x);
     }
   }
-  // x, y in two 16-bit terms, as weights of keys 2 i, 2 i + 1
+  // x, y in PT 16-bit terms, as weights of keys 2 i, 2 i + 1
   static __device__ __forceinline__ void pair_to(int i, float x, float y, op8 (&w)[2], op8 (&wl)[2]) {
     typedef T T2 __attribute__((ext_vector_type(2)));
     typedef float F2 __attribute__((ext_vector_type(2)));
@@ -198,6 +198,7 @@ struct RowTile {
     u32x4 v = __builtin_bit_cast(u32x4, w[i >> 2]);
     v[i & 3] = h;
     w[i >> 2] = __builtin_bit_cast(op8, v);
+    if constexpr (PT == 1) return;
     F2 rest;
     if constexpr (F16) {
       const T2 t = __builtin_bit_cast(T2, h);
@@ -227,6 +228,7 @@ struct RowTile {
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), p[j], o[dt]);
+    if constexpr (PT == 1) return;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -314,7 +316,72 @@ __device__ __forceinline__ void copy_pieces(const char* src, int lane, unsigned 
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host pass knows no such builtin and would silently drop the kernel's stub)
   const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), 0, CP * 1024, GOOSE_BUFFER_WORD3);
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(cp), 16, lane * 16, 0, 0, 0);
-  if (CP == 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(cp), 16, lane * 16, 0, 1024, 0);  // (the offset counts on both sides)
+  if (CP > 1) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(cp), 16, lane * 16, 0, 1024, 0);  // (the offset counts on both sides)
+  if (CP > 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(cp), 16, lane * 16, 0, 2048, 0);
+  if (CP > 3) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(cp), 16, lane * 16, 0, 3072, 0);
 #endif
 }
+// Step j of a wavefront: scores of block j + 1 (to z1), weights of block j (from z0 to w0), outputs of block j - 1 (its weights in w).  None of the three
+// needs another, so the vector work is dealt out evenly beside the matrix instructions, and the last quarter of them hides the maximum of z1.
+// The operand pieces come from the ring AHEAD uses before they are needed; with
+// one key group pc holds the first ones and is left with those of the next step.  k1, k2: keys of blocks j + 1 and j + 2, v0: values of block j - 1.
+// The order is written down: the compiler's own collects the vector work where it waits for the scores.
+// edge(s): what becomes of the scores of block j + 1 before their maximum is taken.
+template <int D, int QT, bool F16, int PT, int G, int AHEAD, typename Edge>
+__device__ __forceinline__ void ring_step(RowTile<D, QT, F16, PT>& t, u32x4 (&pc)[AHEAD], const u32x4* __restrict__ k1, const u32x4* __restrict__ v0,
+                                          const u32x4* __restrict__ k2, const f32x16& z0, f32x16& z1,
+                                          const typename RowTile<D, QT, F16, PT>::op8 (&w)[2], const typename RowTile<D, QT, F16, PT>::op8 (&wl)[2],
+                                          typename RowTile<D, QT, F16, PT>::op8 (&w0)[2], typename RowTile<D, QT, F16, PT>::op8 (&wl0)[2],
+                                          bool more, float scale, Edge edge) {
+  typedef RowTile<D, QT, F16, PT> Tile;
+  typedef typename Tile::op8 op8;
+  constexpr int NS = Tile::NS, NDT = Tile::NDT, ALL = NS * (QT + PT), SPREAD = ALL * 3 / 4;
+  u32x4 piece[2 * NS + AHEAD];
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n) piece[n] = G == 1 ? pc[n] : k1[n * 64];
+  f32x16 sum;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) sum[r] = 0.f;
+  float part[4];
+#pragma unroll
+  for (int n = 0; n < 2 * NS; ++n) {
+    {
+      const int m = n + AHEAD, x = m - NS;
+      if (m < NS) piece[m] = k1[m * 64];
+      else if (m < 2 * NS) piece[m] = v0[(x % NDT * 2 + x / NDT) * 64];
+      else if (G == 1) piece[m] = k2[(m - 2 * NS) * 64];
+    }
+    const op8 a = __builtin_bit_cast(op8, piece[n]);
+    if (n < NS) {
+      sum = Mma16<F16>::mfma(a, t.q[n], sum);
+      if (QT == 2) sum = Mma16<F16>::mfma(a, t.ql[n % (QT == 2 ? NS : 1)], sum);
+      GOOSE_HERE(sum);
+    } else {
+      const int x = n - NS, j = x / NDT, dt = x % NDT;
+      t.o[dt] = Mma16<F16>::mfma(a, w[j], t.o[dt]);
+      if (PT == 2) t.o[dt] = Mma16<F16>::mfma(a, wl[j], t.o[dt]);
+      GOOSE_HERE(t.o[dt]);
+    }
+    const int before = n < NS ? n * QT : NS * QT + (n - NS) * PT, behind = before + (n < NS ? QT : PT);  // matrix instructions so far
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= 8 * before / SPREAD && i < 8 * behind / SPREAD) t.weights_of(i, z0, w0, wl0);
+    GOOSE_HERE(t.l);
+    if (n == 2 * NS - NS / 2 - 1) edge(sum);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (2 * NS - NS / 2 + r * NS / 8 == n) {
+        part[r] = Tile::partial_max(sum, r);
+        GOOSE_HERE(part[r]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  z1 = sum;
+  t.top = Tile::join_max(part);
+  t.rescale_later(scale, z1, more);  // (behind the last block the scores are of a block that is not this loop's)
+#pragma unroll
+  for (int n = 0; n < AHEAD; ++n)
+    if (G == 1) pc[n] = piece[2 * NS + n];
+}
+
 }  // namespace

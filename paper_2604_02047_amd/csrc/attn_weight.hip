@@ -3,9 +3,9 @@
 //   w[s] = decay w[s] + sum over tokens i >= first with s <= P + i, and over the query heads of the KV head, of
 //          2^(q . K[s] c - lse log2(e)),   c = log2(e) / sqrt(d)
 //
-// A workgroup owns the 64 slots of a page under one KV head: their keys stay in registers, the rows (token, query head of the group)
-// stream by, 32 of them a tile, dealt out to four wavefronts.  S^T = K Q^T leaves 16 keys of one row in a lane, so a slot's sum
-// grows in one register and is joined over lanes and wavefronts at the end, in a fixed order.
+// A wavefront owns the 64 slots of a page under one KV head: their keys stay in registers while the rows (token, query head of the
+// group) stream by, 32 of them a tile.  S^T = K Q^T leaves 16 keys of one row in a lane, so a slot's sum grows in one register and is
+// joined over lanes and wavefronts at the end, in a fixed order.
 #include "chunk.h"
 
 namespace {
@@ -20,93 +20,194 @@ struct WeightArgs {
   int32_t* flags;
   size_t ldq, ld_lse;
   int32_t table_ld, n_pages, n_kv, group, n;
+  uint32_t group_inv;  // ceil(2^32 / group): exact for rows below 2^32 / group
+  int32_t sg, rg;  // a workgroup's wavefronts: sg pages x rg of the tiles in turn
   float decay;
   ChunkReq r[GOOSE_MAX_REQUESTS];
 };
 
+// Scores of a tile and 64 keys (to s), and beside the matrix instructions the weights of the tile before (scores z, its rows' logarithms l2), which
+// need nothing of this one: a workgroup's wavefronts meet at every tile, so that without it they would all be at the matrix instructions
+// together and at the exponentials together.
+// (The kernel has one LDS array, and it is read here through a pointer of its own: else each read waits for the copies into other parts of it.)
 template <int D, int QT, bool F16>
-__global__ __launch_bounds__(256, 2) void k_slot_weights(const WeightArgs a) {
-  typedef typename Mma16<F16>::T T;
+__device__ __forceinline__ void tile_step(const u32x4* __restrict__ tile, const u32x4 (&k)[2][D / 16], f32x16 (&s)[2], const f32x16 (&z)[2], float l2,
+                                          float scale, f32x16 (&sum)[2]) {
   typedef typename Mma16<F16>::v8 op8;
-  constexpr int NS = D / 16;
-  __shared__ float part[4][64];
+  constexpr int PIECES = D / 16 * QT, AHEAD = 2;
+  u32x4 piece[PIECES];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) piece[i] = tile[i * 64];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    if (i + AHEAD < PIECES) piece[i + AHEAD] = tile[(i + AHEAD) * 64];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      s[b] = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[b][i % (D / 16)]), __builtin_bit_cast(op8, piece[i]), s[b]);
+#pragma unroll
+      for (int e = (2 * i + b) * 16 / PIECES; e < (2 * i + b + 1) * 16 / PIECES; ++e) {
+        float x = sum[e >> 4][e & 15] + __builtin_amdgcn_exp2f(fmaf(z[e >> 4][e & 15], scale, -l2));
+        GOOSE_HERE(x);  // (the compiler would move it behind the matrix instructions)
+        sum[e >> 4][e & 15] = x;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+// The tiles come into LDS in operand order, two sets of rg tiles: while one is worked on the other one arrives, every wavefront copying its
+// share (a lane fetches the 16 bytes that belong at its place).
+template <int D, int QT, bool F16>
+__global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
+  typedef typename Mma16<F16>::T T;
+  constexpr int NS = D / 16, PIECES = NS * QT, MOST = 4;  // 1 KiB pieces of a tile: the high terms' first; the most rg
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2][MOST][PIECES * 1024];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l31 = lane & 31, hh = lane >> 5;
-  int page_i = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)a.n_kv));
-  const int kvh = (int)blockIdx.x - page_i * a.n_kv;
+  const int SG = a.sg, RG = a.rg, rg = __builtin_amdgcn_readfirstlane((int)((unsigned)wave / (unsigned)SG)), sg = wave - rg * SG;
+  const int first_page = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)a.n_kv)) * SG;
+  const int kvh = (int)blockIdx.x % a.n_kv;
   const ChunkReq& rq = a.r[blockIdx.y];
   const int P = __builtin_amdgcn_readfirstlane(a.len[rq.seq]);
   if (P < 0 || P > rq.P_max) {
     if (tid == 0 && blockIdx.x == 0) atomicOr(a.flags, GOOSE_FLAG_CAPACITY);
     return;
   }
-  const int slot0 = page_i * GOOSE_PAGE, end = P + rq.C;
-  if (slot0 >= end) return;
-  const int page = a.table[(size_t)rq.seq * a.table_ld + page_i];
+  const int end = P + rq.C;
+  if (first_page * GOOSE_PAGE >= end) return;
+  const int slot0 = (first_page + sg) * GOOSE_PAGE;
+  bool live = slot0 < end;
+  const int page = __builtin_amdgcn_readfirstlane(live ? a.table[(size_t)rq.seq * a.table_ld + first_page + sg] : 0);
   if ((unsigned)page >= (unsigned)a.n_pages) {
-    if (tid == 0) atomicOr(a.flags, GOOSE_FLAG_PAGES);
-    return;
+    if (lane == 0) atomicOr(a.flags, GOOSE_FLAG_PAGES);
+    live = false;
   }
   u32x4 k[2][NS];
-  const T* const kp = static_cast<const T*>(a.kpool) + page_head<D>(page, a.n_kv, kvh);
-  fetch(kp, lane, k[0]);
-  fetch(kp + 32 * D, lane, k[1]);
-  const int first = max(rq.first, slot0 - P);  // the first token that sees one of them
-  const int rows = rq.C * a.group;
+  if (live) {
+    const T* const kp = static_cast<const T*>(a.kpool) + page_head<D>(page, a.n_kv, kvh);
+    fetch(kp, lane, k[0]);
+    fetch(kp + 32 * D, lane, k[1]);
+  }
+  // rows: from the first token that sees a slot of the workgroup
+  const int rows = rq.C * a.group, row0 = max(rq.first, first_page * GOOSE_PAGE - P) * a.group, steps = (rows - row0 + 32 * RG - 1) / (32 * RG);
   const float scale = softmax_scale(D);
+  const T* const q0 = static_cast<const T*>(a.q) + (size_t)rq.row0 * a.ldq;
+  auto place = [&](int rho, int& tok, int& h) {  // of a row (behind the last one: the last one's)
+    const int at = min(rho, rows - 1);
+    tok = a.group == 1 ? at : (int)__umulhi((unsigned)at, a.group_inv);
+    h = kvh * a.group + at - tok * a.group;
+  };
+  auto copy = [&](int step) {  // this wavefront's share of the tiles of a step
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int most = RG * PIECES;
+    int held = -1;
+    unsigned at = 0;
+    const T* q1 = q0;
+    for (int i = wave; i < most; i += SG * RG) {
+      const int t = i / PIECES, p = i - t * PIECES;
+      if (t != held) {
+        int tok, h;
+        place(row0 + (step * RG + t) * 32 + l31, tok, h);
+        const int tok0 = __builtin_amdgcn_readfirstlane(tok);  // (the tile's first token: 32 rows reach less than 2^32 bytes from there)
+        q1 = q0 + (size_t)tok0 * a.ldq;
+        at = (unsigned)(((size_t)(tok - tok0) * a.ldq + ((size_t)h * D + hh * 8) * QT) * 2);
+        held = t;
+      }
+      const int s = p % NS, term = p / NS;
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(q1), 0, 0xFFFFFFFFu, GOOSE_BUFFER_WORD3);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(&tiles[step & 1][t][p * 1024]), 16, at, (s * 16 * QT + term * 8) * 2, 0, 0);
+    }
+#endif
+  };
   f32x16 sum[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum[b][r] = 0.f;
-  for (int row0 = first * a.group + wave * 32; row0 < rows; row0 += 128) {
-    const bool live = row0 + l31 < rows;
-    const int rho = live ? row0 + l31 : rows - 1;
-    const int tok = (int)((unsigned)rho / (unsigned)a.group), h = kvh * a.group + rho - tok * a.group;
-    const size_t row = (size_t)rq.row0 + tok;
-    const T* const at = static_cast<const T*>(a.q) + row * a.ldq + ((size_t)h * D + hh * 8) * QT;
-    const float lse = a.lse[(size_t)h * a.ld_lse + row];
-    op8 q[NS], ql[QT == 2 ? NS : 1];
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      q[s] = *reinterpret_cast<const op8*>(at + s * 16 * QT);
-      if (QT == 2) ql[s] = *reinterpret_cast<const op8*>(at + s * 32 + 8);
-    }
-    // (a row of scores of -infinity only: its logarithm would make them NaN)
-    const float l2 = lse * 1.4426950408889634f;
-    const int last = live && lse != -INFINITY ? P + tok - slot0 - hh * 16 : -1;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      f32x16 s;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NS; ++i) s = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[b][i]), q[i], s);
-      if (QT == 2) {
-#pragma unroll
-        for (int i = 0; i < NS; ++i) s = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[b][i]), ql[i], s);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -l2));
-        sum[b][r] += b * 32 + r <= last ? w : 0.f;
-      }
-    }
-  }
-  // over the 32 rows of a tile, then over the wavefronts; register r of half hh is key 16 hh + r
+  // this lane's row of the next step: its token (-1: none) and logarithm
+  int tok_next;
+  float lse_next;
+  auto ask = [&](int step) {
+    const int rho = row0 + (step * RG + rg) * 32 + l31;
+    int tok, h;
+    place(rho, tok, h);
+    lse_next = a.lse[(size_t)h * a.ld_lse + rq.row0 + tok];
+    tok_next = rho < rows ? tok : -1;
+  };
+  copy(0);
+  ask(0);
+  f32x16 s0[2], s1[2];  // scores of the tile before; -infinity: no weight
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      float x = sum[b][r];
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) x += __shfl_xor(x, off, 64);
-      if (l31 == 0) part[wave][b * 32 + hh * 16 + r] = x;
+    for (int r = 0; r < 16; ++r) s1[b][r] = -INFINITY;
+  float l2 = 0.f;
+  auto one = [&](int step, f32x16 (&s)[2], const f32x16 (&z)[2]) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int tok = tok_next;
+    const float lse = lse_next;
+    if (step + 1 < steps) {
+      copy(step + 1);
+      ask(step + 1);
     }
+    tile_step<D, QT, F16>(reinterpret_cast<const u32x4*>(tiles[step & 1][rg]) + lane, k, s, z, l2, scale, sum);
+    // (a row of scores of -infinity only has that as its logarithm, too, and weighs nothing; a NaN concerns the keys that the row sees: it goes into their scores)
+    const bool none = lse == -INFINITY, nan = lse != lse;
+    l2 = none || nan ? 0.f : lse * 1.4426950408889634f;
+    const int last = tok >= 0 && !none ? P + tok - slot0 - hh * 16 : -1;
+    if (__builtin_amdgcn_ballot_w64(last < 47 || nan) != 0) {  // some row does not see all of the lane's keys
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] = b * 32 + r <= last ? (nan ? lse : s[b][r]) : -INFINITY;
+    }
+  };
+  auto rest = [&](const f32x16 (&z)[2]) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[b][r] += __builtin_amdgcn_exp2f(fmaf(z[b][r], scale, -l2));
+  };
+  int step = 0;
+  for (; step + 1 < steps; step += 2) {
+    one(step, s0, s1);
+    one(step + 1, s1, s0);
+  }
+  if (step < steps) {
+    one(step, s0, s1);
+    rest(s0);
+  } else {
+    rest(s1);
+  }
+  // over the 32 rows of a tile: lane l31 is left with value l31 = 16 b + r of its half, slot 32 b + 16 hh + r
+  float v[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = sum[i >> 4][i & 15];
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    const bool upper = (l31 & off) != 0;
+#pragma unroll
+    for (int i = 0; i < off; ++i) {
+      const float keep = upper ? v[i + off] : v[i], send = upper ? v[i] : v[i + off];
+      v[i] = keep + __shfl_xor(send, off, 64);
+    }
+  }
+  const int mine = (l31 >> 4) * 32 + hh * 16 + (l31 & 15);
+  float* const part = reinterpret_cast<float*>(tiles);  // [wavefront][slot]
   __syncthreads();
-  const int slot = slot0 + tid;
-  if (tid >= GOOSE_PAGE || slot >= end) return;
-  float w = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
+  part[wave * 64 + mine] = v[0];
+  __syncthreads();
+  if (rg != 0 || !live) return;
+  float w = part[wave * 64 + lane];
+  for (int i = 1; i < RG; ++i) w += part[(i * SG + sg) * 64 + lane];
+  const int slot = slot0 + lane;
+  if (slot >= end) return;
   float* const out = a.weight + ((size_t)rq.seq * a.n_kv + kvh) * a.table_ld * GOOSE_PAGE + slot;
   if (slot < P && a.decay != 0.f) w += a.decay * *out;
   *out = w;
@@ -115,11 +216,11 @@ __global__ __launch_bounds__(256, 2) void k_slot_weights(const WeightArgs a) {
 template <int D>
 void launch_d(bool f16, int q_terms, dim3 grid, const WeightArgs& a, hipStream_t st) {
   if (q_terms == 2) {
-    if (f16) hipLaunchKernelGGL((k_slot_weights<D, 2, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_slot_weights<D, 2, false>), grid, dim3(256), 0, st, a);
+    if (f16) hipLaunchKernelGGL((k_slot_weights<D, 2, true>), grid, dim3(64 * a.sg * a.rg), 0, st, a);
+    else hipLaunchKernelGGL((k_slot_weights<D, 2, false>), grid, dim3(64 * a.sg * a.rg), 0, st, a);
   } else {
-    if (f16) hipLaunchKernelGGL((k_slot_weights<D, 1, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_slot_weights<D, 1, false>), grid, dim3(256), 0, st, a);
+    if (f16) hipLaunchKernelGGL((k_slot_weights<D, 1, true>), grid, dim3(64 * a.sg * a.rg), 0, st, a);
+    else hipLaunchKernelGGL((k_slot_weights<D, 1, false>), grid, dim3(64 * a.sg * a.rg), 0, st, a);
   }
 }
 
@@ -141,16 +242,25 @@ int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads,
   a.n_pages = pg.n_pages;
   a.n_kv = n_kv;
   a.group = n_heads / n_kv;
+  a.group_inv = UINT32_MAX / (uint32_t)a.group + 1;  // (not used where group is 1)
   a.n = ck.n;
   a.decay = decay;
-  int most = 0;
+  int most = 0, tiles = 0;
+  long long waves = 0;  // pages x KV heads
   for (int i = 0; i < ck.n; ++i) {
     a.r[i] = ck.r[i];
-    const int pages = (ck.r[i].P_max + ck.r[i].C + GOOSE_PAGE - 1) / GOOSE_PAGE;
+    const int pages = (ck.r[i].P_max + ck.r[i].C + GOOSE_PAGE - 1) / GOOSE_PAGE, t = ((ck.r[i].C - ck.r[i].first) * a.group + 31) / 32;
     most = pages > most ? pages : most;
+    tiles = t > tiles ? t : tiles;
+    waves += (long long)pages * n_kv;
   }
-  if ((long long)most * n_kv > INT32_MAX) return GOOSE_ERR_CAPACITY;
-  const dim3 grid((unsigned)most * (unsigned)n_kv, (unsigned)ck.n);
+  a.rg = 1;
+  while (a.rg < 4 && waves * a.rg < 2048 && tiles >= 4 * a.rg) a.rg *= 2;
+  a.sg = 1;
+  while (a.sg * a.rg < 8 && waves * a.rg >= 512ll * a.sg * a.rg) a.sg *= 2;
+  const int groups = (most + a.sg - 1) / a.sg;
+  if ((long long)groups * n_kv > INT32_MAX) return GOOSE_ERR_CAPACITY;
+  const dim3 grid((unsigned)groups * (unsigned)n_kv, (unsigned)ck.n);
   const bool f16 = dtype == GOOSE_DTYPE_F16;
   if (head_dim == 128) launch_d<128>(f16, q_terms, grid, a, st);
   else if (head_dim == 64) launch_d<64>(f16, q_terms, grid, a, st);

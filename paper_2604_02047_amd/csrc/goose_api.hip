@@ -510,8 +510,8 @@ static int layer_impl(goose_ctx* c, const char* w, float* d_x, void* d_kcache, v
                            q_terms, c->flags, st);
     if (rc) return rc;
     if (paged->chunks) {
-      rc = launch_attn_chunk(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, *paged->chunks, c->o, c->ld_o,
-                             c->act_dtype, T, paged->weight ? c->lse : nullptr, c->Bpad, c->flags, st);
+      rc = launch_attn_chunk(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, *paged->chunks, c->att_o, c->att_ml,
+                             attn_records(c), c->o, c->ld_o, c->act_dtype, T, paged->weight ? c->lse : nullptr, c->Bpad, c->flags, st);
       if (!rc && paged->weight)
         rc = launch_attn_weight(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, *paged->chunks, c->lse,
                                 c->Bpad, paged->decay, paged->weight, c->flags, st);
@@ -1074,8 +1074,8 @@ int goose_attn_chunk_paged(goose_ctx* c, const goose_pages* pg, int layer, const
   rc = chunk_reqs(pg, chunks, n, true, &ck);
   if (rc) return rc;
   if (d_lse && ld_lse < (size_t)ck.rows) return GOOSE_ERR_ARG;
-  return launch_attn_chunk(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, d_q, ldq, q_terms, ck, d_o, ldo, o_dtype, o_terms, d_lse,
-                           ld_lse, c->flags, as_stream(stream));
+  return launch_attn_chunk(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, d_q, ldq, q_terms, ck, c->att_o, c->att_ml, attn_records(c), d_o,
+                           ldo, o_dtype, o_terms, d_lse, ld_lse, c->flags, as_stream(stream));
 }
 
 int goose_attn_weight_paged(goose_ctx* c, const goose_pages* pg, int layer, const void* d_q, size_t ldq, int q_terms, const goose_chunk* chunks,
@@ -1083,7 +1083,7 @@ int goose_attn_weight_paged(goose_ctx* c, const goose_pages* pg, int layer, cons
   int rc = check_pages(c, pg);
   if (rc) return rc;
   if (!d_q || !d_lse || !d_weight || layer < 0 || layer >= c->d.n_layers || (q_terms != 1 && q_terms != 2) || !decay_ok(decay)) return GOOSE_ERR_ARG;
-  if (ldq < (size_t)c->Hq * q_terms || (ldq & 7) || ((uintptr_t)d_q & 15) || ((uintptr_t)d_lse & 3) || ((uintptr_t)d_weight & 3)) return GOOSE_ERR_ARG;
+  if (ldq < (size_t)c->Hq * q_terms || ldq > (1u << 26) || (ldq & 7) || ((uintptr_t)d_q & 15) || ((uintptr_t)d_lse & 3) || ((uintptr_t)d_weight & 3)) return GOOSE_ERR_ARG;
   ChunkReqs ck;
   rc = chunk_reqs(pg, chunks, n, true, &ck);
   if (!rc) rc = check_first(ck);

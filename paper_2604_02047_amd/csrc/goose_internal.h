@@ -312,10 +312,11 @@ static inline size_t page_layer_elems(const goose_pages& pg, int n_kv, int head_
 int launch_rope_paged(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const double* inv_freq, float eps,
                       const float* part, int ks, size_t split_stride, size_t ld, const void* gq, const void* gk, const PagedReqs& rq,
                       void* q, size_t ldq, int q_terms, int32_t* flags, hipStream_t st);
-// ws_o: f32 [records][head_dim], ws_ml: f32 [records][2]; max_records of them
+// ws_o: f32 [records][head_dim], ws_ml: f32 [records][2]; max_records of them.  A request without a mask is a chain of its nodes.
+// lse (or null): f32 [n_heads][ld_lse] receives the logarithm of every row's sum of exponentials.
 int launch_attn_paged(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
                       const PagedReqs& rq, int shared_pages, float* ws_o, float* ws_ml, size_t max_records, void* o, size_t ldo,
-                      int o_dtype, int o_terms, int32_t* flags, hipStream_t st);
+                      int o_dtype, int o_terms, int32_t* flags, hipStream_t st, float* lse = nullptr, size_t ld_lse = 0);
 
 // ---- chunks of new tokens on a paged cache, eviction (attn_chunk.hip, attn_weight.hip, pages_evict.hip; 16-bit types)
 struct ChunkReq {
@@ -328,8 +329,8 @@ struct ChunkReqs {
   ChunkReq r[GOOSE_MAX_REQUESTS];
 };
 int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
-                      const ChunkReqs& ck, void* o, size_t ldo, int o_dtype, int o_terms, float* lse, size_t ld_lse, int32_t* flags,
-                      hipStream_t st);
+                      const ChunkReqs& ck, float* ws_o, float* ws_ml, size_t max_records, void* o, size_t ldo, int o_dtype, int o_terms, float* lse,
+                      size_t ld_lse, int32_t* flags, hipStream_t st);
 int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
                        const ChunkReqs& ck, const float* lse, size_t ld_lse, float decay, float* weight, int32_t* flags, hipStream_t st);
 int launch_pages_append(const goose_pages& pg, const ChunkReqs& ck, int32_t* flags, hipStream_t st);
