@@ -20,11 +20,14 @@ struct WeightArgs {
   int32_t* flags;
   size_t ldq, ld_lse;
   int32_t table_ld, n_pages, n_kv, group, n;
-  uint32_t group_inv;  // ceil(2^32 / group): exact for rows below 2^32 / group
+  uint32_t group_inv;  // ceil(2^32 / group), 0 for groups of one: row / group = mulhi(row, group_inv) for rows below 2^32 / group
   int32_t sg, rg;  // a workgroup's wavefronts: sg pages x rg of the tiles in turn
   float decay;
   ChunkReq r[GOOSE_MAX_REQUESTS];
 };
+
+// Row groups of a workgroup: what fits 128 KiB of LDS.
+constexpr int most_rg(int pieces) { return pieces > 8 ? 2 : 4; }
 
 // Scores of a tile and 64 keys (to s), and beside the matrix instructions the weights of the tile before (scores z, its rows' logarithms l2), which
 // need nothing of this one: a workgroup's wavefronts meet at every tile, so that without it they would all be at the matrix instructions
@@ -59,18 +62,18 @@ __device__ __forceinline__ void tile_step(const u32x4* __restrict__ tile, const 
   }
 }
 
-// The tiles come into LDS in operand order, two sets of rg tiles: while one is worked on the other one arrives, every wavefront copying its
-// share (a lane fetches the 16 bytes that belong at its place).
+// The tiles come into LDS in operand order, two sets of U rg tiles: while one is worked on the other one arrives, the wavefronts of a tile
+// copying their share of it (a lane fetches the 16 bytes that belong at its place).
 template <int D, int QT, bool F16>
 __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
   typedef typename Mma16<F16>::T T;
-  constexpr int NS = D / 16, PIECES = NS * QT, MOST = 4;  // 1 KiB pieces of a tile: the high terms' first; the most rg
-  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2][MOST][PIECES * 1024];
+  constexpr int NS = D / 16, PIECES = NS * QT, U = 2;  // 1 KiB pieces of a tile: the high terms' first
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2][U * most_rg(PIECES)][PIECES * 1024];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l31 = lane & 31, hh = lane >> 5;
   const int SG = a.sg, RG = a.rg, rg = __builtin_amdgcn_readfirstlane((int)((unsigned)wave / (unsigned)SG)), sg = wave - rg * SG;
   const int first_page = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)a.n_kv)) * SG;
-  const int kvh = (int)blockIdx.x % a.n_kv;
+  const int kvh = (int)(blockIdx.x % (unsigned)a.n_kv);
   const ChunkReq& rq = a.r[blockIdx.y];
   const int P = __builtin_amdgcn_readfirstlane(a.len[rq.seq]);
   if (P < 0 || P > rq.P_max) {
@@ -87,76 +90,47 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
     live = false;
   }
   u32x4 k[2][NS];
-  if (live) {
-    const T* const kp = static_cast<const T*>(a.kpool) + page_head<D>(page, a.n_kv, kvh);
-    fetch(kp, lane, k[0]);
-    fetch(kp + 32 * D, lane, k[1]);
-  }
+  const T* const kp = static_cast<const T*>(a.kpool) + page_head<D>(live ? page : 0, a.n_kv, kvh);
+  fetch(kp, lane, k[0]);
+  fetch(kp + 32 * D, lane, k[1]);
   // rows: from the first token that sees a slot of the workgroup
-  const int rows = rq.C * a.group, row0 = max(rq.first, first_page * GOOSE_PAGE - P) * a.group, steps = (rows - row0 + 32 * RG - 1) / (32 * RG);
+  const int group = a.group, rows = rq.C * group, row0 = max(rq.first, first_page * GOOSE_PAGE - P) * group;
+  const int steps = (rows - row0 + 32 * U * RG - 1) / (32 * U * RG);
   const float scale = softmax_scale(D);
-  const T* const q0 = static_cast<const T*>(a.q) + (size_t)rq.row0 * a.ldq;
-  auto place = [&](int rho, int& tok, int& h) {  // of a row (behind the last one: the last one's)
-    const int at = min(rho, rows - 1);
-    tok = a.group == 1 ? at : (int)__umulhi((unsigned)at, a.group_inv);
-    h = kvh * a.group + at - tok * a.group;
-  };
-  auto copy = [&](int step) {  // this wavefront's share of the tiles of a step
+  const T* const q0 = static_cast<const T*>(a.q) + (size_t)rq.row0 * a.ldq + (size_t)kvh * group * D * QT;
+  const float* const lse0 = a.lse + (size_t)kvh * group * a.ld_lse + rq.row0;
+  const unsigned ldq = (unsigned)a.ldq, ld_lse = (unsigned)a.ld_lse, inv = a.group_inv;
+  // of the next step's tiles: this lane's rows' tokens (-1: none) and logarithms
+  int tok_next[U];
+  float lse_next[U];
+  auto copy = [&](int step) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int rho = row0 + ((step * U + u) * RG + rg) * 32 + l31, at = min(rho, rows - 1);
+      const int tok = inv == 0 ? at : (int)__umulhi((unsigned)at, inv), h = at - tok * group;  // (behind the last row: that one)
+      lse_next[u] = lse0[(size_t)(unsigned)h * ld_lse + (unsigned)tok];
+      tok_next[u] = rho < rows ? tok : -1;
 #if defined(__HIP_DEVICE_COMPILE__)
-    const int most = RG * PIECES;
-    int held = -1;
-    unsigned at = 0;
-    const T* q1 = q0;
-    for (int i = wave; i < most; i += SG * RG) {
-      const int t = i / PIECES, p = i - t * PIECES;
-      if (t != held) {
-        int tok, h;
-        place(row0 + (step * RG + t) * 32 + l31, tok, h);
-        const int tok0 = __builtin_amdgcn_readfirstlane(tok);  // (the tile's first token: 32 rows reach less than 2^32 bytes from there)
-        q1 = q0 + (size_t)tok0 * a.ldq;
-        at = (unsigned)(((size_t)(tok - tok0) * a.ldq + ((size_t)h * D + hh * 8) * QT) * 2);
-        held = t;
-      }
-      const int s = p % NS, term = p / NS;
-      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(q1), 0, 0xFFFFFFFFu, GOOSE_BUFFER_WORD3);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(&tiles[step & 1][t][p * 1024]), 16, at, (s * 16 * QT + term * 8) * 2, 0, 0);
-    }
+      const int tok0 = __builtin_amdgcn_readfirstlane(tok);  // (the tile's first token: 32 rows reach less than 2^32 bytes from there)
+      const __amdgpu_buffer_rsrc_t rsrc =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(q0 + (size_t)(unsigned)tok0 * ldq), 0, 0xFFFFFFFFu, GOOSE_BUFFER_WORD3);
+      const unsigned offset = (((unsigned)(tok - tok0) * ldq) + (unsigned)(h * D + hh * 8) * QT) * 2;
+      for (int p = sg; p < PIECES; p += SG)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(&tiles[step & 1][u * RG + rg][p * 1024]), 16, offset, (p % NS * 16 * QT + p / NS * 8) * 2, 0, 0);
 #endif
-  };
-  f32x16 sum[2];
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sum[b][r] = 0.f;
-  // this lane's row of the next step: its token (-1: none) and logarithm
-  int tok_next;
-  float lse_next;
-  auto ask = [&](int step) {
-    const int rho = row0 + (step * RG + rg) * 32 + l31;
-    int tok, h;
-    place(rho, tok, h);
-    lse_next = a.lse[(size_t)h * a.ld_lse + rq.row0 + tok];
-    tok_next = rho < rows ? tok : -1;
-  };
-  copy(0);
-  ask(0);
-  f32x16 s0[2], s1[2];  // scores of the tile before; -infinity: no weight
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s1[b][r] = -INFINITY;
-  float l2 = 0.f;
-  auto one = [&](int step, f32x16 (&s)[2], const f32x16 (&z)[2]) {
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    const int tok = tok_next;
-    const float lse = lse_next;
-    if (step + 1 < steps) {
-      copy(step + 1);
-      ask(step + 1);
     }
-    tile_step<D, QT, F16>(reinterpret_cast<const u32x4*>(tiles[step & 1][rg]) + lane, k, s, z, l2, scale, sum);
+  };
+  f32x16 sum[2], s0[2], s1[2];  // scores of the tile before; -infinity: no weight
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      sum[b][r] = 0.f;
+      s1[b][r] = -INFINITY;
+    }
+  float l2 = 0.f;
+  auto one = [&](const unsigned char* tile, int tok, float lse, f32x16 (&s)[2], const f32x16 (&z)[2]) {
+    tile_step<D, QT, F16>(reinterpret_cast<const u32x4*>(tile) + lane, k, s, z, l2, scale, sum);
     // (a row of scores of -infinity only has that as its logarithm, too, and weighs nothing; a NaN concerns the keys that the row sees: it goes into their scores)
     const bool none = lse == -INFINITY, nan = lse != lse;
     l2 = none || nan ? 0.f : lse * 1.4426950408889634f;
@@ -168,22 +142,38 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
         for (int r = 0; r < 16; ++r) s[b][r] = b * 32 + r <= last ? (nan ? lse : s[b][r]) : -INFINITY;
     }
   };
+  auto arrive = [&]() {
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
   auto rest = [&](const f32x16 (&z)[2]) {
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum[b][r] += __builtin_amdgcn_exp2f(fmaf(z[b][r], scale, -l2));
   };
+  copy(0);
   int step = 0;
-  for (; step + 1 < steps; step += 2) {
-    one(step, s0, s1);
-    one(step + 1, s1, s0);
+  for (; step + 1 < steps; ++step) {
+    arrive();
+    const int t0 = tok_next[0], t1 = tok_next[1];
+    const float e0 = lse_next[0], e1 = lse_next[1];
+    copy(step + 1);
+    one(tiles[step & 1][rg], t0, e0, s0, s1);
+    one(tiles[step & 1][RG + rg], t1, e1, s1, s0);
   }
-  if (step < steps) {
-    one(step, s0, s1);
-    rest(s0);
-  } else {
+  arrive();  // the last step, in which tiles may have no rows
+  if (__builtin_amdgcn_ballot_w64(tok_next[0] >= 0) == 0) {
     rest(s1);
+  } else {
+    one(tiles[step & 1][rg], tok_next[0], lse_next[0], s0, s1);
+    if (__builtin_amdgcn_ballot_w64(tok_next[1] >= 0) == 0) {
+      rest(s0);
+    } else {
+      one(tiles[step & 1][RG + rg], tok_next[1], lse_next[1], s1, s0);
+      rest(s1);
+    }
   }
   // over the 32 rows of a tile: lane l31 is left with value l31 = 16 b + r of its half, slot 32 b + 16 hh + r
   float v[32];
@@ -242,7 +232,7 @@ int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads,
   a.n_pages = pg.n_pages;
   a.n_kv = n_kv;
   a.group = n_heads / n_kv;
-  a.group_inv = UINT32_MAX / (uint32_t)a.group + 1;  // (not used where group is 1)
+  a.group_inv = a.group == 1 ? 0 : UINT32_MAX / (uint32_t)a.group + 1;
   a.n = ck.n;
   a.decay = decay;
   int most = 0, tiles = 0;
@@ -255,7 +245,7 @@ int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads,
     waves += (long long)pages * n_kv;
   }
   a.rg = 1;
-  while (a.rg < 4 && waves * a.rg < 2048 && tiles >= 4 * a.rg) a.rg *= 2;
+  while (a.rg < most_rg(head_dim / 16 * q_terms) && waves * a.rg < 2048 && tiles >= 8 * a.rg) a.rg *= 2;
   a.sg = 1;
   while (a.sg * a.rg < 8 && waves * a.rg >= 512ll * a.sg * a.rg) a.sg *= 2;
   const int groups = (most + a.sg - 1) / a.sg;

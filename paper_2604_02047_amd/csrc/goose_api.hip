@@ -1088,7 +1088,7 @@ int goose_attn_weight_paged(goose_ctx* c, const goose_pages* pg, int layer, cons
   rc = chunk_reqs(pg, chunks, n, true, &ck);
   if (!rc) rc = check_first(ck);
   if (rc) return rc;
-  if (ld_lse < (size_t)ck.rows) return GOOSE_ERR_ARG;
+  if (ld_lse < (size_t)ck.rows || ld_lse > UINT32_MAX) return GOOSE_ERR_ARG;
   return launch_attn_weight(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, d_q, ldq, q_terms, ck, d_lse, ld_lse, decay, d_weight,
                             c->flags, as_stream(stream));
 }
