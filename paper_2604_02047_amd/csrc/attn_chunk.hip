@@ -11,7 +11,8 @@ namespace {
 
 struct ChunkItems {
   int32_t tiles, splits;  // work items: tiles of 256 rows x ranges of their blocks, for every KV head
-  int32_t pair0;          // its first (token, head) pair in the merge
+  int32_t waves;          // 32-row tiles of a KV head
+  int32_t join0;          // its first 32-row tile in the merge
   uint32_t rec0;          // its first record
 };
 struct ChunkArgs {
@@ -20,8 +21,8 @@ struct ChunkArgs {
   const int32_t* table;
   const int32_t* len;
   const void* q;
-  float* ws_o;    // [record][d]; records of a chunk: [split][token][head]
-  float* ws_ml;   // [record][2]: largest score (unscaled), sum of weights
+  float* ws_o;    // [record][d / 8][64 lanes][4], a wavefront's accumulators as it holds them; records of a chunk: [split][KV head][32-row tile]
+  float* ws_ml;   // [record][32][2]: largest score (unscaled), sum of weights
   unsigned short* o;
   float* lse;
   int32_t* flags;
@@ -58,21 +59,30 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
   const int kvh = (int)blockIdx.x - y * a.n_kv;  // the fast index: where 8 divides the KV heads, all items of a head run on one XCD
   int ri = 0;
   while (y >= a.it[ri].tiles * a.it[ri].splits) { y -= a.it[ri].tiles * a.it[ri].splits; ++ri; }
+  ri = __builtin_amdgcn_readfirstlane(ri);
+  y = __builtin_amdgcn_readfirstlane(y);
   const ChunkReq& rq = a.r[ri];
   const ChunkItems& ci = a.it[ri];
-  const int P = chunk_length(a.len, rq, a.flags, tid == 0 && y == 0 && kvh == 0);
   const int split = __builtin_amdgcn_readfirstlane((int)((unsigned)y / (unsigned)ci.tiles));
   const int tile = ci.tiles - 1 - (y - split * ci.tiles);  // (the longest first)
   const int rows = rq.C * a.group, wg_first = tile * 256, row_first = wg_first + wave * 32;
+  auto query = [&](int rho) -> const T* {
+    const int at = min(rho, rows - 1), tok = (int)((unsigned)at / (unsigned)a.group), h = kvh * a.group + at - tok * a.group;
+    return static_cast<const T*>(a.q) + ((size_t)rq.row0 + tok) * a.ldq + ((size_t)h * D + hh * 8) * QT;
+  };
+  Tile t;
+  t.init(query(row_first + l31));  // (asked for in front of the length, which all else waits for)
+  const int P = chunk_length(a.len, rq, a.flags, tid == 0 && y == 0 && kvh == 0);
   auto token_of = [&](int rho) { return __builtin_amdgcn_readfirstlane((int)((unsigned)min(rho, rows - 1) / (unsigned)a.group)); };
   auto clamp = [](int x, int lo, int hi) { return min(max(x, lo), hi); };
   // blocks that the tile's last row sees, this item's range of them, and the blocks of it in front of the chunk's end
   const int total = (P + token_of(wg_first + 255)) / 32 + 1;
-  const int b_lo = __builtin_amdgcn_readfirstlane((int)((unsigned)(total * split) / (unsigned)ci.splits));
-  const int b_hi = __builtin_amdgcn_readfirstlane((int)((unsigned)(total * (split + 1)) / (unsigned)ci.splits));
-  const int units = clamp((P + rq.C) / 32 - b_lo, 0, b_hi - b_lo);
+  const int b_lo = __builtin_amdgcn_readfirstlane((int)((unsigned)total * (unsigned)split / (unsigned)ci.splits));
+  const int b_hi = __builtin_amdgcn_readfirstlane((int)((unsigned)total * (unsigned)(split + 1) / (unsigned)ci.splits));
+  const int units = __builtin_amdgcn_readfirstlane(clamp((P + rq.C) / 32 - b_lo, 0, b_hi - b_lo));
   // of the ring's units: from `whole` on some rows of this wavefront do not see all of it, from `seen` on none sees any
-  const int whole = (P + token_of(row_first) + 1) / 32 - b_lo, seen = row_first < rows ? clamp((P + token_of(row_first + 31)) / 32 + 1 - b_lo, 0, units) : -1;
+  const int whole = __builtin_amdgcn_readfirstlane((P + token_of(row_first) + 1) / 32 - b_lo);
+  const int seen = __builtin_amdgcn_readfirstlane(row_first < rows ? clamp((P + token_of(row_first + 31)) / 32 + 1 - b_lo, 0, units) : -1);
   PageIds pg{a.table + (size_t)rq.seq * a.table_ld, a.flags, b_lo >> 1, (b_hi - 1) >> 1, a.n_pages, 0};
   if (b_hi > b_lo) pg.load(lane);
   const char* const kp = static_cast<const char*>(a.kpool);
@@ -81,12 +91,6 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
     return (size_t)(unsigned)((pg.of(b, lane) * a.n_kv + kvh) * 2 + (b & 1)) * (32 * D * 2);
   };
   const int last = P + (int)((unsigned)min(row_first + l31, rows - 1) / (unsigned)a.group) - b_lo * 32 - hh * 16;  // the last slot that this lane's row sees
-  auto query = [&](int rho) -> const T* {
-    const int at = min(rho, rows - 1), tok = (int)((unsigned)at / (unsigned)a.group), h = kvh * a.group + at - tok * a.group;
-    return static_cast<const T*>(a.q) + ((size_t)rq.row0 + tok) * a.ldq + ((size_t)h * D + hh * 8) * QT;
-  };
-  Tile t;
-  t.init(query(row_first + l31));
   const float scale = softmax_scale(D);
   const bool keys = wave < 4;          // the first four wavefronts copy keys, the others values
   const int share = wave * CP * 1024;  // this wavefront's pieces of a block
@@ -105,10 +109,10 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
       copy_pieces<CP>(pool + block_at(min(b_lo + next, b_hi - 1)), lane, ring + (next & (RING - 1)) * BLOCK + share);
       ++next;
     };
-    const int first = keys ? RING : RING - 1;
+    const int first = keys ? RING : RING - 2;
     while (next < first) copy();
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3) * CP));  // units 0 to 2 (values: 0 and 1)
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3) * CP));  // units 0 to 2 (values: 0)
     barrier();
     u32x4 pc[AHEAD];
     f32x16 z1;
@@ -131,15 +135,16 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) pc[n] = keys_of(2)[n * 64];
     }
-    barrier();
-    if (keys) copy();  // (unit RING, where unit 0 was)
-    // Before step j the keys of unit j + 2 and the values of unit j - 1 have landed in every wavefront's share; keys of unit j and values of
-    // unit j - 2 are no longer read, and make room for those RING units later.
-    auto step = [&](int j, const f32x16& za, f32x16& zb, const auto& w, const auto& wl, auto& wn, auto& wln) {
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3) * CP));
+    // Steps j and j + 1 between two barriers.  Before them the keys of units up to j + 3 and the values of units up to j have landed in every
+    // wavefront's share; keys of units up to j and values of units up to j - 2 are no longer read, and make room for those RING units later.
+    auto arrive = [&]() {
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(3 * CP));
       barrier();
       __builtin_amdgcn_sched_barrier(0);
       copy();
+      copy();
+    };
+    auto step = [&](int j, const f32x16& za, f32x16& zb, const auto& w, const auto& wl, auto& wn, auto& wln) {
       if (j > seen || seen == 0) return;
       ring_step<D, QT, F16, PT, 1, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale,
                                           [&](f32x16& s) {
@@ -152,10 +157,12 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
     };
     int j = 1;
     for (; j + 1 < units; j += 2) {
+      arrive();
       step(j, t.s, z1, t.p, t.pl, w1, wl1);
       step(j + 1, z1, t.s, w1, wl1, t.p, t.pl);
     }
     if (j < units) {
+      arrive();
       step(j, t.s, z1, t.p, t.pl, w1, wl1);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -216,35 +223,35 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
     }
   }
   const float l = t.l + __shfl_xor(t.l, 32, 64);
-  if (rho >= rows) return;
+  auto quads = [&](auto each) {  // (accumulators 4 q to 4 q + 3 of column tile dt are columns 32 dt + 8 q + 4 hh .. + 3)
 #pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
+    for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 x = {t.o[dt][q * 4], t.o[dt][q * 4 + 1], t.o[dt][q * 4 + 2], t.o[dt][q * 4 + 3]};
-      const int c = (dt * 4 + q) * 8 + hh * 4;
-      if (ci.splits == 1) {
-        finish(a, (size_t)rq.row0 + tok, h, D, c, x, t.m, l);
-      } else {
-        const size_t rec = ci.rec0 + ((size_t)split * rq.C + tok) * a.n_heads + h;
-        if (c == 0) *reinterpret_cast<float2*>(a.ws_ml + rec * 2) = make_float2(t.m, l);
-        *reinterpret_cast<f32x4*>(a.ws_o + rec * D + c) = x;
-      }
-    }
+      for (int q = 0; q < 4; ++q) each(dt * 4 + q, f32x4{t.o[dt][q * 4], t.o[dt][q * 4 + 1], t.o[dt][q * 4 + 2], t.o[dt][q * 4 + 3]});
+  };
+  if (ci.splits > 1) {
+    const size_t rec = ci.rec0 + ((size_t)split * a.n_kv + kvh) * ci.waves + tile * 8 + wave;
+    if (hh == 0) *reinterpret_cast<float2*>(a.ws_ml + (rec * 32 + l31) * 2) = make_float2(t.m, l);
+    quads([&](int i, const f32x4& x) { *reinterpret_cast<f32x4*>(a.ws_o + (rec * (D / 8) + i) * 256 + lane * 4) = x; });
+  } else if (rho < rows) {
+    quads([&](int i, const f32x4& x) { finish(a, (size_t)rq.row0 + tok, h, D, i * 8 + hh * 4, x, t.m, l); });
+  }
 }
 
-// Joins the splits of a row: D / 4 threads a (token, head), four columns each, records in their order, four in flight together.
+// Joins the splits of a 32-row tile: a thread the four columns that a lane held, records in their order, four in flight together.
 template <int D>
-__global__ __launch_bounds__(256) void k_chunk_merge(const ChunkArgs a, int pairs) {
-  constexpr int TPR = D / 4;
-  const int tid = threadIdx.x, c = (tid % TPR) * 4;
-  int pair = blockIdx.x * (256 / TPR) + tid / TPR;
-  if (pair >= pairs) return;
+__global__ __launch_bounds__(256) void k_chunk_merge(const ChunkArgs a) {
+  constexpr int PER = D / 32;  // workgroups a tile, four quads of columns each
+  const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, hh = lane >> 5;
+  const int wg = blockIdx.x / PER, quad = (blockIdx.x - wg * PER) * 4 + (tid >> 6);
   int r = 0;
-  while (r + 1 < a.n && pair >= a.it[r + 1].pair0) ++r;
-  pair -= a.it[r].pair0;
-  const size_t step = (size_t)a.r[r].C * a.n_heads, rec0 = a.it[r].rec0 + (size_t)pair;
-  const int n = a.it[r].splits;
+  while (r + 1 < a.n && wg >= a.it[r + 1].join0) ++r;
+  const ChunkItems& ci = a.it[r];
+  const int kvh = (wg - ci.join0) / ci.waves, wt = wg - ci.join0 - kvh * ci.waves;
+  const int rho = wt * 32 + l31;
+  if (rho >= a.r[r].C * a.group) return;
+  const size_t rec0 = ci.rec0 + (size_t)kvh * ci.waves + wt, step = (size_t)a.n_kv * ci.waves;
+  const int n = ci.splits;
   const float scale = softmax_scale(D);
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
   float den = 0.f, m = -INFINITY;
@@ -254,8 +261,8 @@ __global__ __launch_bounds__(256) void k_chunk_merge(const ChunkArgs a, int pair
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const size_t rec = rec0 + (size_t)min(s0 + k, n - 1) * step;
-      ml[k] = *reinterpret_cast<const float2*>(a.ws_ml + rec * 2);
-      ov[k] = *reinterpret_cast<const f32x4*>(a.ws_o + rec * D + c);
+      ml[k] = *reinterpret_cast<const float2*>(a.ws_ml + (rec * 32 + l31) * 2);
+      ov[k] = *reinterpret_cast<const f32x4*>(a.ws_o + (rec * (D / 8) + quad) * 256 + lane * 4);
     }
     float m_new = m;
 #pragma unroll
@@ -272,8 +279,8 @@ __global__ __launch_bounds__(256) void k_chunk_merge(const ChunkArgs a, int pair
         num += w * ov[k];
       }
   }
-  const int tok = (int)((unsigned)pair / (unsigned)a.n_heads);
-  finish(a, (size_t)a.r[r].row0 + tok, pair - tok * a.n_heads, D, c, num, m, den);
+  const int tok = (int)((unsigned)rho / (unsigned)a.group), h = kvh * a.group + rho - tok * a.group;
+  finish(a, (size_t)a.r[r].row0 + tok, h, D, quad * 8 + hh * 4, num, m, den);
 }
 
 template <int D, int QT, bool F16>
@@ -294,13 +301,13 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
                       size_t ld_lse, int32_t* flags, hipStream_t st) {
   if (head_dim != 64 && head_dim != 128) return GOOSE_ERR_SHAPE;
   const int group = n_heads / n_kv;
-  // Chunks of few rows are chains of nodes for the tree kernels, which have shapes for them.
+  // Chunks of few rows are chains of nodes for the tree kernels, which have shapes for them: one token of 32 / 8 heads behind 4000 slots 17 us (the ring 26), 64 of
+  // them behind 2000, four requests 35 (44); of a multi-head model only up to 32 tokens (64 behind 8000: 53, the ring 33; behind 300: 13 and 16).
   PagedReqs few{};
   ChunkReqs many{};
-  const int few_rows = 128;
   for (int i = 0; i < ck.n; ++i) {
     const ChunkReq& c = ck.r[i];
-    if (c.C <= GOOSE_MAX_B && c.C * group <= few_rows) {
+    if (c.C <= GOOSE_MAX_B && c.C * group <= 256 && (group > 1 || c.C <= 32)) {
       few.r[few.n++] = PagedReq{c.seq, c.C, c.P_max, c.row0, few.rows, nullptr, nullptr};
       few.rows += c.C;
     } else {
@@ -359,36 +366,36 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
       items += tiles * splits * n_kv;
       const long long len = splits_of(blocks, splits) * step + fixed;
       most = len > most ? len : most;
-      if (splits > 1) records += (long long)splits * c.C * n_heads;
+      if (splits > 1) records += (long long)splits * n_kv * ((c.C * group + 31) / 32);
     }
-    if (records > (long long)max_records || records > UINT32_MAX) continue;
+    if (records * 32 > (long long)max_records) continue;
     const long long rounds = (items + 255) / 256, time = rounds * (work / items);
-    const long long cost = (time > most ? time : most) + (records > 0 ? 600 + records * head_dim * 8 / 50000 : 0);
+    const long long cost = (time > most ? time : most) + (records > 0 ? 600 + records * 32 * head_dim * 8 / 50000 : 0);
     if (cost < best) { best = cost; best_per = per; }
   }
   if (best_per == 0) best_per = longest;
-  size_t records = 0, pairs = 0;
+  uint32_t records = 0;
+  int joins = 0;
   long long items = 0;
   for (int i = 0; i < many.n; ++i) {
     const ChunkReq& c = many.r[i];
-    const int tiles = (c.C * group + 255) / 256, splits = splits_of((c.P_max + c.C + 31) / 32, best_per);
-    a.it[i] = ChunkItems{tiles, splits, (int32_t)pairs, (uint32_t)records};
+    const int tiles = (c.C * group + 255) / 256, waves = (c.C * group + 31) / 32, splits = splits_of((c.P_max + c.C + 31) / 32, best_per);
+    a.it[i] = ChunkItems{tiles, splits, waves, joins, records};
     if (splits > 1) {
-      records += (size_t)splits * c.C * n_heads;
-      pairs += (size_t)c.C * n_heads;
+      records += (uint32_t)(splits * n_kv * waves);
+      joins += n_kv * waves;
     }
     a.r[i] = c;
     items += (long long)tiles * splits * n_kv;
   }
-  if (items > INT32_MAX || pairs > INT32_MAX) return GOOSE_ERR_CAPACITY;
+  if (items * 512 > UINT32_MAX) return GOOSE_ERR_CAPACITY;  // (threads of a launch)
   const bool f16 = dtype == GOOSE_DTYPE_F16;
   if (head_dim == 128) launch_d<128>(f16, q_terms, p_terms, dim3((unsigned)items), a, st);
   else launch_d<64>(f16, q_terms, p_terms, dim3((unsigned)items), a, st);
   const int rc = goose_launch_status();
-  if (rc != GOOSE_OK || pairs == 0) return rc;
-  const unsigned per_wg = 1024u / (unsigned)head_dim;
-  const dim3 grid((unsigned)((pairs + per_wg - 1) / per_wg));
-  if (head_dim == 128) hipLaunchKernelGGL(k_chunk_merge<128>, grid, dim3(256), 0, st, a, (int)pairs);
-  else hipLaunchKernelGGL(k_chunk_merge<64>, grid, dim3(256), 0, st, a, (int)pairs);
+  if (rc != GOOSE_OK || joins == 0) return rc;
+  const dim3 grid((unsigned)(joins * (head_dim / 32)));
+  if (head_dim == 128) hipLaunchKernelGGL(k_chunk_merge<128>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_chunk_merge<64>, grid, dim3(256), 0, st, a);
   return goose_launch_status();
 }
