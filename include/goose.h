@@ -393,7 +393,7 @@ int goose_verify_step_paged(goose_ctx* ctx, const goose_model_ptrs* model, const
 enum { GOOSE_MAX_CHUNK = 32768 };
 typedef struct {
   int32_t seq;            /* its sequence, none twice in a call */
-  int32_t C;              /* new tokens, 1 .. GOOSE_MAX_CHUNK */
+  int32_t C;              /* new tokens, 1 .. GOOSE_MAX_CHUNK, with query heads of a group at most 2^30 rows */
   int32_t P_max;          /* host upper bound of d_len[seq]; P_max + C <= table_ld * 64 */
   int32_t first;          /* tokens before it leave no weight (0 .. C - 1) */
   const int32_t* d_pos;   /* [C] positions of the rotation, NULL: P + i */
@@ -414,7 +414,8 @@ int goose_attn_chunk_paged(goose_ctx* ctx, const goose_pages* pages, int layer, 
 /* What the slots of n sequences weigh: d_weight fp32 [n_layers][n_seqs][n_kv_heads][table_ld * 64].  For layer `layer` and every KV head,
  *   w[s] = decay * w[s] + sum over tokens i >= first with s <= P + i and over the head's query heads of exp(score - lse),   s < P,
  * and the sum alone for the chunk's own slots P <= s < P + C; other entries stay as they are.  With decay = 0 what was there is not
- * read.  d_q, d_lse: as for and from goose_attn_chunk_paged (P_max, first of each chunk); rows before `first` are not read; ldq <= 2^26.  0 <= decay, finite.
+ * read.  d_q, d_lse: as for and from goose_attn_chunk_paged (P_max, first of each chunk); rows before `first` are not read; ldq <= 2^26,
+ * ld_lse < 2^32.  0 <= decay, finite.
  * A row whose lse is -infinity weighs nothing; a NaN in a token's score or lse makes the slots NaN that it concerns.  The sums are
  * formed in a fixed order.  A sequence whose length is out of range, slots of pages out of range: flagged and left alone. */
 int goose_attn_weight_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,

@@ -20,7 +20,7 @@ struct WeightArgs {
   int32_t* flags;
   size_t ldq, ld_lse;
   int32_t table_ld, n_pages, n_kv, group, n;
-  uint32_t group_inv;  // ceil(2^32 / group), 0 for groups of one: row / group = mulhi(row, group_inv) for rows below 2^32 / group
+  uint32_t group_inv;  // ceil(2^32 / group), 0 for groups of one: mulhi(row, group_inv) is row / group, or one more
   int32_t sg, rg;  // a workgroup's wavefronts: sg pages x rg of the tiles in turn
   float decay;
   ChunkReq r[GOOSE_MAX_REQUESTS];
@@ -80,10 +80,10 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
     if (tid == 0 && blockIdx.x == 0) atomicOr(a.flags, GOOSE_FLAG_CAPACITY);
     return;
   }
-  const int end = P + rq.C;
-  if (first_page * GOOSE_PAGE >= end) return;
-  const int slot0 = (first_page + sg) * GOOSE_PAGE;
-  bool live = slot0 < end;
+  const int end = P + rq.C, pages = (end + GOOSE_PAGE - 1) / GOOSE_PAGE;
+  if (first_page >= pages) return;
+  bool live = first_page + sg < pages;
+  const int slot0 = live ? (first_page + sg) * GOOSE_PAGE : 0;
   const int page = __builtin_amdgcn_readfirstlane(live ? a.table[(size_t)rq.seq * a.table_ld + first_page + sg] : 0);
   if ((unsigned)page >= (unsigned)a.n_pages) {
     if (lane == 0) atomicOr(a.flags, GOOSE_FLAG_PAGES);
@@ -107,7 +107,9 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int rho = row0 + ((step * U + u) * RG + rg) * 32 + l31, at = min(rho, rows - 1);
-      const int tok = inv == 0 ? at : (int)__umulhi((unsigned)at, inv), h = at - tok * group;  // (behind the last row: that one)
+      // (behind the last row: that one)
+      int tok = inv == 0 ? at : (int)__umulhi((unsigned)at, inv), h = at - tok * group;
+      if (h < 0) { --tok; h += group; }
       lse_next[u] = lse0[(size_t)(unsigned)h * ld_lse + (unsigned)tok];
       tok_next[u] = rho < rows ? tok : -1;
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -249,7 +251,7 @@ int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads,
   a.sg = 1;
   while (a.sg * a.rg < 8 && waves * a.rg >= 512ll * a.sg * a.rg) a.sg *= 2;
   const int groups = (most + a.sg - 1) / a.sg;
-  if ((long long)groups * n_kv > INT32_MAX) return GOOSE_ERR_CAPACITY;
+  if ((long long)groups * n_kv * (64 * a.sg * a.rg) > UINT32_MAX) return GOOSE_ERR_CAPACITY;  // (threads of a launch)
   const dim3 grid((unsigned)groups * (unsigned)n_kv, (unsigned)ck.n);
   const bool f16 = dtype == GOOSE_DTYPE_F16;
   if (head_dim == 128) launch_d<128>(f16, q_terms, grid, a, st);

@@ -1036,7 +1036,7 @@ int goose_verify_step_paged(goose_ctx* c, const goose_model_ptrs* m, const goose
 
 // ---- chunks of new tokens, eviction
 // rows: the call works on stacked rows and launches by P_max.
-static int chunk_reqs(const goose_pages* pg, const goose_chunk* chunks, int n, bool rows, ChunkReqs* out) {
+static int chunk_reqs(const goose_ctx* c, const goose_pages* pg, const goose_chunk* chunks, int n, bool rows, ChunkReqs* out) {
   if (!chunks || n < 1 || n > GOOSE_MAX_REQUESTS) return GOOSE_ERR_ARG;
   int row0 = 0;
   out->n = n;
@@ -1048,6 +1048,7 @@ static int chunk_reqs(const goose_pages* pg, const goose_chunk* chunks, int n, b
     if (rows) {
       if (q.P_max < 0) return GOOSE_ERR_ARG;
       if ((long long)q.P_max + q.C > (long long)pg->table_ld * GOOSE_PAGE) return GOOSE_ERR_CAPACITY;
+      if ((long long)q.C * (c->d.n_heads / c->n_kv) > (1 << 30)) return GOOSE_ERR_CAPACITY;  // (rows of a KV head, and of the tiles around them, are an int)
     }
     out->r[i] = ChunkReq{q.seq, q.C, rows ? q.P_max : 0, q.first, row0, q.d_pos};
     out->rows = row0 + q.C;
@@ -1071,7 +1072,7 @@ int goose_attn_chunk_paged(goose_ctx* c, const goose_pages* pg, int layer, const
   if (ldq < (size_t)c->Hq * q_terms || (ldq & 7) || ldo < (size_t)c->Hq * o_terms || (ldo & 7)) return GOOSE_ERR_ARG;
   if (((uintptr_t)d_q & 15) || ((uintptr_t)d_o & 15) || ((uintptr_t)d_lse & 3)) return GOOSE_ERR_ARG;
   ChunkReqs ck;
-  rc = chunk_reqs(pg, chunks, n, true, &ck);
+  rc = chunk_reqs(c, pg, chunks, n, true, &ck);
   if (rc) return rc;
   if (d_lse && ld_lse < (size_t)ck.rows) return GOOSE_ERR_ARG;
   return launch_attn_chunk(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, d_q, ldq, q_terms, ck, c->att_o, c->att_ml, attn_records(c), d_o,
@@ -1085,7 +1086,7 @@ int goose_attn_weight_paged(goose_ctx* c, const goose_pages* pg, int layer, cons
   if (!d_q || !d_lse || !d_weight || layer < 0 || layer >= c->d.n_layers || (q_terms != 1 && q_terms != 2) || !decay_ok(decay)) return GOOSE_ERR_ARG;
   if (ldq < (size_t)c->Hq * q_terms || ldq > (1u << 26) || (ldq & 7) || ((uintptr_t)d_q & 15) || ((uintptr_t)d_lse & 3) || ((uintptr_t)d_weight & 3)) return GOOSE_ERR_ARG;
   ChunkReqs ck;
-  rc = chunk_reqs(pg, chunks, n, true, &ck);
+  rc = chunk_reqs(c, pg, chunks, n, true, &ck);
   if (!rc) rc = check_first(ck);
   if (rc) return rc;
   if (ld_lse < (size_t)ck.rows || ld_lse > UINT32_MAX) return GOOSE_ERR_ARG;
@@ -1096,7 +1097,7 @@ int goose_attn_weight_paged(goose_ctx* c, const goose_pages* pg, int layer, cons
 int goose_pages_append(goose_ctx* c, const goose_pages* pg, const goose_chunk* chunks, int n, void* stream) {
   int rc = check_pages(c, pg);
   ChunkReqs ck;
-  if (!rc) rc = chunk_reqs(pg, chunks, n, false, &ck);
+  if (!rc) rc = chunk_reqs(c, pg, chunks, n, false, &ck);
   return rc ? rc : launch_pages_append(*pg, ck, c->flags, as_stream(stream));
 }
 
@@ -1130,7 +1131,7 @@ int goose_chunk_layer_paged(goose_ctx* c, const void* d_packed_layer, const goos
   pass.weight = d_weight;
   pass.decay = decay;
   ChunkReqs ck;
-  rc = chunk_reqs(pg, chunks, n, true, &ck);
+  rc = chunk_reqs(c, pg, chunks, n, true, &ck);
   if (!rc && d_weight) rc = check_first(ck);
   if (rc) return rc;
   if (round_up(ck.rows, 32) > c->max_rows) return GOOSE_ERR_CAPACITY;

@@ -125,15 +125,15 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
       for (int i = tid; i < bins; i += NT) hist[i] = 0;
       __syncthreads();
       const unsigned above = pass == 0 ? 0u : key >> (pass == 1 ? 21 : 10);
-      for (int s0 = lo; s0 < hi; s0 += SEG) {
+      for (unsigned s0 = lo; s0 < (unsigned)hi; s0 += SEG) {
         float v[WORDS];
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i) v[i] = s0 + i * NT < hi ? w[min(s0 + i * NT + tid, hi - 1)] : 0.f;
+        for (int i = 0; i < WORDS; ++i) v[i] = s0 + i * NT < (unsigned)hi ? w[min(s0 + i * NT + tid, (unsigned)hi - 1)] : 0.f;
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) {
-          if (s0 + i * NT >= hi) break;
+          if (s0 + i * NT >= (unsigned)hi) break;
           const unsigned x = key_of(v[i]);
-          if (s0 + i * NT + tid < hi && (pass == 0 || x >> (pass == 1 ? 21 : 10) == above)) atomicAdd(&hist[(x >> shift) & (bins - 1)], 1u);
+          if (s0 + i * NT + tid < (unsigned)hi && (pass == 0 || x >> (pass == 1 ? 21 : 10) == above)) atomicAdd(&hist[(x >> shift) & (bins - 1)], 1u);
         }
       }
       __syncthreads();
@@ -163,8 +163,8 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
   // ---- the words, ties to the lowest slots, and weights to the front: none of them is behind where it goes, and all of a segment are loaded before one
   // is stored
   int left = ties, base = 0;
-  for (int c0 = 0; c0 < len; c0 += SEG) {
-    const int first = (c0 >> 6) + wave * WORDS;  // this wavefront's words
+  for (unsigned c0 = 0; c0 < (unsigned)len; c0 += SEG) {
+    const int first = (int)(c0 >> 6) + wave * WORDS;  // this wavefront's words
     float v[WORDS];
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) v[i] = first + i < n_words ? w[min((first + i) * GOOSE_PAGE + lane, len - 1)] : 0.f;
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
     int mine = 0;
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) {
-      const int s = (first + i) * GOOSE_PAGE + lane;
+      const int s = first + i < n_words ? (first + i) * GOOSE_PAGE + lane : INT32_MAX;  // (behind the last word: no slot)
       const unsigned x = key_of(v[i]);
       const bool mid = m > 0 && s >= lo && s < hi;
       same[i] = __builtin_amdgcn_ballot_w64(mid && x == key);

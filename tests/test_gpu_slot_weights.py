@@ -8,7 +8,7 @@ import torch
 
 import paper_2604_02047_amd as goose
 from paper_2604_02047_amd import binding as gb
-from paged_ref import PAGE, rows_of
+from paged_ref import PAGE, pack_pages, rows_of
 from prompt_ref import chunk_attention64, slot_weights64
 from test_gpu_chunk_attn import Case as AttnCase
 
@@ -197,3 +197,63 @@ def test_refusals():
     call()
     c.first = [3]
     c.check_weights(1.0)
+
+
+def test_many_heads_under_one_and_many_rows():
+    """1991 query heads of one KV head x 1200 tokens: the row count times the heads passes 32 bits.  (lse: any numbers serve.)"""
+    C, P, first = 1200, 70, 1140
+    c = Case(1991, 1, 64, "bf16", [C], [P], seed=9, scale=0.5)
+    c.place()
+    c.first = [first]
+    c.chunks = goose.PagedChunks([{"seq": 0, "C": C, "P_max": P, "first": first}])
+    c.lse[:, :C] = torch.linspace(2.0, 6.0, 1991).view(-1, 1) + torch.arange(C).view(1, -1) * 1e-3
+    c.k64 = [rows_of(c.k[0], c.table[0], P + C).double()]
+    c.old = torch.zeros((1, 1, 1, c.cache.table.shape[1] * PAGE))
+    c.weight = c.old.to(DEV)
+    c.weigh()
+    c.check_weights(1.0)
+
+
+def test_the_longest_table():
+    """2^31 - 64 slots, all of them in one page: every page of 64 entries gets the same sums."""
+    slots, C, d = 2 ** 31 - 64, 3, 64
+    g = torch.Generator().manual_seed(10)
+    k = torch.randn((1, 1, 1, PAGE, d), generator=g).half()
+    kp, vp = pack_pages(k, k)
+    table = torch.zeros((1, slots // PAGE), dtype=torch.int32, device=DEV)
+    P = slots - C
+    cache = goose.PagedCache(kp.to(DEV), vp.to(DEV), table, torch.tensor([P], dtype=torch.int32, device=DEV),
+                             torch.full((1,), slots // PAGE, dtype=torch.int32, device=DEV))
+    ctx = goose.GooseContext(goose.ModelDesc(1, 128, 1, d, 128, 1024, dtype="f16", n_kv_heads=1), 8, 64, 32)
+    q = torch.randn((C, d), generator=g).half()
+    lse = torch.full((1, C), 3.0)
+    weight = torch.full((1, 1, 1, slots), 7.0, device=DEV)
+    ctx.goose_attn_weight_paged(cache, 0, q.to(DEV), 1, [{"seq": 0, "C": C, "P_max": P}], lse.to(DEV), weight, 0.0)
+    assert ctx.goose_device_flags() == 0
+    ctx.close()
+    new, err = slot_weights64(q.double().view(C, 1, d), k[0, 0].double().repeat(1, 2, 1), lse.double(), 2 * PAGE - C, 0)
+    tol = (err + new * 4 * 2.0 ** -24 + C * 2.0 ** -126) * 1.001
+    w = weight.view(-1, PAGE)
+    assert ((w[0].cpu().double() - new[0, :PAGE]).abs() <= tol[0, :PAGE]).all()
+    assert ((w[-1].cpu().double() - new[0, PAGE:]).abs() <= tol[0, PAGE:]).all()
+    for at in range(0, w.shape[0] - 1, 1 << 22):
+        assert (w[at:min(at + (1 << 22), w.shape[0] - 1)] == w[0]).all()
+
+
+def test_more_rows_under_a_head_than_are_counted():
+    """2^30 rows at most; refused before anything is looked at."""
+    n = 32769
+    c = Case(4, 2, 64, "bf16", [40], [100], seed=8)
+    c.setup()
+    table = torch.zeros((1, 600), dtype=torch.int32, device=DEV)
+    pool = torch.zeros((1, 1, 1, PAGE * 64), dtype=torch.bfloat16, device=DEV)
+    one = torch.ones(1, dtype=torch.int32, device=DEV)
+    cache = goose.PagedCache(pool, pool.clone(), table, one * 0, one)
+    ctx = goose.GooseContext(goose.ModelDesc(1, 128, n, 64, 128, 1024, dtype="bf16", n_kv_heads=1), 1, 64, 32)
+    chunks = goose.PagedChunks([{"seq": 0, "C": 32768, "P_max": 0}])
+    at = c.q.data_ptr()
+    rc = ctx.lib.goose_attn_weight_paged(ctx._h, cache._ref, 0, at, n * 64, 1, chunks._c, 1, at, 32768, 1.0, at, 0)
+    assert rc == gb.GOOSE_ERR_CAPACITY
+    rc = ctx.lib.goose_attn_chunk_paged(ctx._h, cache._ref, 0, at, n * 64, 1, chunks._c, 1, at, n * 64, gb.GOOSE_DTYPE_BF16, 1, 0, 0, 0)
+    assert rc == gb.GOOSE_ERR_CAPACITY
+    ctx.close()
