@@ -42,7 +42,7 @@ __device__ __forceinline__ void finish(const ChunkArgs& a, size_t row, int h, in
 // registers, into a ring that runs several blocks ahead; a wavefront has three blocks under way at once (ring_step).  Blocks that a
 // wavefront's rows do not see whole are masked on the way, and behind the last one that it sees it only goes on copying.
 // A weight of zero does not keep a NaN or an infinity of an unseen slot's values out of the matrix instruction: a wavefront that has such a thing in its
-// outputs at the end starts again, block by block with values_odd.  The block that the chunk ends in, whose other slots may hold anything, follows that way always.
+// outputs at the end starts again, block by block with values_odd and sums in the ring's order: rows that do not see the thing keep their bits.  The block that the chunk ends in, whose other slots may hold anything, follows that way always.
 template <int D, int QT, bool F16, int PT>
 __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
   typedef RowTile<D, QT, F16, PT> Tile;
@@ -121,14 +121,14 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
       u32x4 k[NS];
 #pragma unroll
       for (int s = 0; s < NS; ++s) k[s] = keys_of(0)[s * 64];
-      t.scores(k);
+      t.template scores<true>(k);
       if (whole <= 0) t.mask(seen16(last));
       t.maximum();
       t.rescale(scale);
       t.weights();
 #pragma unroll
       for (int s = 0; s < NS; ++s) k[s] = keys_of(1)[s * 64];
-      t.scores(k);
+      t.template scores<true>(k);
       if (whole <= 1) t.mask(seen16(last - 32));
       t.maximum();
       t.rescale_later(scale, t.s, units > 1);
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
       u32x4 v[NS];
 #pragma unroll
       for (int s = 0; s < NS; ++s) v[s] = keys_of(units - 1)[BU / 2 + s * 64];
-      t.values(v);
+      t.template values<true>(v);
     }
   }
   if (row_first >= rows) return;
@@ -212,14 +212,14 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
         fetch(vp + at, lane, v);
       }
       const unsigned vis = seen16(P + tok - b * 32 - hh * 16);
-      t.scores(k);
+      t.template scores<true>(k);
       t.mask(vis);
       const bool odd = clean_values<F16>(v, P + rq.C - b * 32 - hh * 16);
       t.maximum();
       t.rescale(scale);
       t.weights();
-      if (odd) t.values_odd(v, vis);
-      else t.values(v);
+      if (odd) t.template values_odd<true>(v, vis);
+      else t.template values<true>(v);
     }
   }
   const float l = t.l + __shfl_xor(t.l, 32, 64);

@@ -118,13 +118,18 @@ struct RowTile {
       if (QT == 2) ql[k] = *reinterpret_cast<const op8*>(at + k * 32 + 8);
     }
   }
+  // PAIRED, here and in values(): the two terms of a piece one after the other, as ring_step adds them up.
+  template <bool PAIRED = false>
   __device__ __forceinline__ void scores(const u32x4 (&k)[NS]) {
     f32x16 sum;
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum[r] = 0.f;
 #pragma unroll
-    for (int i = 0; i < NS; ++i) sum = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[i]), q[i], sum);
-    if (QT == 2) {
+    for (int i = 0; i < NS; ++i) {
+      sum = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[i]), q[i], sum);
+      if (PAIRED && QT == 2) sum = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[i]), ql[i % (QT == 2 ? NS : 1)], sum);
+    }
+    if (!PAIRED && QT == 2) {
 #pragma unroll
       for (int i = 0; i < NS; ++i) sum = Mma16<F16>::mfma(__builtin_bit_cast(op8, k[i]), ql[i], sum);
     }
@@ -223,12 +228,16 @@ struct RowTile {
 #pragma unroll
     for (int i = 0; i < 8; ++i) weights_of(i, s, p, pl);
   }
+  template <bool PAIRED = false>
   __device__ __forceinline__ void values(const u32x4 (&v)[NS]) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), p[j], o[dt]);
-    if constexpr (PT == 1) return;
+      for (int dt = 0; dt < NDT; ++dt) {
+        o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), p[j], o[dt]);
+        if constexpr (PAIRED && PT == 2) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), pl[j], o[dt]);
+      }
+    if constexpr (PAIRED || PT == 1) return;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -237,6 +246,7 @@ struct RowTile {
   // The second product of a block with a NaN or an infinity in a value that some rows do not see (through the matrix instruction it
   // would reach them as 0 * NaN): those elements count as zero there, and a product of indicators (is it +inf, -inf, NaN) x (is it visible) tells
   // which outputs they reach.  Rare.
+  template <bool PAIRED = false>
   __device__ __forceinline__ void values_odd(const u32x4 (&v)[NS], unsigned vis) {
     constexpr unsigned short EXP = F16 ? 0x7C00 : 0x7F80;
     const unsigned short ONE = __builtin_bit_cast(unsigned short, (T)1.f);
@@ -275,7 +285,7 @@ struct RowTile {
       for (int i = 0; i < 8; ++i) e[i] = (e[i] & EXP) == EXP ? (unsigned short)0 : e[i];
       w[k] = __builtin_bit_cast(u32x4, e);
     }
-    values(w);
+    values<PAIRED>(w);
   }
 };
 

@@ -336,3 +336,29 @@ def test_refusals():
     assert e.value.status == gb.GOOSE_ERR_CAPACITY
     call([dict(good[0], P_max=cap - 40)])
     assert ctx.goose_device_flags() == 0
+
+
+@pytest.mark.parametrize("nh,nkv,C", [(8, 2, 64), (8, 2, 65), (8, 1, 32), (8, 1, 33), (4, 4, 32), (4, 4, 33), (6, 2, 85), (6, 2, 86), (512, 2, 1), (514, 2, 1)])
+def test_both_sides_of_few_rows(nh, nkv, C):
+    for Cs, Ps in (([C], [1500]), ([C, 1, 200, C], [70, 900, 33, 0])):
+        c = Case(nh, nkv, 64, "bf16", Cs, Ps, seed=C)
+        c.check(c.run(), heads=sorted({0, nh // 2, nh - 1}))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("terms,o_terms", [(1, 1), (2, 1), (2, 2)])
+def test_odd_values_where_the_keys_are_split(dtype, d, terms, o_terms):
+    """NaN and infinities among the values of a long prefix, in a slot in the midst of the chunk and in its last one: only rows that see them have them."""
+    want = Case(4, 2, d, dtype, [290], [2501], seed=20, terms=terms, o_terms=o_terms)
+    o = want.run()[0]
+    for slot in (5, 1300, 2500, 2600, 2790):
+        c = Case(4, 2, d, dtype, [290], [2501], seed=20, terms=terms, o_terms=o_terms)
+        c.v[0, c.table[0, slot // PAGE], 0, slot % PAGE, 7] = float("nan")
+        c.v[0, c.table[0, slot // PAGE], 1, slot % PAGE, 9] = float("inf") if o_terms == 1 else float("nan")   # (two terms of infinity add up to NaN)
+        got = c.run()
+        c.check(got)
+        first = max(0, slot - 2501)
+        assert torch.equal(got[0][:first], o[:first])
+        x = got[0][first:290, :c.cols].view(-1, 4 * d // 8, o_terms, 8)[:, :, 0].reshape(-1, 4, d)
+        assert x[:, :2, 7].isnan().all() and (x[:, 2:, 9].isinf() if o_terms == 1 else x[:, 2:, 9].isnan()).all() and int((~x.isfinite()).sum()) == 4 * x.shape[0]
