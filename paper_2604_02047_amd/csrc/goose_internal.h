@@ -295,7 +295,7 @@ struct SeqList {
 // Device memory of the context through which the kernels of a paged call tell each other what they found.
 struct PageScratch {
   int4 copies[GOOSE_MAX_REQUESTS];      // of a reservation: page to copy (-1: none), its copy, 32-slot blocks; w of the first: it has failed
-  int32_t verdict[GOOSE_MAX_REQUESTS];  // of a commit: flags that a request raises instead of being done
+  int32_t verdict[GOOSE_MAX_REQUESTS];  // of a commit or an eviction: flags that a request raises instead of being done
 };
 int launch_pages_clear(const goose_pages& pg, hipStream_t st);
 int launch_pages_fork(const goose_pages& pg, int src, int len, const SeqList& dst, int32_t* flags, hipStream_t st);

@@ -3,10 +3,11 @@
 // An eviction keeps, per layer and KV head, the first `sink` slots, the last `recent` ones and the heaviest of the others.  Three launches:
 //   k_evict_select  a workgroup per (layer, KV head): the m-th largest weight by radix selection over order-preserving bit patterns
 //                   (2048 + 2048 + 1024 bins), ties to the lowest slots, the kept slots as bit words, weights to the front
-//   k_evict_move    a wavefront per (layer, KV head, K or V, 2 KiB of a 32-slot block): the blocks stream through registers in order,
+//   k_evict_move    one wavefront or eight per (layer, KV head, K or V, 2 KiB of a 32-slot block): the blocks stream through registers in order,
 //                   kept rows are collected in LDS and leave as whole blocks.  In place: a destination block never lies behind the
-//                   block that its last row came from, and blocks ahead are only read.
-//   k_evict_settle  lengths and pages
+//                   block that its last row came from, and blocks ahead are only read
+//   k_evict_settle  lengths and pages (the last workgroup to move could do it, but thousands that count themselves in one word cost more than the launch:
+//                   13B, 8 layers of 4 sequences of 28 slots 139 us against 67)
 // A rotation by the position that a key gives up needs both halves of its pairs, which is why a wavefront of the keys has columns
 // 16 u .. 16 u + 15 and those d/2 further.
 #include "mma16.h"
@@ -14,6 +15,9 @@
 
 namespace {
 
+#ifndef EVICT_FEW
+#define EVICT_FEW 1024
+#endif
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 
@@ -51,8 +55,6 @@ __global__ __launch_bounds__(256) void k_pages_append(const goose_pages pg, cons
   if (tid == 0) pg.d_len[q.seq] = end;
 }
 
-constexpr int NT = 1024;
-
 // Larger weights have larger keys; -0 is 0; a NaN is below every number.
 __device__ __forceinline__ unsigned key_of(float w) {
   if (w != w) return 0;
@@ -61,7 +63,9 @@ __device__ __forceinline__ unsigned key_of(float w) {
 }
 
 // Which flags a request raises instead of being cut (every workgroup of a launch that changes no table comes to the same verdict).
-__device__ inline int verdict_of(const goose_pages& pg, const goose_eviction& q, int len, int tid) {
+// mine: entry tid of its table (asked for beside the length).
+template <int NT>
+__device__ inline int verdict_of(const goose_pages& pg, const goose_eviction& q, int len, int tid, int mine) {
   if (len < 0 || (long long)len > (long long)pg.table_ld * GOOSE_PAGE) return GOOSE_FLAG_CAPACITY;
   const int pages = (len + GOOSE_PAGE - 1) / GOOSE_PAGE;
   // pages that rows move into must be the sequence's own
@@ -69,40 +73,51 @@ __device__ inline int verdict_of(const goose_pages& pg, const goose_eviction& q,
   const int own_lo = q.sink / GOOSE_PAGE, own_hi = moves ? (q.keep - 1) / GOOSE_PAGE : -1;
   bool bad = false;
   for (int i = tid; i < pages; i += NT) {
-    const int e = pg.d_table[(size_t)q.seq * pg.table_ld + i];
+    const int e = i == tid ? mine : pg.d_table[(size_t)q.seq * pg.table_ld + i];
     bad = bad || (unsigned)e >= (unsigned)pg.n_pages || (i >= own_lo && i <= own_hi && pg.d_refs[e] != 1);
   }
   return __syncthreads_or(bad) ? GOOSE_FLAG_PAGES : 0;
 }
 
 // What the wavefronts in front of this one have left in ws, and all of them.
-__device__ __forceinline__ void sums_of(const int (&ws)[NT / 64], int wave, int* before, int* all) {
-  int v[NT / 64];
+template <int W>
+__device__ __forceinline__ void sums_of(const int (&ws)[W], int wave, int* before, int* all) {
+  int v[W];
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) v[i] = ws[i];
+  for (int i = 0; i < W; ++i) v[i] = ws[i];
   *before = *all = 0;
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) {
+  for (int i = 0; i < W; ++i) {
     *before += i < wave ? v[i] : 0;
     *all += v[i];
   }
 }
 
+// Latency counts here, not bandwidth: what does not depend on the length is loaded beside it, and the slots that the workgroup takes at a time, WORDS words a
+// wavefront, stay in registers over all passes where they are all there are.
+template <int NT>
 __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const Evictions ev, int n_layers, int n_kv, float* __restrict__ weight,
                                                      uint64_t* __restrict__ kept, int32_t* __restrict__ verdict) {
-  constexpr int WORDS = 8, SEG = NT * WORDS;  // slots that the workgroup takes at a time: WORDS words a wavefront, all their loads in flight together
+  constexpr int WORDS = 8, SEG = NT * WORDS, W = NT / 64, PER = 2048 / NT;  // PER: bins of a thread
   __shared__ unsigned hist[2048];
-  __shared__ __attribute__((aligned(16))) int ws[NT / 64], wt[NT / 64];
+  __shared__ __attribute__((aligned(16))) int ws[W], wt[W];
   __shared__ int found[2];
   const goose_eviction q = ev.r[blockIdx.y];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int layer = blockIdx.x / n_kv, head = blockIdx.x - layer * n_kv;
-  const int len = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]);
-  const int bad = verdict_of(pg, q, len, tid);
-  if (blockIdx.x == 0 && tid == 0) verdict[blockIdx.y] = bad;
-  if (bad) return;
   uint64_t* const words = kept + (((size_t)blockIdx.y * n_layers + layer) * n_kv + head) * pg.table_ld;
   float* const w = weight + (((size_t)layer * pg.n_seqs + q.seq) * n_kv + head) * pg.table_ld * GOOSE_PAGE;
+  float v[WORDS];  // of words first_word .. first_word + WORDS - 1
+  auto fetch = [&](int first_word, int end) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) v[i] = first_word + i < end ? w[(size_t)(first_word + i) * GOOSE_PAGE + lane] : 0.f;
+  };
+  const int mine = tid < pg.table_ld ? pg.d_table[(size_t)q.seq * pg.table_ld + tid] : 0;
+  fetch(wave * WORDS, pg.table_ld);
+  const int len = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]);
+  const int bad = verdict_of<NT>(pg, q, len, tid, mine);
+  if (blockIdx.x == 0 && tid == 0) verdict[blockIdx.y] = bad;
+  if (bad) return;
   const int n_words = (len + GOOSE_PAGE - 1) / GOOSE_PAGE;
   for (int i = n_words + tid; i < pg.table_ld; i += NT) words[i] = 0;
   if (len <= q.keep) {
@@ -114,6 +129,7 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
   }
   // ---- the m-th largest weight of slots lo .. hi - 1: its key, and how many slots of just that weight are kept (ties)
   const int lo = q.sink, hi = len - q.recent, m = q.keep - q.sink - q.recent;
+  const bool one = len <= SEG;
   unsigned key = 0;
   int ties = 0;
   if (m > 0) {
@@ -125,22 +141,36 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
       for (int i = tid; i < bins; i += NT) hist[i] = 0;
       __syncthreads();
       const unsigned above = pass == 0 ? 0u : key >> (pass == 1 ? 21 : 10);
-      for (unsigned s0 = lo; s0 < (unsigned)hi; s0 += SEG) {
-        float v[WORDS];
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) v[i] = s0 + i * NT < (unsigned)hi ? w[min(s0 + i * NT + tid, (unsigned)hi - 1)] : 0.f;
+#pragma unroll 1
+      for (unsigned c0 = one ? 0 : (unsigned)lo / SEG * SEG; c0 < (unsigned)hi; c0 += SEG) {
+        const int first = (int)(c0 >> 6) + wave * WORDS;
+        if (!one) fetch(first, n_words);
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) {
-          if (s0 + i * NT >= (unsigned)hi) break;
+          if (first + i >= n_words) break;
+          const int s = (first + i) * GOOSE_PAGE + lane;
           const unsigned x = key_of(v[i]);
-          if (s0 + i * NT + tid < (unsigned)hi && (pass == 0 || x >> (pass == 1 ? 21 : 10) == above)) atomicAdd(&hist[(x >> shift) & (bins - 1)], 1u);
+          if (s >= lo && s < hi && (pass == 0 || x >> (pass == 1 ? 21 : 10) == above)) {
+            const unsigned bin = (x >> shift) & (bins - 1), some = __builtin_amdgcn_readfirstlane(bin);
+            const uint64_t here = __builtin_amdgcn_ballot_w64(true);
+            if (__builtin_amdgcn_ballot_w64(bin == some) == here) {  // (equal weights would come one after the other)
+              if ((here & ((1ull << lane) - 1)) == 0) atomicAdd(&hist[some], (unsigned)__popcll(here));
+            } else {
+              atomicAdd(&hist[bin], 1u);
+            }
+          }
         }
       }
       __syncthreads();
-      // thread t owns the bins 2 t, 2 t + 1 from the top: how many slots lie above them
-      const int b0 = bins - 1 - 2 * tid;
-      const int c0 = b0 >= 0 ? (int)hist[b0] : 0, c1 = b0 >= 1 ? (int)hist[b0 - 1] : 0;
-      int x = c0 + c1;
+      // thread t owns PER bins, from the top: how many slots lie above them
+      const int top = bins - 1 - PER * tid;
+      int c[PER], x = 0;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        c[j] = top >= j ? (int)hist[top - j] : 0;
+        x += c[j];
+      }
+      const int own = x;
 #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
         const int up = __shfl_up(x, off, 64);
@@ -150,9 +180,12 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
       __syncthreads();
       int before, all;
       sums_of(ws, wave, &before, &all);
-      before += x - c0 - c1;
-      if (before < ties && ties <= before + c0) { found[0] = b0; found[1] = before; }
-      else if (before + c0 < ties && ties <= before + c0 + c1) { found[0] = b0 - 1; found[1] = before + c0; }
+      before += x - own;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        if (before < ties && ties <= before + c[j]) { found[0] = top - j; found[1] = before; }
+        before += c[j];
+      }
       __syncthreads();
       key |= (unsigned)found[0] << shift;
       ties -= found[1];
@@ -163,11 +196,10 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
   // ---- the words, ties to the lowest slots, and weights to the front: none of them is behind where it goes, and all of a segment are loaded before one
   // is stored
   int left = ties, base = 0;
+#pragma unroll 1
   for (unsigned c0 = 0; c0 < (unsigned)len; c0 += SEG) {
     const int first = (int)(c0 >> 6) + wave * WORDS;  // this wavefront's words
-    float v[WORDS];
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) v[i] = first + i < n_words ? w[min((first + i) * GOOSE_PAGE + lane, len - 1)] : 0.f;
+    if (!one) fetch(first, n_words);
     uint64_t same[WORDS], more[WORDS];
     int mine = 0;
 #pragma unroll
@@ -214,19 +246,42 @@ __device__ __forceinline__ void in_order() {  // LDS of one wavefront: its instr
   asm volatile("" ::: "memory");
 }
 
-template <int D, bool F16>
-__global__ __launch_bounds__(64) void k_evict_move(const goose_pages pg, const Evictions ev, int n_layers, int n_kv, const double* __restrict__ inv_freq,
-                                                   const uint64_t* __restrict__ kept, bool reposition, const int32_t* __restrict__ verdict) {
+// Sine and cosine of 2 pi t for |t| <= 1/2: power series on an eighth of a turn to both sides (what they leave out is below 2^-25).
+__device__ __forceinline__ void turn(float t, float* sine, float* cosine) {
+  const float k = rintf(4.f * t), x = fmaf(k, -0.25f, t) * 6.2831853071795865f, z = x * x;
+  const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), x);
+  const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.f / 40320, -1.f / 720), 1.f / 24), -0.5f), 1.f);
+  const int q = (int)k;
+  const float a = (q & 1) ? c : s, b = (q & 1) ? s : c;
+  *sine = (q & 2) ? -a : a;
+  *cosine = ((q + 1) & 2) ? -b : b;
+}
+
+// A window is NW * AHEAD blocks, AHEAD next to each other a wavefront.  Its rows go into LDS, at the places of the destination blocks that they fill, while the next
+// window's loads are on their way; then the blocks that are full leave, and the wavefronts take turns at them.
+template <int D, bool F16, int NW>
+__global__ __launch_bounds__(64 * NW) void k_evict_move(const goose_pages pg, const Evictions ev, int n_layers, int n_kv, const double* __restrict__ inv_freq,
+                                                        const uint64_t* __restrict__ kept, bool reposition, const int32_t* __restrict__ verdict) {
   typedef typename Mma16<F16>::T T;
   typedef typename Mma16<F16>::v8 op8;
-  constexpr int UNITS = D / 32, AHEAD = 6, STAGES = 8;
-  // destination blocks that fill up (AHEAD blocks reach into AHEAD + 1 of them at most): [block % STAGES][piece][...], and the slots that their keys come from
-  __shared__ __attribute__((aligned(16))) unsigned short stage[STAGES][2][64 * 8];
+  constexpr int UNITS = D / 32, AHEAD = NW == 1 ? 6 : 3, WINDOW = NW * AHEAD, STAGES = NW == 1 ? 8 : 32;
+  static_assert(WINDOW + 1 <= STAGES, "a window reaches into WINDOW + 1 destination blocks");
+  // Destination blocks that fill up.  Keys: [block % STAGES][piece][...], and the slots that they come from.  Values: [column][slot % (32 STAGES)], a column's slots
+  // turned on by eight against those of the one before (else all would be in one bank), and behind them what takes the slots that go.
+  constexpr unsigned RING = STAGES * 32;
+  __shared__ __attribute__((aligned(16))) unsigned short stage[32 * RING + 64];
   __shared__ int from[STAGES][32];
   const goose_eviction q = ev.r[blockIdx.y];
-  const int lane = threadIdx.x, l31 = lane & 31, hh = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l31 = lane & 31, hh = lane >> 5;
   const int len = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]);
   if (__builtin_amdgcn_readfirstlane(verdict[blockIdx.y]) != 0 || len <= q.keep || q.sink >= q.keep) return;
+  auto sync = [&]() {  // LDS only: __syncthreads would wait for every load in flight
+    if constexpr (NW == 1) {
+      in_order();
+    } else {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+  };
   const int lh = blockIdx.x / (2 * UNITS), unit = blockIdx.x - lh * (2 * UNITS);
   const int layer = lh / n_kv, head = lh - layer * n_kv;
   const bool keys = unit < UNITS;
@@ -237,56 +292,78 @@ __global__ __launch_bounds__(64) void k_evict_move(const goose_pages pg, const E
   auto block_of = [&](int page, int b) -> T* { return pool + ((size_t)page * n_kv + head) * (GOOSE_PAGE * D) + (size_t)(b & 1) * 32 * D + lane * 8; };
   // a lane of the keys has eight columns of slot kk of a block; one of the values has 16 slots of a column: 16 hh to 16 hh + 15
   const int kk = ((l31 >> 2) & 1) * 16 + (l31 >> 3) * 4 + (l31 & 3);
-  double freq[8];
+  double turns[8];  // of a pair from one position to the next
   if (keys && reposition) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) freq[e] = inv_freq[unit * 16 + hh * 8 + e];
+    for (int e = 0; e < 8; ++e) turns[e] = inv_freq[unit * 16 + hh * 8 + e] * 0.15915494309189533577;
   }
-  const int b0 = q.sink >> 5, b_end = (len + 31) >> 5;
-  int at = b0 * 32;  // rows placed so far (all slots in front of b0 stay)
+  const int b0 = q.sink >> 5, b_end = (len + 31) >> 5;  // (all slots in front of b0 stay)
   u32x4 r0[AHEAD], r1[AHEAD];
   unsigned masks[AHEAD];
-  // Ids and words of 64 pages at a time, one a lane, where blocks come from; ids where they go (which never steps ahead of that): asked for block by
-  // block they would be two trips to memory each.
+  int places[AHEAD];  // where their first kept rows go
+  // Ids and words of 64 pages at a time, one a lane, where blocks come from, with the kept rows in front of each; ids where they go (which never
+  // steps ahead of that): asked for block by block they would be two trips to memory each.
   const int pages = (len + GOOSE_PAGE - 1) / GOOSE_PAGE;
-  int src0 = b0 >> 1, dst0 = src0, src_ids, dst_ids;
+  int src0 = b0 >> 1, dst0 = src0, src_ids, dst_ids, front = src0 * GOOSE_PAGE, sum;
   uint64_t src_words;
   auto src_window = [&]() {
     const int i = min(src0 + lane, pages - 1);
     src_ids = row[i];
     src_words = words[i];
+    sum = src0 + lane < pages ? (int)__popcll(src_words) : 0;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int up = __shfl_up(sum, off, 64);
+      if (lane >= off) sum += up;
+    }
+  };
+  // the word of block c's page, and how many kept rows lie in front of c (c never steps back)
+  auto word_of = [&](int c, int* before) -> unsigned {
+    while ((c >> 1) - src0 >= 64) {
+      front += __builtin_amdgcn_readlane(sum, 63);
+      src0 += 64;
+      src_window();
+    }
+    const int l = (c >> 1) - src0;
+    const unsigned low = (unsigned)__builtin_amdgcn_readlane((int)src_words, l), high = (unsigned)__builtin_amdgcn_readlane((int)(src_words >> 32), l);
+    *before = front + __builtin_amdgcn_readlane(sum, l) - __popc(high) - ((c & 1) ? 0 : __popc(low));
+    return (c & 1) ? high : low;
   };
   src_window();
   dst_ids = src_ids;
   const T* fetched = block_of(__builtin_amdgcn_readlane(src_ids, 0), b0);
   // (Always a load, of the last block again where nothing of this one is kept: one that may or may not be in flight would make the others wait for all.)
-  auto load = [&](int b, unsigned& mask, u32x4& x, u32x4& y) {
+  auto load = [&](int b, unsigned& mask, int& place, u32x4& x, u32x4& y) {
     const int c = min(b, b_end - 1);
-    if ((c >> 1) - src0 >= 64) { src0 = c >> 1; src_window(); }
-    const int l = (c >> 1) - src0;
-    const unsigned word = (c & 1) ? (unsigned)__builtin_amdgcn_readlane((int)(src_words >> 32), l) : (unsigned)__builtin_amdgcn_readlane((int)src_words, l);
+    const unsigned word = word_of(c, &place);
     mask = b < b_end ? word : 0;
-    if (mask != 0) fetched = block_of(__builtin_amdgcn_readlane(src_ids, l), c);
+    if (mask != 0) fetched = block_of(__builtin_amdgcn_readlane(src_ids, (c >> 1) - src0), c);
     x = *reinterpret_cast<const u32x4*>(fetched + p0 * 512);
     y = *reinterpret_cast<const u32x4*>(fetched + p1 * 512);
   };
   // whole destination block b, or its first n < 32 slots.  Keys are turned here, where every lane has one that is kept
   auto flush = [&](int b, int n) {
-    in_order();
-    if ((b >> 1) - dst0 >= 64) { dst0 = b >> 1; dst_ids = row[min(dst0 + lane, pages - 1)]; }
+    while ((b >> 1) - dst0 >= 64) { dst0 += 64; dst_ids = row[min(dst0 + lane, pages - 1)]; }
     T* const p = block_of(__builtin_amdgcn_readlane(dst_ids, (b >> 1) - dst0), b);
-    u32x4 x = *reinterpret_cast<const u32x4*>(&stage[b & (STAGES - 1)][0][lane * 8]), y = *reinterpret_cast<const u32x4*>(&stage[b & (STAGES - 1)][1][lane * 8]);
+    u32x4 x, y;
+    if (keys) {
+      x = *reinterpret_cast<const u32x4*>(&stage[(b & (STAGES - 1)) * 1024 + lane * 8]);
+      y = *reinterpret_cast<const u32x4*>(&stage[(b & (STAGES - 1)) * 1024 + 512 + lane * 8]);
+    } else {
+      const unsigned at = (unsigned)(b * 32 + hh * 16 + l31 * 8);
+      x = *reinterpret_cast<const u32x4*>(&stage[l31 * RING + (at & (RING - 1))]);
+      y = *reinterpret_cast<const u32x4*>(&stage[l31 * RING + ((at + 8) & (RING - 1))]);
+    }
     if (keys && reposition) {
       const int delta = b * 32 + kk - from[b & (STAGES - 1)][kk];
       if (delta != 0 && kk < n) {
         op8 lo = __builtin_bit_cast(op8, x), hi = __builtin_bit_cast(op8, y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const double two_pi = 6.283185307179586476925286766559;
-          double ang = (double)delta * freq[e];
-          ang -= two_pi * rint(ang / two_pi);
+          double t = (double)delta * turns[e];
+          t -= rint(t);
           float sn, c;
-          sincosf((float)ang, &sn, &c);
+          turn((float)t, &sn, &c);
           const float u = (float)lo[e], v = (float)hi[e];
           lo[e] = (T)(u * c - v * sn);
           hi[e] = (T)(v * c + u * sn);
@@ -308,54 +385,53 @@ __global__ __launch_bounds__(64) void k_evict_move(const goose_pages pg, const E
         if (hh * 16 + 8 + e < n) d1[e] = c[e];
       }
     }
-    in_order();
   };
-  auto place = [&](int b, unsigned mask, const u32x4& x, const u32x4& y) {
+  auto place = [&](int b, unsigned mask, int at, const u32x4& x, const u32x4& y) {
     if (mask == 0) return;
     if (keys) {
       const int to = at + __popc(mask & ((1u << kk) - 1)), d = to & 31;
       if ((mask >> kk) & 1) {
         const int l = (((d >> 2) & 3) << 3 | (d >> 4) << 2 | (d & 3)) + 32 * hh;
-        *reinterpret_cast<u32x4*>(&stage[(to >> 5) & (STAGES - 1)][0][l * 8]) = x;
-        *reinterpret_cast<u32x4*>(&stage[(to >> 5) & (STAGES - 1)][1][l * 8]) = y;
+        *reinterpret_cast<u32x4*>(&stage[((to >> 5) & (STAGES - 1)) * 1024 + l * 8]) = x;
+        *reinterpret_cast<u32x4*>(&stage[((to >> 5) & (STAGES - 1)) * 1024 + 512 + l * 8]) = y;
         from[(to >> 5) & (STAGES - 1)][d] = b * 32 + kk;
       }
     } else {
-      // slots e and 16 + e at once, one a half; where they go is the same for all columns, so scalar registers find it out
+      // (every slot is written, those that go behind the ring: no branches)
       const u16x8 a = __builtin_bit_cast(u16x8, x), c = __builtin_bit_cast(u16x8, y);
-      unsigned short* const base = &stage[0][0][l31 * 8];
-      int lo = at, hi = at + __popc(mask & 0xFFFFu);
-      auto offset = [](int to) { return ((to >> 5) & (STAGES - 1)) * 1024 + ((to >> 3) & 1) * 512 + ((to >> 4) & 1) * 256 + (to & 7); };
+      const int mine = (int)(hh ? mask >> 16 : mask & 0xFFFFu);
+      unsigned to = (unsigned)(at + (hh ? __popc(mask & 0xFFFFu) : 0) + l31 * 8);
+      const unsigned column = l31 * RING, gone = 32 * RING + lane;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const unsigned in_lo = (mask >> e) & 1, in_hi = (mask >> (16 + e)) & 1;
-        if ((in_lo | in_hi) == 0) continue;
-        const int o = hh ? offset(hi) : offset(lo);
-        if (hh ? in_hi : in_lo) base[o] = e < 8 ? a[e & 7] : c[e & 7];
-        lo += in_lo;
-        hi += in_hi;
+        const unsigned stays = (unsigned)((mine << (31 - e)) >> 31);  // all ones or none
+        const unsigned there = (to & (RING - 1)) | column;
+        stage[(there & stays) | (gone & ~stays)] = e < 8 ? a[e & 7] : c[e & 7];
+        to -= stays;
       }
     }
-    at += __popc(mask);
   };
 #pragma unroll
-  for (int k = 0; k < AHEAD; ++k) load(b0 + k, masks[k], r0[k], r1[k]);
+  for (int k = 0; k < AHEAD; ++k) load(b0 + wave * AHEAD + k, masks[k], places[k], r0[k], r1[k]);
   // (one copy of flush: its code, eight sines and cosines, would not fit the instruction cache several times; 690 us instead of 440 for 4 x 8192 slots)
   int done = b0;  // destination blocks written
 #pragma unroll 1
-  for (int b = b0;; b += AHEAD) {
-    const bool last = b >= b_end;
-    if (!last) {
+  for (int b = b0;; b += WINDOW) {
+    const bool last = b + WINDOW >= b_end;
+    int rows = q.keep;  // that the windows so far hold
+    if (!last) word_of(b + WINDOW, &rows);
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        place(b + k, masks[k], r0[k], r1[k]);
-        load(b + k + AHEAD, masks[k], r0[k], r1[k]);
-      }
+    for (int k = 0; k < AHEAD; ++k) {
+      place(b + wave * AHEAD + k, masks[k], places[k], r0[k], r1[k]);
+      load(b + WINDOW + wave * AHEAD + k, masks[k], places[k], r0[k], r1[k]);
     }
-    const int full = last ? (at + 31) >> 5 : at >> 5;
+    sync();
+    const int full = last ? (rows + 31) >> 5 : rows >> 5;
 #pragma unroll 1
-    for (; done < full; ++done) flush(done, min(32, at - done * 32));
+    for (int d = done + wave; d < full; d += NW) flush(d, min(32, rows - d * 32));
+    done = full;
     if (last) break;
+    sync();
   }
 }
 
@@ -382,15 +458,24 @@ int launch_pages_append(const goose_pages& pg, const ChunkReqs& ck, int32_t* fla
 
 int launch_pages_evict(int dtype, const goose_pages& pg, const Evictions& ev, int n_layers, int n_kv, int head_dim, const double* inv_freq,
                        float* weight, uint64_t* kept, bool reposition, PageScratch* scratch, int32_t* flags, hipStream_t st) {
-  hipLaunchKernelGGL(k_evict_select, dim3(n_layers * n_kv, ev.n), dim3(NT), 0, st, pg, ev, n_layers, n_kv, weight, kept, scratch->verdict);
+  // One segment in registers: 256 threads, of which more workgroups run side by side (13B, 8 layers of 4 sequences of 28 slots 11 us, with 1024 55).
+  const dim3 heads(n_layers * n_kv, ev.n);
+  if (pg.table_ld * GOOSE_PAGE <= 2048)
+    hipLaunchKernelGGL(k_evict_select<256>, heads, dim3(256), 0, st, pg, ev, n_layers, n_kv, weight, kept, scratch->verdict);
+  else
+    hipLaunchKernelGGL(k_evict_select<1024>, heads, dim3(1024), 0, st, pg, ev, n_layers, n_kv, weight, kept, scratch->verdict);
   int rc = goose_launch_status();
   if (rc != GOOSE_OK) return rc;
   const dim3 grid(n_layers * n_kv * (head_dim / 16), ev.n);
-  const bool f16 = dtype == GOOSE_DTYPE_F16;
-#define GOOSE_MOVE(D, H) hipLaunchKernelGGL((k_evict_move<D, H>), grid, dim3(64), 0, st, pg, ev, n_layers, n_kv, inv_freq, kept, reposition, scratch->verdict)
-  if (head_dim == 128) { if (f16) GOOSE_MOVE(128, true); else GOOSE_MOVE(128, false); }
-  else if (head_dim == 64) { if (f16) GOOSE_MOVE(64, true); else GOOSE_MOVE(64, false); }
+  const bool f16 = dtype == GOOSE_DTYPE_F16, few = (long long)grid.x * grid.y <= EVICT_FEW;
+#define GOOSE_MOVE(D, H, NW) hipLaunchKernelGGL((k_evict_move<D, H, NW>), grid, dim3(64 * NW), 0, st, pg, ev, n_layers, n_kv, inv_freq, kept, reposition, scratch->verdict)
+#define GOOSE_MOVE_D(D)                                                \
+  if (few) { if (f16) GOOSE_MOVE(D, true, 8); else GOOSE_MOVE(D, false, 8); } \
+  else { if (f16) GOOSE_MOVE(D, true, 1); else GOOSE_MOVE(D, false, 1); }
+  if (head_dim == 128) { GOOSE_MOVE_D(128) }
+  else if (head_dim == 64) { GOOSE_MOVE_D(64) }
   else return GOOSE_ERR_SHAPE;
+#undef GOOSE_MOVE_D
 #undef GOOSE_MOVE
   rc = goose_launch_status();
   if (rc != GOOSE_OK) return rc;
