@@ -15,9 +15,6 @@
 
 namespace {
 
-#ifndef EVICT_FEW
-#define EVICT_FEW 1024
-#endif
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
 
@@ -101,9 +98,11 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
   constexpr int WORDS = 8, SEG = NT * WORDS, W = NT / 64, PER = 2048 / NT;  // PER: bins of a thread
   __shared__ unsigned hist[2048];
   __shared__ __attribute__((aligned(16))) int ws[W], wt[W];
-  __shared__ int found[2];
+  __shared__ int found[3];
   const goose_eviction q = ev.r[blockIdx.y];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+#pragma unroll
+  for (int j = 0; j < PER; ++j) hist[j * NT + tid] = 0;
   const int layer = blockIdx.x / n_kv, head = blockIdx.x - layer * n_kv;
   uint64_t* const words = kept + (((size_t)blockIdx.y * n_layers + layer) * n_kv + head) * pg.table_ld;
   float* const w = weight + (((size_t)layer * pg.n_seqs + q.seq) * n_kv + head) * pg.table_ld * GOOSE_PAGE;
@@ -116,16 +115,19 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
   fetch(wave * WORDS, pg.table_ld);
   const int len = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]);
   const int bad = verdict_of<NT>(pg, q, len, tid, mine);
-  if (blockIdx.x == 0 && tid == 0) verdict[blockIdx.y] = bad;
-  if (bad) return;
-  const int n_words = (len + GOOSE_PAGE - 1) / GOOSE_PAGE;
-  for (int i = n_words + tid; i < pg.table_ld; i += NT) words[i] = 0;
+  const int n_words = bad ? 0 : (len + GOOSE_PAGE - 1) / GOOSE_PAGE;
+  auto close = [&]() {  // (behind everything else: a barrier would wait for these stores)
+    if (blockIdx.x == 0 && tid == 0) verdict[blockIdx.y] = bad;
+    if (!bad)
+      for (int i = n_words + tid; i < pg.table_ld; i += NT) words[i] = 0;
+  };
+  if (bad) return close();
   if (len <= q.keep) {
     for (int i = tid; i < n_words; i += NT) {
       const int m = min(GOOSE_PAGE, len - i * GOOSE_PAGE);
       words[i] = m == 64 ? ~0ull : (1ull << m) - 1;
     }
-    return;
+    return close();
   }
   // ---- the m-th largest weight of slots lo .. hi - 1: its key, and how many slots of just that weight are kept (ties)
   const int lo = q.sink, hi = len - q.recent, m = q.keep - q.sink - q.recent;
@@ -138,8 +140,6 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
       const int bins = pass < 2 ? 2048 : 1024;
-      for (int i = tid; i < bins; i += NT) hist[i] = 0;
-      __syncthreads();
       const unsigned above = pass == 0 ? 0u : key >> (pass == 1 ? 21 : 10);
 #pragma unroll 1
       for (unsigned c0 = one ? 0 : (unsigned)lo / SEG * SEG; c0 < (unsigned)hi; c0 += SEG) {
@@ -168,6 +168,7 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
         c[j] = top >= j ? (int)hist[top - j] : 0;
+        if (top >= j) hist[top - j] = 0;  // (for the next pass)
         x += c[j];
       }
       const int own = x;
@@ -183,14 +184,18 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
       before += x - own;
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
-        if (before < ties && ties <= before + c[j]) { found[0] = top - j; found[1] = before; }
+        if (before < ties && ties <= before + c[j]) { found[0] = top - j; found[1] = before; found[2] = c[j]; }
         before += c[j];
       }
       __syncthreads();
       key |= (unsigned)found[0] << shift;
       ties -= found[1];
+      if (ties == found[2] && key != 0) {  // all of this bin stay: no need to look into it
+        --key;
+        ties = 0;
+        break;
+      }
       shift = pass == 0 ? 10 : 0;
-      __syncthreads();
     }
   }
   // ---- the words, ties to the lowest slots, and weights to the front: none of them is behind where it goes, and all of a segment are loaded before one
@@ -236,8 +241,9 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
       if ((more[i] >> lane) & 1) w[at + (int)__popcll(more[i] & ((1ull << lane) - 1))] = v[i];
       at += (int)__popcll(more[i]);
     }
-    __syncthreads();
+    if (!one) __syncthreads();
   }
+  close();
 }
 
 __device__ __forceinline__ void in_order() {  // LDS of one wavefront: its instructions execute in order, the compiler is to keep them so
@@ -264,7 +270,7 @@ __global__ __launch_bounds__(64 * NW) void k_evict_move(const goose_pages pg, co
                                                         const uint64_t* __restrict__ kept, bool reposition, const int32_t* __restrict__ verdict) {
   typedef typename Mma16<F16>::T T;
   typedef typename Mma16<F16>::v8 op8;
-  constexpr int UNITS = D / 32, AHEAD = NW == 1 ? 6 : 3, WINDOW = NW * AHEAD, STAGES = NW == 1 ? 8 : 32;
+  constexpr int UNITS = D / 32, AHEAD = NW == 1 ? 6 : 3, WINDOW = NW * AHEAD, STAGES = NW == 8 ? 32 : (NW == 4 ? 16 : 8);
   static_assert(WINDOW + 1 <= STAGES, "a window reaches into WINDOW + 1 destination blocks");
   // Destination blocks that fill up.  Keys: [block % STAGES][piece][...], and the slots that they come from.  Values: [column][slot % (32 STAGES)], a column's slots
   // turned on by eight against those of the one before (else all would be in one bank), and behind them what takes the slots that go.
@@ -466,14 +472,17 @@ int launch_pages_evict(int dtype, const goose_pages& pg, const Evictions& ev, in
     hipLaunchKernelGGL(k_evict_select<1024>, heads, dim3(1024), 0, st, pg, ev, n_layers, n_kv, weight, kept, scratch->verdict);
   int rc = goose_launch_status();
   if (rc != GOOSE_OK) return rc;
+  // Wavefronts of a stream of blocks, by the streams and the slots that a sequence may have.  us a call with 1 / 4 / 8: 64 streams (Llama 3 8B, one layer of 8192 slots
+  // to 2048) 127 / 62 / 52; 512 (8 layers) 138 / 79 / 71; 1024 (two sequences) 156 / 111 / 116; 2048 (four) 226 / 197 / 209; 5120 of 500 slots 163 / 155 / 180;
+  // 10240 of 28 slots 41 / 53 / 82.
   const dim3 grid(n_layers * n_kv * (head_dim / 16), ev.n);
-  const bool f16 = dtype == GOOSE_DTYPE_F16, few = (long long)grid.x * grid.y <= EVICT_FEW;
+  const long long streams = (long long)grid.x * grid.y;
+  const bool f16 = dtype == GOOSE_DTYPE_F16;
+  const int waves = streams <= 512 ? 8 : (streams > 2048 && pg.table_ld <= 4 ? 1 : 4);
 #define GOOSE_MOVE(D, H, NW) hipLaunchKernelGGL((k_evict_move<D, H, NW>), grid, dim3(64 * NW), 0, st, pg, ev, n_layers, n_kv, inv_freq, kept, reposition, scratch->verdict)
-#define GOOSE_MOVE_D(D)                                                \
-  if (few) { if (f16) GOOSE_MOVE(D, true, 8); else GOOSE_MOVE(D, false, 8); } \
-  else { if (f16) GOOSE_MOVE(D, true, 1); else GOOSE_MOVE(D, false, 1); }
-  if (head_dim == 128) { GOOSE_MOVE_D(128) }
-  else if (head_dim == 64) { GOOSE_MOVE_D(64) }
+#define GOOSE_MOVE_D(D, H) do { if (waves == 8) GOOSE_MOVE(D, H, 8); else if (waves == 4) GOOSE_MOVE(D, H, 4); else GOOSE_MOVE(D, H, 1); } while (0)
+  if (head_dim == 128) { if (f16) GOOSE_MOVE_D(128, true); else GOOSE_MOVE_D(128, false); }
+  else if (head_dim == 64) { if (f16) GOOSE_MOVE_D(64, true); else GOOSE_MOVE_D(64, false); }
   else return GOOSE_ERR_SHAPE;
 #undef GOOSE_MOVE_D
 #undef GOOSE_MOVE
