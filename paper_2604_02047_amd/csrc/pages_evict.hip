@@ -90,30 +90,49 @@ __device__ __forceinline__ void sums_of(const int (&ws)[W], int wave, int* befor
   }
 }
 
-// Latency counts here, not bandwidth: what does not depend on the length is loaded beside it, and the slots that the workgroup takes at a time, WORDS words a
-// wavefront, stay in registers over all passes where they are all there are.
+// Sum of x over the lanes in front: within rows of 16 by shifts, then from the last lane of a row to the next row, and of the first half to the second.
+__device__ __forceinline__ int lanes_before(int x) {
+  int sum = x;
+#define GOOSE_ADD(CONTROL, ROWS) sum += __builtin_amdgcn_update_dpp(0, sum, CONTROL, ROWS, 0xF, false)
+  GOOSE_ADD(0x111, 0xF);
+  GOOSE_ADD(0x112, 0xF);
+  GOOSE_ADD(0x114, 0xF);
+  GOOSE_ADD(0x118, 0xF);
+  GOOSE_ADD(0x142, 0xA);
+  GOOSE_ADD(0x143, 0xC);
+#undef GOOSE_ADD
+  return sum - x;
+}
+
+// Latency counts here, not bandwidth.  What does not depend on the length is loaded beside it; the slots that the workgroup takes at a time, WORDS words a
+// wavefront, stay in LDS over all passes where they are all there are; and loops stay rolled, since code that runs once is paid for by its bytes
+// (10 KB unrolled; 200 slots of 8 heads 8.8 us, 10.1 so; 256 heads of 8192 slots 17 us).
 template <int NT>
 __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const Evictions ev, int n_layers, int n_kv, float* __restrict__ weight,
                                                      uint64_t* __restrict__ kept, int32_t* __restrict__ verdict) {
   constexpr int WORDS = 8, SEG = NT * WORDS, W = NT / 64, PER = 2048 / NT;  // PER: bins of a thread
-  __shared__ unsigned hist[2048];
+  __shared__ __attribute__((aligned(32))) unsigned hist[2048];
+  __shared__ float seg[SEG];
   __shared__ __attribute__((aligned(16))) int ws[W], wt[W];
   __shared__ int found[3];
   const goose_eviction q = ev.r[blockIdx.y];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-#pragma unroll
-  for (int j = 0; j < PER; ++j) hist[j * NT + tid] = 0;
   const int layer = blockIdx.x / n_kv, head = blockIdx.x - layer * n_kv;
   uint64_t* const words = kept + (((size_t)blockIdx.y * n_layers + layer) * n_kv + head) * pg.table_ld;
   float* const w = weight + (((size_t)layer * pg.n_seqs + q.seq) * n_kv + head) * pg.table_ld * GOOSE_PAGE;
-  float v[WORDS];  // of words first_word .. first_word + WORDS - 1
+  float* const own = seg + wave * WORDS * GOOSE_PAGE + lane;  // of words first_word .. first_word + WORDS - 1
   auto fetch = [&](int first_word, int end) {
+    float v[WORDS];
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) v[i] = first_word + i < end ? w[(size_t)(first_word + i) * GOOSE_PAGE + lane] : 0.f;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) own[i * GOOSE_PAGE] = v[i];
   };
   const int mine = tid < pg.table_ld ? pg.d_table[(size_t)q.seq * pg.table_ld + tid] : 0;
-  fetch(wave * WORDS, pg.table_ld);
   const int len = __builtin_amdgcn_readfirstlane(pg.d_len[q.seq]);
+  fetch(wave * WORDS, pg.table_ld);
+#pragma unroll 1
+  for (int j = tid; j < 2048; j += NT) hist[j] = 0;
   const int bad = verdict_of<NT>(pg, q, len, tid, mine);
   const int n_words = bad ? 0 : (len + GOOSE_PAGE - 1) / GOOSE_PAGE;
   auto close = [&]() {  // (behind everything else: a barrier would wait for these stores)
@@ -145,11 +164,11 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
       for (unsigned c0 = one ? 0 : (unsigned)lo / SEG * SEG; c0 < (unsigned)hi; c0 += SEG) {
         const int first = (int)(c0 >> 6) + wave * WORDS;
         if (!one) fetch(first, n_words);
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-          if (first + i >= n_words) break;
+        const int some_words = min(WORDS, n_words - first);
+#pragma unroll 1
+        for (int i = 0; i < some_words; ++i) {
           const int s = (first + i) * GOOSE_PAGE + lane;
-          const unsigned x = key_of(v[i]);
+          const unsigned x = key_of(own[i * GOOSE_PAGE]);
           if (s >= lo && s < hi && (pass == 0 || x >> (pass == 1 ? 21 : 10) == above)) {
             const unsigned bin = (x >> shift) & (bins - 1), some = __builtin_amdgcn_readfirstlane(bin);
             const uint64_t here = __builtin_amdgcn_ballot_w64(true);
@@ -164,24 +183,25 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
       __syncthreads();
       // thread t owns PER bins, from the top: how many slots lie above them
       const int top = bins - 1 - PER * tid;
+      typedef int Bins __attribute__((ext_vector_type(PER)));
       int c[PER], x = 0;
+      Bins some = 0;
+      if (top >= 0) {
+        Bins* const at = reinterpret_cast<Bins*>(&hist[top + 1 - PER]);
+        some = *at;
+        *at = 0;  // (for the next pass)
+      }
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
-        c[j] = top >= j ? (int)hist[top - j] : 0;
-        if (top >= j) hist[top - j] = 0;  // (for the next pass)
+        c[j] = some[PER - 1 - j];
         x += c[j];
       }
-      const int own = x;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int up = __shfl_up(x, off, 64);
-        if (lane >= off) x += up;
-      }
-      if (lane == 63) ws[wave] = x;
+      const int mine_before = lanes_before(x);
+      if (lane == 63) ws[wave] = mine_before + x;
       __syncthreads();
       int before, all;
       sums_of(ws, wave, &before, &all);
-      before += x - own;
+      before += mine_before;
 #pragma unroll
       for (int j = 0; j < PER; ++j) {
         if (before < ties && ties <= before + c[j]) { found[0] = top - j; found[1] = before; found[2] = c[j]; }
@@ -199,48 +219,45 @@ __global__ __launch_bounds__(NT) void k_evict_select(const goose_pages pg, const
     }
   }
   // ---- the words, ties to the lowest slots, and weights to the front: none of them is behind where it goes, and all of a segment are loaded before one
-  // is stored
+  // is stored.  Lane i has word i of the wavefront.
   int left = ties, base = 0;
 #pragma unroll 1
   for (unsigned c0 = 0; c0 < (unsigned)len; c0 += SEG) {
-    const int first = (int)(c0 >> 6) + wave * WORDS;  // this wavefront's words
+    const int first = (int)(c0 >> 6) + wave * WORDS, some_words = min(WORDS, n_words - first);
     if (!one) fetch(first, n_words);
-    uint64_t same[WORDS], more[WORDS];
-    int mine = 0;
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-      const int s = first + i < n_words ? (first + i) * GOOSE_PAGE + lane : INT32_MAX;  // (behind the last word: no slot)
-      const unsigned x = key_of(v[i]);
+    uint64_t same = 0, stay = 0;
+#pragma unroll 1
+    for (int i = 0; i < some_words; ++i) {
+      const int s = (first + i) * GOOSE_PAGE + lane;
+      const unsigned x = key_of(own[i * GOOSE_PAGE]);
       const bool mid = m > 0 && s >= lo && s < hi;
-      same[i] = __builtin_amdgcn_ballot_w64(mid && x == key);
-      more[i] = __builtin_amdgcn_ballot_w64(s < lo || (s >= hi && s < len) || (mid && x > key));
-      mine += (int)__popcll(same[i]);
+      const uint64_t equal = __builtin_amdgcn_ballot_w64(mid && x == key);
+      const uint64_t more = __builtin_amdgcn_ballot_w64(s < lo || (s >= hi && s < len) || (mid && x > key));
+      if (lane == i) { same = equal; stay = more; }
     }
-    if (lane == 0) wt[wave] = mine;
+    const int n_same = (int)__popcll(same), same_before = lanes_before(n_same);
+    if (lane == 63) wt[wave] = same_before + n_same;
     __syncthreads();
-    int before, all, count = 0;
+    int before, all;
     sums_of(wt, wave, &before, &all);
-    int here = left - before;  // ties that are left for this wavefront
+    const int take = min(max(left - before - same_before, 0), n_same);  // of its word's ties
     left -= all;
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-      // (counts are unsigned, and what is left may be negative)
-      const bool tie = ((same[i] >> lane) & 1) != 0 && (int)__popcll(same[i] & ((1ull << lane) - 1)) < here;
-      here -= (int)__popcll(same[i]);
-      more[i] |= __builtin_amdgcn_ballot_w64(tie);
-      count += (int)__popcll(more[i]);
-    }
-    if (lane == 0) ws[wave] = count;
+    uint64_t rest = same;
+    if (take == n_same) rest = 0;
+    else for (int k = 0; k < take; ++k) rest &= rest - 1;
+    stay |= same & ~rest;
+    const int n_stay = (int)__popcll(stay), stay_before = lanes_before(n_stay);
+    if (lane == 63) ws[wave] = stay_before + n_stay;
     __syncthreads();
     sums_of(ws, wave, &before, &all);
-    int at = base + before;
-    base += all;
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-      if (lane == 0 && first + i < n_words) words[first + i] = more[i];
-      if ((more[i] >> lane) & 1) w[at + (int)__popcll(more[i] & ((1ull << lane) - 1))] = v[i];
-      at += (int)__popcll(more[i]);
+    if (lane < some_words) words[first + lane] = stay;
+#pragma unroll 1
+    for (int i = 0; i < some_words; ++i) {
+      const uint64_t word = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(stay >> 32), i) << 32 | (unsigned)__builtin_amdgcn_readlane((int)stay, i);
+      const int at = base + before + __builtin_amdgcn_readlane(stay_before, i);
+      if ((word >> lane) & 1) w[at + (int)__popcll(word & ((1ull << lane) - 1))] = own[i * GOOSE_PAGE];
     }
+    base += all;
     if (!one) __syncthreads();
   }
   close();
@@ -317,11 +334,7 @@ __global__ __launch_bounds__(64 * NW) void k_evict_move(const goose_pages pg, co
     src_ids = row[i];
     src_words = words[i];
     sum = src0 + lane < pages ? (int)__popcll(src_words) : 0;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int up = __shfl_up(sum, off, 64);
-      if (lane >= off) sum += up;
-    }
+    sum += lanes_before(sum);
   };
   // the word of block c's page, and how many kept rows lie in front of c (c never steps back)
   auto word_of = [&](int c, int* before) -> unsigned {
@@ -464,7 +477,7 @@ int launch_pages_append(const goose_pages& pg, const ChunkReqs& ck, int32_t* fla
 
 int launch_pages_evict(int dtype, const goose_pages& pg, const Evictions& ev, int n_layers, int n_kv, int head_dim, const double* inv_freq,
                        float* weight, uint64_t* kept, bool reposition, PageScratch* scratch, int32_t* flags, hipStream_t st) {
-  // One segment in registers: 256 threads, of which more workgroups run side by side (13B, 8 layers of 4 sequences of 28 slots 11 us, with 1024 55).
+  // One segment in registers: 256 threads, of which more workgroups run side by side (1280 heads of 28 slots 11 us, with 1024 55).
   const dim3 heads(n_layers * n_kv, ev.n);
   if (pg.table_ld * GOOSE_PAGE <= 2048)
     hipLaunchKernelGGL(k_evict_select<256>, heads, dim3(256), 0, st, pg, ev, n_layers, n_kv, weight, kept, scratch->verdict);
