@@ -10,7 +10,7 @@
 namespace {
 
 struct ChunkItems {
-  int32_t tiles, splits;  // work items: tiles of 256 rows x ranges of their blocks, for every KV head
+  int32_t tiles, splits;  // work items: tiles of 32 NW rows x ranges of their blocks, for every KV head
   int32_t waves;          // 32-row tiles of a KV head
   int32_t join0;          // its first 32-row tile in the merge
   uint32_t rec0;          // its first record
@@ -28,7 +28,7 @@ struct ChunkArgs {
   int32_t* flags;
   size_t ldq, ldo, ld_lse;
   int32_t table_ld, n_pages, n_heads, n_kv, group, n;
-  int32_t o_terms, o_f16;
+  int32_t o_terms, o_f16, paired;
   ChunkItems it[GOOSE_MAX_REQUESTS];
   ChunkReq r[GOOSE_MAX_REQUESTS];
 };
@@ -38,19 +38,20 @@ __device__ __forceinline__ void finish(const ChunkArgs& a, size_t row, int h, in
   if (a.lse != nullptr && c == 0) a.lse[(size_t)h * a.ld_lse + row] = log_of_sum(m, l, softmax_scale(D));
 }
 
-// One workgroup = eight wavefronts, two on a SIMD, 32 rows each x a range of blocks.  Every block comes into LDS once, global -> LDS without
+// One workgroup = NW wavefronts, two on a SIMD (of one workgroup of eight or two of four), 32 rows each x a range of blocks.  Every block comes into LDS once, global -> LDS without
 // registers, into a ring that runs several blocks ahead; a wavefront has three blocks under way at once (ring_step).  Blocks that a
 // wavefront's rows do not see whole are masked on the way, and behind the last one that it sees it only goes on copying.
 // A weight of zero does not keep a NaN or an infinity of an unseen slot's values out of the matrix instruction: a wavefront that has such a thing in its
 // outputs at the end starts again, block by block with values_odd and sums in the ring's order: rows that do not see the thing keep their bits.  The block that the chunk ends in, whose other slots may hold anything, follows that way always.
-template <int D, int QT, bool F16, int PT>
-__global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
+template <int D, int QT, bool F16, int PT, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
   typedef RowTile<D, QT, F16, PT> Tile;
   typedef typename Tile::T T;
   constexpr int NS = D / 16;
   constexpr int BLOCK = 2 * NS * 1024, BU = BLOCK / 16;  // keys and values of 32 slots: bytes, 16-byte units
-  constexpr int RING = 8;                                // blocks
-  constexpr int CP = 2 * NS / 8;                         // pieces of 1 KiB that a wavefront copies of a block
+  constexpr int RING = NW;                               // blocks
+  constexpr int CP = 2 * NS / NW;                        // pieces of 1 KiB that a wavefront copies of a block
+  constexpr int ROWS = 32 * NW;
   constexpr int AHEAD = 4;
   __shared__ __attribute__((aligned(1024))) unsigned char ring[RING * BLOCK];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -63,9 +64,11 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
   y = __builtin_amdgcn_readfirstlane(y);
   const ChunkReq& rq = a.r[ri];
   const ChunkItems& ci = a.it[ri];
-  const int split = __builtin_amdgcn_readfirstlane((int)((unsigned)y / (unsigned)ci.tiles));
-  const int tile = ci.tiles - 1 - (y - split * ci.tiles);  // (the longest first)
-  const int rows = rq.C * a.group, wg_first = tile * 256, row_first = wg_first + wave * 32;
+  // Items from the longest to the shortest.  Where two fit a CU and all run at once, the second of a CU comes from the other end.
+  const int items = ci.tiles * ci.splits, half = (items + 1) / 2;
+  const unsigned i = a.paired && y >= half ? items - 1 - (y - half) : y, longest = __builtin_amdgcn_readfirstlane(i / (unsigned)ci.splits);
+  const int tile = ci.tiles - 1 - (int)longest, split = __builtin_amdgcn_readfirstlane((int)(i - longest * ci.splits));
+  const int rows = rq.C * a.group, wg_first = tile * ROWS, row_first = wg_first + wave * 32;
   auto query = [&](int rho) -> const T* {
     const int at = min(rho, rows - 1), tok = (int)((unsigned)at / (unsigned)a.group), h = kvh * a.group + at - tok * a.group;
     return static_cast<const T*>(a.q) + ((size_t)rq.row0 + tok) * a.ldq + ((size_t)h * D + hh * 8) * QT;
@@ -76,7 +79,7 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
   auto token_of = [&](int rho) { return __builtin_amdgcn_readfirstlane((int)((unsigned)min(rho, rows - 1) / (unsigned)a.group)); };
   auto clamp = [](int x, int lo, int hi) { return min(max(x, lo), hi); };
   // blocks that the tile's last row sees, this item's range of them, and the blocks of it in front of the chunk's end
-  const int total = (P + token_of(wg_first + 255)) / 32 + 1;
+  const int total = (P + token_of(wg_first + ROWS - 1)) / 32 + 1;
   const int b_lo = __builtin_amdgcn_readfirstlane((int)((unsigned)total * (unsigned)split / (unsigned)ci.splits));
   const int b_hi = __builtin_amdgcn_readfirstlane((int)((unsigned)total * (unsigned)(split + 1) / (unsigned)ci.splits));
   const int units = __builtin_amdgcn_readfirstlane(clamp((P + rq.C) / 32 - b_lo, 0, b_hi - b_lo));
@@ -92,9 +95,9 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
   };
   const int last = P + (int)((unsigned)min(row_first + l31, rows - 1) / (unsigned)a.group) - b_lo * 32 - hh * 16;  // the last slot that this lane's row sees
   const float scale = softmax_scale(D);
-  const bool keys = wave < 4;          // the first four wavefronts copy keys, the others values
+  const bool keys = wave < NW / 2;     // the first half of the wavefronts copy keys, the others values
   const int share = wave * CP * 1024;  // this wavefront's pieces of a block
-  const char* const pool = (keys ? kp : vp) + (wave & 3) * CP * 1024;
+  const char* const pool = (keys ? kp : vp) + (wave & (NW / 2 - 1)) * CP * 1024;
   auto barrier = [&]() {  // (raw: __syncthreads would also drain every copy in flight)
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -109,10 +112,10 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
       copy_pieces<CP>(pool + block_at(min(b_lo + next, b_hi - 1)), lane, ring + (next & (RING - 1)) * BLOCK + share);
       ++next;
     };
-    const int first = keys ? RING : RING - 2;
+    const int first = keys ? RING : RING - (NW == 8 ? 2 : 1);
     while (next < first) copy();
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3) * CP));  // units 0 to 2 (values: 0)
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 3) * CP));  // units 0 to 2 (values: 0, with the short ring 0 and 1)
     barrier();
     u32x4 pc[AHEAD];
     f32x16 z1;
@@ -135,14 +138,17 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
 #pragma unroll
       for (int n = 0; n < AHEAD; ++n) pc[n] = keys_of(2)[n * 64];
     }
-    // Steps j and j + 1 between two barriers.  Before them the keys of units up to j + 3 and the values of units up to j have landed in every
+    // With the long ring steps j and j + 1 between two barriers.  Before them the keys of units up to j + 3 and the values of units up to j have landed in every
     // wavefront's share; keys of units up to j and values of units up to j - 2 are no longer read, and make room for those RING units later.
-    auto arrive = [&]() {
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm(3 * CP));
+    // With the short one step j: keys up to j + 2 and values up to j - 1 have landed, keys up to j and values up to j - 2 make room.
+    auto arrive = [&](int j) {
+      if constexpr (NW == 8) __builtin_amdgcn_s_waitcnt(vmcnt_imm(3 * CP));
+      else if (j == 1) __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      else __builtin_amdgcn_s_waitcnt(vmcnt_imm(CP));
       barrier();
       __builtin_amdgcn_sched_barrier(0);
       copy();
-      copy();
+      if (NW == 8 || (j == 1 && keys)) copy();
     };
     auto step = [&](int j, const f32x16& za, f32x16& zb, const auto& w, const auto& wl, auto& wn, auto& wln) {
       if (j > seen || seen == 0) return;
@@ -157,12 +163,13 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
     };
     int j = 1;
     for (; j + 1 < units; j += 2) {
-      arrive();
+      arrive(j);
       step(j, t.s, z1, t.p, t.pl, w1, wl1);
+      if constexpr (NW == 4) arrive(j + 1);
       step(j + 1, z1, t.s, w1, wl1, t.p, t.pl);
     }
     if (j < units) {
-      arrive();
+      arrive(j);
       step(j, t.s, z1, t.p, t.pl, w1, wl1);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -230,7 +237,7 @@ __global__ __launch_bounds__(512, 2) void k_chunk_ring(const ChunkArgs a) {
       for (int q = 0; q < 4; ++q) each(dt * 4 + q, f32x4{t.o[dt][q * 4], t.o[dt][q * 4 + 1], t.o[dt][q * 4 + 2], t.o[dt][q * 4 + 3]});
   };
   if (ci.splits > 1) {
-    const size_t rec = ci.rec0 + ((size_t)split * a.n_kv + kvh) * ci.waves + tile * 8 + wave;
+    const size_t rec = ci.rec0 + ((size_t)split * a.n_kv + kvh) * ci.waves + tile * NW + wave;
     if (hh == 0) *reinterpret_cast<float2*>(a.ws_ml + (rec * 32 + l31) * 2) = make_float2(t.m, l);
     quads([&](int i, const f32x4& x) { *reinterpret_cast<f32x4*>(a.ws_o + (rec * (D / 8) + i) * 256 + lane * 4) = x; });
   } else if (rho < rows) {
@@ -283,15 +290,15 @@ __global__ __launch_bounds__(256) void k_chunk_merge(const ChunkArgs a) {
   finish(a, (size_t)a.r[r].row0 + tok, h, D, quad * 8 + hh * 4, num, m, den);
 }
 
-template <int D, int QT, bool F16>
-void launch_t(int p_terms, dim3 grid, const ChunkArgs& a, hipStream_t st) {
-  if (p_terms == 1) hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, 1>), grid, dim3(512), 0, st, a);
-  else hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, 2>), grid, dim3(512), 0, st, a);
+template <int D, int QT, bool F16, int NW>
+void launch_t(int p_terms, unsigned items, const ChunkArgs& a, hipStream_t st) {
+  if (p_terms == 1) hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, 1, NW>), dim3(items), dim3(64 * NW), 0, st, a);
+  else hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, 2, NW>), dim3(items), dim3(64 * NW), 0, st, a);
 }
-template <int D>
-void launch_d(bool f16, int q_terms, int p_terms, dim3 grid, const ChunkArgs& a, hipStream_t st) {
-  if (q_terms == 2) f16 ? launch_t<D, 2, true>(p_terms, grid, a, st) : launch_t<D, 2, false>(p_terms, grid, a, st);
-  else f16 ? launch_t<D, 1, true>(p_terms, grid, a, st) : launch_t<D, 1, false>(p_terms, grid, a, st);
+template <int D, int NW>
+void launch_d(bool f16, int q_terms, int p_terms, unsigned items, const ChunkArgs& a, hipStream_t st) {
+  if (q_terms == 2) f16 ? launch_t<D, 2, true, NW>(p_terms, items, a, st) : launch_t<D, 2, false, NW>(p_terms, items, a, st);
+  else f16 ? launch_t<D, 1, true, NW>(p_terms, items, a, st) : launch_t<D, 1, false, NW>(p_terms, items, a, st);
 }
 
 }  // namespace
@@ -344,7 +351,7 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.o_f16 = o_dtype == GOOSE_DTYPE_F16;
   // a weight carries as many bits as the output keeps
   const int p_terms = o_terms == 1 && (o_dtype == GOOSE_DTYPE_BF16 || dtype == GOOSE_DTYPE_F16) ? 1 : 2;
-  // Work items run in rounds of 256 workgroups, the longest first.  In units of 10 ns: an item's fixed part, a block of it, the merge and its records.
+  // Work items run in rounds of as many as the CUs hold, the longest first.  In units of 10 ns: an item's fixed part, a block of it, the merge and its records.
   const long long fixed = 700, step = (30 + 34 * (q_terms + p_terms)) * (head_dim + 64) / 192;
   long long best = INT64_MAX;
   int best_per = 0;
@@ -353,13 +360,16 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
     const int blocks = (many.r[i].P_max + many.r[i].C + 31) / 32;
     longest = blocks > longest ? blocks : longest;
   }
+  // Two workgroups of four wavefronts a CU hide each other's beginnings and ends, one of eight copies every block once: us with 4 / 8 at 16 blocks (512 tokens of 32
+  // heads) 17 / 22, 63 (2000 tokens of 52 heads) 73 / 77, 126 (512 of 32 / 8 heads behind 3500) 71 / 79, 282 (1024 behind 8000) 160 / 158, 512 (4096 behind 12288) 918 / 888.
+  const int nw = longest <= 256 ? 4 : 8, slots = 2048 / nw, tile_rows = 32 * nw;
   auto splits_of = [](int blocks, int per) { return (blocks + per - 1) / per; };
   for (int parts = 1; parts <= 32 && parts <= longest; ++parts) {
     const int per = splits_of(longest, parts);
     long long work = 0, items = 0, most = 0, records = 0;
     for (int i = 0; i < many.n; ++i) {
       const ChunkReq& c = many.r[i];
-      const long long tiles = ((long long)c.C * group + 255) / 256;
+      const long long tiles = ((long long)c.C * group + tile_rows - 1) / tile_rows;
       const int blocks = (c.P_max + c.C + 31) / 32, splits = splits_of(blocks, per);
       const long long sum = tiles * (2ll * c.P_max + c.C) / 64 + 2 * tiles;  // blocks of all tiles
       work += (sum * step + tiles * splits * fixed) * n_kv;
@@ -369,7 +379,7 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
       if (splits > 1) records += (long long)splits * n_kv * ((c.C * group + 31) / 32);
     }
     if (records * 32 > (long long)max_records) continue;
-    const long long rounds = (items + 255) / 256, time = rounds * (work / items);
+    const long long rounds = (items + slots - 1) / slots, time = rounds * (work / items);
     const long long cost = (time > most ? time : most) + (records > 0 ? 600 + records * 32 * head_dim * 8 / 50000 : 0);
     if (cost < best) { best = cost; best_per = per; }
   }
@@ -379,7 +389,7 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   long long items = 0;
   for (int i = 0; i < many.n; ++i) {
     const ChunkReq& c = many.r[i];
-    const int tiles = (c.C * group + 255) / 256, waves = (c.C * group + 31) / 32, splits = splits_of((c.P_max + c.C + 31) / 32, best_per);
+    const int tiles = (c.C * group + tile_rows - 1) / tile_rows, waves = (c.C * group + 31) / 32, splits = splits_of((c.P_max + c.C + 31) / 32, best_per);
     a.it[i] = ChunkItems{tiles, splits, waves, joins, records};
     if (splits > 1) {
       records += (uint32_t)(splits * n_kv * waves);
@@ -388,10 +398,11 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
     a.r[i] = c;
     items += (long long)tiles * splits * n_kv;
   }
-  if (items * 512 > UINT32_MAX) return GOOSE_ERR_CAPACITY;  // (threads of a launch)
+  if (items * 64 * nw > UINT32_MAX) return GOOSE_ERR_CAPACITY;  // (threads of a launch)
+  a.paired = nw == 4 && items > 256 && items <= 512;
   const bool f16 = dtype == GOOSE_DTYPE_F16;
-  if (head_dim == 128) launch_d<128>(f16, q_terms, p_terms, dim3((unsigned)items), a, st);
-  else launch_d<64>(f16, q_terms, p_terms, dim3((unsigned)items), a, st);
+  if (head_dim == 128) nw == 4 ? launch_d<128, 4>(f16, q_terms, p_terms, (unsigned)items, a, st) : launch_d<128, 8>(f16, q_terms, p_terms, (unsigned)items, a, st);
+  else nw == 4 ? launch_d<64, 4>(f16, q_terms, p_terms, (unsigned)items, a, st) : launch_d<64, 8>(f16, q_terms, p_terms, (unsigned)items, a, st);
   const int rc = goose_launch_status();
   if (rc != GOOSE_OK || joins == 0) return rc;
   const dim3 grid((unsigned)(joins * (head_dim / 32)));

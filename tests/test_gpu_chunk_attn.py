@@ -362,3 +362,51 @@ def test_odd_values_where_the_keys_are_split(dtype, d, terms, o_terms):
         assert torch.equal(got[0][:first], o[:first])
         x = got[0][first:290, :c.cols].view(-1, 4 * d // 8, o_terms, 8)[:, :, 0].reshape(-1, 4, d)
         assert x[:, :2, 7].isnan().all() and (x[:, 2:, 9].isinf() if o_terms == 1 else x[:, 2:, 9].isnan()).all() and int((~x.isfinite()).sum()) == 4 * x.shape[0]
+
+
+# A bound of more than 256 blocks: workgroups of eight wavefronts and the longer ring, whatever the lengths.
+LONG = 8400
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("terms,o_dtype,o_terms", [(1, HF, 1), (2, HF, 2), (2, BF, 1), (1, BF, 2)])
+def test_the_longer_ring_types_and_terms(dtype, d, terms, o_dtype, o_terms):
+    for Cs, Ps in (([37, 1, 70], [130, 64, 261]), ([150, 300], [333, 0])):
+        c = Case(4, 1, d, dtype, Cs, Ps, seed=21, terms=terms, o_dtype=o_dtype, o_terms=o_terms)
+        c.check(c.run(bound=LONG))
+
+
+@pytest.mark.parametrize("blocks", range(1, 14))
+def test_the_longer_ring_every_number_of_blocks(blocks):
+    for dtype, o in (("f16", HF), ("bf16", HF)):
+        c = Case(4, 1, 128, dtype, [130], [blocks * 32 - 31 + 7 * blocks % 32], seed=blocks, o_dtype=o)
+        c.check(c.run(bound=LONG))
+
+
+@pytest.mark.parametrize("C", [65, 127, 128, 129, 255, 256, 257])
+def test_the_longer_ring_every_end_of_a_tile(C):
+    for P in (0, 31, 32, 33, 1000):
+        c = Case(4, 2, 64, "f16", [C], [P], seed=C)
+        c.check(c.run(bound=LONG))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_the_longer_ring_odd_values(dtype):
+    o = Case(4, 2, 128, dtype, [290], [2501], seed=22).run(bound=LONG)[0]
+    for slot in (5, 2500, 2600, 2790):
+        c = Case(4, 2, 128, dtype, [290], [2501], seed=22)
+        c.v[0, c.table[0, slot // PAGE], 0, slot % PAGE, 7] = float("nan")
+        for s in range(2791, 2816):
+            c.k[0, c.table[0, s // PAGE], :, s % PAGE] = float("nan")
+            c.v[0, c.table[0, s // PAGE], :, s % PAGE] = float("inf")
+        got = c.run(bound=LONG)
+        c.check(got)
+        assert torch.equal(got[0][:max(0, slot - 2501)], o[:max(0, slot - 2501)])
+
+
+def test_all_at_once_and_more_than_fit():
+    """Work items in pairs (more than 256, at most 512), with one range of the keys and with several, and in rounds."""
+    for nh, nkv, C, P in ((8, 8, 4200, 0), (4, 4, 2100, 1500), (24, 8, 1500, 700), (16, 16, 4097, 31)):
+        c = Case(nh, nkv, 64, "f16", [C], [P], seed=C)
+        c.check(c.run(), heads=[0, nh - 1])
