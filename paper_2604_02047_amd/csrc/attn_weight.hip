@@ -22,12 +22,18 @@ struct WeightArgs {
   int32_t table_ld, n_pages, n_kv, group, n;
   uint32_t group_inv;  // ceil(2^32 / group), 0 for groups of one: mulhi(row, group_inv) is row / group, or one more
   int32_t sg, rg;  // a workgroup's wavefronts: sg pages x rg of the tiles in turn
+  int32_t splits;  // of the rows
+  float* part;     // splits > 1: [split][chunk][KV head][part_ld]
+  size_t part_ld;
   float decay;
   ChunkReq r[GOOSE_MAX_REQUESTS];
 };
 
-// Row groups of a workgroup: what fits 128 KiB of LDS.
-constexpr int most_rg(int pieces) { return pieces > 8 ? 2 : 4; }
+__device__ __forceinline__ void store_weight(const WeightArgs& a, const ChunkReq& rq, int kvh, int slot, int P, float w) {
+  float* const out = a.weight + ((size_t)rq.seq * a.n_kv + kvh) * a.table_ld * GOOSE_PAGE + slot;
+  if (slot < P && a.decay != 0.f) w += a.decay * *out;
+  *out = w;
+}
 
 // Scores of a tile and 64 keys (to s), and beside the matrix instructions the weights of the tile before (scores z, its rows' logarithms l2), which
 // need nothing of this one: a workgroup's wavefronts meet at every tile, so that without it they would all be at the matrix instructions
@@ -68,12 +74,14 @@ template <int D, int QT, bool F16>
 __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
   typedef typename Mma16<F16>::T T;
   constexpr int NS = D / 16, PIECES = NS * QT, U = 2;  // 1 KiB pieces of a tile: the high terms' first
-  __shared__ __attribute__((aligned(1024))) unsigned char tiles[2][U * most_rg(PIECES)][PIECES * 1024];
+  constexpr int TILE = PIECES * 1024;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char tiles[];  // [step % 2][U rg][TILE]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l31 = lane & 31, hh = lane >> 5;
   const int SG = a.sg, RG = a.rg, rg = __builtin_amdgcn_readfirstlane((int)((unsigned)wave / (unsigned)SG)), sg = wave - rg * SG;
-  const int first_page = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)a.n_kv)) * SG;
-  const int kvh = (int)(blockIdx.x % (unsigned)a.n_kv);
+  const unsigned item = __builtin_amdgcn_readfirstlane(blockIdx.x / (unsigned)a.n_kv), kvh = blockIdx.x - item * a.n_kv;
+  const unsigned page_group = __builtin_amdgcn_readfirstlane(item / (unsigned)a.splits), split = item - page_group * a.splits;
+  const int first_page = (int)page_group * SG;
   const ChunkReq& rq = a.r[blockIdx.y];
   const int P = __builtin_amdgcn_readfirstlane(a.len[rq.seq]);
   if (P < 0 || P > rq.P_max) {
@@ -90,12 +98,15 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
     live = false;
   }
   u32x4 k[2][NS];
-  const T* const kp = static_cast<const T*>(a.kpool) + page_head<D>(live ? page : 0, a.n_kv, kvh);
+  const T* const kp = static_cast<const T*>(a.kpool) + page_head<D>(live ? page : 0, a.n_kv, (int)kvh);
   fetch(kp, lane, k[0]);
   fetch(kp + 32 * D, lane, k[1]);
   // rows: from the first token that sees a slot of the workgroup
   const int group = a.group, rows = rq.C * group, row0 = max(rq.first, first_page * GOOSE_PAGE - P) * group;
-  const int steps = (rows - row0 + 32 * U * RG - 1) / (32 * U * RG);
+  const unsigned all = (unsigned)(rows - row0 + 32 * U * RG - 1) / (unsigned)(32 * U * RG);
+  int step = (int)(all * split / (unsigned)a.splits);
+  const int steps = (int)(all * (split + 1) / (unsigned)a.splits);  // from `step`: this split's
+  auto tile_of = [&](int step, int u) { return tiles + ((step & 1) * (U * RG) + u * RG + rg) * TILE; };
   const float scale = softmax_scale(D);
   const T* const q0 = static_cast<const T*>(a.q) + (size_t)rq.row0 * a.ldq + (size_t)kvh * group * D * QT;
   const float* const lse0 = a.lse + (size_t)kvh * group * a.ld_lse + rq.row0;
@@ -118,7 +129,7 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
           __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(q0 + (size_t)(unsigned)tok0 * ldq), 0, 0xFFFFFFFFu, GOOSE_BUFFER_WORD3);
       const unsigned offset = (((unsigned)(tok - tok0) * ldq) + (unsigned)(h * D + hh * 8) * QT) * 2;
       for (int p = sg; p < PIECES; p += SG)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(&tiles[step & 1][u * RG + rg][p * 1024]), 16, offset, (p % NS * 16 * QT + p / NS * 8) * 2, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, GOOSE_LDS_PTR(tile_of(step, u) + p * 1024), 16, offset, (p % NS * 16 * QT + p / NS * 8) * 2, 0, 0);
 #endif
     }
   };
@@ -155,25 +166,25 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum[b][r] += __builtin_amdgcn_exp2f(fmaf(z[b][r], scale, -l2));
   };
-  copy(0);
-  int step = 0;
+  if (step < steps) copy(step);
   for (; step + 1 < steps; ++step) {
     arrive();
     const int t0 = tok_next[0], t1 = tok_next[1];
     const float e0 = lse_next[0], e1 = lse_next[1];
     copy(step + 1);
-    one(tiles[step & 1][rg], t0, e0, s0, s1);
-    one(tiles[step & 1][RG + rg], t1, e1, s1, s0);
+    one(tile_of(step, 0), t0, e0, s0, s1);
+    one(tile_of(step, 1), t1, e1, s1, s0);
   }
   arrive();  // the last step, in which tiles may have no rows
-  if (__builtin_amdgcn_ballot_w64(tok_next[0] >= 0) == 0) {
+  if (step >= steps) {
+  } else if (__builtin_amdgcn_ballot_w64(tok_next[0] >= 0) == 0) {
     rest(s1);
   } else {
-    one(tiles[step & 1][rg], tok_next[0], lse_next[0], s0, s1);
+    one(tile_of(step, 0), tok_next[0], lse_next[0], s0, s1);
     if (__builtin_amdgcn_ballot_w64(tok_next[1] >= 0) == 0) {
       rest(s0);
     } else {
-      one(tiles[step & 1][RG + rg], tok_next[1], lse_next[1], s1, s0);
+      one(tile_of(step, 1), tok_next[1], lse_next[1], s1, s0);
       rest(s1);
     }
   }
@@ -200,26 +211,49 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
   for (int i = 1; i < RG; ++i) w += part[(i * SG + sg) * 64 + lane];
   const int slot = slot0 + lane;
   if (slot >= end) return;
-  float* const out = a.weight + ((size_t)rq.seq * a.n_kv + kvh) * a.table_ld * GOOSE_PAGE + slot;
-  if (slot < P && a.decay != 0.f) w += a.decay * *out;
-  *out = w;
+  if (a.splits > 1) {
+    a.part[((size_t)(split * a.n + blockIdx.y) * a.n_kv + kvh) * a.part_ld + slot] = w;
+    return;
+  }
+  store_weight(a, rq, (int)kvh, slot, P, w);
+}
+
+// Joins the splits, a thread a slot, in their order.
+__global__ __launch_bounds__(256) void k_weight_merge(const WeightArgs a) {
+  const unsigned block = blockIdx.x / (unsigned)a.n_kv, kvh = blockIdx.x - block * a.n_kv;
+  const ChunkReq& rq = a.r[blockIdx.y];
+  const int P = a.len[rq.seq], slot = (int)(block * 256 + threadIdx.x);
+  if (P < 0 || P > rq.P_max || slot >= P + rq.C) return;
+  if ((unsigned)a.table[(size_t)rq.seq * a.table_ld + slot / GOOSE_PAGE] >= (unsigned)a.n_pages) return;
+  const size_t step = (size_t)a.n * a.n_kv * a.part_ld;
+  const float* const from = a.part + ((size_t)blockIdx.y * a.n_kv + kvh) * a.part_ld + slot;
+  float w = 0.f;
+  for (int s0 = 0; s0 < a.splits; s0 += 4) {
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = from[min(s0 + k, a.splits - 1) * step];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w += s0 + k < a.splits ? v[k] : 0.f;
+  }
+  store_weight(a, rq, (int)kvh, slot, P, w);
 }
 
 template <int D>
-void launch_d(bool f16, int q_terms, dim3 grid, const WeightArgs& a, hipStream_t st) {
+void launch_d(bool f16, int q_terms, dim3 grid, size_t lds, const WeightArgs& a, hipStream_t st) {
+  const dim3 threads(64 * a.sg * a.rg);
   if (q_terms == 2) {
-    if (f16) hipLaunchKernelGGL((k_slot_weights<D, 2, true>), grid, dim3(64 * a.sg * a.rg), 0, st, a);
-    else hipLaunchKernelGGL((k_slot_weights<D, 2, false>), grid, dim3(64 * a.sg * a.rg), 0, st, a);
+    if (f16) hipLaunchKernelGGL((k_slot_weights<D, 2, true>), grid, threads, lds, st, a);
+    else hipLaunchKernelGGL((k_slot_weights<D, 2, false>), grid, threads, lds, st, a);
   } else {
-    if (f16) hipLaunchKernelGGL((k_slot_weights<D, 1, true>), grid, dim3(64 * a.sg * a.rg), 0, st, a);
-    else hipLaunchKernelGGL((k_slot_weights<D, 1, false>), grid, dim3(64 * a.sg * a.rg), 0, st, a);
+    if (f16) hipLaunchKernelGGL((k_slot_weights<D, 1, true>), grid, threads, lds, st, a);
+    else hipLaunchKernelGGL((k_slot_weights<D, 1, false>), grid, threads, lds, st, a);
   }
 }
 
 }  // namespace
 
 int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
-                       const ChunkReqs& ck, const float* lse, size_t ld_lse, float decay, float* weight, int32_t* flags, hipStream_t st) {
+                       const ChunkReqs& ck, const float* lse, size_t ld_lse, float decay, float* weight, float* ws, size_t ws_floats, int32_t* flags, hipStream_t st) {
   WeightArgs a{};
   a.kpool = static_cast<const char*>(pg.d_kpool) + (size_t)layer * page_layer_elems(pg, n_kv, head_dim) * 2;
   a.table = pg.d_table;
@@ -246,16 +280,43 @@ int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads,
     tiles = t > tiles ? t : tiles;
     waves += (long long)pages * n_kv;
   }
-  a.rg = 1;
-  while (a.rg < most_rg(head_dim / 16 * q_terms) && waves * a.rg < 2048 && tiles >= 8 * a.rg) a.rg *= 2;
-  a.sg = 1;
-  while (a.sg * a.rg < 8 && waves * a.rg >= 512ll * a.sg * a.rg) a.sg *= 2;
+  a.rg = a.sg = a.splits = 1;
+  a.part = ws;
+  a.part_ld = (size_t)most * GOOSE_PAGE;
+  if (tiles >= 16) {
+    a.rg = 2;
+    while (a.sg < 4 && a.sg < most) a.sg *= 2;
+    // A CU holds one such workgroup.  Those of committed pages go through all rows, those of the chunk's own about half; the rows are split so that the last round of 256
+    // is not left half empty, and chunks with few pages fill the CUs.  In units of 10 ns: a workgroup's beginning and end 500, a tile of a wavefront, the merge 500.
+    // (2048 tokens of 32 / 8 heads from the start 46 us in four parts, 38 in eight, 71 in one; 512 behind 4000 slots with two-term queries 64 in two, 52 in three, 83 in one.)
+    long long full = 0, own = 0, best = INT64_MAX;
+    for (int i = 0; i < ck.n; ++i) {
+      const int before = ck.r[i].P_max / (GOOSE_PAGE * a.sg), all = (ck.r[i].P_max + ck.r[i].C + GOOSE_PAGE * a.sg - 1) / (GOOSE_PAGE * a.sg);
+      full += (long long)before * n_kv;
+      own += (long long)(all - before) * n_kv;
+    }
+    const long long tile = (q_terms == 1 ? 115 : 180) * (head_dim + 32) / 160;
+    for (int s = 1; s <= 32 && s * 8 <= tiles && (size_t)s * ck.n * n_kv * a.part_ld <= ws_floats; ++s) {
+      const long long one = 500 + (tiles / a.rg + s - 1) / s * tile, half = (500 + one) / 2;
+      const long long rounds = (full * s + 255) / 256, left = own * s - 2 * (rounds * 256 - full * s);  // (two of the chunk's own in a place that is left over)
+      long long cost = rounds * one + (left > 0 ? (left + 255) / 256 * half : 0);
+      cost = (cost > one ? cost : one) + (s > 1 ? 500 : 0);
+      if (cost < best) { best = cost; a.splits = s; }
+    }
+  } else {
+    while (a.sg < 4 && waves >= 512ll * a.sg) a.sg *= 2;
+  }
   const int groups = (most + a.sg - 1) / a.sg;
-  if ((long long)groups * n_kv * (64 * a.sg * a.rg) > UINT32_MAX) return GOOSE_ERR_CAPACITY;  // (threads of a launch)
-  const dim3 grid((unsigned)groups * (unsigned)n_kv, (unsigned)ck.n);
+  if ((long long)groups * a.splits * n_kv * (64 * a.sg * a.rg) > UINT32_MAX) return GOOSE_ERR_CAPACITY;  // (threads of a launch)
+  const dim3 grid((unsigned)groups * (unsigned)a.splits * (unsigned)n_kv, (unsigned)ck.n);
   const bool f16 = dtype == GOOSE_DTYPE_F16;
-  if (head_dim == 128) launch_d<128>(f16, q_terms, grid, a, st);
-  else if (head_dim == 64) launch_d<64>(f16, q_terms, grid, a, st);
+  const int sets = tiles > 2 * a.rg ? 2 : 1;  // (one step needs one)
+  const size_t lds = (size_t)sets * 2 * a.rg * (head_dim / 16 * q_terms) * 1024;
+  if (head_dim == 128) launch_d<128>(f16, q_terms, grid, lds, a, st);
+  else if (head_dim == 64) launch_d<64>(f16, q_terms, grid, lds, a, st);
   else return GOOSE_ERR_SHAPE;
+  const int rc = goose_launch_status();
+  if (rc != GOOSE_OK || a.splits == 1) return rc;
+  hipLaunchKernelGGL(k_weight_merge, dim3((unsigned)((most * GOOSE_PAGE + 255) / 256 * n_kv), (unsigned)ck.n), dim3(256), 0, st, a);
   return goose_launch_status();
 }

@@ -514,7 +514,7 @@ static int layer_impl(goose_ctx* c, const char* w, float* d_x, void* d_kcache, v
                              attn_records(c), c->o, c->ld_o, c->act_dtype, T, paged->weight ? c->lse : nullptr, c->Bpad, c->flags, st);
       if (!rc && paged->weight)
         rc = launch_attn_weight(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, *paged->chunks, c->lse,
-                                c->Bpad, paged->decay, paged->weight, c->flags, st);
+                                c->Bpad, paged->decay, paged->weight, c->att_o, attn_records(c) * d.head_dim, c->flags, st);
     } else {
       rc = launch_attn_paged(d.dtype, *paged->pages, paged->layer, d.n_heads, c->n_kv, d.head_dim, c->q, ldq, q_terms, paged->mask,
                              paged->shared_pages, c->att_o, c->att_ml, attn_records(c), c->o, c->ld_o, c->act_dtype, T, c->flags, st);
@@ -1091,7 +1091,7 @@ int goose_attn_weight_paged(goose_ctx* c, const goose_pages* pg, int layer, cons
   if (rc) return rc;
   if (ld_lse < (size_t)ck.rows || ld_lse > UINT32_MAX) return GOOSE_ERR_ARG;
   return launch_attn_weight(c->d.dtype, *pg, layer, c->d.n_heads, c->n_kv, c->d.head_dim, d_q, ldq, q_terms, ck, d_lse, ld_lse, decay, d_weight,
-                            c->flags, as_stream(stream));
+                            c->att_o, attn_records(c) * c->d.head_dim, c->flags, as_stream(stream));
 }
 
 int goose_pages_append(goose_ctx* c, const goose_pages* pg, const goose_chunk* chunks, int n, void* stream) {

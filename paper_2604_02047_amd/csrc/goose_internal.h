@@ -332,7 +332,7 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
                       const ChunkReqs& ck, float* ws_o, float* ws_ml, size_t max_records, void* o, size_t ldo, int o_dtype, int o_terms, float* lse,
                       size_t ld_lse, int32_t* flags, hipStream_t st);
 int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads, int n_kv, int head_dim, const void* q, size_t ldq, int q_terms,
-                       const ChunkReqs& ck, const float* lse, size_t ld_lse, float decay, float* weight, int32_t* flags, hipStream_t st);
+                       const ChunkReqs& ck, const float* lse, size_t ld_lse, float decay, float* weight, float* ws, size_t ws_floats, int32_t* flags, hipStream_t st);
 int launch_pages_append(const goose_pages& pg, const ChunkReqs& ck, int32_t* flags, hipStream_t st);
 struct Evictions {
   int32_t n;

@@ -257,3 +257,54 @@ def test_more_rows_under_a_head_than_are_counted():
     rc = ctx.lib.goose_attn_chunk_paged(ctx._h, cache._ref, 0, at, n * 64, 1, chunks._c, 1, at, n * 64, gb.GOOSE_DTYPE_BF16, 1, 0, 0, 0)
     assert rc == gb.GOOSE_ERR_CAPACITY
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype,d,terms", [("bf16", 128, 2), ("f16", 64, 1), ("f16", 128, 1), ("bf16", 64, 2)])
+def test_rows_in_parts(dtype, d, terms):
+    """Many rows over few pages: parts of the rows, joined afterwards."""
+    for nh, nkv, Cs, Ps, first, bound in ((4, 2, [900], [0], [0], None), (8, 1, [600, 3, 700], [70, 900, 0], [5, 0, 699], None), (4, 4, [520, 513], [64, 63], [0, 500], 2000),
+                                          (2, 1, [1025], [640], [0], 800)):
+        for decay in (0.0, 0.75):
+            c = Case(nh, nkv, d, dtype, Cs, Ps, seed=11, terms=terms)
+            c.setup(first, bound)
+            c.weigh(decay)
+            assert c.ctx.goose_device_flags() == 0
+            c.check_weights(decay)
+
+
+def test_rows_in_parts_flags_and_a_graph():
+    c = Case(8, 2, 128, "f16", [800, 1], [200, 100], seed=12)
+    c.setup(bound=400)
+    c.weigh(0.5)
+    want = c.weight.clone()
+    c.check_weights(0.5)
+    # a page out of range: its slots stay, and the others are the same bits
+    old = int(c.cache.table[0, 4])
+    c.cache.table[0, 4] = -1
+    c.weight.copy_(c.old)
+    c.weigh(0.5)
+    assert c.ctx.goose_device_flags() == gb.GOOSE_FLAG_PAGES
+    got = c.weight.clone()
+    assert torch.equal(got[0, 0, :, 256:320].cpu(), c.old[0, 0, :, 256:320])
+    got[0, 0, :, 256:320] = want[0, 0, :, 256:320]
+    assert torch.equal(got, want)
+    c.cache.table[0, 4] = old
+    for n in (-1, 401):
+        c.cache.len[0] = n
+        c.weight.copy_(c.old)
+        c.weigh(0.5)
+        assert c.ctx.goose_device_flags() == gb.GOOSE_FLAG_CAPACITY
+        assert torch.equal(c.weight[0, 0].cpu(), c.old[0, 0]) and torch.equal(c.weight[0, 1], want[0, 1])
+    c.cache.len[0] = 200
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        c.weigh(0.5)
+    for _ in range(3):
+        c.weight.copy_(c.old)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.weight, want)
+        # what the context's workspace holds in between does not matter
+        c.call(lse=False)
+        torch.cuda.synchronize()
