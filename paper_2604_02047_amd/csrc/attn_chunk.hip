@@ -308,13 +308,30 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
                       size_t ld_lse, int32_t* flags, hipStream_t st) {
   if (head_dim != 64 && head_dim != 128) return GOOSE_ERR_SHAPE;
   const int group = n_heads / n_kv;
-  // Chunks of few rows are chains of nodes for the tree kernels, which have shapes for them: one token of 32 / 8 heads behind 4000 slots 17 us (the ring 26), 64 of
-  // them behind 2000, four requests 35 (44); of a multi-head model only up to 32 tokens (64 behind 8000: 53, the ring 33; behind 300: 13 and 16).
+  // Chunks of few rows are chains of nodes for the tree kernels, which have shapes for them, unless there are hardly any slots to read or so many rows in all that
+  // the ring has enough to do.  us, tree / ring, of 32 / 8 heads: one token behind 2000 slots 14 / 20, 16 requests 26 / 34; 64 tokens behind 600 16 / 18, four requests
+  // 18 / 22, 15 50 / 27; 64 tokens behind 8000 33 / 28; 40 heads, 15 requests of one token behind nothing 22 / 17, 200 slots 30 / 28, 600 44 / 48; of 16 tokens 53 / 50.
+  // (Of a multi-head model chunks of more than 32 tokens always: 64 behind 300 16 / 13, behind 8000 53 / 33.)
+  auto blocks_of = [](const ChunkReq& c) { return (c.P_max + c.C + 31) / 32; };
+  auto small = [&](const ChunkReq& c) { return c.C <= GOOSE_MAX_B && c.C * group <= 256 && (group > 1 || c.C <= 32); };
+  long long small_tiles = 0, small_work = 0;  // tiles of 32 rows, times blocks
+  for (int i = 0; i < ck.n; ++i)
+    if (small(ck.r[i])) {
+      const long long t = (long long)n_kv * ((ck.r[i].C * group + 31) / 32);
+      small_tiles += t;
+      small_work += t * blocks_of(ck.r[i]);
+    }
+  auto by_tree = [&](const ChunkReq& c) {
+    const int rows = c.C * group, blocks = blocks_of(c);
+    if (!small(c) || blocks <= 2) return false;
+    if (small_tiles >= 400 && (rows >= 16 || blocks <= 8)) return false;
+    return small_work < 16000 || rows < 64;
+  };
   PagedReqs few{};
   ChunkReqs many{};
   for (int i = 0; i < ck.n; ++i) {
     const ChunkReq& c = ck.r[i];
-    if (c.C <= GOOSE_MAX_B && c.C * group <= 256 && (group > 1 || c.C <= 32)) {
+    if (by_tree(c)) {
       few.r[few.n++] = PagedReq{c.seq, c.C, c.P_max, c.row0, few.rows, nullptr, nullptr};
       few.rows += c.C;
     } else {
@@ -357,7 +374,7 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   int best_per = 0;
   int longest = 0;
   for (int i = 0; i < many.n; ++i) {
-    const int blocks = (many.r[i].P_max + many.r[i].C + 31) / 32;
+    const int blocks = blocks_of(many.r[i]);
     longest = blocks > longest ? blocks : longest;
   }
   // Two workgroups of four wavefronts a CU hide each other's beginnings and ends, one of eight copies every block once: us with 4 / 8 at 16 blocks (512 tokens of 32
@@ -370,7 +387,7 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
     for (int i = 0; i < many.n; ++i) {
       const ChunkReq& c = many.r[i];
       const long long tiles = ((long long)c.C * group + tile_rows - 1) / tile_rows;
-      const int blocks = (c.P_max + c.C + 31) / 32, splits = splits_of(blocks, per);
+      const int blocks = blocks_of(c), splits = splits_of(blocks, per);
       const long long sum = tiles * (2ll * c.P_max + c.C) / 64 + 2 * tiles;  // blocks of all tiles
       work += (sum * step + tiles * splits * fixed) * n_kv;
       items += tiles * splits * n_kv;
@@ -389,7 +406,7 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   long long items = 0;
   for (int i = 0; i < many.n; ++i) {
     const ChunkReq& c = many.r[i];
-    const int tiles = (c.C * group + tile_rows - 1) / tile_rows, waves = (c.C * group + 31) / 32, splits = splits_of((c.P_max + c.C + 31) / 32, best_per);
+    const int tiles = (c.C * group + tile_rows - 1) / tile_rows, waves = (c.C * group + 31) / 32, splits = splits_of(blocks_of(c), best_per);
     a.it[i] = ChunkItems{tiles, splits, waves, joins, records};
     if (splits > 1) {
       records += (uint32_t)(splits * n_kv * waves);
