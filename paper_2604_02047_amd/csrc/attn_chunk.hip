@@ -38,11 +38,16 @@ __device__ __forceinline__ void finish(const ChunkArgs& a, size_t row, int h, in
   if (a.lse != nullptr && c == 0) a.lse[(size_t)h * a.ld_lse + row] = log_of_sum(m, l, softmax_scale(D));
 }
 
-// One workgroup = NW wavefronts, two on a SIMD (of one workgroup of eight or two of four), 32 rows each x a range of blocks.  Every block comes into LDS once, global -> LDS without
-// registers, into a ring that runs several blocks ahead; a wavefront has three blocks under way at once (ring_step).  Blocks that a
-// wavefront's rows do not see whole are masked on the way, and behind the last one that it sees it only goes on copying.
+// One workgroup = NW wavefronts, two on a SIMD (of one workgroup of eight or two of four), 32 rows each x a range of blocks.  Every block comes into LDS
+// once, global -> LDS without registers, into a ring that runs several blocks ahead; a wavefront has three blocks under way at once (ring_step).  Blocks
+// that a wavefront's rows do not see whole are masked on the way, and behind the last one that it sees it only goes on copying.
 // A weight of zero does not keep a NaN or an infinity of an unseen slot's values out of the matrix instruction: a wavefront that has such a thing in its
-// outputs at the end starts again, block by block with values_odd and sums in the ring's order: rows that do not see the thing keep their bits.  The block that the chunk ends in, whose other slots may hold anything, follows that way always.
+// outputs at the end starts again, block by block with values_odd and sums in the ring's order: rows that do not see the thing keep their bits.  The block
+// that the chunk ends in, whose other slots may hold anything, follows that way always.
+// What bounds it: the matrix and vector pipes together, at the clock that their load leaves.  4096 tokens of 32 / 8 heads behind 12288 slots, fp16, 890 us, 1080
+// TFLOP/s (a large matrix product alone 1430): matrix pipe busy 58 %, vector ALU 49 %, clock 1.5 GHz; 838 without the copies behind the first ring, 871 without
+// maxima.  Short ranges: 33B, 2000 tokens, 73 us (720 TFLOP/s), of which copies 6 and masks 2.  64 rows a wavefront, one on a SIMD, would read LDS half as often,
+// but reached 940 TFLOP/s.
 template <int D, int QT, bool F16, int PT, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
   typedef RowTile<D, QT, F16, PT> Tile;
@@ -245,7 +250,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
   }
 }
 
-// Joins the splits of a 32-row tile: a thread the four columns that a lane held, records in their order, four in flight together.
+// Joins the splits of a 32-row tile: a thread the four columns that a lane held, records in their order, four in flight together.  512 tokens of 32 heads in four
+// splits: 34 MB of records out of the caches behind the L2s, 8.5 us.
 template <int D>
 __global__ __launch_bounds__(256) void k_chunk_merge(const ChunkArgs a) {
   constexpr int PER = D / 32;  // workgroups a tile, four quads of columns each
@@ -366,9 +372,14 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.n = many.n;
   a.o_terms = o_terms;
   a.o_f16 = o_dtype == GOOSE_DTYPE_F16;
-  // a weight carries as many bits as the output keeps
+  // A weight carries as many bits as the output keeps: in one term it is off by up to 2^-8 (bf16) or 2^-11 of itself, independently of the others, which leaves
+  // the output about as far from the exact one as its own rounding does (fp16 0.00029 of its size instead of 0.00021 with two, bf16 0.0021 and 0.0016).  A
+  // second term costs 4096 tokens behind 12288 slots 899 -> 1226 us, five ragged prompts of 32 heads 65 -> 86, 2000 tokens of 52 heads 74 -> 96; outputs in two
+  // terms get it, and fp16 outputs of a bf16 cache.
   const int p_terms = o_terms == 1 && (o_dtype == GOOSE_DTYPE_BF16 || dtype == GOOSE_DTYPE_F16) ? 1 : 2;
-  // Work items run in rounds of as many as the CUs hold, the longest first.  In units of 10 ns: an item's fixed part, a block of it, the merge and its records.
+  // Work items run in rounds of as many as the CUs hold, the longest first.  In units of 10 ns: an item's fixed part (length, table and first blocks one after the
+  // other, the last block, stores), a block of it (measured over one and two terms), the merge and its records.  (300 or 1000 for the fixed part choose splits
+  // that take as long, or up to 16 % longer.)
   const long long fixed = 700, step = (30 + 34 * (q_terms + p_terms)) * (head_dim + 64) / 192;
   long long best = INT64_MAX;
   int best_per = 0;

@@ -8,6 +8,8 @@
 //                   block that its last row came from, and blocks ahead are only read
 //   k_evict_settle  lengths and pages (the last workgroup to move could do it, but thousands that count themselves in one word cost more than the launch:
 //                   13B, 8 layers of 4 sequences of 28 slots 139 us against 67)
+// What bounds it: memory, where there is much to move (Llama 3 8B heads, 8 layers of 4 sequences from 8192 to 2048 slots: 1.28 GB in 245 us with cold caches, 5.2 TB/s; 7B, 4
+// layers of 2 from 3001 to 2500: 0.73 GB in 146 us), else the launches and the trips to memory that follow from each other.
 // A rotation by the position that a key gives up needs both halves of its pairs, which is why a wavefront of the keys has columns
 // 16 u .. 16 u + 15 and those d/2 further.
 #include "mma16.h"
