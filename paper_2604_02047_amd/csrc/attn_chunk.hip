@@ -28,7 +28,8 @@ struct ChunkArgs {
   int32_t* flags;
   size_t ldq, ldo, ld_lse;
   int32_t table_ld, n_pages, n_heads, n_kv, group, n;
-  int32_t o_terms, o_f16, paired;
+  int32_t o_terms, o_f16;
+  int32_t groups, turn;  // of items (one for every KV head); from group `turn` on (0: never) the shortest come first
   ChunkItems it[GOOSE_MAX_REQUESTS];
   ChunkReq r[GOOSE_MAX_REQUESTS];
 };
@@ -63,16 +64,16 @@ __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
   const int l31 = lane & 31, hh = lane >> 5;
   int y = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / (unsigned)a.n_kv));
   const int kvh = (int)blockIdx.x - y * a.n_kv;  // the fast index: where 8 divides the KV heads, all items of a head run on one XCD
+  // (Items run from the longest to the shortest.  Where two fit a CU and all run at once, the second of a CU comes from the other end.)
+  if (a.turn > 0 && y >= a.turn) y = a.groups - 1 - (y - a.turn);
   int ri = 0;
   while (y >= a.it[ri].tiles * a.it[ri].splits) { y -= a.it[ri].tiles * a.it[ri].splits; ++ri; }
   ri = __builtin_amdgcn_readfirstlane(ri);
   y = __builtin_amdgcn_readfirstlane(y);
   const ChunkReq& rq = a.r[ri];
   const ChunkItems& ci = a.it[ri];
-  // Items from the longest to the shortest.  Where two fit a CU and all run at once, the second of a CU comes from the other end.
-  const int items = ci.tiles * ci.splits, half = (items + 1) / 2;
-  const unsigned i = a.paired && y >= half ? items - 1 - (y - half) : y, longest = __builtin_amdgcn_readfirstlane(i / (unsigned)ci.splits);
-  const int tile = ci.tiles - 1 - (int)longest, split = __builtin_amdgcn_readfirstlane((int)(i - longest * ci.splits));
+  const unsigned longest = __builtin_amdgcn_readfirstlane((unsigned)y / (unsigned)ci.splits);
+  const int tile = ci.tiles - 1 - (int)longest, split = y - (int)longest * ci.splits;
   const int rows = rq.C * a.group, wg_first = tile * ROWS, row_first = wg_first + wave * 32;
   auto query = [&](int rho) -> const T* {
     const int at = min(rho, rows - 1), tok = (int)((unsigned)at / (unsigned)a.group), h = kvh * a.group + at - tok * a.group;
@@ -341,7 +342,9 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
       few.r[few.n++] = PagedReq{c.seq, c.C, c.P_max, c.row0, few.rows, nullptr, nullptr};
       few.rows += c.C;
     } else {
-      many.r[many.n++] = c;
+      int at = many.n++;
+      for (; at > 0 && blocks_of(many.r[at - 1]) < blocks_of(c); --at) many.r[at] = many.r[at - 1];  // the longest first
+      many.r[at] = c;
     }
   }
   if (few.n > 0) {
@@ -379,7 +382,7 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   const int p_terms = o_terms == 1 && (o_dtype == GOOSE_DTYPE_BF16 || dtype == GOOSE_DTYPE_F16) ? 1 : 2;
   // Work items run in rounds of as many as the CUs hold, the longest first.  In units of 10 ns: an item's fixed part (length, table and first blocks one after the
   // other, the last block, stores), a block of it (measured over one and two terms), the merge and its records.  (300 or 1000 for the fixed part choose splits
-  // that take as long, or up to 16 % longer.)
+  // that take as long, or up to 16 % longer.)  Alone on its CU a workgroup of four takes two thirds of a block's time, which is what the longest item comes to.
   const long long fixed = 700, step = (30 + 34 * (q_terms + p_terms)) * (head_dim + 64) / 192;
   long long best = INT64_MAX;
   int best_per = 0;
@@ -402,12 +405,12 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
       const long long sum = tiles * (2ll * c.P_max + c.C) / 64 + 2 * tiles;  // blocks of all tiles
       work += (sum * step + tiles * splits * fixed) * n_kv;
       items += tiles * splits * n_kv;
-      const long long len = splits_of(blocks, splits) * step + fixed;
+      const long long len = splits_of(blocks, splits) * (nw == 4 ? step * 13 / 20 : step) + fixed;
       most = len > most ? len : most;
       if (splits > 1) records += (long long)splits * n_kv * ((c.C * group + 31) / 32);
     }
     if (records * 32 > (long long)max_records) continue;
-    const long long rounds = (items + slots - 1) / slots, time = rounds * (work / items);
+    const long long rounds = (items + slots - 1) / slots, time = items <= 256 ? 0 : rounds * (work / items);
     const long long cost = (time > most ? time : most) + (records > 0 ? 600 + records * 32 * head_dim * 8 / 50000 : 0);
     if (cost < best) { best = cost; best_per = per; }
   }
@@ -427,7 +430,8 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
     items += (long long)tiles * splits * n_kv;
   }
   if (items * 64 * nw > UINT32_MAX) return GOOSE_ERR_CAPACITY;  // (threads of a launch)
-  a.paired = nw == 4 && items > 256 && items <= 512;
+  a.groups = (int)(items / n_kv);
+  a.turn = nw == 4 && items > 256 && items <= 512 ? 256 / n_kv : 0;
   const bool f16 = dtype == GOOSE_DTYPE_F16;
   if (head_dim == 128) nw == 4 ? launch_d<128, 4>(f16, q_terms, p_terms, (unsigned)items, a, st) : launch_d<128, 8>(f16, q_terms, p_terms, (unsigned)items, a, st);
   else nw == 4 ? launch_d<64, 4>(f16, q_terms, p_terms, (unsigned)items, a, st) : launch_d<64, 8>(f16, q_terms, p_terms, (unsigned)items, a, st);
