@@ -81,19 +81,26 @@ __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
   };
   Tile t;
   t.init(query(row_first + l31));  // (asked for in front of the length, which all else waits for)
-  const int P = chunk_length(a.len, rq, a.flags, tid == 0 && y == 0 && kvh == 0);
+  const int32_t* const table = a.table + (size_t)rq.seq * a.table_ld;
   auto token_of = [&](int rho) { return __builtin_amdgcn_readfirstlane((int)((unsigned)min(rho, rows - 1) / (unsigned)a.group)); };
+  // blocks that the tile's last row sees behind a length, and those before part s of them
+  auto total_of = [&](int P) { return (P + token_of(wg_first + ROWS - 1)) / 32 + 1; };
+  auto part_of = [&](int total, int s) { return __builtin_amdgcn_readfirstlane((int)((unsigned)total * (unsigned)s / (unsigned)ci.splits)); };
+  // (the first page ids, too: where they are if the length is its bound)
+  const int likely = part_of(total_of(rq.P_max), split) >> 1, entry = likely + lane < a.table_ld ? table[likely + lane] : 0;
+  const int P = chunk_length(a.len, rq, a.flags, tid == 0 && y == 0 && kvh == 0);
   auto clamp = [](int x, int lo, int hi) { return min(max(x, lo), hi); };
-  // blocks that the tile's last row sees, this item's range of them, and the blocks of it in front of the chunk's end
-  const int total = (P + token_of(wg_first + ROWS - 1)) / 32 + 1;
-  const int b_lo = __builtin_amdgcn_readfirstlane((int)((unsigned)total * (unsigned)split / (unsigned)ci.splits));
-  const int b_hi = __builtin_amdgcn_readfirstlane((int)((unsigned)total * (unsigned)(split + 1) / (unsigned)ci.splits));
+  // this item's range of blocks, and those of it in front of the chunk's end
+  const int total = total_of(P), b_lo = part_of(total, split), b_hi = part_of(total, split + 1);
   const int units = __builtin_amdgcn_readfirstlane(clamp((P + rq.C) / 32 - b_lo, 0, b_hi - b_lo));
   // of the ring's units: from `whole` on some rows of this wavefront do not see all of it, from `seen` on none sees any
   const int whole = __builtin_amdgcn_readfirstlane((P + token_of(row_first) + 1) / 32 - b_lo);
   const int seen = __builtin_amdgcn_readfirstlane(row_first < rows ? clamp((P + token_of(row_first + 31)) / 32 + 1 - b_lo, 0, units) : -1);
-  PageIds pg{a.table + (size_t)rq.seq * a.table_ld, a.flags, b_lo >> 1, (b_hi - 1) >> 1, a.n_pages, 0};
-  if (b_hi > b_lo) pg.load(lane);
+  PageIds pg{table, a.flags, b_lo >> 1, (b_hi - 1) >> 1, a.n_pages, 0};
+  if (b_hi > b_lo) {
+    if (pg.base == likely) pg.take(lane, entry);
+    else pg.load(lane);
+  }
   const char* const kp = static_cast<const char*>(a.kpool);
   const char* const vp = static_cast<const char*>(a.vpool);
   auto block_at = [&](int b) -> size_t {  // bytes (pages times KV heads stays below 2^29: checked on the host)
@@ -194,7 +201,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
   }
   if (row_first >= rows) return;
   // ---- the block that the chunk ends in (in LDS already where the ring ran), or all of them again from memory
-  // (the row and its query again: kept over the ring's loop they would take registers that it needs)
+  // (the row again: kept over the ring's loop it would take registers that it needs)
   int rho = row_first + l31;
   GOOSE_HERE(rho);
   const int tok = (int)((unsigned)min(rho, rows - 1) / (unsigned)a.group), h = kvh * a.group + rho - tok * a.group;
@@ -207,7 +214,6 @@ __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
   const bool again = units > 0 && __builtin_amdgcn_ballot_w64(odd_out != 0.f) != 0;
   if (again || b_lo + units < end) {
     if (again) t.init(query(rho));
-    else t.load_q(query(rho));
     pg.base = (again ? b_lo : b_lo + units) >> 1;  // (the window may have run ahead)
     pg.load(lane);
 #pragma unroll 1

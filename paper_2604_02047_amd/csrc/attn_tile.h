@@ -58,9 +58,9 @@ struct PageIds {
   const int32_t* row;
   int32_t* flags;
   int base, last, n_pages, ids;
-  __device__ __forceinline__ void load(int lane) {
-    const int e = base + lane;
-    ids = e <= last ? row[e] : 0;
+  __device__ __forceinline__ void load(int lane) { take(lane, base + lane <= last ? row[base + lane] : 0); }
+  __device__ __forceinline__ void take(int lane, int entry) {
+    ids = base + lane <= last ? entry : 0;
     if ((unsigned)ids >= (unsigned)n_pages) { atomicOr(flags, GOOSE_FLAG_PAGES); ids = 0; }
   }
   // the id of block b's page; b never steps below the window, and block_last bounds it
