@@ -282,7 +282,7 @@ __device__ __forceinline__ void turn(float t, float* sine, float* cosine) {
   *cosine = ((q + 1) & 2) ? -b : b;
 }
 
-// A window is NW * AHEAD blocks, AHEAD next to each other a wavefront.  Its rows go into LDS, at the places of the destination blocks that they fill, while the next
+// A window is NW * AHEAD blocks, AHEAD in a row a wavefront.  Its rows go into LDS, at the places of the destination blocks that they fill, while the next
 // window's loads are on their way; then the blocks that are full leave, and the wavefronts take turns at them.
 template <int D, bool F16, int NW>
 __global__ __launch_bounds__(64 * NW) void k_evict_move(const goose_pages pg, const Evictions ev, int n_layers, int n_kv, const double* __restrict__ inv_freq,
@@ -322,43 +322,50 @@ __global__ __launch_bounds__(64 * NW) void k_evict_move(const goose_pages pg, co
 #pragma unroll
     for (int e = 0; e < 8; ++e) turns[e] = inv_freq[unit * 16 + hh * 8 + e] * 0.15915494309189533577;
   }
-  const int b0 = q.sink >> 5, b_end = (len + 31) >> 5;  // (all slots in front of b0 stay)
   u32x4 r0[AHEAD], r1[AHEAD];
   unsigned masks[AHEAD];
-  int places[AHEAD];  // where their first kept rows go
-  // Ids and words of 64 pages at a time, one a lane, where blocks come from, with the kept rows in front of each; ids where they go (which never
-  // steps ahead of that): asked for block by block they would be two trips to memory each.
+  int blocks[AHEAD], places[AHEAD];  // which they are, and where their first kept rows go
+  // Only blocks of which something stays are looked at.  Ids and words of 64 pages at a time, one a lane, with a sum over the lanes of kept rows and of such blocks; ids where
+  // rows go (which never steps ahead of that): asked for block by block they would be two trips to memory each.
   const int pages = (len + GOOSE_PAGE - 1) / GOOSE_PAGE;
-  int src0 = b0 >> 1, dst0 = src0, src_ids, dst_ids, front = src0 * GOOSE_PAGE, sum;
+  int src0 = q.sink / GOOSE_PAGE, dst0 = src0, src_ids, dst_ids, sum;  // sum: blocks << 16 | rows
+  int rows_passed = src0 * GOOSE_PAGE, blocks_passed = 0;  // in front of these pages (all slots in front of the first stay)
   uint64_t src_words;
   auto src_window = [&]() {
     const int i = min(src0 + lane, pages - 1);
     src_ids = row[i];
-    src_words = words[i];
-    sum = src0 + lane < pages ? (int)__popcll(src_words) : 0;
+    const uint64_t word = words[i];
+    src_words = src0 + lane < pages ? word : 0;
+    sum = (int)__popcll(src_words) + (((unsigned)src_words != 0) + ((src_words >> 32) != 0)) * 65536;
     sum += lanes_before(sum);
   };
-  // the word of block c's page, and how many kept rows lie in front of c (c never steps back)
-  auto word_of = [&](int c, int* before) -> unsigned {
-    while ((c >> 1) - src0 >= 64) {
-      front += __builtin_amdgcn_readlane(sum, 63);
+  // the n-th such block (n never falls): its number or -1, its word, its page, and how many kept rows lie in front of it
+  auto find = [&](int n, unsigned* word, int* page, int* before) -> int {
+    for (int all; n - blocks_passed >= (all = __builtin_amdgcn_readlane(sum, 63)) >> 16;) {
+      if (src0 + 64 >= pages) return -1;
+      blocks_passed += all >> 16;
+      rows_passed += all & 0xFFFF;
       src0 += 64;
       src_window();
     }
-    const int l = (c >> 1) - src0;
+    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum >> 16 > n - blocks_passed)), upto = __builtin_amdgcn_readlane(sum, l);
     const unsigned low = (unsigned)__builtin_amdgcn_readlane((int)src_words, l), high = (unsigned)__builtin_amdgcn_readlane((int)(src_words >> 32), l);
-    *before = front + __builtin_amdgcn_readlane(sum, l) - __popc(high) - ((c & 1) ? 0 : __popc(low));
-    return (c & 1) ? high : low;
+    // (the last of its page's if the sum up to there leaves none behind it)
+    const bool second = high != 0 && upto >> 16 == n - blocks_passed + 1;
+    *word = second ? high : low;
+    *page = __builtin_amdgcn_readlane(src_ids, l);
+    *before = rows_passed + (upto & 0xFFFF) - __popc(high) - (second ? 0 : __popc(low));
+    return 2 * (src0 + l) + (second ? 1 : 0);
   };
   src_window();
   dst_ids = src_ids;
-  const T* fetched = block_of(__builtin_amdgcn_readlane(src_ids, 0), b0);
-  // (Always a load, of the last block again where nothing of this one is kept: one that may or may not be in flight would make the others wait for all.)
-  auto load = [&](int b, unsigned& mask, int& place, u32x4& x, u32x4& y) {
-    const int c = min(b, b_end - 1);
-    const unsigned word = word_of(c, &place);
-    mask = b < b_end ? word : 0;
-    if (mask != 0) fetched = block_of(__builtin_amdgcn_readlane(src_ids, (c >> 1) - src0), c);
+  const T* fetched = block_of(__builtin_amdgcn_readlane(src_ids, 0), 2 * src0);
+  // (Always a load, of the last block again behind the end: one that may or may not be in flight would make the others wait for all.)
+  auto load = [&](int n, unsigned& mask, int& block, int& place, u32x4& x, u32x4& y) {
+    int page;
+    block = find(n, &mask, &page, &place);
+    if (block >= 0) fetched = block_of(page, block);
+    else mask = 0;
     x = *reinterpret_cast<const u32x4*>(fetched + p0 * 512);
     y = *reinterpret_cast<const u32x4*>(fetched + p1 * 512);
   };
@@ -433,18 +440,19 @@ __global__ __launch_bounds__(64 * NW) void k_evict_move(const goose_pages pg, co
     }
   };
 #pragma unroll
-  for (int k = 0; k < AHEAD; ++k) load(b0 + wave * AHEAD + k, masks[k], places[k], r0[k], r1[k]);
-  // (one copy of flush: its code, eight sines and cosines, would not fit the instruction cache several times; 690 us instead of 440 for 4 x 8192 slots)
-  int done = b0;  // destination blocks written
+  for (int k = 0; k < AHEAD; ++k) load(wave * AHEAD + k, masks[k], blocks[k], places[k], r0[k], r1[k]);
+  // (one copy of flush: its code would not fit the instruction cache several times; with library sines and cosines 690 us instead of 440 for 4 x 8192 slots)
+  int done = 2 * dst0;  // destination blocks written
 #pragma unroll 1
-  for (int b = b0;; b += WINDOW) {
-    const bool last = b + WINDOW >= b_end;
-    int rows = q.keep;  // that the windows so far hold
-    if (!last) word_of(b + WINDOW, &rows);
+  for (int n = WINDOW;; n += WINDOW) {
+    unsigned word;
+    int page, rows;  // that the windows so far hold
+    const bool last = find(n, &word, &page, &rows) < 0;
+    if (last) rows = q.keep;
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      place(b + wave * AHEAD + k, masks[k], places[k], r0[k], r1[k]);
-      load(b + WINDOW + wave * AHEAD + k, masks[k], places[k], r0[k], r1[k]);
+      place(blocks[k], masks[k], places[k], r0[k], r1[k]);
+      load(n + wave * AHEAD + k, masks[k], blocks[k], places[k], r0[k], r1[k]);
     }
     sync();
     const int full = last ? (rows + 31) >> 5 : rows >> 5;
