@@ -221,7 +221,7 @@ __global__ __launch_bounds__(512, 2) void k_slot_weights(const WeightArgs a) {
   store_weight(a, rq, (int)kvh, slot, P, w);
 }
 
-// Joins the splits, a thread a slot, in their order.
+// Joins the splits, a thread a slot and a workgroup four pages, in their order.
 __global__ __launch_bounds__(256) void k_weight_merge(const WeightArgs a) {
   const unsigned block = blockIdx.x / (unsigned)a.n_kv, kvh = blockIdx.x - block * a.n_kv;
   const ChunkReq& rq = a.r[blockIdx.y];
@@ -322,6 +322,6 @@ int launch_attn_weight(int dtype, const goose_pages& pg, int layer, int n_heads,
   else return GOOSE_ERR_SHAPE;
   const int rc = goose_launch_status();
   if (rc != GOOSE_OK || a.splits == 1) return rc;
-  hipLaunchKernelGGL(k_weight_merge, dim3((unsigned)((most * GOOSE_PAGE + 255) / 256 * n_kv), (unsigned)ck.n), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(k_weight_merge, dim3((unsigned)((most + 3) / 4) * (unsigned)n_kv, (unsigned)ck.n), dim3(256), 0, st, a);
   return goose_launch_status();
 }
