@@ -240,3 +240,24 @@ def test_refusals():
     s.check()
     call([good])
     assert s.ctx.goose_device_flags() == 0
+
+
+@pytest.mark.parametrize("reposition", [True, False])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
+def test_more_streams_than_the_card_has_units(dtype, d, reposition):
+    """Four wavefronts a stream of blocks, and one where there are thousands of short ones."""
+    for weights in ("random", "ties"):
+        s = Setup([700, 333, 65], layers=6, nkv=16 if d == 64 else 8, d=d, dtype=dtype, seed=11, weights=weights)
+        s.evict([{"seq": 1, "keep": 300, "sink": 40, "recent": 64}, {"seq": 0, "keep": 129, "sink": 65, "recent": 1}, {"seq": 2, "keep": 64}], reposition)
+    for keep in (1, 33, 64, 127):
+        s = Setup([130, 192, 129, 128, 191, 7], layers=6, nkv=16 if d == 64 else 8, d=d, dtype=dtype, seed=keep)
+        s.evict([{"seq": r, "keep": keep, "sink": min(keep, r), "recent": min(keep - min(keep, r), 3)} for r in range(6)], reposition)
+
+
+def test_long_sequences_of_many_streams():
+    """More pages than a wavefront's lanes, blocks of which nothing stays, a window that ends with the pages."""
+    for n, keep, sink, recent in ((4500, 4096, 3, 100), (4500, 70, 64, 2), (8300, 40, 0, 33), (4096, 4000, 4000, 0), (4161, 66, 1, 65)):
+        s = Setup([n], layers=9, nkv=15, seed=keep, weights="ties")
+        s.evict([{"seq": 0, "keep": keep, "sink": sink, "recent": recent}], reposition=False)
+        s = Setup([n, 100], layers=1, nkv=2, seed=keep)
+        s.evict([{"seq": 0, "keep": keep, "sink": sink, "recent": recent}])
