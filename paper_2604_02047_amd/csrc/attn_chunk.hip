@@ -45,13 +45,13 @@ __device__ __forceinline__ void finish(const ChunkArgs& a, size_t row, int h, in
 // A weight of zero does not keep a NaN or an infinity of an unseen slot's values out of the matrix instruction: a wavefront that has such a thing in its
 // outputs at the end starts again, block by block with values_odd and sums in the ring's order: rows that do not see the thing keep their bits.  The block
 // that the chunk ends in, whose other slots may hold anything, follows that way always.
-// What bounds it: the matrix and vector pipes together, at the clock that their load leaves.  4096 tokens of 32 / 8 heads behind 12288 slots, fp16, 890 us, 1080
-// TFLOP/s (a large matrix product alone 1430): matrix pipe busy 58 %, vector ALU 49 %, clock 1.5 GHz; 838 without the copies behind the first ring, 871 without
-// maxima.  Short ranges: 33B, 2000 tokens, 73 us (720 TFLOP/s), of which copies 6 and masks 2.  64 rows a wavefront, one on a SIMD, would read LDS half as often,
-// but reached 940 TFLOP/s.
-template <int D, int QT, bool F16, int PT, int NW>
+// A weight enters the second product in two 16-bit terms whatever the output keeps: one term would be off by half a step of the type, as much again as the store of a
+// one-term output, and by all of that in a row that a single key with a weight other than one dominates (4096 tokens behind 12288 slots 890 us so instead of 1195).
+// What bounds it: the matrix and vector pipes together, at the clock that their load leaves.  4096 tokens of 32 / 8 heads behind 12288 slots, fp16, 1195 us: 805
+// TFLOP/s, 1210 counting both terms of the weights (a large matrix product alone 1430).  Short ranges: 33B, 2000 tokens, 92 us (575 and 860 TFLOP/s).
+template <int D, int QT, bool F16, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
-  typedef RowTile<D, QT, F16, PT> Tile;
+  typedef RowTile<D, QT, F16> Tile;
   typedef typename Tile::T T;
   constexpr int NS = D / 16;
   constexpr int BLOCK = 2 * NS * 1024, BU = BLOCK / 16;  // keys and values of 32 slots: bytes, 16-byte units
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
     };
     auto step = [&](int j, const f32x16& za, f32x16& zb, const auto& w, const auto& wl, auto& wn, auto& wln) {
       if (j > seen || seen == 0) return;
-      ring_step<D, QT, F16, PT, 1, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale,
+      ring_step<D, QT, F16, 1, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale,
                                           [&](f32x16& s) {
                                             if (j + 1 >= whole) {
                                               const unsigned vis = seen16(last - (j + 1) * 32);
@@ -304,14 +304,13 @@ __global__ __launch_bounds__(256) void k_chunk_merge(const ChunkArgs a) {
 }
 
 template <int D, int QT, bool F16, int NW>
-void launch_t(int p_terms, unsigned items, const ChunkArgs& a, hipStream_t st) {
-  if (p_terms == 1) hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, 1, NW>), dim3(items), dim3(64 * NW), 0, st, a);
-  else hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, 2, NW>), dim3(items), dim3(64 * NW), 0, st, a);
+void launch_t(unsigned items, const ChunkArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((k_chunk_ring<D, QT, F16, NW>), dim3(items), dim3(64 * NW), 0, st, a);
 }
 template <int D, int NW>
-void launch_d(bool f16, int q_terms, int p_terms, unsigned items, const ChunkArgs& a, hipStream_t st) {
-  if (q_terms == 2) f16 ? launch_t<D, 2, true, NW>(p_terms, items, a, st) : launch_t<D, 2, false, NW>(p_terms, items, a, st);
-  else f16 ? launch_t<D, 1, true, NW>(p_terms, items, a, st) : launch_t<D, 1, false, NW>(p_terms, items, a, st);
+void launch_d(bool f16, int q_terms, unsigned items, const ChunkArgs& a, hipStream_t st) {
+  if (q_terms == 2) f16 ? launch_t<D, 2, true, NW>(items, a, st) : launch_t<D, 2, false, NW>(items, a, st);
+  else f16 ? launch_t<D, 1, true, NW>(items, a, st) : launch_t<D, 1, false, NW>(items, a, st);
 }
 
 }  // namespace
@@ -322,9 +321,9 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   if (head_dim != 64 && head_dim != 128) return GOOSE_ERR_SHAPE;
   const int group = n_heads / n_kv;
   // Chunks of few rows are chains of nodes for the tree kernels, which have shapes for them, unless there are hardly any slots to read or so many rows in all that
-  // the ring has enough to do.  us, tree / ring, of 32 / 8 heads: one token behind 2000 slots 14 / 20, 16 requests 26 / 34; 64 tokens behind 600 16 / 18, four requests
-  // 18 / 22, 15 50 / 27; 64 tokens behind 8000 33 / 28; 40 heads, 15 requests of one token behind nothing 22 / 17, 200 slots 30 / 28, 600 44 / 48; of 16 tokens 53 / 50.
-  // (Of a multi-head model chunks of more than 32 tokens always: 64 behind 300 16 / 13, behind 8000 53 / 33.)
+  // the ring has enough to do.  us, tree / ring, of 32 / 8 heads: one token behind 2000 slots 12 / 19, 16 requests 32 / 34; 64 tokens behind 600 15 / 17, four requests
+  // 17 / 23, 15 50 / 30; 64 tokens behind 8000 32 / 27; 40 heads, 15 requests of one token behind nothing 22 / 16, 200 slots 30 / 28, 600 43 / 48; of 16 tokens 52 / 51.
+  // (Of a multi-head model chunks of more than 32 tokens always: 64 behind 8000 53 / 35, though behind 300 13 / 16.)
   auto blocks_of = [](const ChunkReq& c) { return (c.P_max + c.C + 31) / 32; };
   auto small = [&](const ChunkReq& c) { return c.C <= GOOSE_MAX_B && c.C * group <= 256 && (group > 1 || c.C <= 32); };
   long long small_tiles = 0, small_work = 0;  // tiles of 32 rows, times blocks
@@ -381,15 +380,10 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.n = many.n;
   a.o_terms = o_terms;
   a.o_f16 = o_dtype == GOOSE_DTYPE_F16;
-  // A weight carries as many bits as the output keeps: in one term it is off by up to 2^-8 (bf16) or 2^-11 of itself, independently of the others, which leaves
-  // the output about as far from the exact one as its own rounding does (fp16 0.00029 of its size instead of 0.00021 with two, bf16 0.0021 and 0.0016).  A
-  // second term costs 4096 tokens behind 12288 slots 899 -> 1226 us, five ragged prompts of 32 heads 65 -> 86, 2000 tokens of 52 heads 74 -> 96; outputs in two
-  // terms get it, and fp16 outputs of a bf16 cache.
-  const int p_terms = o_terms == 1 && (o_dtype == GOOSE_DTYPE_BF16 || dtype == GOOSE_DTYPE_F16) ? 1 : 2;
   // Work items run in rounds of as many as the CUs hold, the longest first.  In units of 10 ns: an item's fixed part (length, table and first blocks one after the
-  // other, the last block, stores), a block of it (measured over one and two terms), the merge and its records.  (300 or 1000 for the fixed part choose splits
+  // other, the last block, stores), a block of it (measured over the terms), the merge and its records.  (300 or 1000 for the fixed part choose splits
   // that take as long, or up to 16 % longer.)  Alone on its CU a workgroup of four takes two thirds of a block's time, which is what the longest item comes to.
-  const long long fixed = 700, step = (30 + 34 * (q_terms + p_terms)) * (head_dim + 64) / 192;
+  const long long fixed = 700, step = (30 + 34 * (q_terms + 2)) * (head_dim + 64) / 192;
   long long best = INT64_MAX;
   int best_per = 0;
   int longest = 0;
@@ -398,7 +392,8 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
     longest = blocks > longest ? blocks : longest;
   }
   // Two workgroups of four wavefronts a CU hide each other's beginnings and ends, one of eight copies every block once: us with 4 / 8 at 16 blocks (512 tokens of 32
-  // heads) 17 / 22, 63 (2000 tokens of 52 heads) 73 / 77, 126 (512 of 32 / 8 heads behind 3500) 71 / 79, 282 (1024 behind 8000) 160 / 158, 512 (4096 behind 12288) 918 / 888.
+  // heads) 18 / 25, 63 (2000 tokens of 52 heads) 96 / 96, 126 (512 of 32 / 8 heads behind 3500) 69 / 74, 188 (1024 behind 5000) 141 / 144, 282 (behind 8000) 202 / 201, 512
+  // (4096 behind 12288) 1222 / 1192.
   const int nw = longest <= 256 ? 4 : 8, slots = 2048 / nw, tile_rows = 32 * nw;
   auto splits_of = [](int blocks, int per) { return (blocks + per - 1) / per; };
   for (int parts = 1; parts <= 32 && parts <= longest; ++parts) {
@@ -439,8 +434,8 @@ int launch_attn_chunk(int dtype, const goose_pages& pg, int layer, int n_heads, 
   a.groups = (int)(items / n_kv);
   a.turn = nw == 4 && items > 256 && items <= 512 ? 256 / n_kv : 0;
   const bool f16 = dtype == GOOSE_DTYPE_F16;
-  if (head_dim == 128) nw == 4 ? launch_d<128, 4>(f16, q_terms, p_terms, (unsigned)items, a, st) : launch_d<128, 8>(f16, q_terms, p_terms, (unsigned)items, a, st);
-  else nw == 4 ? launch_d<64, 4>(f16, q_terms, p_terms, (unsigned)items, a, st) : launch_d<64, 8>(f16, q_terms, p_terms, (unsigned)items, a, st);
+  if (head_dim == 128) nw == 4 ? launch_d<128, 4>(f16, q_terms, (unsigned)items, a, st) : launch_d<128, 8>(f16, q_terms, (unsigned)items, a, st);
+  else nw == 4 ? launch_d<64, 4>(f16, q_terms, (unsigned)items, a, st) : launch_d<64, 8>(f16, q_terms, (unsigned)items, a, st);
   const int rc = goose_launch_status();
   if (rc != GOOSE_OK || joins == 0) return rc;
   const dim3 grid((unsigned)(joins * (head_dim / 32)));

@@ -385,7 +385,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_tiles(const PagedAttnArgs a) {
       barrier();
       __builtin_amdgcn_sched_barrier(0);
       copy();
-      if (work) ring_step<D, QT, F16, 2, G, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale, [](f32x16&) {});
+      if (work) ring_step<D, QT, F16, G, AHEAD>(t, pc, keys_of(j + 1), keys_of(j - 1) + BU / 2, keys_of(j + 2), za, zb, w, wl, wn, wln, j + 1 < units, scale, [](f32x16&) {});
     };
     int j = 1;
     for (; j + 1 < units; j += 2) {

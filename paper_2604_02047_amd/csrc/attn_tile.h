@@ -77,8 +77,8 @@ struct PageIds {
 #define GOOSE_HERE(x) (void)(x)
 #endif
 
-// ---- 32 rows of the softmax; weights enter the second product in PT terms --------------------------------------------------
-template <int D, int QT, bool F16, int PT = 2>
+// ---- 32 rows of the softmax; weights enter the second product in two terms --------------------------------------------------
+template <int D, int QT, bool F16>
 struct RowTile {
   static constexpr int NS = D / 16, NDT = D / 32;
   static constexpr float SLACK = 8.f;
@@ -152,8 +152,8 @@ struct RowTile {
   }
   __device__ __forceinline__ bool grown() const { return __builtin_amdgcn_ballot_w64(top > lim) != 0; }
   // m, and with it l and O, follows only where a row's largest score has grown so far that weights would pass 2^SLACK: weights up to there are as
-  // good as those up to one (in two terms, of which 16 bits hold both with room to spare: a weight other than one is rounded for the second product and not in
-  // l, so with one term a row that a single key dominates would be off by that term's rounding), and with 32 rows in a tile some row's maximum grows by a
+  // good as those up to one in two terms, of which 16 bits hold both with room to spare (a weight other than one is rounded for the second product and not in
+  // l: one term would leave a row that a single key dominates off by its whole rounding), and with 32 rows in a tile some row's maximum grows by a
   // little in most blocks (512 rows over 16384 slots: in 3 of 4).
   // A weight is 2^(s c - ref) in one fused multiply-add; the rounding of ref is the same factor in O and l.  Far out
   // the block's scores (x) become differences to m first.
@@ -194,7 +194,7 @@ struct RowTile {
       if (grows) late = raise(c, x);
     }
   }
-  // x, y in PT 16-bit terms, as weights of keys 2 i, 2 i + 1
+  // x, y in two 16-bit terms, as weights of keys 2 i, 2 i + 1
   static __device__ __forceinline__ void pair_to(int i, float x, float y, op8 (&w)[2], op8 (&wl)[2]) {
     typedef T T2 __attribute__((ext_vector_type(2)));
     typedef float F2 __attribute__((ext_vector_type(2)));
@@ -203,7 +203,6 @@ struct RowTile {
     u32x4 v = __builtin_bit_cast(u32x4, w[i >> 2]);
     v[i & 3] = h;
     w[i >> 2] = __builtin_bit_cast(op8, v);
-    if constexpr (PT == 1) return;
     F2 rest;
     if constexpr (F16) {
       const T2 t = __builtin_bit_cast(T2, h);
@@ -235,9 +234,9 @@ struct RowTile {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
         o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), p[j], o[dt]);
-        if constexpr (PAIRED && PT == 2) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), pl[j], o[dt]);
+        if constexpr (PAIRED) o[dt] = Mma16<F16>::mfma(__builtin_bit_cast(op8, v[dt * 2 + j]), pl[j], o[dt]);
       }
-    if constexpr (PAIRED || PT == 1) return;
+    if constexpr (PAIRED) return;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -337,15 +336,15 @@ __device__ __forceinline__ void copy_pieces(const char* src, int lane, unsigned 
 // one key group pc holds the first ones and is left with those of the next step.  k1, k2: keys of blocks j + 1 and j + 2, v0: values of block j - 1.
 // The order is written down: the compiler's own collects the vector work where it waits for the scores.
 // edge(s): what becomes of the scores of block j + 1 before their maximum is taken.
-template <int D, int QT, bool F16, int PT, int G, int AHEAD, typename Edge>
-__device__ __forceinline__ void ring_step(RowTile<D, QT, F16, PT>& t, u32x4 (&pc)[AHEAD], const u32x4* __restrict__ k1, const u32x4* __restrict__ v0,
+template <int D, int QT, bool F16, int G, int AHEAD, typename Edge>
+__device__ __forceinline__ void ring_step(RowTile<D, QT, F16>& t, u32x4 (&pc)[AHEAD], const u32x4* __restrict__ k1, const u32x4* __restrict__ v0,
                                           const u32x4* __restrict__ k2, const f32x16& z0, f32x16& z1,
-                                          const typename RowTile<D, QT, F16, PT>::op8 (&w)[2], const typename RowTile<D, QT, F16, PT>::op8 (&wl)[2],
-                                          typename RowTile<D, QT, F16, PT>::op8 (&w0)[2], typename RowTile<D, QT, F16, PT>::op8 (&wl0)[2],
+                                          const typename RowTile<D, QT, F16>::op8 (&w)[2], const typename RowTile<D, QT, F16>::op8 (&wl)[2],
+                                          typename RowTile<D, QT, F16>::op8 (&w0)[2], typename RowTile<D, QT, F16>::op8 (&wl0)[2],
                                           bool more, float scale, Edge edge) {
-  typedef RowTile<D, QT, F16, PT> Tile;
+  typedef RowTile<D, QT, F16> Tile;
   typedef typename Tile::op8 op8;
-  constexpr int NS = Tile::NS, NDT = Tile::NDT, ALL = NS * (QT + PT), SPREAD = ALL * 3 / 4;
+  constexpr int NS = Tile::NS, NDT = Tile::NDT, ALL = NS * (QT + 2), SPREAD = ALL * 3 / 4;
   u32x4 piece[2 * NS + AHEAD];
 #pragma unroll
   for (int n = 0; n < AHEAD; ++n) piece[n] = G == 1 ? pc[n] : k1[n * 64];
@@ -369,10 +368,10 @@ __device__ __forceinline__ void ring_step(RowTile<D, QT, F16, PT>& t, u32x4 (&pc
     } else {
       const int x = n - NS, j = x / NDT, dt = x % NDT;
       t.o[dt] = Mma16<F16>::mfma(a, w[j], t.o[dt]);
-      if (PT == 2) t.o[dt] = Mma16<F16>::mfma(a, wl[j], t.o[dt]);
+      t.o[dt] = Mma16<F16>::mfma(a, wl[j], t.o[dt]);
       GOOSE_HERE(t.o[dt]);
     }
-    const int before = n < NS ? n * QT : NS * QT + (n - NS) * PT, behind = before + (n < NS ? QT : PT);  // matrix instructions so far
+    const int before = n < NS ? n * QT : NS * QT + (n - NS) * 2, behind = before + (n < NS ? QT : 2);  // matrix instructions so far
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i >= 8 * before / SPREAD && i < 8 * behind / SPREAD) t.weights_of(i, z0, w0, wl0);
