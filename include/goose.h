@@ -403,7 +403,8 @@ typedef struct {
  * d_q as goose_qk_norm_rope_paged writes it (q_terms = 1 or 2); d_o: 16-bit [rows][ldo] of type o_dtype in o_terms terms; d_lse (or NULL):
  * fp32 [n_heads][ld_lse], the natural logarithm of every row's sum of exp(score), ld_lse at least the rows.  Rows between chunks and
  * behind the last one are neither read nor written.  Sums and statistics are fp32; probabilities enter the second product in two terms of the
- * cache's type (as in goose_attn_paged), whatever the output keeps.
+ * cache's type (as in goose_attn_paged), whatever the output keeps.  The order of the sums goes by the sizes and bounds of all chunks of a call: the same
+ * call gives the same bits again, but a chunk's bits, unlike its precision, may be others beside other chunks or with another P_max.
  * What slots behind a token hold (NaN, infinities) has no effect on it; a NaN in what a row sees makes the row NaN, and so does a score of
  * +infinity; an infinity among the values of committed slots makes its columns infinite or NaN; a row of scores of -infinity only is zero,
  * its logarithm -infinity.  With a flag raised (GOOSE_FLAG_CAPACITY, GOOSE_FLAG_PAGES) d_o and d_lse mean nothing.

@@ -6,6 +6,7 @@ throughout, A = sum p |v| / sum p: less than the store of a one-term output by 2
 import pytest
 import torch
 
+import paper_2604_02047_amd as goose
 import test_gpu_chunk_attn as chunk_attn
 from test_gpu_chunk_attn import BF, HF, LONG, Case
 
@@ -46,3 +47,24 @@ def test_a_dominating_key_that_raises_no_maximum(dtype, rise, nh, nkv, C, bound)
     c.k[0, c.table[0, 0], :, 3, 0] = 0.0
     c.k[0, c.table[0, 0], :, 40, 0] = 8.0 * rise
     c.check(c.run(bound=bound), heads=sorted({0, nh - 1}))
+
+
+@pytest.mark.parametrize("dtype,o_dtype", [("bf16", BF), ("f16", HF), ("bf16", HF)])
+@pytest.mark.parametrize("nh,nkv,C,P", [(32, 8, 64, 200), (32, 8, 33, 70), (40, 40, 1, 600), (40, 40, 16, 300), (8, 2, 300, 100)])
+def test_a_chunk_alone_and_among_others(dtype, o_dtype, nh, nkv, C, P):
+    """Which kernel takes a chunk and how its keys are split goes by the whole call and by P_max (alone: few rows, the tree kernels; with fifteen others: the ring; with
+    a far bound: more parts): the bits may differ, the precision does not."""
+    n = 16 if C < 100 else 4
+    Cs, Ps = [C] + [max(1, C - r) for r in range(1, n)], [P] + [P + 3 * r for r in range(1, n)]
+    heads = sorted({0, nh - 1})
+    for count, bound in ((n, None), (1, None), (1, 3000), (1, LONG)):
+        c = Case(nh, nkv, 64, dtype, Cs, Ps, seed=33, o_dtype=o_dtype)
+        c.place(bound)
+        c.chunks = goose.PagedChunks([{"seq": r, "C": Cs[r], "P_max": bound or Ps[r]} for r in range(count)])
+        c.call()
+        assert c.ctx.goose_device_flags() == 0
+        c.ctx.close()
+        if count == 1:
+            assert (c.o[C:] == 77).all()
+            c.Cs, c.Ps, c.rows = Cs[:1], Ps[:1], C
+        c.check((c.o.cpu(), c.lse.cpu()), heads=heads)
