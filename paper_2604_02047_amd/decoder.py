@@ -280,11 +280,13 @@ class PagedGooseDecoder(BatchedGooseDecoder):
         _require_clean(c.goose_device_flags())
         return int(gm.argmax[b - 1].item())
 
+    def _sinks(self, shared_pages):
+        """Slots in front that no request gives up: what it shares with the others stays where it is."""
+        return max(self.sink, shared_pages * gb.GOOSE_PAGE)
+
     def _cut(self):
-        """Every request down to `keep` slots; what it shares with the others stays where it is."""
-        n, sink = len(self.reqs), max(self.sink, self.shared_pages * gb.GOOSE_PAGE)
-        if any(q.P > self.keep for q in self.reqs) and sink + self.recent > self.keep:
-            raise gb.GooseError(gb.GOOSE_ERR_ARG, f"{self.keep} slots do not hold the {sink} first and the {self.recent} last ones")
+        """Every request down to `keep` slots."""
+        sink = self._sinks(self.shared_pages)
         cut = [r for r, q in enumerate(self.reqs) if q.P > self.keep]
         if not cut:
             return
@@ -302,6 +304,9 @@ class PagedGooseDecoder(BatchedGooseDecoder):
         common, most = 0, min(len(p) for p in prompts) - 1   # (every request feeds one token at least: its logits are needed)
         while common < most and len({p[common] for p in prompts}) == 1:
             common += 1
+        sinks = self._sinks(common // gb.GOOSE_PAGE)
+        if self.keep and any(len(p) > self.keep for p in prompts) and sinks + self.recent > self.keep:
+            raise gb.GooseError(gb.GOOSE_ERR_ARG, f"{self.keep} slots do not hold the {sinks} first and the {self.recent} last ones")
         c, first = self.gm.ctx, self.reqs[0]
         c.goose_pages_clear(self.cache)
         for q in self.reqs:                                  # a new round: nothing is left of the tables of the last one
