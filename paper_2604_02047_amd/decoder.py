@@ -216,8 +216,8 @@ class PagedGooseDecoder(BatchedGooseDecoder):
     `gm` as for BatchedGooseDecoder; its own contiguous caches are not used.  n_pages: pages of the pool; max_slots: cache slots of a request.
     prompt_rows > 0: prompts are fed in chunks of up to that many tokens (goose_chunk_layer_paged; at most gm's max_rows) instead of chain trees of
     max_B nodes.  keep > 0 (with prompt_rows): a request whose prompt has more than `keep` tokens goes on with that many cache slots
-    (goose_pages_evict): the first `sink` and whatever it shares, the last `recent`, and those that its prompt's attention weighs most.  Its output is then no longer
-    that of greedy decoding over the whole prompt."""
+    (goose_pages_evict): the first `sink` and whatever it shares, the last `recent`, and those that its prompt's attention weighs most.  It is cut before the
+    next prompt is fed: the pool has to hold the cut requests and one whole prompt.  Its output is then no longer that of greedy decoding over the whole prompt."""
 
     def __init__(self, gm: GooseModel, n_requests, n_pages, max_slots, prompt_rows=0, keep=0, sink=4, recent=64, **options):
         super().__init__(gm, n_requests, **options)
@@ -284,18 +284,14 @@ class PagedGooseDecoder(BatchedGooseDecoder):
         """Slots in front that no request gives up: what it shares with the others stays where it is."""
         return max(self.sink, shared_pages * gb.GOOSE_PAGE)
 
-    def _cut(self):
-        """Every request down to `keep` slots."""
-        sink = self._sinks(self.shared_pages)
-        cut = [r for r, q in enumerate(self.reqs) if q.P > self.keep]
-        if not cut:
-            return
-        d = self.gm.desc
-        kept = torch.empty((len(cut), d.n_layers, d.kv_heads, self.cache.table.shape[1]), dtype=torch.int64, device=self.gm.device)
-        self.gm.ctx.goose_pages_evict(self.cache, [{"seq": r + 1, "keep": self.keep, "sink": sink, "recent": self.recent} for r in cut], self.weight, kept)
+    def _cut(self, r):
+        """Request r down to `keep` slots."""
+        d, q = self.gm.desc, self.reqs[r]
+        kept = torch.empty((1, d.n_layers, d.kv_heads, self.cache.table.shape[1]), dtype=torch.int64, device=self.gm.device)
+        cut = {"seq": r + 1, "keep": self.keep, "sink": self._sinks(self.shared_pages), "recent": self.recent}
+        self.gm.ctx.goose_pages_evict(self.cache, [cut], self.weight, kept)
         _require_clean(self.gm.ctx.goose_device_flags())
-        for r in cut:
-            self.reqs[r].P = self.keep
+        q.P = self.keep
 
     def prefill(self, prompts):
         """The common beginning once, then every prompt's rest; returns the first generated token of each."""
@@ -331,8 +327,8 @@ class PagedGooseDecoder(BatchedGooseDecoder):
             q.P, q.seq = len(p), p + [q.anchor]
             q.mirror_rows(p)
             out.append(q.anchor)
-        if self.keep:
-            self._cut()
+            if self.keep and q.P > self.keep:
+                self._cut(r)
         return out
 
     def cycle(self, active):

@@ -1,4 +1,4 @@
-"""When the paged decoder cuts its prompts: not at all where the sizes do not fit."""
+"""When the paged decoder cuts its prompts: each before the next one is fed, and not at all where the sizes do not fit."""
 import pytest
 import torch
 
@@ -14,6 +14,29 @@ SHAPE = "small_gqa_qknorm_f16"
 def prompts_of(vocab, n, common, rest):
     head = gi.prefix_tokens(51, common, vocab).tolist() if common else []
     return [head + gi.prefix_tokens(60 + r, rest, vocab).tolist() for r in range(n)]
+
+
+@pytest.mark.parametrize("common", [0, 70, 128])
+def test_a_pool_for_cut_requests_and_one_whole_prompt(common):
+    """Four prompts of 400 further tokens, cut to 200 slots.  The pages of the common beginning, of three cut requests and of one whole prompt are enough (whole ones
+    would be more than twice as many), and the tokens and caches are those of a pool that holds everything."""
+    shape = gi.SHAPES[SHAPE]
+    gm = gpu_model(shape, torch_model(shape, seed=6, gain_jitter=0.1), max_B=64, cap=512, max_rows=192)
+    prompts = prompts_of(shape.vocab, 4, common, 400)
+    pages = lambda n: (n + 63) // 64  # noqa: E731
+    shared = common // 64
+    few = pages(common) + 3 * (pages(200) - shared) + pages(common + 400) - shared
+    assert few < pages(common) + 4 * (pages(common + 400) - shared)
+    outs, lens = [], []
+    for n_pages in (64, few):
+        pd = PagedGooseDecoder(gm, 4, n_pages=n_pages, max_slots=704, B=32, min_score=0.0, prompt_rows=192, keep=200, sink=4, recent=40)
+        outs.append(pd.prefill(prompts))
+        lens.append(pd.cache.len.tolist())
+        assert [q.P for q in pd.reqs] == [200] * 4 and lens[-1] == [common] + [200] * 4
+        assert int(pd.cache.refs.clamp(max=1).sum()) == pages(common) + 4 * (pages(200) - shared)
+        outs.append(pd.generate(prompts, 12) if n_pages == 64 else None)
+    assert outs[0] == outs[2] and [o[0] for o in outs[1]] == outs[0]
+    gm.ctx.close()
 
 
 def test_sizes_that_do_not_fit_are_refused_before_anything_is_fed():
