@@ -417,6 +417,9 @@ int goose_attn_chunk_paged(goose_ctx* ctx, const goose_pages* pages, int layer, 
  * and the sum alone for the chunk's own slots P <= s < P + C; other entries stay as they are.  With decay = 0 what was there is not
  * read.  d_q, d_lse: as for and from goose_attn_chunk_paged (P_max, first of each chunk); rows before `first` are not read; ldq <= 2^26,
  * ld_lse < 2^32.  0 <= decay, finite.
+ * Nothing else writes d_weight but goose_pages_evict, which moves the entries of kept slots: slots that are committed without this call (by
+ * goose_pages_commit, goose_verify_step_paged, chunks that are not weighed) and forked ones have whatever their entries held, after an eviction the weights of slots
+ * that have moved or gone.  Before an eviction ranks such slots the caller writes their entries, in every layer and KV head (0: the first to go; +infinity: the last).
  * A row whose lse is -infinity weighs nothing; a NaN in a token's score or lse makes the slots NaN that it concerns.  The sums are
  * formed in a fixed order.  A sequence whose length is out of range, slots of pages out of range: flagged and left alone. */
 int goose_attn_weight_paged(goose_ctx* ctx, const goose_pages* pages, int layer, const void* d_q, size_t ldq, int q_terms,
@@ -427,7 +430,7 @@ int goose_attn_weight_paged(goose_ctx* ctx, const goose_pages* pages, int layer,
 int goose_pages_append(goose_ctx* ctx, const goose_pages* pages, const goose_chunk* chunks, int n, void* stream);
 
 /* Cuts sequences of more than `keep` committed slots down to `keep`: in every layer and KV head its first `sink` slots stay, its last `recent`
- * ones, and of the others the keep - sink - recent with the largest weights (d_weight as above; equal weights: the lower slot; a NaN is
+ * ones, and of the others the keep - sink - recent with the largest weights (d_weight as above, entries of slots that no call has weighed included; equal weights: the lower slot; a NaN is
  * below every number).  Kept slots move to the front in their order, K and V rows and weights; slots from `keep` on hold what they held, in the
  * weights too; pages behind the new length are given back.  reposition != 0: a key that moves from slot s to t is turned by the
  * rotary angle of position t - s (rounded once), so that slot and position stay the same thing for every call that comes after; 0: rows are exact

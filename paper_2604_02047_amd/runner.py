@@ -107,7 +107,8 @@ class GooseModel:
         return cache
 
     def slot_weights(self, cache: PagedCache):
-        """What goose_attn_weight_paged writes for a paged cache of this model, all zero."""
+        """What goose_attn_weight_paged writes for a paged cache of this model, all zero.  Entries of slots that are committed without that call (trees) or forked
+        are the caller's to write before goose_pages_evict ranks them."""
         shape = (self.desc.n_layers, cache.table.shape[0], self.desc.kv_heads, cache.table.shape[1] * GOOSE_PAGE)
         return torch.zeros(shape, dtype=torch.float32, device=self.device)
 
