@@ -48,7 +48,8 @@ __device__ __forceinline__ void finish(const ChunkArgs& a, size_t row, int h, in
 // A weight enters the second product in two 16-bit terms whatever the output keeps: one term would be off by half a step of the type, as much again as the store of a
 // one-term output, and by all of that in a row that a single key with a weight other than one dominates (4096 tokens behind 12288 slots 890 us so instead of 1195).
 // What bounds it: the matrix and vector pipes together, at the clock that their load leaves.  4096 tokens of 32 / 8 heads behind 12288 slots, fp16, 1195 us: 805
-// TFLOP/s, 1210 counting both terms of the weights (a large matrix product alone 1430).  Short ranges: 33B, 2000 tokens, 92 us (575 and 860 TFLOP/s).
+// TFLOP/s, 1210 counting both terms of the weights (a large matrix product alone 1430); matrix pipe busy 66 %, vector ALU 53 %, clock 1.5 GHz (up to 1360 us on
+// other cards and under the profiler).  Short ranges: 33B, 2000 tokens, 92 us (575 and 860 TFLOP/s), matrix pipe 39 %, 2.1 GHz.
 template <int D, int QT, bool F16, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void k_chunk_ring(const ChunkArgs a) {
   typedef RowTile<D, QT, F16> Tile;

@@ -63,7 +63,7 @@ struct PageIds {
     ids = base + lane <= last ? entry : 0;
     if ((unsigned)ids >= (unsigned)n_pages) { atomicOr(flags, GOOSE_FLAG_PAGES); ids = 0; }
   }
-  // the id of block b's page; b never steps below the window, and block_last bounds it
+  // the id of block b's page; b never steps below the window, nor beyond page `last`
   __device__ __forceinline__ int of(int b, int lane) {
     if ((b >> 1) - base >= 64) { base = b >> 1; load(lane); }
     return __builtin_amdgcn_readlane(ids, (b >> 1) - base);

@@ -3,13 +3,14 @@
 // An eviction keeps, per layer and KV head, the first `sink` slots, the last `recent` ones and the heaviest of the others.  Three launches:
 //   k_evict_select  a workgroup per (layer, KV head): the m-th largest weight by radix selection over order-preserving bit patterns
 //                   (2048 + 2048 + 1024 bins), ties to the lowest slots, the kept slots as bit words, weights to the front
-//   k_evict_move    one wavefront or eight per (layer, KV head, K or V, 2 KiB of a 32-slot block): the blocks stream through registers in order,
+//   k_evict_move    one, four or eight wavefronts per (layer, KV head, K or V, 2 KiB of a 32-slot block): the blocks stream through registers in order,
 //                   kept rows are collected in LDS and leave as whole blocks.  In place: a destination block never lies behind the
 //                   block that its last row came from, and blocks ahead are only read
 //   k_evict_settle  lengths and pages (the last workgroup to move could do it, but thousands that count themselves in one word cost more than the launch:
 //                   13B, 8 layers of 4 sequences of 28 slots 139 us against 67)
-// What bounds it: memory, where there is much to move (Llama 3 8B heads, 8 layers of 4 sequences from 8192 to 2048 slots: 1.28 GB in 245 us with cold caches, 5.2 TB/s; 7B, 4
-// layers of 2 from 3001 to 2500: 0.73 GB in 146 us), else the launches and the trips to memory that follow from each other.
+// What bounds it: memory, where there is much to move (the move of Llama 3 8B heads, 8 layers of 4 sequences from 8192 to 2048 slots that lie anywhere: 1.33 GB in 285 us, 4.7 TB/s;
+// 7B, 4 layers of 2 from 3001 to 2500: 0.73 GB in 128 to 147 us), else the launches and the trips to memory that follow from each other.  (Where earlier cuts have left the heavy slots
+// side by side there is less to read: the same 8192 to 2048 over and over on one cache, whose old weights stay behind the cut, come down from 320 to 185 us a call.)
 // A rotation by the position that a key gives up needs both halves of its pairs, which is why a wavefront of the keys has columns
 // 16 u .. 16 u + 15 and those d/2 further.
 #include "mma16.h"
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(64 * NW) void k_evict_move(const goose_pages pg, co
   u32x4 r0[AHEAD], r1[AHEAD];
   unsigned masks[AHEAD];
   int blocks[AHEAD], places[AHEAD];  // which they are, and where their first kept rows go
-  // Only blocks of which something stays are looked at (8192 to 512 slots 98 -> 73 us).  Ids and words of 64 pages at a time, one a lane, with a sum over the lanes
+  // Only blocks of which something stays are looked at (8192 to 512 slots: level at 186 us where they lie anywhere, 108 -> 73 where earlier cuts left them side by side).  Ids and words of 64 pages at a time, one a lane, with a sum over the lanes
   // of kept rows and of such blocks; ids where rows go (which never steps ahead of that): asked for block by block they would be two trips to memory each.
   const int pages = (len + GOOSE_PAGE - 1) / GOOSE_PAGE;
   int src0 = q.sink / GOOSE_PAGE, dst0 = src0, src_ids, dst_ids, sum;  // sum: blocks << 16 | rows
@@ -441,7 +442,7 @@ __global__ __launch_bounds__(64 * NW) void k_evict_move(const goose_pages pg, co
   };
 #pragma unroll
   for (int k = 0; k < AHEAD; ++k) load(wave * AHEAD + k, masks[k], blocks[k], places[k], r0[k], r1[k]);
-  // (one copy of flush: its code would not fit the instruction cache several times; with library sines and cosines 690 us instead of 440 for 4 x 8192 slots)
+  // (one copy of flush: its code would not fit the instruction cache several times)
   int done = 2 * dst0;  // destination blocks written
 #pragma unroll 1
   for (int n = WINDOW;; n += WINDOW) {
@@ -487,7 +488,7 @@ int launch_pages_append(const goose_pages& pg, const ChunkReqs& ck, int32_t* fla
 
 int launch_pages_evict(int dtype, const goose_pages& pg, const Evictions& ev, int n_layers, int n_kv, int head_dim, const double* inv_freq,
                        float* weight, uint64_t* kept, bool reposition, PageScratch* scratch, int32_t* flags, hipStream_t st) {
-  // One segment in registers: 256 threads, of which more workgroups run side by side (1280 heads of 28 slots 11 us, with 1024 55).
+  // Where 256 threads' segment in LDS holds a whole table: workgroups of that size, of which more run side by side (1280 heads of 28 slots 11 us, with 1024 55).
   const dim3 heads(n_layers * n_kv, ev.n);
   if (pg.table_ld * GOOSE_PAGE <= 2048)
     hipLaunchKernelGGL(k_evict_select<256>, heads, dim3(256), 0, st, pg, ev, n_layers, n_kv, weight, kept, scratch->verdict);
@@ -495,9 +496,9 @@ int launch_pages_evict(int dtype, const goose_pages& pg, const Evictions& ev, in
     hipLaunchKernelGGL(k_evict_select<1024>, heads, dim3(1024), 0, st, pg, ev, n_layers, n_kv, weight, kept, scratch->verdict);
   int rc = goose_launch_status();
   if (rc != GOOSE_OK) return rc;
-  // Wavefronts of a stream of blocks, by the streams and the slots that a sequence may have.  us a call with 1 / 4 / 8: 64 streams (Llama 3 8B, one layer of 8192 slots
-  // to 2048) 127 / 62 / 52; 512 (8 layers) 138 / 79 / 71; 1024 (two sequences) 156 / 111 / 116; 2048 (four) 226 / 197 / 209; 5120 of 500 slots 163 / 155 / 180;
-  // 10240 of 28 slots 41 / 53 / 82.
+  // Wavefronts of a stream of blocks, by the streams and the slots that a sequence may have.  us a call with 1 / 4 / 8, from slots that lie anywhere: 64 streams (Llama 3 8B, one
+  // layer of 8192 slots to 2048) 215 / 89 / 63; 512 (8 layers) 250 / 116 / 104; 1024 (two sequences) 282 / 172 / 172; 2048 (four) 352 / 313 / 310; 5120 of 500 slots to 250
+  // 100 / 90 / 95; 10240 of 28 slots to 14 41 / 59 / 92, of 100 to 70 70 / 79 / 118.
   const dim3 grid(n_layers * n_kv * (head_dim / 16), ev.n);
   const long long streams = (long long)grid.x * grid.y;
   const bool f16 = dtype == GOOSE_DTYPE_F16;
